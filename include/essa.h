@@ -50,6 +50,7 @@ extern "C" {
 #define ESSA_ERR_CUDA (-4)              /* a CUDA runtime/driver call returned an error            */
 #define ESSA_ERR_DEVICE_TIMEOUT (-5)    /* a bounded device-side wait expired (see essa_get_status) */
 #define ESSA_ERR_NO_DEVICE (-6)         /* no CUDA device, or not compute capability 10.x          */
+#define ESSA_ERR_CACHE (-7)             /* a cache call met a bad slot, length or page, or too few free pages (see essa_get_status) */
 
 #define ESSA_W0_BF16 0            /* W0 stored as bf16                                               */
 #define ESSA_W0_INT8_PERCHANNEL 1 /* W0[o][i] = q[o][i] * scale[o], q int8, scale fp16 per out-channel */
@@ -368,6 +369,102 @@ int32_t essa_apply_projection_static(essa_ctx* ctx, const essa_adapter* adapter,
 int32_t essa_apply_projection_simt(essa_ctx* ctx, const essa_adapter* adapter, const void* x, int64_t T,
                                    const int32_t* seg_offsets, int32_t P, const float* sigma,
                                    int32_t ld_sigma, int32_t sA_col, int32_t sB_col, void* y, void* stream);
+
+/* ---- Key / value cache in 4 bits, and attention over it -------------------------------------------------------------
+ * What stands between the q, k, v projections of a block and its o projection when a population is evaluated: every
+ * candidate's adapters give it keys and values of its own, so the cache is as many times larger as there are sequences,
+ * and it is stored in 4 bits (as ESSA_W0_INT4_GROUP128 stores weights).  (No counterpart in the paper beyond its use of
+ * a quantised inference engine, Section 5; the storage scheme is the library's.)
+ *
+ * Storage.  Keys and values of one token and kv head are cut into groups of ESSA_CACHE_GROUP channels.  With min and max
+ * over a group: minimum = fp16(min), scale = fp16((max - minimum) / 15), code = rint((x - minimum) / scale) in 0 .. 15
+ * (0 where scale is 0), in fp32; a stored value stands for code * scale + minimum.  A token of a kv head whose keys or
+ * values hold a NaN or an infinity, or whose minimum or scale does not fit fp16, is stored as NaN: every query row that sees it
+ * becomes NaN (rows that do not see it are not touched).
+ * A page holds ESSA_CACHE_PAGE_TOKENS tokens of one layer: for each kv head one run of 72 * head_dim bytes,
+ *   codes of K, then of V:            [head_dim / 32][64 tokens][16 bytes], two codes per byte, low nibble = even channel;
+ *   (scale, minimum) of K, then of V: [head_dim / 64][64 tokens][2] fp16.
+ *
+ * Sequences.  Sequence s holds lengths[s] tokens; token i lives in page table[s][i / 64] of every layer.  refs[p] is the
+ * number of table entries that name page p; a page with refs 0 is free.  Only full pages are ever shared: the page a
+ * sequence is still filling is its own.  The caller owns the four buffers (essa_cache_reset makes them an empty cache) and
+ * may read them at any time; they are device-resident, so that a whole decode step (grow, append, attend) can be captured
+ * into a CUDA graph and replayed while the sequences grow.
+ *
+ * Errors that only the device can see (a slot outside the cache, the same slot twice, a length beyond the table, a page
+ * outside the pool, too few free pages) are recorded as ESSA_ERR_CACHE in the status word that essa_get_status reads.
+ * essa_cache_grow, _fork, _free and _compact then change nothing at all; _append and _read skip the tokens in
+ * question; _attend treats tokens on a bad page as hidden.
+ *
+ * Entries.  append, read and attend work on n entries: entry i stands for rows tok_offsets[i] .. tok_offsets[i + 1] - 1 of
+ * the token-major buffers (T rows in all; tok_offsets NULL: n = T, one row each) and belongs to sequence slots[i] (slots
+ * NULL: sequence i).  The rows are the sequence's LAST tokens: row j of L is token lengths[slot] - L + j.  Rows outside all
+ * entries are left as they are.  Segment offsets of a projection call (seg_offsets) serve as tok_offsets.
+ *
+ * Workspaces are the caller's, 16-byte aligned, with any contents; two calls that may overlap on the GPU (two streams, two captured graphs)
+ * need one each.  No cache call uses the context's scratch, synchronises, or allocates. */
+#define ESSA_CACHE_PAGE_TOKENS 64
+#define ESSA_CACHE_GROUP 64
+#define ESSA_CACHE_MAX_SEQS 65536
+
+typedef struct essa_cache_desc {
+  int32_t layers;     /* >= 1                                                                            */
+  int32_t num_pages;  /* pages of the pool (each spans all layers), >= 1                                 */
+  int32_t kv_heads;   /* >= 1                                                                            */
+  int32_t head_dim;   /* 64 or 128                                                                       */
+  int32_t max_seqs;   /* 1 .. ESSA_CACHE_MAX_SEQS                                                        */
+  int32_t max_pages;  /* pages of one sequence: a sequence holds at most max_pages * 64 tokens (< 2^31)  */
+  void* pages;        /* [layers][num_pages][essa_cache_page_bytes] dev, 16-byte aligned                 */
+  int32_t* table;     /* [max_seqs][max_pages] dev; -1 beyond a sequence's pages                         */
+  int32_t* lengths;   /* [max_seqs] dev                                                                  */
+  int32_t* refs;      /* [num_pages] dev                                                                 */
+} essa_cache_desc;
+
+/* Bytes of one page of one layer: 72 * kv_heads * head_dim (0 for sizes that are not supported).  Needs no device. */
+int64_t essa_cache_page_bytes(int32_t kv_heads, int32_t head_dim);
+/* Host-side check of a descriptor: ESSA_OK, ESSA_ERR_INVALID_ARG or ESSA_ERR_UNSUPPORTED_SHAPE.  Needs no device. */
+int32_t essa_cache_validate(const essa_cache_desc* cache);
+/* Workspace of essa_cache_grow, _fork and _compact on this cache.  Needs no device. */
+int32_t essa_cache_pages_workspace(const essa_cache_desc* cache, int64_t* bytes);
+/* Workspace of essa_cache_attend with these arguments on a GPU of sm_count SMs.  Needs no device. */
+int32_t essa_cache_attend_workspace(const essa_cache_desc* cache, int32_t q_heads, int32_t max_new, int32_t sm_count, int64_t* bytes);
+
+/* All sequences empty, all pages free. */
+int32_t essa_cache_reset(essa_ctx* ctx, const essa_cache_desc* cache, void* stream);
+/* Make room: sequence slots[i] (dev; NULL: i) becomes counts[i] (dev, >= 0) tokens longer, i < n, and gets the pages for
+ * them: the free pages with the lowest numbers, in the order of the entries. */
+int32_t essa_cache_grow(essa_ctx* ctx, const essa_cache_desc* cache, const int32_t* slots, const int32_t* counts, int32_t n, void* workspace,
+                        int64_t workspace_bytes, void* stream);
+/* Store k and v ([T] rows of kv_heads * head_dim bf16, ld_k / ld_v elements apart: multiples of 8; 16-byte aligned) of the
+ * entries' tokens in layer `layer`.  Tokens on a page that another sequence shares are skipped (ESSA_ERR_CACHE). */
+int32_t essa_cache_append(essa_ctx* ctx, const essa_cache_desc* cache, int32_t layer, const void* k, int64_t ld_k, const void* v, int64_t ld_v, int32_t T,
+                          const int32_t* slots, const int32_t* tok_offsets, int32_t n, void* stream);
+/* The inverse: the entries' tokens of layer `layer` as dense bf16 [T][kv_heads][head_dim] (k_out, v_out; either may be
+ * NULL), code * scale + minimum in fp32 rounded once.  Tokens that are not in the cache (see Errors) read as 0. */
+int32_t essa_cache_read(essa_ctx* ctx, const essa_cache_desc* cache, int32_t layer, void* k_out, void* v_out, int32_t T, const int32_t* slots,
+                        const int32_t* tok_offsets, int32_t n, void* stream);
+/* Attention: for every row r (token at position pos) and query head h
+ *   out[r][h] = sum_s p_s v_s,  p = softmax over s <= pos of scale * (q[r][h] . k_s),  kv head h / (q_heads / kv_heads),
+ * over the tokens 0 .. pos of the row's sequence (its own included: append comes first).  A row that sees no token is 0.
+ *   q, out [T] rows of q_heads * head_dim bf16, ld_q / ld_out elements apart (multiples of 8; 16-byte aligned); q_heads a
+ *   multiple of kv_heads; scale > 0, finite.
+ *   max_new >= 1: the most rows an entry is expected to have.  It only chooses the schedule (1 for decode steps); any value
+ *   gives right results.
+ * Scores, maximum, sums and the accumulators are fp32.  Weights are rounded to bf16 once before the product with V (2^-9
+ * relative), out once at the end. */
+int32_t essa_cache_attend(essa_ctx* ctx, const essa_cache_desc* cache, int32_t layer, const void* q, int64_t ld_q, int32_t q_heads, int32_t T,
+                          const int32_t* slots, const int32_t* tok_offsets, int32_t n, int32_t max_new, float scale, void* out, int64_t ld_out,
+                          void* workspace, int64_t workspace_bytes, void* stream);
+/* Sequence dst[i] becomes a copy of the first lens[i] (dev; NULL: all) tokens of sequence src[i], i < n: it shares the full
+ * pages and gets a copy, in all layers, of a partly filled last one (the free pages with the lowest numbers, in the order of
+ * the entries).  What dst[i] held is freed first.  The dst are distinct and none of them is a src. */
+int32_t essa_cache_fork(essa_ctx* ctx, const essa_cache_desc* cache, const int32_t* src, const int32_t* dst, const int32_t* lens, int32_t n, void* workspace,
+                        int64_t workspace_bytes, void* stream);
+/* Sequences slots[i], i < n, become empty; pages that no other sequence shares become free. */
+int32_t essa_cache_free(essa_ctx* ctx, const essa_cache_desc* cache, const int32_t* slots, int32_t n, void* stream);
+/* Move pages so that the pages in use are 0 .. U - 1: the i-th used page at or above U (ascending) moves to the i-th free page
+ * below U.  *used (dev, may be NULL) = U.  The pool can then be shortened, or its end given back. */
+int32_t essa_cache_compact(essa_ctx* ctx, const essa_cache_desc* cache, int32_t* used, void* workspace, int64_t workspace_bytes, void* stream);
 
 /* How essa_apply_projection would schedule a call (host-only arithmetic; needs no device). */
 typedef struct essa_plan {

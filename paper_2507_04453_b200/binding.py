@@ -7,6 +7,7 @@ been built, or no sm_100 GPU is present, the calls raise.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 from typing import Optional
@@ -23,6 +24,7 @@ ESSA_ERR_ALLOC = -3
 ESSA_ERR_CUDA = -4
 ESSA_ERR_DEVICE_TIMEOUT = -5
 ESSA_ERR_NO_DEVICE = -6
+ESSA_ERR_CACHE = -7
 ESSA_W0_BF16 = 0
 ESSA_W0_INT8_PERCHANNEL = 1
 ESSA_W0_INT4_GROUP128 = 2
@@ -47,6 +49,9 @@ EXPORTED_SYMBOLS = (
     "essa_apply_projection_static", "essa_get_launch_count", "essa_reserve_dequant", "essa_apply_block", "essa_apply_block_host", "essa_set_option",
     "essa_top_alpha_index", "essa_sample_population_masked", "essa_export_candidates", "essa_sample_apply_block",
     "essa_apply_layers", "essa_cma_create", "essa_cma_destroy", "essa_cma_ask", "essa_tell", "essa_cma_set", "essa_cma_get", "essa_cma_params",
+    "essa_cache_page_bytes", "essa_cache_validate", "essa_cache_pages_workspace", "essa_cache_attend_workspace",
+    "essa_cache_reset", "essa_cache_grow", "essa_cache_append", "essa_cache_read", "essa_cache_attend", "essa_cache_fork",
+    "essa_cache_free", "essa_cache_compact",
 )
 
 
@@ -81,6 +86,12 @@ class AdapterDesc(C.Structure):
 
 class BlockItem(C.Structure):
     _fields_ = [("adapter", C.c_void_p), ("x", C.c_void_p), ("sA_col", C.c_int32), ("sB_col", C.c_int32), ("y", C.c_void_p)]
+
+
+class CacheDesc(C.Structure):
+    _fields_ = [("layers", C.c_int32), ("num_pages", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("max_seqs", C.c_int32), ("max_pages", C.c_int32), ("pages", C.c_void_p), ("table", C.c_void_p),
+                ("lengths", C.c_void_p), ("refs", C.c_void_p)]
 
 
 class Plan(C.Structure):
@@ -150,6 +161,18 @@ def load_library() -> C.CDLL:
         "essa_debug_core_matrix": (i32, [vp, vp, vp]),
         "essa_profile_begin": (i32, [vp, i32]),
         "essa_profile_end": (i32, [vp, C.POINTER(Profile)]),
+        "essa_cache_page_bytes": (i64, [i32, i32]),
+        "essa_cache_validate": (i32, [C.POINTER(CacheDesc)]),
+        "essa_cache_pages_workspace": (i32, [C.POINTER(CacheDesc), C.POINTER(i64)]),
+        "essa_cache_attend_workspace": (i32, [C.POINTER(CacheDesc), i32, i32, i32, C.POINTER(i64)]),
+        "essa_cache_reset": (i32, [vp, C.POINTER(CacheDesc), vp]),
+        "essa_cache_grow": (i32, [vp, C.POINTER(CacheDesc), vp, vp, i32, vp, i64, vp]),
+        "essa_cache_append": (i32, [vp, C.POINTER(CacheDesc), i32, vp, i64, vp, i64, i32, vp, vp, i32, vp]),
+        "essa_cache_read": (i32, [vp, C.POINTER(CacheDesc), i32, vp, vp, i32, vp, vp, i32, vp]),
+        "essa_cache_attend": (i32, [vp, C.POINTER(CacheDesc), i32, vp, i64, i32, i32, vp, vp, i32, i32, f32, vp, i64, vp, i64, vp]),
+        "essa_cache_fork": (i32, [vp, C.POINTER(CacheDesc), vp, vp, vp, i32, vp, i64, vp]),
+        "essa_cache_free": (i32, [vp, C.POINTER(CacheDesc), vp, i32, vp]),
+        "essa_cache_compact": (i32, [vp, C.POINTER(CacheDesc), vp, vp, i64, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -350,6 +373,176 @@ class CmaState:
         return dict(zip(names, (float(x) for x in v)))
 
 
+class KvCache:
+    """A paged 4-bit key / value cache (essa_cache_*): four torch tensors and the calls on them, argument marshalling only.
+
+    pages [layers, num_pages, page_bytes] uint8, table [max_seqs, max_pages], lengths [max_seqs], refs [num_pages] int32.
+    Index and count arguments are int32 tensors on the cache's device.  ``stream``: a torch.cuda.Stream; None = the current
+    stream of the cache's device.  Workspaces and outputs come from torch's allocator, on that stream."""
+
+    def __init__(self, ctx, layers, num_pages, kv_heads, head_dim, max_seqs, max_pages, pages=None, table=None, lengths=None, refs=None):
+        torch = ctx.torch
+        page_bytes = ctx.lib.essa_cache_page_bytes(kv_heads, head_dim)
+        if page_bytes == 0:
+            raise EssaError(ESSA_ERR_UNSUPPORTED_SHAPE, "kv_cache: head_dim must be 64 or 128, kv_heads positive")
+        given = [t is not None for t in (pages, table, lengths, refs)]
+        if any(given) != all(given):
+            raise EssaError(ESSA_ERR_INVALID_ARG, "kv_cache: pass all four buffers or none")
+        self.ctx, self.device = ctx, ctx.device
+        fresh = not all(given)
+        if fresh:
+            pages = torch.empty((layers, num_pages, page_bytes), dtype=torch.uint8, device=self.device)
+            table = torch.empty((max_seqs, max_pages), dtype=torch.int32, device=self.device)
+            lengths = torch.empty(max_seqs, dtype=torch.int32, device=self.device)
+            refs = torch.empty(num_pages, dtype=torch.int32, device=self.device)
+        for name, t, dtype, shape in (("pages", pages, torch.uint8, (layers, num_pages, page_bytes)), ("table", table, torch.int32, (max_seqs, max_pages)),
+                                      ("lengths", lengths, torch.int32, (max_seqs,)), ("refs", refs, torch.int32, (num_pages,))):
+            if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous() or t.device != self.device:
+                raise EssaError(ESSA_ERR_INVALID_ARG, f"kv_cache: {name} must be a contiguous {dtype} tensor of shape {shape} on {self.device}")
+        self.pages, self.table, self.lengths, self.refs = pages, table, lengths, refs
+        self.kv_heads, self.head_dim, self.max_seqs = kv_heads, head_dim, max_seqs
+        self.desc = CacheDesc(layers, num_pages, kv_heads, head_dim, max_seqs, max_pages, pages.data_ptr(), table.data_ptr(),
+                              lengths.data_ptr(), refs.data_ptr())
+        st = ctx.lib.essa_cache_validate(C.byref(self.desc))
+        if st != ESSA_OK:
+            raise EssaError(st, "kv_cache: " + ctx.lib.essa_status_string(st).decode())
+        need = C.c_int64(0)
+        ctx._check(ctx.lib.essa_cache_pages_workspace(C.byref(self.desc), C.byref(need)))
+        self._pages_ws = need.value
+        self._sms = torch.cuda.get_device_properties(self.device).multi_processor_count
+        self._attend_ws = {}  # (q_heads, max_new) -> bytes
+        if fresh:
+            self.reset()
+
+    # -- plumbing
+    def _on(self, stream):
+        """(stream to enqueue on, context manager under which torch allocates for it)"""
+        torch = self.ctx.torch
+        return (torch.cuda.current_stream(self.device), contextlib.nullcontext()) if stream is None else (stream, torch.cuda.stream(stream))
+
+    def _ints(self, name, t, n=None):
+        """Checks an int32 index tensor; its pointer (None for None)."""
+        if t is None:
+            return None
+        if t.dtype != self.ctx.torch.int32 or t.dim() != 1 or not t.is_contiguous() or t.device != self.device or (n is not None and t.numel() != n):
+            raise EssaError(ESSA_ERR_INVALID_ARG, f"kv_cache: {name} must be a contiguous int32 vector on {self.device}" + ("" if n is None else f" of {n} elements"))
+        return t.data_ptr() if t.numel() else None
+
+    def _entries(self, T, slots, tok_offsets):
+        n = T if tok_offsets is None else tok_offsets.numel() - 1
+        if n < 0:
+            raise EssaError(ESSA_ERR_INVALID_ARG, "kv_cache: tok_offsets is empty")
+        return self._ints("slots", slots, n), self._ints("tok_offsets", tok_offsets), n
+
+    def _rows(self, name, t, heads):
+        """Checks a token-major [T, heads, head_dim] or [T, heads * head_dim] bf16 tensor; (pointer, elements between rows)."""
+        ok = t.dtype == self.ctx.torch.bfloat16 and t.device == self.device
+        if ok and t.dim() == 3:
+            ok = t.shape[1:] == (heads, self.head_dim) and (t.numel() == 0 or (t.stride(2) == 1 and (heads == 1 or t.stride(1) == self.head_dim)))
+        elif ok:
+            ok = t.dim() == 2 and t.shape[1] == heads * self.head_dim and (t.numel() == 0 or t.stride(1) == 1)
+        if not ok:
+            raise EssaError(ESSA_ERR_INVALID_ARG, f"kv_cache: {name} must be a bf16 tensor [T, {heads}, {self.head_dim}] on {self.device} whose rows are contiguous")
+        T = t.shape[0]
+        return (t.data_ptr() if T else None), (t.stride(0) if T > 1 else heads * self.head_dim)
+
+    def _space(self, bytes_):
+        return self.ctx.torch.empty(bytes_, dtype=self.ctx.torch.uint8, device=self.device)
+
+    # -- pages
+    def reset(self, stream=None):
+        """essa_cache_reset: all sequences empty, all pages free."""
+        s, _ = self._on(stream)
+        self.ctx._check(self.ctx.lib.essa_cache_reset(self.ctx.handle, C.byref(self.desc), s.cuda_stream or None))
+
+    def grow(self, slots, counts, stream=None):
+        """essa_cache_grow: sequence slots[i] (None: i) becomes counts[i] tokens longer."""
+        n = counts.numel()
+        a, b = self._ints("slots", slots, n), self._ints("counts", counts)
+        s, alloc = self._on(stream)
+        with alloc:
+            ws = self._space(self._pages_ws)
+        self.ctx._check(self.ctx.lib.essa_cache_grow(self.ctx.handle, C.byref(self.desc), a, b, n, ws.data_ptr(), self._pages_ws, s.cuda_stream or None))
+
+    def fork(self, src, dst, lens=None, stream=None):
+        """essa_cache_fork: sequence dst[i] becomes a copy of the first lens[i] (None: all) tokens of src[i]."""
+        n = src.numel()
+        a, b, c = self._ints("src", src), self._ints("dst", dst, n), self._ints("lens", lens, n)
+        s, alloc = self._on(stream)
+        with alloc:
+            ws = self._space(self._pages_ws)
+        self.ctx._check(self.ctx.lib.essa_cache_fork(self.ctx.handle, C.byref(self.desc), a, b, c, n, ws.data_ptr(), self._pages_ws, s.cuda_stream or None))
+
+    def free(self, slots, stream=None):
+        """essa_cache_free: the sequences become empty."""
+        s, _ = self._on(stream)
+        self.ctx._check(self.ctx.lib.essa_cache_free(self.ctx.handle, C.byref(self.desc), self._ints("slots", slots), slots.numel(), s.cuda_stream or None))
+
+    def compact(self, used=None, stream=None):
+        """essa_cache_compact: the pages in use become 0 .. U - 1; used (int32, one element) receives U."""
+        u = self._ints("used", used, 1)
+        s, alloc = self._on(stream)
+        with alloc:
+            ws = self._space(self._pages_ws)
+        self.ctx._check(self.ctx.lib.essa_cache_compact(self.ctx.handle, C.byref(self.desc), u, ws.data_ptr(), self._pages_ws, s.cuda_stream or None))
+
+    # -- tokens
+    def append(self, layer: int, k, v, tok_offsets=None, slots=None, stream=None):
+        """essa_cache_append: k, v [T, kv_heads, head_dim] bf16 become the last tokens of the entries' sequences."""
+        T = k.shape[0]
+        if v.shape[0] != T:
+            raise EssaError(ESSA_ERR_INVALID_ARG, "kv_cache: k and v must have the same number of rows")
+        pk, ldk = self._rows("k", k, self.kv_heads)
+        pv, ldv = self._rows("v", v, self.kv_heads)
+        a, b, n = self._entries(T, slots, tok_offsets)
+        s, _ = self._on(stream)
+        self.ctx._check(self.ctx.lib.essa_cache_append(self.ctx.handle, C.byref(self.desc), layer, pk, ldk, pv, ldv, T, a, b, n, s.cuda_stream or None))
+
+    def read(self, layer: int, tok_offsets, T: int, slots=None, k_out=None, v_out=None, stream=None):
+        """essa_cache_read: (k, v) [T, kv_heads, head_dim] bf16, the last tokens of the entries' sequences as they are stored."""
+        torch = self.ctx.torch
+        a, b, n = self._entries(T, slots, tok_offsets)
+        s, alloc = self._on(stream)
+        with alloc:
+            shape = (T, self.kv_heads, self.head_dim)
+            k_out = torch.empty(shape, dtype=torch.bfloat16, device=self.device) if k_out is None else k_out
+            v_out = torch.empty(shape, dtype=torch.bfloat16, device=self.device) if v_out is None else v_out
+        for name, t in (("k_out", k_out), ("v_out", v_out)):
+            self._rows(name, t, self.kv_heads)
+            if t.shape[0] != T or not t.is_contiguous():
+                raise EssaError(ESSA_ERR_INVALID_ARG, f"kv_cache: {name} must be contiguous with T rows")
+        self.ctx._check(self.ctx.lib.essa_cache_read(self.ctx.handle, C.byref(self.desc), layer, k_out.data_ptr() if T else None,
+                                                     v_out.data_ptr() if T else None, T, a, b, n, s.cuda_stream or None))
+        return k_out, v_out
+
+    def attend(self, layer: int, q, tok_offsets=None, slots=None, max_new: int = 1, scale=None, out=None, stream=None):
+        """essa_cache_attend: q [T, heads, head_dim] (or [T, heads * head_dim]) bf16 over the cached tokens; the result has q's
+        shape.  max_new: the most rows an entry is expected to have (chooses the schedule only); scale: None = head_dim ** -0.5."""
+        torch = self.ctx.torch
+        T = q.shape[0]
+        heads = q.shape[1] if q.dim() == 3 else q.shape[-1] // self.head_dim
+        pq, ldq = self._rows("q", q, heads)
+        a, b, n = self._entries(T, slots, tok_offsets)
+        key = (heads, max_new)
+        need = self._attend_ws.get(key)
+        if need is None:
+            got = C.c_int64(0)
+            st = self.ctx.lib.essa_cache_attend_workspace(C.byref(self.desc), heads, max_new, self._sms, C.byref(got))
+            if st != ESSA_OK:
+                raise EssaError(st, "kv_cache: the number of query heads must be a multiple of kv_heads and max_new at least 1")
+            need = self._attend_ws[key] = got.value
+        s, alloc = self._on(stream)
+        with alloc:
+            out = torch.empty(q.shape, dtype=q.dtype, device=self.device) if out is None else out
+            ws = self._space(need)
+        if out.shape != q.shape:
+            raise EssaError(ESSA_ERR_INVALID_ARG, "kv_cache: out must have q's shape")
+        po, ldo = self._rows("out", out, heads)
+        self.ctx._check(self.ctx.lib.essa_cache_attend(self.ctx.handle, C.byref(self.desc), layer, pq, ldq, heads, T, a, b, n, max_new,
+                                                       self.head_dim ** -0.5 if scale is None else scale, po, ldo, ws.data_ptr(), need, s.cuda_stream or None))
+        return out
+
+
 class Context:
     """Owns one essa_ctx on a CUDA device."""
 
@@ -432,6 +625,10 @@ class Context:
     def cma_state(self, d: int, lam: int, mean0, step0: float) -> "CmaState":
         """essa_cma_create: search-distribution state (m_0 = mean0 host array, sigma_0 = step0, C_0 = I) on the device."""
         return CmaState(self, d, lam, mean0, step0)
+
+    def kv_cache(self, layers: int, num_pages: int, kv_heads: int, head_dim: int, max_seqs: int, max_pages: int, **buffers) -> "KvCache":
+        """A paged 4-bit key / value cache on this context's device; buffers: the four tensors of an existing one."""
+        return KvCache(self, layers, num_pages, kv_heads, head_dim, max_seqs, max_pages, **buffers)
 
     # -- sampling
     def sample_population(self, mean, step: float, Bfactor, Dvec, seed: int, P: int, out=None, k_begin: int = 0,

@@ -130,6 +130,7 @@ const char* essa_status_string(int32_t status) {
     case ESSA_ERR_CUDA: return "CUDA error";
     case ESSA_ERR_DEVICE_TIMEOUT: return "a bounded device-side wait expired";
     case ESSA_ERR_NO_DEVICE: return "no usable sm_100 CUDA device";
+    case ESSA_ERR_CACHE: return "a cache call met a bad slot, length or page, or too few free pages";
     default: return "unknown status";
   }
 }

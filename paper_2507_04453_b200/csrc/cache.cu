@@ -1,0 +1,705 @@
+// Paged 4-bit key / value cache: storing and reading tokens, page management, and the C entry points of include/essa.h.
+#include <cmath>
+
+#include "cache.cuh"
+
+namespace essa {
+namespace {
+
+constexpr int kPlanThreads = 1024;
+
+// ------------------------------------------------------------------------------------------------ tokens
+// The entry that row t belongs to (off[i] <= t < off[i + 1]); -1 if none.
+__device__ __forceinline__ int entry_of(const CacheEntries& e, int t) {
+  if (!e.off) return t;
+  if (e.n == 0 || t < __ldg(e.off) || t >= __ldg(e.off + e.n)) return -1;
+  return find_candidate(e.off, e.n, t);
+}
+
+// Where row t of the call is cached: page (>= 0) and offset in it; -1 if the row belongs to no entry, -2 if it should be in
+// the cache and is not.
+__device__ __forceinline__ int locate_token(const CacheView& v, const CacheEntries& e, int t, int* offset) {
+  const int i = entry_of(e, t);
+  if (i < 0) return -1;
+  const EntryInfo info = load_entry(v, e, i);
+  const int pos = info.len - info.rows + (t - info.row0);
+  if (info.slot < 0 || t >= info.row0 + info.rows || pos < 0) return -2;
+  const int page = __ldg(v.table + (int64_t)info.slot * v.max_pages + pos / kPageTokens);
+  if (page < 0 || page >= v.num_pages) return -2;
+  *offset = pos % kPageTokens;
+  return page;
+}
+
+struct Packed {
+  uint32_t codes;
+  __half scale, low;
+};
+
+// 4-bit storage of a group of 64 channels of which this thread holds eight, the other seven neighbours (lanes of an aligned
+// group of eight) the rest.
+__device__ __forceinline__ void group_stats(const float (&x)[8], float& low, float& high, bool& finite) {
+  low = x[0];
+  high = x[0];
+  float probe = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    low = fminf(low, x[i]);
+    high = fmaxf(high, x[i]);
+    probe = fmaf(x[i], 0.f, probe);  // NaN if any is NaN or infinite
+  }
+  finite = probe == 0.f;
+#pragma unroll
+  for (int d = 1; d < 8; d <<= 1) {
+    low = fminf(low, __shfl_xor_sync(0xffffffffu, low, d));
+    high = fmaxf(high, __shfl_xor_sync(0xffffffffu, high, d));
+  }
+}
+__device__ __forceinline__ Packed pack_group(const float (&x)[8], float low, float high) {
+  Packed p;
+  p.low = __float2half_rn(low);
+  const float base = __half2float(p.low);
+  p.scale = __float2half_rn(__fdiv_rn(high - base, 15.f));
+  const float s = __half2float(p.scale);
+  p.codes = 0;
+  if (s > 0.f) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float c = fminf(fmaxf(rintf(__fdiv_rn(x[i] - base, s)), 0.f), 15.f);
+      p.codes |= (uint32_t)c << (4 * i);
+    }
+  }
+  return p;
+}
+__device__ __forceinline__ void unpack8(const __nv_bfloat16* src, float (&x)[8]) {
+  const uint4 u = *reinterpret_cast<const uint4*>(src);
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = __uint_as_float(w[i] << 16);
+    x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+  }
+}
+
+// One thread per eight channels of K and of V of one (token, kv head): D / 8 neighbouring lanes per token, tokens innermost so
+// that the 16-byte pieces of neighbouring tokens (adjacent in a page) meet in one sector.  Bound by HBM: 4 * D bytes in and
+// 1.125 * D out per (token, kv head).
+template <int D>
+__global__ void __launch_bounds__(256) append_kernel(CacheView v, CacheEntries e, const __nv_bfloat16* k, int64_t ld_k, const __nv_bfloat16* val, int64_t ld_v,
+                                                     int32_t* status) {
+  constexpr int L = D / 8;  // lanes per token
+  const int64_t unit = ((int64_t)blockIdx.x * 256 + threadIdx.x) / L;
+  const int lane = threadIdx.x % L;
+  const int t = (int)(unit % e.T), h = (int)(unit / e.T);
+  const bool in = h < v.kv_heads;
+  int offset = 0;
+  int page = in ? locate_token(v, e, t, &offset) : -1;
+  if (page >= 0 && __ldg(v.refs + page) != 1) page = -2;  // shared (or free): not this sequence's to write
+  if (page == -2) cache_fault(status);
+  float xk[8], xv[8];
+  if (page >= 0) {
+    unpack8(k + t * ld_k + h * D + lane * 8, xk);
+    unpack8(val + t * ld_v + h * D + lane * 8, xv);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) xk[i] = xv[i] = 0.f;
+  }
+  float lk, hk, lv, hv;
+  bool fk, fv;
+  group_stats(xk, lk, hk, fk);
+  group_stats(xv, lv, hv, fv);
+  Packed pk = pack_group(xk, lk, hk), pv = pack_group(xv, lv, hv);
+  const bool fits = fk && fv && !__hisinf(pk.low) && !__hisinf(pk.scale) && !__hisinf(pv.low) && !__hisinf(pv.scale);
+  // one lane that does not fit makes the token (its L lanes) NaN
+  const uint32_t misfits = __ballot_sync(0xffffffffu, !fits) >> ((threadIdx.x & 31) / L * L) & ((1u << L) - 1);
+  if (page < 0) return;
+  if (misfits) {
+    pk.codes = pv.codes = 0;
+    pk.scale = pv.scale = __ushort_as_half(0);
+    pk.low = pv.low = __ushort_as_half(0x7e00);
+  }
+  uint8_t* run = v.pages + page * v.page_bytes + (int64_t)h * 72 * D;
+  uint8_t* code = run + (lane >> 2) * 1024 + offset * 16 + (lane & 3) * 4;
+  *reinterpret_cast<uint32_t*>(code) = pk.codes;
+  *reinterpret_cast<uint32_t*>(code + 32 * D) = pv.codes;
+  if ((lane & 7) == 0) {
+    __half2* meta = reinterpret_cast<__half2*>(run + 64 * D + ((lane >> 3) * kPageTokens + offset) * 4);
+    meta[0] = __halves2half2(pk.scale, pk.low);
+    meta[D] = __halves2half2(pv.scale, pv.low);
+  }
+}
+
+// The inverse, with the same mapping of threads.
+template <int D>
+__global__ void __launch_bounds__(256) read_kernel(CacheView v, CacheEntries e, __nv_bfloat16* k_out, __nv_bfloat16* v_out, int32_t* status) {
+  constexpr int L = D / 8;
+  const int64_t unit = ((int64_t)blockIdx.x * 256 + threadIdx.x) / L;
+  const int lane = threadIdx.x % L;
+  const int t = (int)(unit % e.T), h = (int)(unit / e.T);
+  if (h >= v.kv_heads) return;
+  int offset = 0;
+  const int page = locate_token(v, e, t, &offset);
+  if (page == -1) return;
+  if (page == -2) cache_fault(status);
+  const uint8_t* run = v.pages + (int64_t)max(page, 0) * v.page_bytes + (int64_t)h * 72 * D;
+  const int64_t at = ((int64_t)t * v.kv_heads + h) * D + lane * 8;
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    __nv_bfloat16* out = which ? v_out : k_out;
+    if (!out) continue;
+    uint32_t w = 0;
+    float2 m = make_float2(0.f, 0.f);
+    if (page >= 0) {
+      w = *reinterpret_cast<const uint32_t*>(run + which * 32 * D + (lane >> 2) * 1024 + offset * 16 + (lane & 3) * 4);
+      m = __half22float2(*reinterpret_cast<const __half2*>(run + 64 * D + which * 4 * D + ((lane >> 3) * kPageTokens + offset) * 4));
+    }
+    uint32_t y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      // product and sum rounded apart (as the definition reads), then once to bf16
+      const float a = __fadd_rn(__fmul_rn((float)((w >> (8 * i)) & 15), m.x), m.y), b = __fadd_rn(__fmul_rn((float)((w >> (8 * i + 4)) & 15), m.x), m.y);
+      const __nv_bfloat162 r = __floats2bfloat162_rn(a, b);
+      y[i] = *reinterpret_cast<const uint32_t*>(&r);
+    }
+    *reinterpret_cast<uint4*>(out + at) = make_uint4(y[0], y[1], y[2], y[3]);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ pages
+// The plan of a page operation, in the caller's workspace.
+struct PlanHead {
+  int32_t ok;      // 0: refused, nothing may change
+  int32_t copies;  // pages to copy (from[i] -> to[i], in every layer)
+};
+struct PlanSpace {
+  PlanHead* head;
+  int32_t *from, *to;  // [num_pages] each
+  int32_t* extra;      // [max(num_pages, max_seqs)]: fork: new last page of entry i or -1; compact: where page p goes
+};
+PlanSpace plan_space(void* ws, const CacheView& v) {
+  PlanSpace p;
+  p.head = static_cast<PlanHead*>(ws);
+  p.from = reinterpret_cast<int32_t*>(static_cast<uint8_t*>(ws) + 256);
+  p.to = p.from + v.num_pages;
+  p.extra = p.to + v.num_pages;
+  return p;
+}
+
+__device__ __forceinline__ int pages_of(int tokens) { return tokens / kPageTokens + (tokens % kPageTokens != 0); }
+
+// Whether the n slots lie in [0, max_seqs) and are distinct.  `seen`: shared bitmap of max_seqs bits, left with the slots' bits
+// set.  Every thread of the block gets the answer.
+__device__ bool slots_distinct(const int32_t* slots, int n, int max_seqs, uint32_t* seen) {
+  for (int i = threadIdx.x; i < (max_seqs + 31) / 32; i += blockDim.x) seen[i] = 0;
+  __syncthreads();
+  bool ok = true;
+  for (int i = threadIdx.x; i < n; i += blockDim.x) {
+    const int s = slots ? slots[i] : i;
+    if (s < 0 || s >= max_seqs) { ok = false; continue; }
+    if (atomicOr(&seen[s >> 5], 1u << (s & 31)) >> (s & 31) & 1) ok = false;
+  }
+  return __syncthreads_and(ok);
+}
+
+// The numbers of the first `want` pages with refs 0 into list (in global memory, visible to the block afterwards); false if there are fewer.
+__device__ bool first_free(const CacheView& v, int want, int32_t* list, long long* scan_sm) {
+  long long have = 0;
+  constexpr int kPer = 4;
+  for (int base = 0; base < v.num_pages && have < want; base += blockDim.x * kPer) {
+    const int p0 = base + threadIdx.x * kPer;
+    uint32_t bits = 0;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+      if (p0 + i < v.num_pages && __ldcg(v.refs + p0 + i) == 0) bits |= 1u << i;
+    long long total;
+    long long at = have + block_scan(__popc(bits), &total, scan_sm);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+      if (bits >> i & 1) {
+        if (at < want) list[at] = p0 + i;
+        ++at;
+      }
+    have += total;
+  }
+  __syncthreads();
+  return have >= want;
+}
+
+__global__ void __launch_bounds__(kPlanThreads) grow_kernel(CacheView v, const int32_t* slots, const int32_t* counts, int n, PlanSpace ws, int32_t* status) {
+  extern __shared__ uint32_t seen[];
+  __shared__ long long scan_sm[33];
+  bool ok = slots_distinct(slots, n, v.max_seqs, seen);
+  long long want = 0;
+  if (ok) {
+    bool fine = true;
+    for (int base = 0; base < n; base += blockDim.x) {
+      const int i = base + threadIdx.x;
+      long long need = 0, total;
+      if (i < n) {
+        const int len = v.lengths[slots ? slots[i] : i], add = counts[i];
+        if (len < 0 || add < 0 || (long long)len + add > (long long)v.max_pages * kPageTokens) fine = false;
+        else need = pages_of(len + add) - pages_of(len);
+      }
+      block_scan(need, &total, scan_sm);
+      want += total;
+    }
+    ok = __syncthreads_and(fine) && want <= v.num_pages && first_free(v, (int)want, ws.from, scan_sm);
+  }
+  if (!ok) {
+    if (threadIdx.x == 0) cache_fault(status);
+    return;
+  }
+  long long before = 0;
+  for (int base = 0; base < n; base += blockDim.x) {
+    const int i = base + threadIdx.x;
+    long long need = 0, total;
+    int slot = 0, len = 0, add = 0;
+    if (i < n) {
+      slot = slots ? slots[i] : i;
+      len = v.lengths[slot];
+      add = counts[i];
+      need = pages_of(len + add) - pages_of(len);
+    }
+    const long long at = before + block_scan(need, &total, scan_sm);
+    before += total;
+    for (int j = 0; j < need; ++j) {
+      const int page = ws.from[at + j];
+      v.table[(int64_t)slot * v.max_pages + pages_of(len) + j] = page;
+      v.refs[page] = 1;
+    }
+    if (i < n) v.lengths[slot] = len + add;
+  }
+}
+
+__global__ void __launch_bounds__(256) free_kernel(CacheView v, const int32_t* slots, int n, int32_t* status) {
+  extern __shared__ uint32_t seen[];
+  // every thread block comes to the same verdict, from the slots alone
+  if (!slots_distinct(slots, n, v.max_seqs, seen)) {
+    if (threadIdx.x == 0) cache_fault(status);
+    return;
+  }
+  for (int i = blockIdx.x; i < n; i += gridDim.x) {
+    const int slot = slots ? slots[i] : i;
+    int32_t* row = v.table + (int64_t)slot * v.max_pages;
+    for (int j = threadIdx.x; j < v.max_pages; j += blockDim.x) {
+      const int page = row[j];
+      if (page >= 0 && page < v.num_pages) atomicSub(v.refs + page, 1);
+      row[j] = -1;
+    }
+    if (threadIdx.x == 0) v.lengths[slot] = 0;
+  }
+}
+
+// Adds `by` to the refs of all pages of the sequences dst (warps take sequences in turn).
+__device__ void count_rows(const CacheView& v, const int32_t* dst, int n, int by) {
+  for (int i = threadIdx.x >> 5; i < n; i += blockDim.x >> 5) {
+    const int32_t* row = v.table + (int64_t)dst[i] * v.max_pages;
+    for (int j = threadIdx.x & 31; j < v.max_pages; j += 32) {
+      const int page = row[j];
+      if (page >= 0 && page < v.num_pages) atomicAdd(v.refs + page, by);
+    }
+  }
+  __threadfence();
+  __syncthreads();
+}
+
+__global__ void __launch_bounds__(kPlanThreads) fork_plan_kernel(CacheView v, const int32_t* src, const int32_t* dst, const int32_t* lens, int n, PlanSpace ws,
+                                                                 int32_t* status) {
+  extern __shared__ uint32_t seen[];
+  __shared__ long long scan_sm[33];
+  bool ok = slots_distinct(dst, n, v.max_seqs, seen);
+  long long want = 0;
+  if (ok) {
+    bool fine = true;
+    for (int base = 0; base < n; base += blockDim.x) {
+      const int i = base + threadIdx.x;
+      long long need = 0, total;
+      if (i < n) {
+        const int s = src[i];
+        if (s < 0 || s >= v.max_seqs || (seen[s >> 5] >> (s & 31) & 1)) {
+          fine = false;
+        } else {
+          const int have = v.lengths[s], len = lens ? lens[i] : have;
+          if (len < 0 || len > have || have > v.max_pages * kPageTokens) fine = false;
+          else need = len % kPageTokens != 0;
+        }
+      }
+      block_scan(need, &total, scan_sm);
+      want += total;
+    }
+    ok = __syncthreads_and(fine);
+    if (ok) {  // every page that will be shared or copied is a page
+      for (int i = threadIdx.x >> 5; i < n; i += blockDim.x >> 5) {
+        const int32_t* row = v.table + (int64_t)src[i] * v.max_pages;
+        const int pages = pages_of(lens ? lens[i] : v.lengths[src[i]]);
+        for (int j = threadIdx.x & 31; j < pages; j += 32) fine = fine && row[j] >= 0 && row[j] < v.num_pages;
+      }
+      ok = __syncthreads_and(fine) && want <= v.num_pages;
+    }
+  }
+  if (ok) {
+    count_rows(v, dst, n, -1);  // what the destinations held counts as free
+    ok = first_free(v, (int)want, ws.to, scan_sm);
+    if (!ok) count_rows(v, dst, n, 1);
+  }
+  if (threadIdx.x == 0) {
+    ws.head->ok = ok;
+    ws.head->copies = (int)want;
+    if (!ok) cache_fault(status);
+  }
+  if (!ok) return;
+  long long before = 0;
+  for (int base = 0; base < n; base += blockDim.x) {
+    const int i = base + threadIdx.x;
+    long long need = 0, total;
+    int len = 0, s = 0;
+    if (i < n) {
+      s = src[i];
+      len = lens ? lens[i] : v.lengths[s];
+      need = len % kPageTokens != 0;
+    }
+    const long long at = before + block_scan(need, &total, scan_sm);
+    before += total;
+    if (i < n) {
+      ws.extra[i] = need ? ws.to[at] : -1;
+      if (need) ws.from[at] = v.table[(int64_t)s * v.max_pages + len / kPageTokens];
+    }
+  }
+}
+
+// Page copies from[i] -> to[i], i < copies, in every layer: units of 256 threads x 4 x 16 bytes over the whole grid.
+__device__ __forceinline__ void copy_pages(const CacheView& v, const PlanSpace& ws, int copies) {
+  constexpr int kPer = 4;
+  const int per_page = (int)(v.page_bytes / 16);  // 16-byte words (a multiple of 288)
+  const int pieces = (per_page + 256 * kPer - 1) / (256 * kPer);
+  const int64_t units = (int64_t)copies * v.layers * pieces;
+  for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
+    const int piece = (int)(u % pieces);
+    const int64_t rest = u / pieces;
+    const int i = (int)(rest % copies), layer = (int)(rest / copies);
+    uint8_t* base = v.pages + layer * v.layer_bytes;
+    const uint4* src = reinterpret_cast<const uint4*>(base + ws.from[i] * v.page_bytes);
+    uint4* dst = reinterpret_cast<uint4*>(base + ws.to[i] * v.page_bytes);
+    uint4 x[kPer];
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      const int at = (piece * kPer + j) * 256 + threadIdx.x;
+      if (at < per_page) x[j] = __ldcs(src + at);
+    }
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      const int at = (piece * kPer + j) * 256 + threadIdx.x;
+      if (at < per_page) __stcs(dst + at, x[j]);
+    }
+  }
+}
+
+__global__ void __launch_bounds__(256) fork_kernel(CacheView v, const int32_t* src, const int32_t* dst, const int32_t* lens, int n, PlanSpace ws) {
+  if (!ws.head->ok) return;
+  for (int i = blockIdx.x; i < n; i += gridDim.x) {
+    const int s = src[i], d = dst[i], len = lens ? lens[i] : v.lengths[s], full = len / kPageTokens, last = ws.extra[i];
+    const int32_t* from = v.table + (int64_t)s * v.max_pages;
+    int32_t* to = v.table + (int64_t)d * v.max_pages;
+    for (int j = threadIdx.x; j < v.max_pages; j += 256) {
+      const int page = j < full ? from[j] : j == full ? last : -1;
+      to[j] = page;
+      if (page >= 0) atomicAdd(v.refs + page, 1);
+    }
+    if (threadIdx.x == 0) v.lengths[d] = len;
+  }
+  copy_pages(v, ws, ws.head->copies);
+}
+
+__global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(CacheView v, PlanSpace ws, int32_t* used_out) {
+  __shared__ long long scan_sm[33];
+  long long used = 0;
+  for (int base = 0; base < v.num_pages; base += blockDim.x) {
+    const int p = base + threadIdx.x;
+    long long total;
+    block_scan(p < v.num_pages && v.refs[p] > 0, &total, scan_sm);
+    used += total;
+  }
+  long long holes = 0, movers = 0;
+  for (int base = 0; base < v.num_pages; base += blockDim.x) {
+    const int p = base + threadIdx.x;
+    const bool in = p < v.num_pages, busy = in && v.refs[p] > 0;
+    const bool hole = in && !busy && p < used, mover = busy && p >= used;
+    long long total;
+    const long long both = block_scan((hole ? 1LL << 32 : 0) + mover, &total, scan_sm);
+    if (hole) ws.to[holes + (both >> 32)] = p;
+    if (mover) ws.from[movers + (both & 0xffffffff)] = p;
+    if (in) ws.extra[p] = p;
+    holes += total >> 32;
+    movers += total & 0xffffffff;
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < movers; i += blockDim.x) {
+    const int from = ws.from[i], to = ws.to[i];
+    ws.extra[from] = to;
+    v.refs[to] = v.refs[from];
+    v.refs[from] = 0;
+  }
+  if (threadIdx.x == 0) {
+    ws.head->ok = 1;
+    ws.head->copies = (int)movers;
+    if (used_out) *used_out = (int)used;
+  }
+}
+__global__ void __launch_bounds__(256) compact_kernel(CacheView v, PlanSpace ws) {
+  const int copies = ws.head->copies;
+  if (copies == 0) return;
+  const int64_t entries = (int64_t)v.max_seqs * v.max_pages;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < entries; i += (int64_t)gridDim.x * 256) {
+    const int page = v.table[i];
+    if (page >= 0 && page < v.num_pages) {
+      const int to = ws.extra[page];
+      if (to != page) v.table[i] = to;
+    }
+  }
+  copy_pages(v, ws, copies);
+}
+
+// ------------------------------------------------------------------------------------------------ host side
+// The context's device is made current for the length of a call (the caller's is put back).
+class DeviceGuard {
+ public:
+  explicit DeviceGuard(int device) {
+    if (cudaGetDevice(&before_) != cudaSuccess) before_ = device;
+    if (before_ != device) cudaSetDevice(device);
+    device_ = device;
+  }
+  ~DeviceGuard() {
+    if (before_ != device_) cudaSetDevice(before_);
+  }
+  DeviceGuard(const DeviceGuard&) = delete;
+
+ private:
+  int before_ = 0, device_ = 0;
+};
+
+const char* desc_problem(const essa_cache_desc* c, int32_t* code) {
+  *code = ESSA_ERR_INVALID_ARG;
+  if (!c) return "NULL descriptor";
+  if (c->layers < 1 || c->num_pages < 1 || c->kv_heads < 1 || c->max_seqs < 1 || c->max_pages < 1) return "sizes must be positive";
+  if (!c->pages || !c->table || !c->lengths || !c->refs) return "NULL buffer in the descriptor";
+  if (reinterpret_cast<uintptr_t>(c->pages) & 15) return "pages must be 16-byte aligned";
+  if ((reinterpret_cast<uintptr_t>(c->table) | reinterpret_cast<uintptr_t>(c->lengths) | reinterpret_cast<uintptr_t>(c->refs)) & 3) return "table, lengths and refs must be 4-byte aligned";
+  *code = ESSA_ERR_UNSUPPORTED_SHAPE;
+  if (c->head_dim != 64 && c->head_dim != 128) return "head_dim must be 64 or 128";
+  if (c->max_seqs > ESSA_CACHE_MAX_SEQS) return "max_seqs > ESSA_CACHE_MAX_SEQS";
+  if (c->max_pages > 0x7fffffff / ESSA_CACHE_PAGE_TOKENS) return "max_pages * 64 must be below 2^31";
+  if (c->kv_heads > 4096) return "kv_heads > 4096";
+  *code = ESSA_OK;
+  return nullptr;
+}
+
+int32_t view_of(essa_ctx* ctx, const char* what, const essa_cache_desc* c, int32_t layer, CacheView* v) {
+  if (!ctx) return ESSA_ERR_INVALID_ARG;
+  int32_t code;
+  if (const char* why = desc_problem(c, &code)) return fail(ctx, code, std::string(what) + ": " + why);
+  if (layer < 0 || layer >= c->layers) return fail(ctx, ESSA_ERR_INVALID_ARG, std::string(what) + ": layer outside the cache");
+  v->page_bytes = essa_cache_page_bytes(c->kv_heads, c->head_dim);
+  v->layer_bytes = v->page_bytes * c->num_pages;
+  v->pages = static_cast<uint8_t*>(c->pages) + layer * v->layer_bytes;
+  v->table = c->table;
+  v->lengths = c->lengths;
+  v->refs = c->refs;
+  v->num_pages = c->num_pages;
+  v->kv_heads = c->kv_heads;
+  v->head_dim = c->head_dim;
+  v->max_seqs = c->max_seqs;
+  v->max_pages = c->max_pages;
+  v->layers = c->layers;
+  return ESSA_OK;
+}
+
+int32_t check_entries(essa_ctx* ctx, const char* what, const CacheEntries& e) {
+  if (e.n < 0 || e.T < 0) return fail(ctx, ESSA_ERR_INVALID_ARG, std::string(what) + ": negative n or T");
+  if (!e.off && e.n != e.T) return fail(ctx, ESSA_ERR_INVALID_ARG, std::string(what) + ": without tok_offsets every entry has one row (n = T)");
+  return ESSA_OK;
+}
+// A token-major bf16 buffer of `width` elements per row.
+int32_t check_rows(essa_ctx* ctx, const char* what, const char* name, const void* p, int64_t ld, int64_t width) {
+  if (!p) return fail(ctx, ESSA_ERR_INVALID_ARG, std::string(what) + ": " + name + " is NULL");
+  if (reinterpret_cast<uintptr_t>(p) & 15) return fail(ctx, ESSA_ERR_INVALID_ARG, std::string(what) + ": " + name + " must be 16-byte aligned");
+  if (ld < width || ld % 8) return fail(ctx, ESSA_ERR_INVALID_ARG, std::string(what) + ": the row pitch of " + name + " must be a multiple of 8 elements and hold a row");
+  return ESSA_OK;
+}
+int64_t pages_workspace(const essa_cache_desc* c) {
+  return 256 + 4 * (2 * (int64_t)c->num_pages + (c->num_pages > c->max_seqs ? c->num_pages : c->max_seqs));
+}
+int32_t check_workspace(essa_ctx* ctx, const char* what, const void* ws, int64_t bytes, int64_t need) {
+  if (!ws || (reinterpret_cast<uintptr_t>(ws) & 15)) return fail(ctx, ESSA_ERR_INVALID_ARG, std::string(what) + ": the workspace must be a 16-byte aligned device buffer");
+  if (bytes < need) return fail(ctx, ESSA_ERR_INVALID_ARG, std::string(what) + ": the workspace is too small");
+  return ESSA_OK;
+}
+int32_t launched(essa_ctx* ctx, const char* what, int kernels) {
+  ctx->launches += kernels;
+  return check_cuda(ctx, cudaGetLastError(), what);
+}
+size_t seen_bytes(const CacheView& v) { return (size_t)(v.max_seqs + 31) / 32 * 4; }
+int copy_grid(const essa_ctx* ctx) { return ctx->sm_count * 8; }
+
+}  // namespace
+}  // namespace essa
+
+using namespace essa;
+
+#define ESSA_TRY(call)                     \
+  do {                                     \
+    const int32_t st_ = (call);            \
+    if (st_ != ESSA_OK) return st_;        \
+  } while (0)
+
+extern "C" {
+
+int64_t essa_cache_page_bytes(int32_t kv_heads, int32_t head_dim) {
+  return kv_heads < 1 || (head_dim != 64 && head_dim != 128) ? 0 : (int64_t)72 * kv_heads * head_dim;
+}
+
+int32_t essa_cache_validate(const essa_cache_desc* cache) {
+  int32_t code;
+  desc_problem(cache, &code);
+  return code;
+}
+
+int32_t essa_cache_pages_workspace(const essa_cache_desc* cache, int64_t* bytes) {
+  ESSA_TRY(essa_cache_validate(cache));
+  if (!bytes) return ESSA_ERR_INVALID_ARG;
+  *bytes = pages_workspace(cache);
+  return ESSA_OK;
+}
+
+int32_t essa_cache_attend_workspace(const essa_cache_desc* cache, int32_t q_heads, int32_t max_new, int32_t sm_count, int64_t* bytes) {
+  ESSA_TRY(essa_cache_validate(cache));
+  if (!bytes || q_heads < 1 || q_heads % cache->kv_heads || max_new < 1 || sm_count < 1) return ESSA_ERR_INVALID_ARG;
+  *bytes = attend_decode_workspace(cache->head_dim, (int64_t)max_new * (q_heads / cache->kv_heads), sm_count);
+  return ESSA_OK;
+}
+
+int32_t essa_cache_reset(essa_ctx* ctx, const essa_cache_desc* cache, void* stream_v) {
+  CacheView v;
+  ESSA_TRY(view_of(ctx, "cache_reset", cache, 0, &v));
+  DeviceGuard guard(ctx->device);
+  cudaStream_t stream = static_cast<cudaStream_t>(stream_v);
+  ESSA_TRY(check_cuda(ctx, cudaMemsetAsync(v.table, 0xff, (size_t)v.max_seqs * v.max_pages * 4, stream), "cache_reset"));
+  ESSA_TRY(check_cuda(ctx, cudaMemsetAsync(v.lengths, 0, (size_t)v.max_seqs * 4, stream), "cache_reset"));
+  return check_cuda(ctx, cudaMemsetAsync(v.refs, 0, (size_t)v.num_pages * 4, stream), "cache_reset");
+}
+
+int32_t essa_cache_grow(essa_ctx* ctx, const essa_cache_desc* cache, const int32_t* slots, const int32_t* counts, int32_t n, void* workspace,
+                        int64_t workspace_bytes, void* stream) {
+  CacheView v;
+  ESSA_TRY(view_of(ctx, "cache_grow", cache, 0, &v));
+  if (n < 0 || n > v.max_seqs) return fail(ctx, ESSA_ERR_INVALID_ARG, "cache_grow: n outside 0 .. max_seqs");
+  if (n == 0) return ESSA_OK;
+  if (!counts) return fail(ctx, ESSA_ERR_INVALID_ARG, "cache_grow: counts is NULL");
+  ESSA_TRY(check_workspace(ctx, "cache_grow", workspace, workspace_bytes, pages_workspace(cache)));
+  DeviceGuard guard(ctx->device);
+  grow_kernel<<<1, kPlanThreads, seen_bytes(v), static_cast<cudaStream_t>(stream)>>>(v, slots, counts, n, plan_space(workspace, v), ctx->d_status);
+  return launched(ctx, "cache_grow", 1);
+}
+
+int32_t essa_cache_append(essa_ctx* ctx, const essa_cache_desc* cache, int32_t layer, const void* k, int64_t ld_k, const void* val, int64_t ld_v, int32_t T,
+                          const int32_t* slots, const int32_t* tok_offsets, int32_t n, void* stream_v) {
+  CacheView v;
+  ESSA_TRY(view_of(ctx, "cache_append", cache, layer, &v));
+  const CacheEntries e{slots, tok_offsets, n, T};
+  ESSA_TRY(check_entries(ctx, "cache_append", e));
+  if (T == 0 || n == 0) return ESSA_OK;
+  ESSA_TRY(check_rows(ctx, "cache_append", "k", k, ld_k, (int64_t)v.kv_heads * v.head_dim));
+  ESSA_TRY(check_rows(ctx, "cache_append", "v", val, ld_v, (int64_t)v.kv_heads * v.head_dim));
+  DeviceGuard guard(ctx->device);
+  const int64_t blocks = ((int64_t)T * v.kv_heads * (v.head_dim / 8) + 255) / 256;
+  if (blocks > 0x7fffffff) return fail(ctx, ESSA_ERR_UNSUPPORTED_SHAPE, "cache_append: too many tokens");
+  const auto *kk = static_cast<const __nv_bfloat16*>(k), *vv = static_cast<const __nv_bfloat16*>(val);
+  cudaStream_t stream = static_cast<cudaStream_t>(stream_v);
+  if (v.head_dim == 64) append_kernel<64><<<(unsigned)blocks, 256, 0, stream>>>(v, e, kk, ld_k, vv, ld_v, ctx->d_status);
+  else append_kernel<128><<<(unsigned)blocks, 256, 0, stream>>>(v, e, kk, ld_k, vv, ld_v, ctx->d_status);
+  return launched(ctx, "cache_append", 1);
+}
+
+int32_t essa_cache_read(essa_ctx* ctx, const essa_cache_desc* cache, int32_t layer, void* k_out, void* v_out, int32_t T, const int32_t* slots,
+                        const int32_t* tok_offsets, int32_t n, void* stream_v) {
+  CacheView v;
+  ESSA_TRY(view_of(ctx, "cache_read", cache, layer, &v));
+  const CacheEntries e{slots, tok_offsets, n, T};
+  ESSA_TRY(check_entries(ctx, "cache_read", e));
+  if (T == 0 || n == 0 || (!k_out && !v_out)) return ESSA_OK;
+  const int64_t width = (int64_t)v.kv_heads * v.head_dim;
+  if (k_out) ESSA_TRY(check_rows(ctx, "cache_read", "k_out", k_out, width, width));
+  if (v_out) ESSA_TRY(check_rows(ctx, "cache_read", "v_out", v_out, width, width));
+  DeviceGuard guard(ctx->device);
+  const int64_t blocks = ((int64_t)T * v.kv_heads * (v.head_dim / 8) + 255) / 256;
+  if (blocks > 0x7fffffff) return fail(ctx, ESSA_ERR_UNSUPPORTED_SHAPE, "cache_read: too many tokens");
+  auto *kk = static_cast<__nv_bfloat16*>(k_out), *vv = static_cast<__nv_bfloat16*>(v_out);
+  cudaStream_t stream = static_cast<cudaStream_t>(stream_v);
+  if (v.head_dim == 64) read_kernel<64><<<(unsigned)blocks, 256, 0, stream>>>(v, e, kk, vv, ctx->d_status);
+  else read_kernel<128><<<(unsigned)blocks, 256, 0, stream>>>(v, e, kk, vv, ctx->d_status);
+  return launched(ctx, "cache_read", 1);
+}
+
+int32_t essa_cache_attend(essa_ctx* ctx, const essa_cache_desc* cache, int32_t layer, const void* q, int64_t ld_q, int32_t q_heads, int32_t T,
+                          const int32_t* slots, const int32_t* tok_offsets, int32_t n, int32_t max_new, float scale, void* out, int64_t ld_out,
+                          void* workspace, int64_t workspace_bytes, void* stream) {
+  CacheView v;
+  ESSA_TRY(view_of(ctx, "cache_attend", cache, layer, &v));
+  const CacheEntries e{slots, tok_offsets, n, T};
+  ESSA_TRY(check_entries(ctx, "cache_attend", e));
+  if (q_heads < 1 || q_heads % v.kv_heads) return fail(ctx, ESSA_ERR_INVALID_ARG, "cache_attend: q_heads must be a multiple of kv_heads");
+  if (max_new < 1) return fail(ctx, ESSA_ERR_INVALID_ARG, "cache_attend: max_new must be at least 1");
+  if (!(scale > 0.f) || !std::isfinite(scale)) return fail(ctx, ESSA_ERR_INVALID_ARG, "cache_attend: scale must be positive and finite");
+  const int64_t group = q_heads / v.kv_heads;
+  if (group * T > 0x7fffffff) return fail(ctx, ESSA_ERR_UNSUPPORTED_SHAPE, "cache_attend: T * (q_heads / kv_heads) must be below 2^31");
+  if (T == 0 || n == 0) return ESSA_OK;
+  ESSA_TRY(check_rows(ctx, "cache_attend", "q", q, ld_q, (int64_t)q_heads * v.head_dim));
+  ESSA_TRY(check_rows(ctx, "cache_attend", "out", out, ld_out, (int64_t)q_heads * v.head_dim));
+  int64_t need;
+  ESSA_TRY(essa_cache_attend_workspace(cache, q_heads, max_new, ctx->sm_count, &need));
+  ESSA_TRY(check_workspace(ctx, "cache_attend", workspace, workspace_bytes, need));
+  DeviceGuard guard(ctx->device);
+  return launch_attend_decode(ctx, v, e, static_cast<const __nv_bfloat16*>(q), ld_q, q_heads, max_new * group, scale, static_cast<__nv_bfloat16*>(out), ld_out,
+                              workspace, static_cast<cudaStream_t>(stream));
+}
+
+int32_t essa_cache_fork(essa_ctx* ctx, const essa_cache_desc* cache, const int32_t* src, const int32_t* dst, const int32_t* lens, int32_t n, void* workspace,
+                        int64_t workspace_bytes, void* stream_v) {
+  CacheView v;
+  ESSA_TRY(view_of(ctx, "cache_fork", cache, 0, &v));
+  if (n < 0 || n > v.max_seqs) return fail(ctx, ESSA_ERR_INVALID_ARG, "cache_fork: n outside 0 .. max_seqs");
+  if (n == 0) return ESSA_OK;
+  if (!src || !dst) return fail(ctx, ESSA_ERR_INVALID_ARG, "cache_fork: src or dst is NULL");
+  ESSA_TRY(check_workspace(ctx, "cache_fork", workspace, workspace_bytes, pages_workspace(cache)));
+  DeviceGuard guard(ctx->device);
+  cudaStream_t stream = static_cast<cudaStream_t>(stream_v);
+  const PlanSpace ws = plan_space(workspace, v);
+  fork_plan_kernel<<<1, kPlanThreads, seen_bytes(v), stream>>>(v, src, dst, lens, n, ws, ctx->d_status);
+  ESSA_TRY(launched(ctx, "cache_fork", 1));
+  fork_kernel<<<copy_grid(ctx), 256, 0, stream>>>(v, src, dst, lens, n, ws);
+  return launched(ctx, "cache_fork", 1);
+}
+
+int32_t essa_cache_free(essa_ctx* ctx, const essa_cache_desc* cache, const int32_t* slots, int32_t n, void* stream) {
+  CacheView v;
+  ESSA_TRY(view_of(ctx, "cache_free", cache, 0, &v));
+  if (n < 0 || n > v.max_seqs) return fail(ctx, ESSA_ERR_INVALID_ARG, "cache_free: n outside 0 .. max_seqs");
+  if (n == 0) return ESSA_OK;
+  DeviceGuard guard(ctx->device);
+  const int grid = n < ctx->sm_count * 4 ? n : ctx->sm_count * 4;
+  free_kernel<<<grid, 256, seen_bytes(v), static_cast<cudaStream_t>(stream)>>>(v, slots, n, ctx->d_status);
+  return launched(ctx, "cache_free", 1);
+}
+
+int32_t essa_cache_compact(essa_ctx* ctx, const essa_cache_desc* cache, int32_t* used, void* workspace, int64_t workspace_bytes, void* stream_v) {
+  CacheView v;
+  ESSA_TRY(view_of(ctx, "cache_compact", cache, 0, &v));
+  ESSA_TRY(check_workspace(ctx, "cache_compact", workspace, workspace_bytes, pages_workspace(cache)));
+  DeviceGuard guard(ctx->device);
+  cudaStream_t stream = static_cast<cudaStream_t>(stream_v);
+  const PlanSpace ws = plan_space(workspace, v);
+  compact_plan_kernel<<<1, kPlanThreads, 0, stream>>>(v, ws, used);
+  ESSA_TRY(launched(ctx, "cache_compact", 1));
+  compact_kernel<<<copy_grid(ctx), 256, 0, stream>>>(v, ws);
+  return launched(ctx, "cache_compact", 1);
+}
+
+}  // extern "C"

@@ -1,0 +1,577 @@
+// Attention over the paged 4-bit cache for few rows per sequence (decode steps): softmax(scale q K^T) V with
+// K = code * scale + minimum per token and group of 64 channels.
+//
+// What bounds it: the cache is read once and each byte carries two values, so a B200 streams ~46 codes per clock and SM
+// from HBM; what the kernel has to keep up with is widening them.  The mathematics is arranged so that a code needs only
+// (shift, and-or) for K and one subtraction more for V:
+//   S = sum_g s_g (q_g . c_g) + min_g sum(q_g).  The tensor core multiplies q by the bf16 numbers 128 + c (a code dropped
+//   into the mantissa of 128); with acc_g = q_g . (128 + c_g) in fp32, S = sum_g s_g acc_g + (min_g - 128 s_g) sum(q_g).
+//   O = sum_k p_k (s_k (c_k - 8) + (min_k + 8 s_k)): p_k s_k is rounded to bf16 (one rounding, 2^-9 of a centred value: with the
+//   codes not centred it would be 2^-9 of a number 2.6 times as large), the second term stays on the CUDA cores in fp32.
+//   (Leaving the 128 in and subtracting 136 sum(p s) at the end loses the result in fp32: |128 s| against averages of
+//   thousands of values.)
+// K and V are the M = 16 operand of mma.m16n8k16, the query rows (heads of the group x tokens) are the N = 8 columns: a
+// group of up to eight heads fills the tensor core's tile, where q as the M operand would leave half of it empty.
+//
+// Work split: the (entry, kv head, row block, page) list of the whole call is cut into equal runs, one per thread block, so that
+// ragged lengths and single long sequences balance alike; a (row block) cut by a run boundary leaves fp32 partial results
+// in the workspace, which a second kernel joins in a fixed order (no atomics: the same bits every time).
+#include "cache.cuh"
+#include "tc_ptx.cuh"
+
+namespace essa {
+namespace {
+
+constexpr int kWarps = 4;                     // consuming warps: 16 tokens of a page each
+constexpr int kThreads = kWarps * 32 + 32;    // + one copying warp
+constexpr float kLog2e = 1.4426950408889634f;
+
+struct AttendArgs {
+  CacheView v;
+  CacheEntries e;
+  const __nv_bfloat16* q;
+  __nv_bfloat16* out;
+  int64_t ld_q, ld_out;
+  int32_t group;
+  float scale;  // softmax scale * log2(e)
+  float* ws;
+  int32_t* status;
+};
+
+// Row blocks of an entry and the pages each of them reads (at least one, so that rows that see nothing are still written).
+__device__ __forceinline__ void entry_shape(const EntryInfo& e, int group, int R, int& blocks, int& tiles) {
+  blocks = (int)(((int64_t)e.rows * group + R - 1) / R);
+  tiles = max((e.len + kPageTokens - 1) / kPageTokens, 1);
+}
+
+struct Cursor {  // a place in the list of (entry, kv head, row block, page)
+  int entry, kvh, rb, tile, blocks, tiles;
+  EntryInfo info;
+};
+
+// Total number of list elements, and (threads in step) the place of element `at`.  sm: [33] shared.
+__device__ long long list_total(const AttendArgs& a, int R, long long* sm) {
+  long long total = 0;
+  for (int base = 0; base < a.e.n; base += blockDim.x) {
+    const int i = base + threadIdx.x;
+    long long w = 0, t;
+    if (i < a.e.n) {
+      int b, k;
+      entry_shape(load_entry(a.v, a.e, i), a.group, R, b, k);
+      w = (long long)b * k * a.v.kv_heads;
+    }
+    block_scan(w, &t, sm);
+    total += t;
+  }
+  return total;
+}
+__device__ void list_seek(const AttendArgs& a, int R, long long at, Cursor& c, long long* sm, int* found /* shared [3] */) {
+  long long before = 0;
+  for (int base = 0; base < a.e.n; base += blockDim.x) {
+    const int i = base + threadIdx.x;
+    long long w = 0, t;
+    int b = 0, k = 1;
+    if (i < a.e.n) {
+      entry_shape(load_entry(a.v, a.e, i), a.group, R, b, k);
+      w = (long long)b * k * a.v.kv_heads;
+    }
+    const long long pre = before + block_scan(w, &t, sm);
+    if (w > 0 && at >= pre && at < pre + w) {
+      const long long rest = at - pre;
+      found[0] = i;
+      found[1] = (int)(rest / k);  // kv head * blocks + row block
+      found[2] = (int)(rest % k);
+    }
+    before += t;
+    __syncthreads();
+    if (at < before) break;
+  }
+  c.entry = found[0];
+  c.info = load_entry(a.v, a.e, c.entry);
+  entry_shape(c.info, a.group, R, c.blocks, c.tiles);
+  c.kvh = found[1] / c.blocks;
+  c.rb = found[1] % c.blocks;
+  c.tile = found[2];
+}
+// The row block after c's (its first page); false at the end of the list.
+__device__ __forceinline__ void next_block(const AttendArgs& a, int R, Cursor& c) {
+  c.tile = 0;
+  if (++c.rb < c.blocks) return;
+  c.rb = 0;
+  if (++c.kvh < a.v.kv_heads) return;
+  c.kvh = 0;
+  do {
+    if (++c.entry >= a.e.n) return;
+    c.info = load_entry(a.v, a.e, c.entry);
+    entry_shape(c.info, a.group, R, c.blocks, c.tiles);
+  } while (c.blocks == 0);
+}
+
+__device__ __forceinline__ long long run_start(long long total, int runs, int c) { return total * c / runs; }
+// Thread blocks that share the list: every run has at least two pages (a run of one would pay its fixed cost and a join for it).
+__device__ __forceinline__ int run_count(long long total, int grid) { return (int)max(1LL, min((long long)grid, (total + 1) / 2)); }
+
+__device__ __forceinline__ void ldmatrix_x4(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldmatrix_x4_trans(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ uint32_t movmatrix_trans(uint32_t v) {
+  uint32_t r;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
+__device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ float ex2(float x) { return exp2f(x); }
+// Nibble j of both halves of w as the bf16 pair (128 + low, 128 + high).
+template <int J>
+__device__ __forceinline__ uint32_t nibbles(uint32_t w) {
+  return ((w >> (4 * J)) & 0x000f000fu) | 0x43004300u;
+}
+// ... centred: (code - 8), exact.
+template <int J>
+__device__ __forceinline__ uint32_t nibbles_centred(uint32_t w) {
+  const uint32_t x = nibbles<J>(w), o = 0x43084308u;  // 136
+  const __nv_bfloat162 r = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&x), *reinterpret_cast<const __nv_bfloat162*>(&o));
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+__device__ __forceinline__ float2 lds_half2(uint32_t addr) {
+  uint32_t v;
+  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+  return __half22float2(*reinterpret_cast<__half2*>(&v));
+}
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+
+template <int D, int NT>
+struct Shape {
+  static constexpr int R = 8 * NT;             // query rows of a row block
+  static constexpr int kBytes = 72 * D;        // a (page, kv head) run
+  static constexpr int kStages = (D == 128 ? 6 : 10);
+  static constexpr int kPart = R * (D + 2);    // floats of a partial result: O [R][D], max [R], sum [R]
+  static constexpr int kJoin = kWarps * R * (D + 2) * 4;
+  static constexpr int kSmem = kStages * kBytes + kJoin + 256;
+};
+
+// Thread blocks per SM: what shared memory and registers allow.
+constexpr int attend_blocks_per_sm(int head_dim, int nt) { return nt == 1 ? 3 : 2; }
+
+template <int D, int NT>
+__global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_decode_kernel(AttendArgs a) {
+  using S = Shape<D, NT>;
+  constexpr int R = S::R, G = D / kCacheGroup, CH = D / 32;
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ long long scan_sm[33];
+  __shared__ int found[3];
+  __shared__ volatile int abort_flag;
+  __shared__ int bad_page[S::kStages];
+  __shared__ __align__(8) uint64_t bars[2 * S::kStages];
+  float* join = reinterpret_cast<float*>(smem + S::kStages * S::kBytes);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const uint32_t ring = smem_u32(smem), full = smem_u32(bars), empty = full + 8 * S::kStages;
+  grid_dep_launch();
+  if (tid == 0) {
+    abort_flag = 0;
+    for (int s = 0; s < S::kStages; ++s) { mbar_init(full + 8 * s, 1); mbar_init(empty + 8 * s, kWarps); }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncthreads();
+  const long long total = list_total(a, R, scan_sm);
+  if (total == 0) return;
+  const int runs = run_count(total, gridDim.x);
+  if ((int)blockIdx.x >= runs) return;
+  const long long begin = run_start(total, runs, blockIdx.x), end = run_start(total, runs, blockIdx.x + 1);
+  Cursor c;
+  list_seek(a, R, begin, c, scan_sm, found);
+  long long left = end - begin;
+
+  if (warp == kWarps) {  // ---------------------------------------------------------------- copying warp
+    if (lane != 0) return;
+    int st = 0, filled = 0;
+    uint32_t phase = 0;
+    bool ok = true;
+    while (ok && left > 0) {
+      const int stop = (int)min((long long)c.tiles, c.tile + left);
+      left -= stop - c.tile;
+      const int32_t* row = a.v.table + (int64_t)max(c.info.slot, 0) * a.v.max_pages;
+      const bool none = c.info.len == 0;
+      for (; c.tile < stop; ++c.tile) {
+        if (filled >= S::kStages && !mbar_wait(empty + 8 * st, phase ^ 1, &abort_flag, a.status)) { ok = false; break; }
+        const int page = none ? -1 : __ldg(row + c.tile);
+        const bool there = page >= 0 && page < a.v.num_pages;
+        if (!there && (!none || c.info.slot < 0)) cache_fault(a.status);
+        bad_page[st] = !there;
+        if (there) {
+          mbar_expect_tx(full + 8 * st, S::kBytes);
+          bulk_load(ring + st * S::kBytes, a.v.pages + page * a.v.page_bytes + (int64_t)c.kvh * S::kBytes, S::kBytes, full + 8 * st);
+        } else {
+          mbar_arrive(full + 8 * st);
+        }
+        ++filled;
+        if (++st == S::kStages) { st = 0; phase ^= 1; }
+      }
+      if (left > 0) next_block(a, R, c);
+    }
+    if (!ok) {  // the copies in flight land (a bounded wait) before the block's shared memory goes away
+      for (int s = 0; s < S::kStages && s < filled; ++s) {
+        const uint32_t last = ((filled - 1 - s) / S::kStages) & 1;
+        const long long t0 = clock64();
+        while (!mbar_try_wait(full + 8 * s, last) && clock64() - t0 < kWaitLimitCycles / 16) {}
+      }
+    }
+    return;
+  }
+
+  // ----------------------------------------------------------------------------------------- consuming warps
+  const int g = lane >> 2, t = lane & 3;
+  const int key0 = warp * 16;                                                 // this warp's tokens of a page
+  const uint32_t k_lane = (uint32_t)(key0 + (lane & 15)) * 16 + (uint32_t)(lane >> 4) * 1024;  // ldmatrix row addresses: (tokens 0-7, 8-15) x two chunks
+  int st = 0;
+  uint32_t phase = 0;
+  bool dead = false;  // a wait ran out: the warp goes through the barriers with the others and does nothing else
+  while (left > 0) {
+    const int rows = c.info.rows * a.group;  // (fits: T * group is checked on the host)
+    const int r0 = c.rb * R;
+    // --- query operand: lane (g, t) holds channels 32 h + 8 t .. + 7 of column g, in the order that the nibbles come in
+    uint32_t qf[NT][CH][4];
+    float qsum[NT][G][2];
+    int limit[NT][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const int r = r0 + nt * 8 + g;
+      const int j = r / a.group, hd = r - j * a.group;
+      const bool there = r < rows;
+      const uint4* src = reinterpret_cast<const uint4*>(a.q + (int64_t)(c.info.row0 + (there ? j : 0)) * a.ld_q + (int64_t)(c.kvh * a.group + hd) * D) + t;
+      float sum[G];
+#pragma unroll
+      for (int i = 0; i < G; ++i) sum[i] = 0.f;
+#pragma unroll
+      for (int h = 0; h < CH; ++h) {
+        const uint4 u = there ? __ldg(src + h * 4) : make_uint4(0, 0, 0, 0);
+        qf[nt][h][0] = __byte_perm(u.x, u.z, 0x5410);
+        qf[nt][h][1] = __byte_perm(u.x, u.z, 0x7632);
+        qf[nt][h][2] = __byte_perm(u.y, u.w, 0x5410);
+        qf[nt][h][3] = __byte_perm(u.y, u.w, 0x7632);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) sum[h / 2] += __uint_as_float(qf[nt][h][x] << 16) + __uint_as_float(qf[nt][h][x] & 0xffff0000u);
+      }
+#pragma unroll
+      for (int i = 0; i < G; ++i) {
+        sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], 1);
+        sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], 2);
+        qsum[nt][i][0] = __shfl_sync(0xffffffffu, sum[i], 8 * t);
+        qsum[nt][i][1] = __shfl_sync(0xffffffffu, sum[i], 8 * t + 4);
+      }
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {  // tokens that column 2 t + x sees
+        const int rc = r0 + nt * 8 + 2 * t + x;
+        limit[nt][x] = rc < rows ? c.info.len - c.info.rows + rc / a.group + 1 : 0;
+      }
+    }
+    float o[NT][CH][2][4];
+    float mx[NT][2], l[NT][2], om[NT][G][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+      for (int h = 0; h < CH; ++h)
+#pragma unroll
+        for (int x = 0; x < 8; ++x) o[nt][h][x >> 2][x & 3] = 0.f;
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        mx[nt][x] = -INFINITY;
+        l[nt][x] = 0.f;
+#pragma unroll
+        for (int i = 0; i < G; ++i) om[nt][i][x] = 0.f;
+      }
+    }
+    const int first = c.tile, stop = (int)min((long long)c.tiles, c.tile + left);
+    for (int tile = first; tile < stop; ++tile) {
+      dead = dead || !mbar_wait(full + 8 * st, phase, &abort_flag, a.status);
+      if (dead) continue;
+      const uint32_t blk = ring + st * S::kBytes;
+      const int pos = tile * kPageTokens + key0 + g;  // tokens of this lane's scores: pos, pos + 8
+      const bool bad = bad_page[st] != 0;
+      const bool in0 = !bad && pos < c.info.len, in1 = !bad && pos + 8 < c.info.len;
+      if (!bad && tile * kPageTokens + key0 < c.info.len) {
+        // --- scores
+        float s[NT][4];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) s[nt][x] = 0.f;
+#pragma unroll
+        for (int i = 0; i < G; ++i) {
+          float acc[NT][4];
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) acc[nt][x] = 0.f;
+          uint32_t w[4];  // chunk 2i: tokens g, g + 8; chunk 2i + 1: tokens g, g + 8
+          ldmatrix_x4(blk + k_lane + i * 2048, w);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const uint32_t a00 = nibbles<0>(w[2 * h]), a01 = nibbles<0>(w[2 * h + 1]), a02 = nibbles<1>(w[2 * h]), a03 = nibbles<1>(w[2 * h + 1]);
+            const uint32_t a10 = nibbles<2>(w[2 * h]), a11 = nibbles<2>(w[2 * h + 1]), a12 = nibbles<3>(w[2 * h]), a13 = nibbles<3>(w[2 * h + 1]);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+              mma_bf16(acc[nt], a00, a01, a02, a03, qf[nt][2 * i + h][0], qf[nt][2 * i + h][1]);
+              mma_bf16(acc[nt], a10, a11, a12, a13, qf[nt][2 * i + h][2], qf[nt][2 * i + h][3]);
+            }
+          }
+          const uint32_t meta = blk + 64 * D + (i * kPageTokens + key0 + g) * 4;
+          const float2 m0 = lds_half2(meta), m1 = lds_half2(meta + 32);
+          const float z0 = fmaf(-128.f, m0.x, m0.y), z1 = fmaf(-128.f, m1.x, m1.y);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+              s[nt][x] = fmaf(m0.x, acc[nt][x], fmaf(z0, qsum[nt][i][x], s[nt][x]));
+              s[nt][2 + x] = fmaf(m1.x, acc[nt][2 + x], fmaf(z1, qsum[nt][i][x], s[nt][2 + x]));
+            }
+          }
+        }
+        // --- mask (whatever a hidden token's score is, NaN too), running maximum
+        bool grow = false;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            if (!in0 || pos >= limit[nt][x]) s[nt][x] = -INFINITY;
+            if (!in1 || pos + 8 >= limit[nt][x]) s[nt][2 + x] = -INFINITY;
+            // the maximum moves only when a score is 2^6 above it in the softmax: until then weights stay below 2^6
+            grow |= fmaxf(s[nt][x], s[nt][2 + x]) * a.scale > mx[nt][x] * a.scale + 6.f;
+          }
+        if (__any_sync(0xffffffffu, grow)) {
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+              float m = fmaxf(mx[nt][x], fmaxf(s[nt][x], s[nt][2 + x]));
+              m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
+              m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
+              m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
+              const float f = m == mx[nt][x] ? 1.f : ex2((mx[nt][x] - m) * a.scale);
+              mx[nt][x] = m;
+              l[nt][x] *= f;
+#pragma unroll
+              for (int i = 0; i < G; ++i) om[nt][i][x] *= f;
+#pragma unroll
+              for (int h = 0; h < CH; ++h)
+#pragma unroll
+                for (int jj = 0; jj < 2; ++jj) { o[nt][h][jj][x] *= f; o[nt][h][jj][2 + x] *= f; }
+            }
+        }
+        // --- weights
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            const float base = mx[nt][x] == -INFINITY ? 0.f : mx[nt][x] * a.scale;  // a column that sees nothing yet: all weights 0
+            s[nt][x] = ex2(fmaf(s[nt][x], a.scale, -base));
+            s[nt][2 + x] = ex2(fmaf(s[nt][2 + x], a.scale, -base));
+            l[nt][x] += s[nt][x] + s[nt][2 + x];
+          }
+        // --- values
+#pragma unroll
+        for (int i = 0; i < G; ++i) {
+          const uint32_t meta = blk + 64 * D + 4 * D + (i * kPageTokens + key0 + g) * 4;
+          float2 m0 = lds_half2(meta), m1 = lds_half2(meta + 32);
+          // tokens behind the sequence's end hold anything; a token that is not finite has already made its scores NaN
+          if (!in0) m0 = make_float2(0.f, 0.f);
+          if (!in1) m1 = make_float2(0.f, 0.f);
+          float c0 = fmaf(8.f, m0.x, m0.y), c1 = fmaf(8.f, m1.x, m1.y);
+          if (c0 != c0) c0 = 0.f;
+          if (c1 != c1) c1 = 0.f;
+          uint32_t p0[NT], p1[NT];
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+            for (int x = 0; x < 2; ++x) om[nt][i][x] = fmaf(s[nt][x], c0, fmaf(s[nt][2 + x], c1, om[nt][i][x]));
+            p0[nt] = movmatrix_trans(pack_bf16x2(s[nt][0] * m0.x, s[nt][1] * m0.x));
+            p1[nt] = movmatrix_trans(pack_bf16x2(s[nt][2] * m1.x, s[nt][3] * m1.x));
+          }
+          uint32_t w[4];
+          ldmatrix_x4_trans(blk + 32 * D + k_lane + i * 2048, w);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const uint32_t a00 = nibbles_centred<0>(w[2 * h]), a01 = nibbles_centred<1>(w[2 * h]), a02 = nibbles_centred<0>(w[2 * h + 1]),
+                           a03 = nibbles_centred<1>(w[2 * h + 1]);
+            const uint32_t a10 = nibbles_centred<2>(w[2 * h]), a11 = nibbles_centred<3>(w[2 * h]), a12 = nibbles_centred<2>(w[2 * h + 1]),
+                           a13 = nibbles_centred<3>(w[2 * h + 1]);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+              mma_bf16(o[nt][2 * i + h][0], a00, a01, a02, a03, p0[nt], p1[nt]);
+              mma_bf16(o[nt][2 * i + h][1], a10, a11, a12, a13, p0[nt], p1[nt]);
+            }
+          }
+        }
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(empty + 8 * st);
+      if (++st == S::kStages) { st = 0; phase ^= 1; }
+    }
+    left -= stop - first;
+
+    // --- join the four warps: each leaves O, maximum and sum of its tokens in shared memory
+    float* mine = join + warp * S::kPart;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        float sum = l[nt][x];
+        float add[G];
+#pragma unroll
+        for (int i = 0; i < G; ++i) add[i] = om[nt][i][x];
+#pragma unroll
+        for (int d = 4; d < 32; d <<= 1) {
+          sum += __shfl_xor_sync(0xffffffffu, sum, d);
+#pragma unroll
+          for (int i = 0; i < G; ++i) add[i] += __shfl_xor_sync(0xffffffffu, add[i], d);
+        }
+        const int col = nt * 8 + 2 * t + x;
+#pragma unroll
+        for (int h = 0; h < CH; ++h)
+          *reinterpret_cast<float4*>(mine + col * D + 32 * h + 4 * g) =
+              make_float4(o[nt][h][0][x] + add[h / 2], o[nt][h][0][2 + x] + add[h / 2], o[nt][h][1][x] + add[h / 2], o[nt][h][1][2 + x] + add[h / 2]);
+        if (g == 0) { mine[R * D + col] = mx[nt][x]; mine[R * D + R + col] = sum; }
+      }
+    epi_bar_sync();
+    const bool whole = first == 0 && stop == c.tiles;
+    float* part = a.ws + ((int64_t)blockIdx.x * 2 + (first == 0 ? 1 : 0)) * S::kPart;
+    for (int x = tid; x < R * (D / 4); x += kWarps * 32) {
+      const int col = x / (D / 4), d4 = (x % (D / 4)) * 4, r = r0 + col;
+      float m = -INFINITY, sum = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) m = fmaxf(m, join[w * S::kPart + R * D + col]);
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        const float* p = join + w * S::kPart;
+        const float pm = p[R * D + col], f = pm == -INFINITY ? 0.f : ex2((pm - m) * a.scale);
+        const float4 y = *reinterpret_cast<const float4*>(p + col * D + d4);
+        sum = fmaf(f, p[R * D + R + col], sum);
+        v.x = fmaf(f, y.x, v.x); v.y = fmaf(f, y.y, v.y); v.z = fmaf(f, y.z, v.z); v.w = fmaf(f, y.w, v.w);
+      }
+      if (!whole) {
+        *reinterpret_cast<float4*>(part + col * D + d4) = v;
+        if (d4 == 0) { part[R * D + col] = m; part[R * D + R + col] = sum; }
+      } else if (r < rows) {
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;  // a row that sees nothing is 0
+        const int j = r / a.group, hd = r - j * a.group;
+        uint2 y;
+        y.x = pack_bf16x2(v.x * inv, v.y * inv);
+        y.y = pack_bf16x2(v.z * inv, v.w * inv);
+        *reinterpret_cast<uint2*>(a.out + (int64_t)(c.info.row0 + j) * a.ld_out + (int64_t)(c.kvh * a.group + hd) * D + d4) = y;
+      }
+    }
+    epi_bar_sync();
+    if (left > 0) next_block(a, R, c);
+  }
+}
+
+// Joins the partial results of the row blocks that run boundaries cut.  Thread block c looks at the boundary between runs c
+// and c + 1 and works if that boundary is the first one inside its row block; partial results are added in run order.
+template <int D, int NT>
+__global__ void __launch_bounds__(128) attend_join_kernel(AttendArgs a, int grid) {
+  using S = Shape<D, NT>;
+  constexpr int R = S::R;
+  __shared__ long long scan_sm[33];
+  __shared__ int found[3];
+  const long long total = list_total(a, R, scan_sm);
+  const int runs = total ? run_count(total, grid) : 0;
+  Cursor c;
+  long long first = 0;
+  const int run = blockIdx.x;
+  bool work = run + 1 < runs;
+  if (work) {
+    const long long edge = run_start(total, runs, run + 1);
+    list_seek(a, R, edge, c, scan_sm, found);
+    first = edge - c.tile;  // the row block's first page
+    work = c.tile > 0 && first >= run_start(total, runs, run);
+  }
+  grid_dep_wait();
+  if (!work) return;
+  const long long stop = first + c.tiles;
+  const int rows = c.info.rows * a.group, r0 = c.rb * R;
+  for (int x = threadIdx.x; x < R * (D / 4); x += 128) {
+    const int col = x / (D / 4), d4 = (x % (D / 4)) * 4, r = r0 + col;
+    if (r >= rows) continue;
+    float m = -INFINITY, sum = 0.f;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int k = run; k < runs && run_start(total, runs, k) < stop; ++k) {
+      const float* p = a.ws + ((int64_t)k * 2 + (k == run ? 1 : 0)) * S::kPart;
+      const float pm = p[R * D + col], mn = fmaxf(m, pm);
+      const float f0 = m == -INFINITY ? 0.f : ex2((m - mn) * a.scale), f1 = pm == -INFINITY ? 0.f : ex2((pm - mn) * a.scale);
+      const float4 y = *reinterpret_cast<const float4*>(p + col * D + d4);
+      sum = fmaf(f0, sum, f1 * p[R * D + R + col]);
+      v.x = fmaf(f0, v.x, f1 * y.x); v.y = fmaf(f0, v.y, f1 * y.y); v.z = fmaf(f0, v.z, f1 * y.z); v.w = fmaf(f0, v.w, f1 * y.w);
+      m = mn;
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    const int j = r / a.group, hd = r - j * a.group;
+    uint2 y;
+    y.x = pack_bf16x2(v.x * inv, v.y * inv);
+    y.y = pack_bf16x2(v.z * inv, v.w * inv);
+    *reinterpret_cast<uint2*>(a.out + (int64_t)(c.info.row0 + j) * a.ld_out + (int64_t)(c.kvh * a.group + hd) * D + d4) = y;
+  }
+}
+
+template <int D, int NT>
+int32_t launch(essa_ctx* ctx, const AttendArgs& a, cudaStream_t stream) {
+  using S = Shape<D, NT>;
+  cudaError_t e = cudaFuncSetAttribute(attend_decode_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
+  if (e != cudaSuccess) return check_cuda(ctx, e, "cudaFuncSetAttribute (attend)");
+  const int grid = ctx->sm_count * attend_blocks_per_sm(D, NT);
+  attend_decode_kernel<D, NT><<<grid, kThreads, S::kSmem, stream>>>(a);
+  e = cudaGetLastError();
+  if (e != cudaSuccess) return check_cuda(ctx, e, "attend launch");
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid - 1);
+  cfg.blockDim = dim3(128);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  e = cudaLaunchKernelEx(&cfg, attend_join_kernel<D, NT>, a, grid);
+  if (e != cudaSuccess) return check_cuda(ctx, e, "attend join launch");
+  ctx->launches += 2;
+  return ESSA_OK;
+}
+
+}  // namespace
+
+// Column tiles of eight query rows that a row block takes.
+static int attend_nt(int64_t rows_hint) { return rows_hint > 8 ? 2 : 1; }
+
+int64_t attend_decode_workspace(int head_dim, int64_t rows_hint, int sm_count) {
+  const int nt = attend_nt(rows_hint);
+  return (int64_t)sm_count * attend_blocks_per_sm(head_dim, nt) * 2 * (8 * nt) * (head_dim + 2) * 4;
+}
+
+int32_t launch_attend_decode(essa_ctx* ctx, const CacheView& v, const CacheEntries& e, const __nv_bfloat16* q, int64_t ld_q, int32_t q_heads,
+                             int64_t rows_hint, float scale, __nv_bfloat16* out, int64_t ld_out, void* ws, cudaStream_t stream) {
+  AttendArgs a;
+  a.v = v;
+  a.e = e;
+  a.q = q;
+  a.out = out;
+  a.ld_q = ld_q;
+  a.ld_out = ld_out;
+  a.group = q_heads / v.kv_heads;
+  a.scale = scale * kLog2e;
+  a.ws = static_cast<float*>(ws);
+  a.status = ctx->d_status;
+  const int nt = attend_nt(rows_hint);
+  if (v.head_dim == 64) return nt == 1 ? launch<64, 1>(ctx, a, stream) : launch<64, 2>(ctx, a, stream);
+  return nt == 1 ? launch<128, 1>(ctx, a, stream) : launch<128, 2>(ctx, a, stream);
+}
+
+}  // namespace essa
