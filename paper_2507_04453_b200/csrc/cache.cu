@@ -1,7 +1,7 @@
 // Paged 4-bit key / value cache: storing and reading tokens, page management, and the C entry points of include/essa.h.
 #include <cmath>
 
-#include "cache.cuh"
+#include "cache_list.cuh"
 
 namespace essa {
 namespace {
@@ -536,6 +536,9 @@ int32_t launched(essa_ctx* ctx, const char* what, int kernels) {
   ctx->launches += kernels;
   return check_cuda(ctx, cudaGetLastError(), what);
 }
+// Which attention kernel: up to 16 query rows per (entry, kv head) fit the one that widens codes straight into mma operands; from there on
+// the 256-row tiles of tcgen05 re-use a widened page often enough.
+bool few_rows(int64_t rows) { return rows <= 16; }
 size_t seen_bytes(const CacheView& v) { return (size_t)(v.max_seqs + 31) / 32 * 4; }
 int copy_grid(const essa_ctx* ctx) { return ctx->sm_count * 8; }
 
@@ -572,7 +575,8 @@ int32_t essa_cache_pages_workspace(const essa_cache_desc* cache, int64_t* bytes)
 int32_t essa_cache_attend_workspace(const essa_cache_desc* cache, int32_t q_heads, int32_t max_new, int32_t sm_count, int64_t* bytes) {
   ESSA_TRY(essa_cache_validate(cache));
   if (!bytes || q_heads < 1 || q_heads % cache->kv_heads || max_new < 1 || sm_count < 1) return ESSA_ERR_INVALID_ARG;
-  *bytes = attend_decode_workspace(cache->head_dim, (int64_t)max_new * (q_heads / cache->kv_heads), sm_count);
+  const int64_t rows = (int64_t)max_new * (q_heads / cache->kv_heads);
+  *bytes = few_rows(rows) ? attend_decode_workspace(cache->head_dim, rows, sm_count) : attend_tiles_workspace(cache->head_dim, sm_count);
   return ESSA_OK;
 }
 
@@ -657,8 +661,19 @@ int32_t essa_cache_attend(essa_ctx* ctx, const essa_cache_desc* cache, int32_t l
   ESSA_TRY(essa_cache_attend_workspace(cache, q_heads, max_new, ctx->sm_count, &need));
   ESSA_TRY(check_workspace(ctx, "cache_attend", workspace, workspace_bytes, need));
   DeviceGuard guard(ctx->device);
-  return launch_attend_decode(ctx, v, e, static_cast<const __nv_bfloat16*>(q), ld_q, q_heads, max_new * group, scale, static_cast<__nv_bfloat16*>(out), ld_out,
-                              workspace, static_cast<cudaStream_t>(stream));
+  AttendArgs a;
+  a.v = v;
+  a.e = e;
+  a.q = static_cast<const __nv_bfloat16*>(q);
+  a.out = static_cast<__nv_bfloat16*>(out);
+  a.ld_q = ld_q;
+  a.ld_out = ld_out;
+  a.group = (int32_t)group;
+  a.scale = scale * 1.4426950408889634f;
+  a.ws = static_cast<float*>(workspace);
+  a.status = ctx->d_status;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  return few_rows(max_new * group) ? launch_attend_decode(ctx, a, max_new * group, s) : launch_attend_tiles(ctx, a, s);
 }
 
 int32_t essa_cache_fork(essa_ctx* ctx, const essa_cache_desc* cache, const int32_t* src, const int32_t* dst, const int32_t* lens, int32_t n, void* workspace,

@@ -37,10 +37,13 @@ struct EntryInfo {
   int slot, row0, rows, len;
 };
 
-// cache_attend.cu: rows_hint = most query rows (tokens x heads of a group) an entry is expected to have; any number is right.
+struct AttendArgs;  // cache_list.cuh
+// cache_attend.cu (few query rows per sequence) and cache_tiles.cu (many): rows_hint = most query rows (tokens x heads of a group)
+// that an entry is expected to have; both are right for any number.
 int64_t attend_decode_workspace(int head_dim, int64_t rows_hint, int sm_count);
-int32_t launch_attend_decode(essa_ctx* ctx, const CacheView& v, const CacheEntries& e, const __nv_bfloat16* q, int64_t ld_q, int32_t q_heads,
-                             int64_t rows_hint, float scale, __nv_bfloat16* out, int64_t ld_out, void* ws, cudaStream_t stream);
+int32_t launch_attend_decode(essa_ctx* ctx, const AttendArgs& a, int64_t rows_hint, cudaStream_t stream);
+int64_t attend_tiles_workspace(int head_dim, int sm_count);
+int32_t launch_attend_tiles(essa_ctx* ctx, const AttendArgs& a, cudaStream_t stream);
 
 #ifdef __CUDACC__
 __device__ __forceinline__ EntryInfo load_entry(const CacheView& v, const CacheEntries& e, int i) {

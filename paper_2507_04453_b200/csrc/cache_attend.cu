@@ -6,110 +6,29 @@
 // (shift, and-or) for K and one subtraction more for V:
 //   S = sum_g s_g (q_g . c_g) + min_g sum(q_g).  The tensor core multiplies q by the bf16 numbers 128 + c (a code dropped
 //   into the mantissa of 128); with acc_g = q_g . (128 + c_g) in fp32, S = sum_g s_g acc_g + (min_g - 128 s_g) sum(q_g).
-//   O = sum_k p_k (s_k (c_k - 8) + (min_k + 8 s_k)): p_k s_k is rounded to bf16 (one rounding, 2^-9 of a centred value: with the
-//   codes not centred it would be 2^-9 of a number 2.6 times as large), the second term stays on the CUDA cores in fp32.
+//   O = sum_k p_k (s_k (c_k - 8) + (min_k + 8 s_k)): p_k s_k is rounded to bf16 (one rounding, 2^-8 of a centred value at most: with the
+//   codes not centred it would be 2^-8 of a number 2.6 times as large), the second term stays on the CUDA cores in fp32.
 //   (Leaving the 128 in and subtracting 136 sum(p s) at the end loses the result in fp32: |128 s| against averages of
 //   thousands of values.)
 // K and V are the M = 16 operand of mma.m16n8k16, the query rows (heads of the group x tokens) are the N = 8 columns: a
 // group of up to eight heads fills the tensor core's tile, where q as the M operand would leave half of it empty.
 //
-// Work split: the (entry, kv head, row block, page) list of the whole call is cut into equal runs, one per thread block, so that
-// ragged lengths and single long sequences balance alike; a (row block) cut by a run boundary leaves fp32 partial results
-// in the workspace, which a second kernel joins in a fixed order (no atomics: the same bits every time).
-#include "cache.cuh"
-#include "tc_ptx.cuh"
+// Work split: cache_list.cuh, with row blocks of 8 or 16 query rows and key tiles of one page.
+#include "cache_list.cuh"
 
 namespace essa {
 namespace {
 
 constexpr int kWarps = 4;                     // consuming warps: 16 tokens of a page each
 constexpr int kThreads = kWarps * 32 + 32;    // + one copying warp
-constexpr float kLog2e = 1.4426950408889634f;
 
-struct AttendArgs {
-  CacheView v;
-  CacheEntries e;
-  const __nv_bfloat16* q;
-  __nv_bfloat16* out;
-  int64_t ld_q, ld_out;
-  int32_t group;
-  float scale;  // softmax scale * log2(e)
-  float* ws;
-  int32_t* status;
+// Row blocks of R rows; every row block of an entry walks all its pages (the few rows of an entry see nearly the same ones).
+template <int ROWS>
+struct DecodeList {
+  static constexpr int R = ROWS, kMinRun = 2;
+  __device__ static int tiles(const EntryInfo& e, int, int) { return max((e.len + kPageTokens - 1) / kPageTokens, 1); }
+  __device__ static long long per_head(const EntryInfo& e, int group) { return (long long)row_blocks(e, group, R) * tiles(e, group, 0); }
 };
-
-// Row blocks of an entry and the pages each of them reads (at least one, so that rows that see nothing are still written).
-__device__ __forceinline__ void entry_shape(const EntryInfo& e, int group, int R, int& blocks, int& tiles) {
-  blocks = (int)(((int64_t)e.rows * group + R - 1) / R);
-  tiles = max((e.len + kPageTokens - 1) / kPageTokens, 1);
-}
-
-struct Cursor {  // a place in the list of (entry, kv head, row block, page)
-  int entry, kvh, rb, tile, blocks, tiles;
-  EntryInfo info;
-};
-
-// Total number of list elements, and (threads in step) the place of element `at`.  sm: [33] shared.
-__device__ long long list_total(const AttendArgs& a, int R, long long* sm) {
-  long long total = 0;
-  for (int base = 0; base < a.e.n; base += blockDim.x) {
-    const int i = base + threadIdx.x;
-    long long w = 0, t;
-    if (i < a.e.n) {
-      int b, k;
-      entry_shape(load_entry(a.v, a.e, i), a.group, R, b, k);
-      w = (long long)b * k * a.v.kv_heads;
-    }
-    block_scan(w, &t, sm);
-    total += t;
-  }
-  return total;
-}
-__device__ void list_seek(const AttendArgs& a, int R, long long at, Cursor& c, long long* sm, int* found /* shared [3] */) {
-  long long before = 0;
-  for (int base = 0; base < a.e.n; base += blockDim.x) {
-    const int i = base + threadIdx.x;
-    long long w = 0, t;
-    int b = 0, k = 1;
-    if (i < a.e.n) {
-      entry_shape(load_entry(a.v, a.e, i), a.group, R, b, k);
-      w = (long long)b * k * a.v.kv_heads;
-    }
-    const long long pre = before + block_scan(w, &t, sm);
-    if (w > 0 && at >= pre && at < pre + w) {
-      const long long rest = at - pre;
-      found[0] = i;
-      found[1] = (int)(rest / k);  // kv head * blocks + row block
-      found[2] = (int)(rest % k);
-    }
-    before += t;
-    __syncthreads();
-    if (at < before) break;
-  }
-  c.entry = found[0];
-  c.info = load_entry(a.v, a.e, c.entry);
-  entry_shape(c.info, a.group, R, c.blocks, c.tiles);
-  c.kvh = found[1] / c.blocks;
-  c.rb = found[1] % c.blocks;
-  c.tile = found[2];
-}
-// The row block after c's (its first page); false at the end of the list.
-__device__ __forceinline__ void next_block(const AttendArgs& a, int R, Cursor& c) {
-  c.tile = 0;
-  if (++c.rb < c.blocks) return;
-  c.rb = 0;
-  if (++c.kvh < a.v.kv_heads) return;
-  c.kvh = 0;
-  do {
-    if (++c.entry >= a.e.n) return;
-    c.info = load_entry(a.v, a.e, c.entry);
-    entry_shape(c.info, a.group, R, c.blocks, c.tiles);
-  } while (c.blocks == 0);
-}
-
-__device__ __forceinline__ long long run_start(long long total, int runs, int c) { return total * c / runs; }
-// Thread blocks that share the list: every run has at least two pages (a run of one would pay its fixed cost and a join for it).
-__device__ __forceinline__ int run_count(long long total, int grid) { return (int)max(1LL, min((long long)grid, (total + 1) / 2)); }
 
 __device__ __forceinline__ void ldmatrix_x4(uint32_t addr, uint32_t (&r)[4]) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
@@ -127,7 +46,6 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ float ex2(float x) { return exp2f(x); }
 // Nibble j of both halves of w as the bf16 pair (128 + low, 128 + high).
 template <int J>
 __device__ __forceinline__ uint32_t nibbles(uint32_t w) {
@@ -140,21 +58,12 @@ __device__ __forceinline__ uint32_t nibbles_centred(uint32_t w) {
   const __nv_bfloat162 r = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&x), *reinterpret_cast<const __nv_bfloat162*>(&o));
   return *reinterpret_cast<const uint32_t*>(&r);
 }
-__device__ __forceinline__ float2 lds_half2(uint32_t addr) {
-  uint32_t v;
-  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
-  return __half22float2(*reinterpret_cast<__half2*>(&v));
-}
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
-}
-
 template <int D, int NT>
 struct Shape {
   static constexpr int R = 8 * NT;             // query rows of a row block
   static constexpr int kBytes = 72 * D;        // a (page, kv head) run
   static constexpr int kStages = (D == 128 ? 6 : 10);
-  static constexpr int kPart = R * (D + 2);    // floats of a partial result: O [R][D], max [R], sum [R]
+  static constexpr int kPart = Partial<DecodeList<R>, D>::kFloats;
   static constexpr int kJoin = kWarps * R * (D + 2) * 4;
   static constexpr int kSmem = kStages * kBytes + kJoin + 256;
 };
@@ -166,9 +75,10 @@ template <int D, int NT>
 __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_decode_kernel(AttendArgs a) {
   using S = Shape<D, NT>;
   constexpr int R = S::R, G = D / kCacheGroup, CH = D / 32;
+  using L = DecodeList<R>;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ long long scan_sm[33];
-  __shared__ int found[3];
+  __shared__ long long found[2];
   __shared__ volatile int abort_flag;
   __shared__ int bad_page[S::kStages];
   __shared__ __align__(8) uint64_t bars[2 * S::kStages];
@@ -182,13 +92,13 @@ __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   __syncthreads();
-  const long long total = list_total(a, R, scan_sm);
+  const long long total = list_total<L>(a, scan_sm);
   if (total == 0) return;
-  const int runs = run_count(total, gridDim.x);
+  const int runs = run_count<L>(total, gridDim.x);
   if ((int)blockIdx.x >= runs) return;
   const long long begin = run_start(total, runs, blockIdx.x), end = run_start(total, runs, blockIdx.x + 1);
   Cursor c;
-  list_seek(a, R, begin, c, scan_sm, found);
+  list_seek<L>(a, begin, c, scan_sm, found);
   long long left = end - begin;
 
   if (warp == kWarps) {  // ---------------------------------------------------------------- copying warp
@@ -216,15 +126,9 @@ __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_
         ++filled;
         if (++st == S::kStages) { st = 0; phase ^= 1; }
       }
-      if (left > 0) next_block(a, R, c);
+      if (left > 0) next_block<L>(a, c);
     }
-    if (!ok) {  // the copies in flight land (a bounded wait) before the block's shared memory goes away
-      for (int s = 0; s < S::kStages && s < filled; ++s) {
-        const uint32_t last = ((filled - 1 - s) / S::kStages) & 1;
-        const long long t0 = clock64();
-        while (!mbar_try_wait(full + 8 * s, last) && clock64() - t0 < kWaitLimitCycles / 16) {}
-      }
-    }
+    if (!ok) drain_ring(full, S::kStages, filled);  // before the block's shared memory goes away
     return;
   }
 
@@ -292,7 +196,7 @@ __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_
     }
     const int first = c.tile, stop = (int)min((long long)c.tiles, c.tile + left);
     for (int tile = first; tile < stop; ++tile) {
-      dead = dead || !mbar_wait(full + 8 * st, phase, &abort_flag, a.status);
+      if (!dead) dead = !__all_sync(0xffffffffu, mbar_wait(full + 8 * st, phase, &abort_flag, a.status));
       if (dead) continue;
       const uint32_t blk = ring + st * S::kBytes;
       const int pos = tile * kPageTokens + key0 + g;  // tokens of this lane's scores: pos, pos + 8
@@ -443,7 +347,7 @@ __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_
       }
     epi_bar_sync();
     const bool whole = first == 0 && stop == c.tiles;
-    float* part = a.ws + ((int64_t)blockIdx.x * 2 + (first == 0 ? 1 : 0)) * S::kPart;
+    float* part = partial_of<L, D>(a, blockIdx.x, first == 0);
     for (int x = tid; x < R * (D / 4); x += kWarps * 32) {
       const int col = x / (D / 4), d4 = (x % (D / 4)) * 4, r = r0 + col;
       float m = -INFINITY, sum = 0.f;
@@ -471,54 +375,7 @@ __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_
       }
     }
     epi_bar_sync();
-    if (left > 0) next_block(a, R, c);
-  }
-}
-
-// Joins the partial results of the row blocks that run boundaries cut.  Thread block c looks at the boundary between runs c
-// and c + 1 and works if that boundary is the first one inside its row block; partial results are added in run order.
-template <int D, int NT>
-__global__ void __launch_bounds__(128) attend_join_kernel(AttendArgs a, int grid) {
-  using S = Shape<D, NT>;
-  constexpr int R = S::R;
-  __shared__ long long scan_sm[33];
-  __shared__ int found[3];
-  const long long total = list_total(a, R, scan_sm);
-  const int runs = total ? run_count(total, grid) : 0;
-  Cursor c;
-  long long first = 0;
-  const int run = blockIdx.x;
-  bool work = run + 1 < runs;
-  if (work) {
-    const long long edge = run_start(total, runs, run + 1);
-    list_seek(a, R, edge, c, scan_sm, found);
-    first = edge - c.tile;  // the row block's first page
-    work = c.tile > 0 && first >= run_start(total, runs, run);
-  }
-  grid_dep_wait();
-  if (!work) return;
-  const long long stop = first + c.tiles;
-  const int rows = c.info.rows * a.group, r0 = c.rb * R;
-  for (int x = threadIdx.x; x < R * (D / 4); x += 128) {
-    const int col = x / (D / 4), d4 = (x % (D / 4)) * 4, r = r0 + col;
-    if (r >= rows) continue;
-    float m = -INFINITY, sum = 0.f;
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int k = run; k < runs && run_start(total, runs, k) < stop; ++k) {
-      const float* p = a.ws + ((int64_t)k * 2 + (k == run ? 1 : 0)) * S::kPart;
-      const float pm = p[R * D + col], mn = fmaxf(m, pm);
-      const float f0 = m == -INFINITY ? 0.f : ex2((m - mn) * a.scale), f1 = pm == -INFINITY ? 0.f : ex2((pm - mn) * a.scale);
-      const float4 y = *reinterpret_cast<const float4*>(p + col * D + d4);
-      sum = fmaf(f0, sum, f1 * p[R * D + R + col]);
-      v.x = fmaf(f0, v.x, f1 * y.x); v.y = fmaf(f0, v.y, f1 * y.y); v.z = fmaf(f0, v.z, f1 * y.z); v.w = fmaf(f0, v.w, f1 * y.w);
-      m = mn;
-    }
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    const int j = r / a.group, hd = r - j * a.group;
-    uint2 y;
-    y.x = pack_bf16x2(v.x * inv, v.y * inv);
-    y.y = pack_bf16x2(v.z * inv, v.w * inv);
-    *reinterpret_cast<uint2*>(a.out + (int64_t)(c.info.row0 + j) * a.ld_out + (int64_t)(c.kvh * a.group + hd) * D + d4) = y;
+    if (left > 0) next_block<L>(a, c);
   }
 }
 
@@ -531,19 +388,8 @@ int32_t launch(essa_ctx* ctx, const AttendArgs& a, cudaStream_t stream) {
   attend_decode_kernel<D, NT><<<grid, kThreads, S::kSmem, stream>>>(a);
   e = cudaGetLastError();
   if (e != cudaSuccess) return check_cuda(ctx, e, "attend launch");
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(grid - 1);
-  cfg.blockDim = dim3(128);
-  cfg.stream = stream;
-  cudaLaunchAttribute attr;
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
-  e = cudaLaunchKernelEx(&cfg, attend_join_kernel<D, NT>, a, grid);
-  if (e != cudaSuccess) return check_cuda(ctx, e, "attend join launch");
-  ctx->launches += 2;
-  return ESSA_OK;
+  ++ctx->launches;
+  return launch_join<DecodeList<S::R>, D>(ctx, a, grid, 1, stream);
 }
 
 }  // namespace
@@ -556,21 +402,9 @@ int64_t attend_decode_workspace(int head_dim, int64_t rows_hint, int sm_count) {
   return (int64_t)sm_count * attend_blocks_per_sm(head_dim, nt) * 2 * (8 * nt) * (head_dim + 2) * 4;
 }
 
-int32_t launch_attend_decode(essa_ctx* ctx, const CacheView& v, const CacheEntries& e, const __nv_bfloat16* q, int64_t ld_q, int32_t q_heads,
-                             int64_t rows_hint, float scale, __nv_bfloat16* out, int64_t ld_out, void* ws, cudaStream_t stream) {
-  AttendArgs a;
-  a.v = v;
-  a.e = e;
-  a.q = q;
-  a.out = out;
-  a.ld_q = ld_q;
-  a.ld_out = ld_out;
-  a.group = q_heads / v.kv_heads;
-  a.scale = scale * kLog2e;
-  a.ws = static_cast<float*>(ws);
-  a.status = ctx->d_status;
+int32_t launch_attend_decode(essa_ctx* ctx, const AttendArgs& a, int64_t rows_hint, cudaStream_t stream) {
   const int nt = attend_nt(rows_hint);
-  if (v.head_dim == 64) return nt == 1 ? launch<64, 1>(ctx, a, stream) : launch<64, 2>(ctx, a, stream);
+  if (a.v.head_dim == 64) return nt == 1 ? launch<64, 1>(ctx, a, stream) : launch<64, 2>(ctx, a, stream);
   return nt == 1 ? launch<128, 1>(ctx, a, stream) : launch<128, 2>(ctx, a, stream);
 }
 

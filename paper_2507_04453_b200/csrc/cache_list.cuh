@@ -1,0 +1,205 @@
+// How an attention call over the cache is divided: the list of (entry, kv head, row block, key tile) is cut into equal runs, one per
+// thread block, wherever the cuts fall.  A row block inside one run is finished there; one that is cut leaves partial
+// results (O, maximum, sum per row, fp32) in the workspace, two slots per run at most, and attend_join_kernel adds them in
+// run order.  Ragged lengths, causal prompts and single long sequences balance alike, results do not depend on timing, and
+// the workspace is bounded by the grid.
+//
+// A list policy L gives R (query rows of a row block), tiles(info, group, rb) >= 1 (key tiles of a row block, so that rows that
+// see nothing are still written) and per_head(info, group) (their sum over an entry's row blocks).
+#pragma once
+
+#include "cache.cuh"
+#include "tc_ptx.cuh"
+
+namespace essa {
+
+struct AttendArgs {
+  CacheView v;
+  CacheEntries e;
+  const __nv_bfloat16* q;
+  __nv_bfloat16* out;
+  int64_t ld_q, ld_out;
+  int32_t group;
+  float scale;  // softmax scale * log2(e)
+  float* ws;
+  int32_t* status;
+};
+
+#ifdef __CUDACC__
+// 2^x by the special function unit (results below the normal range are 0, which no weight notices).
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+struct Cursor {  // a place in the list
+  int entry, kvh, rb, tile, blocks, tiles;
+  EntryInfo info;
+};
+
+__device__ __forceinline__ int row_blocks(const EntryInfo& e, int group, int R) { return (int)(((int64_t)e.rows * group + R - 1) / R); }
+
+// Elements of the list; all threads of the block.  sm: shared [33].
+template <class L>
+__device__ long long list_total(const AttendArgs& a, long long* sm) {
+  long long total = 0;
+  for (int base = 0; base < a.e.n; base += blockDim.x) {
+    const int i = base + threadIdx.x;
+    long long w = 0, t;
+    if (i < a.e.n) w = L::per_head(load_entry(a.v, a.e, i), a.group) * a.v.kv_heads;
+    block_scan(w, &t, sm);
+    total += t;
+  }
+  return total;
+}
+
+// The place of element `at` < total; all threads of the block.  found: shared [2].
+template <class L>
+__device__ void list_seek(const AttendArgs& a, long long at, Cursor& c, long long* sm, long long* found) {
+  long long before = 0;
+  for (int base = 0; base < a.e.n; base += blockDim.x) {
+    const int i = base + threadIdx.x;
+    long long w = 0, t;
+    if (i < a.e.n) w = L::per_head(load_entry(a.v, a.e, i), a.group) * a.v.kv_heads;
+    const long long pre = before + block_scan(w, &t, sm);
+    if (w > 0 && at >= pre && at < pre + w) {
+      found[0] = i;
+      found[1] = at - pre;
+    }
+    before += t;
+    __syncthreads();
+    if (at < before) break;
+  }
+  c.entry = (int)found[0];
+  c.info = load_entry(a.v, a.e, c.entry);
+  c.blocks = row_blocks(c.info, a.group, L::R);
+  const long long per = L::per_head(c.info, a.group);
+  c.kvh = (int)(found[1] / per);
+  long long rest = found[1] % per;
+  for (c.rb = 0; (c.tiles = L::tiles(c.info, a.group, c.rb)) <= rest; ++c.rb) rest -= c.tiles;
+  c.tile = (int)rest;
+}
+
+// The row block after c's; must not be called at the end of the list.
+template <class L>
+__device__ __forceinline__ void next_block(const AttendArgs& a, Cursor& c) {
+  c.tile = 0;
+  if (++c.rb >= c.blocks) {
+    c.rb = 0;
+    if (++c.kvh >= a.v.kv_heads) {
+      c.kvh = 0;
+      do {
+        if (++c.entry >= a.e.n) return;
+        c.info = load_entry(a.v, a.e, c.entry);
+        c.blocks = row_blocks(c.info, a.group, L::R);
+      } while (c.blocks == 0);
+    }
+  }
+  c.tiles = L::tiles(c.info, a.group, c.rb);
+}
+
+__device__ __forceinline__ long long run_start(long long total, int runs, int c) { return total * c / runs; }
+// Runs that share the list: L::kMinRun elements each at least (a shorter one would pay its fixed cost and a join for little).
+template <class L>
+__device__ __forceinline__ int run_count(long long total, int grid) {
+  return (int)max(1LL, min((long long)grid, (total + L::kMinRun - 1) / L::kMinRun));
+}
+
+template <class L, int D>
+struct Partial {
+  static constexpr int kFloats = L::R * (D + 2);  // O [R][D], maximum [R], sum [R]
+};
+// Slot of the partial result that run `run` leaves for a row block: 1 if the row block begins in this run, else 0.
+template <class L, int D>
+__device__ __forceinline__ float* partial_of(const AttendArgs& a, int run, bool begins) {
+  return a.ws + ((int64_t)run * 2 + (begins ? 1 : 0)) * Partial<L, D>::kFloats;
+}
+
+// Joins the row blocks that run boundaries cut.  Thread blocks (c, *) look at the boundary between runs c and c + 1 and work if it
+// is the first one inside its row block; gridDim.y of them share its rows.  Launched to start beside the attention kernel: it finds
+// its row block meanwhile and waits for the partial results.
+template <class L, int D>
+__global__ void __launch_bounds__(128) attend_join_kernel(AttendArgs a, int grid) {
+  constexpr int R = L::R;
+  __shared__ long long scan_sm[33];
+  __shared__ long long found[2];
+  const long long total = list_total<L>(a, scan_sm);
+  const int runs = total ? run_count<L>(total, grid) : 0;
+  Cursor c;
+  long long first = 0;
+  const int run = blockIdx.x;
+  bool work = run + 1 < runs;
+  if (work) {
+    const long long edge = run_start(total, runs, run + 1);
+    list_seek<L>(a, edge, c, scan_sm, found);
+    first = edge - c.tile;  // the row block's first element
+    work = c.tile > 0 && first >= run_start(total, runs, run);
+  }
+  grid_dep_wait();
+  if (!work) return;
+  const long long stop = first + c.tiles;
+  const int rows = c.info.rows * a.group, r0 = c.rb * R;
+  for (int x = blockIdx.y * 128 + threadIdx.x; x < R * (D / 4); x += gridDim.y * 128) {
+    const int row = x / (D / 4), d4 = (x % (D / 4)) * 4, r = r0 + row;
+    if (r >= rows) break;
+    float m = -INFINITY, sum = 0.f;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int k = run; k < runs && run_start(total, runs, k) < stop; ++k) {
+      const float* p = partial_of<L, D>(a, k, k == run);
+      const float pm = p[R * D + row], mn = fmaxf(m, pm);
+      const float f0 = m == -INFINITY ? 0.f : ex2((m - mn) * a.scale), f1 = pm == -INFINITY ? 0.f : ex2((pm - mn) * a.scale);
+      const float4 y = *reinterpret_cast<const float4*>(p + row * D + d4);
+      sum = fmaf(f0, sum, f1 * p[R * D + R + row]);
+      v.x = fmaf(f0, v.x, f1 * y.x);
+      v.y = fmaf(f0, v.y, f1 * y.y);
+      v.z = fmaf(f0, v.z, f1 * y.z);
+      v.w = fmaf(f0, v.w, f1 * y.w);
+      m = mn;
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    const int j = r / a.group, hd = r - j * a.group;
+    uint2 y;
+    y.x = pack_bf16x2(v.x * inv, v.y * inv);
+    y.y = pack_bf16x2(v.z * inv, v.w * inv);
+    *reinterpret_cast<uint2*>(a.out + (int64_t)(c.info.row0 + j) * a.ld_out + (int64_t)(c.kvh * a.group + hd) * D + d4) = y;
+  }
+}
+
+template <class L, int D>
+int32_t launch_join(essa_ctx* ctx, const AttendArgs& a, int grid, int row_split, cudaStream_t stream) {
+  if (grid < 2) return ESSA_OK;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid - 1, row_split);
+  cfg.blockDim = dim3(128);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, attend_join_kernel<L, D>, a, grid);
+  if (e != cudaSuccess) return check_cuda(ctx, e, "attend join launch");
+  ++ctx->launches;
+  return ESSA_OK;
+}
+
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+__device__ __forceinline__ float2 lds_half2(uint32_t addr) {
+  uint32_t v;
+  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+  return __half22float2(*reinterpret_cast<__half2*>(&v));
+}
+// The copies into `slots` ring slots that were filled `filled` times in all land (a bounded wait each); for leaving early.
+__device__ __forceinline__ void drain_ring(uint32_t full, int slots, int filled) {
+  for (int s = 0; s < slots && s < filled; ++s) {
+    const uint32_t last = ((filled - 1 - s) / slots) & 1;
+    const long long t0 = clock64();
+    while (!mbar_try_wait(full + 8 * s, last) && clock64() - t0 < kWaitLimitCycles / 16) {}
+  }
+}
+#endif
+
+}  // namespace essa

@@ -1,0 +1,606 @@
+// Attention over the paged 4-bit cache for many rows per sequence (prompts, chunks): tcgen05 tiles.
+//
+// A row block is 256 query rows (token-major: row r of an entry is token r / group, head r % group of a kv head, so the heads that
+// share K and V share a tile), two halves of 128; a key tile is two pages.  Per key tile and half: S = Q K^T (fp16, M = 128, N = 128)
+// into tensor memory, softmax by four warps (a thread per row), P back into the same columns of tensor memory as fp16,
+// O += P V (fp16, A from tensor memory, V as stored: MN-major).  The halves alternate: while one is in its softmax, the tensor
+// core works for the other.  Four warps widen the pages, one copies them in (bulk copies), one issues the MMAs.
+//
+// What bounds it: per key tile and SM the MMAs need 2048 cycles (1024 per half), the exponentials of the softmax 2048 on the
+// special function units, the widening ~550 issue slots per scheduler beside ~1300 of the softmax.
+//
+// Roundings: K and V become fp16 as their scale and minimum are applied, (code - 8) * scale + (minimum + 8 scale), with the offset and the
+// result rounded (2^-11 each).  Q is bf16; a row times a power of two, its largest element at 2^13 .. 2^14, is fp16 without loss (elements
+// 2^-27 below the largest lose bits).  P is fp16 (2^-11; weights below 6e-8 of the largest lose bits).  With bf16 operands instead, K's
+// three roundings (scale, offset, result: 2^-8 each) made up most of the error: 3.2e-3 of the result's norm against 1.7e-3 from rounding
+// the result alone.  S, the running maximum, the sums and O are fp32.
+// Channel order inside a group of eight channels is (0, 4, 1, 5, 2, 6, 3, 7), what masking nibbles out of a word gives: Q is stored in
+// the same order, and O's columns are put back on the way out.
+#include "cache_list.cuh"
+
+namespace essa {
+namespace {
+
+struct TileList {
+  static constexpr int R = 256, kKeys = kPageTokens, kMinRun = 2;
+  // keys that the last row of the row block sees, in tiles
+  __device__ static int tiles(const EntryInfo& e, int group, int rb) {
+    const int last = (int)min((int64_t)e.rows - 1, ((int64_t)rb * R + R - 1) / group);
+    return max((e.len - e.rows + last + 1 + kKeys - 1) / kKeys, 1);
+  }
+  __device__ static long long per_head(const EntryInfo& e, int group) {
+    long long sum = 0;
+    const int blocks = row_blocks(e, group, R);
+    for (int rb = 0; rb < blocks; ++rb) sum += tiles(e, group, rb);
+    return sum;
+  }
+};
+
+constexpr int kSoftWarps = 8, kWidenWarps = 4;
+constexpr int kMmaWarp = kSoftWarps + kWidenWarps, kCopyWarp = kMmaWarp + 1;
+constexpr int kThreads = 512;  // four warpgroups; the last two warps only give registers away
+// Registers per thread: launched with 128, of which the softmax takes more.  2 * 152 + 2 * 104 = 4 * 128.
+constexpr int kSoftRegs = 152, kOtherRegs = 104;
+constexpr int kRaw = 3;  // pages in flight
+
+constexpr int kRing = 4;  // key tiles of K and of V
+
+template <int D>
+struct Mem {  // offsets from a 1024-byte boundary
+  static constexpr int kHalf = D / 64 * 128 * 128;    // one half of Q: [64-channel block][128 rows][128 bytes]
+  static constexpr int kSub = 64 * 128;               // 64 keys x 64 channels
+  static constexpr int kTile = D / 64 * kSub;         // a key tile of K or V
+  static constexpr int kQ = 0, kK = 2 * kHalf, kV = kK + kRing * kTile, kRawAt = kV + kRing * kTile;
+  static constexpr int kRun = 72 * D;
+  static constexpr int kBars = kRawAt + kRaw * kRun;
+  static constexpr int kBytes = kBars + 512;
+};
+enum Bar { kRawFull = 0, kRawEmpty = kRaw, kTileFull = 2 * kRaw, kTileEmpty = kTileFull + kRing, kQFull = kTileEmpty + kRing, kOFull = kQFull + 2, kSFull = kOFull + 2 /* [half][buffer] */, kPFull = kSFull + 4, kDone = kPFull + 4, kBarCount };
+static_assert(kBarCount * 8 <= 512, "");
+
+// Instruction descriptor of kind::f16 with both operands fp16 and M = 128; n_contiguous: B is stored with N contiguous.
+__host__ __device__ constexpr uint32_t f16_idesc(int N, bool n_contiguous) {
+  return (1u << 4) | ((n_contiguous ? 1u : 0u) << 16) | ((uint32_t)(N >> 3) << 17) | (8u << 24);
+}
+
+__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
+  const __half2 v = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ uint32_t bits(__half2 v) { return *reinterpret_cast<uint32_t*>(&v); }
+__device__ __forceinline__ __half2 as_half2(uint32_t v) { return *reinterpret_cast<__half2*>(&v); }
+__device__ __forceinline__ __nv_bfloat162 as_bf162(uint32_t v) { return *reinterpret_cast<__nv_bfloat162*>(&v); }
+
+// Operands in shared memory are 128-byte rows under the 128-byte swizzle.  Q and K: a row is 64 channels of a row / key (K contiguous).
+// V as B operand of O += P V: [64-channel block][key][64 channels], i.e. N contiguous: 64 channels x 8 keys per 1024-byte swizzle atom,
+// the next eight keys 1024 bytes on (stride offset), the next 64 channels one sub-tile on (leading offset).
+// Registers of a tmem_ld32_issue are valid from here on (they pass through, so that no use of them can move up).
+__device__ __forceinline__ void tmem_ld_done(uint32_t (&r)[32]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]),
+                 "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]),
+                 "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
+               :
+               : "memory");
+}
+__device__ __forceinline__ void st_global_32(void* p, const uint32_t (&v)[8]) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]),
+               "r"(v[7])
+               : "memory");
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+// Two fp32 operations in one instruction.
+__device__ __forceinline__ uint64_t pack_f32x2(float lo, float hi) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ void unpack_f32x2(uint64_t v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma_f32x2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+// One lane of the (converged) warp, the same one every time.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}\n" : "=r"(p));
+  return p != 0;
+}
+__device__ __forceinline__ void prefetch_l2(const void* p, uint32_t bytes) {
+  asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p), "r"(bytes) : "memory");
+}
+// A shared-memory matrix descriptor whose address part is `lo` (and the leading offset, bits 16-29): only this half changes between MMAs.
+__device__ __forceinline__ uint64_t desc_of(uint32_t lo) {
+  constexpr uint32_t hi = (1024u >> 4) | (1u << 14) | (2u << 29);  // stride 1024 bytes, version 1, 128-byte swizzle
+  return (uint64_t)hi << 32 | lo;
+}
+
+// Eight codes -> fp16 (code - 8) * s + c in the order (0, 4, 1, 5, 2, 6, 3, 7).
+__device__ __forceinline__ uint4 widen(uint32_t w, __half2 s, __half2 c) {
+  const __half2 o = as_half2(0x64086408u), sixteenth = as_half2(0x2c002c00u), o16 = as_half2(0xd480d480u);  // 1032; 1 / 16; -72
+  uint32_t y[4];
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const uint32_t x = w >> (8 * j);
+    y[2 * j] = bits(__hfma2(__hsub2(as_half2((x & 0x000f000fu) | 0x64006400u), o), s, c));                    // 1024 + code
+    y[2 * j + 1] = bits(__hfma2(__hfma2(as_half2((x & 0x00f000f0u) | 0x64006400u), sixteenth, o16), s, c));  // 1024 + 16 code
+  }
+  return make_uint4(y[0], y[1], y[2], y[3]);
+}
+// Scale and centre of a token's group, (scale, minimum) = m.  Values beyond +-65440 are brought there: what fp16 rounds them to
+// has to stay finite.
+__device__ __forceinline__ void scale_of(float2 m, __half2& s, __half2& c) {
+  if (m.y < -65440.f) m.y = -65440.f;
+  if (fmaf(15.f, m.x, m.y) > 65440.f) m.x = (65440.f - m.y) * (1.f / 15.01f);
+  s = __float2half2_rn(m.x);
+  c = __float2half2_rn(fmaf(8.f, m.x, m.y));
+}
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a) {
+  using M = Mem<D>;
+  using L = TileList;
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ long long scan_sm[33];
+  __shared__ long long found[2];
+  __shared__ volatile int abort_flag;
+  __shared__ int raw_bad[kRaw];
+  __shared__ int tile_bad[8];  // the key tile's page is not there
+  __shared__ uint32_t tmem_slot;
+  __shared__ float row_scale[L::R];  // what a row of Q was divided by
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const uint32_t bars = base + M::kBars;
+  const auto bar = [&](int i) { return bars + 8 * i; };
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  grid_dep_launch();
+  if (tid == 0) {
+    abort_flag = 0;
+    for (int i = 0; i < kRaw; ++i) { mbar_init(bar(kRawFull + i), 1); mbar_init(bar(kRawEmpty + i), kWidenWarps); }
+    for (int i = 0; i < kRing; ++i) { mbar_init(bar(kTileFull + i), kWidenWarps); mbar_init(bar(kTileEmpty + i), 1); }
+    for (int i = 0; i < 2; ++i) { mbar_init(bar(kQFull + i), 4); mbar_init(bar(kOFull + i), 1); }
+    for (int i = 0; i < 4; ++i) { mbar_init(bar(kSFull + i), 1); mbar_init(bar(kPFull + i), 4); }
+    mbar_init(bar(kDone), 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncthreads();
+  const long long total = list_total<L>(a, scan_sm);
+  if (total == 0) return;
+  const int runs = run_count<L>(total, gridDim.x);
+  if ((int)blockIdx.x >= runs) return;
+  const long long begin = run_start(total, runs, blockIdx.x);
+  long long left = run_start(total, runs, blockIdx.x + 1) - begin;
+  Cursor c;
+  list_seek<L>(a, begin, c, scan_sm, found);
+  if (warp == kMmaWarp) {
+    tmem_alloc(smem_u32(&tmem_slot), 512);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = tmem_slot;
+  const auto wait = [&](int b, uint32_t parity) { return mbar_wait(bar(b), parity, &abort_flag, a.status); };
+  const auto wait_warp = [&](int b, uint32_t parity) { return __all_sync(0xffffffffu, wait(b, parity)) != 0; };
+
+  if (warp < kSoftWarps) {  // ------------------------------------------------------------------ softmax, a thread per row
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
+    const int h = warp >> 2, row = (warp & 3) * 32 + lane;
+    const uint32_t lanes = (uint32_t)(warp & 3) * 32u << 16;
+    const uint32_t o_at = tmem + 256 + D * h + lanes;
+    int tile = 0;  // key tiles of the run so far
+    uint32_t s_ph = 0, o_ph = 0;  // s_ph: a bit per buffer
+    bool ok = true;
+    // What a thread needs of the row block that it is at.
+    struct Block {
+      int first, n;
+      bool whole, there;  // there: the row exists
+      __nv_bfloat16* out;
+      int limit, lowest;  // keys that the row sees; the fewest of the warp's rows
+      float back;         // what the row of Q was divided by
+    };
+    // Moves on to the next row block in which this half has rows (false: none left) and puts its rows of Q into shared memory: D / 8
+    // lanes per row, channels in the order of the widened codes.
+    const auto enter = [&](Block& b) {
+      for (;; next_block<L>(a, c)) {
+        if (left <= 0) return false;
+        const int stop = (int)min((long long)c.tiles, c.tile + left);
+        b.first = c.tile;
+        b.n = stop - c.tile;
+        b.whole = c.tile == 0 && stop == c.tiles;
+        left -= b.n;
+        if (c.rb * L::R + h * 128 < c.info.rows * a.group) break;
+        tile += b.n;
+        if (left <= 0) return false;
+      }
+      const int rows = c.info.rows * a.group, r0 = c.rb * L::R + h * 128;
+      constexpr int kLanes = D / 8, kRowsAt = 32 / kLanes, kSteps = 32 / kRowsAt;
+      const int ch = lane % kLanes;
+      int r = r0 + (warp & 3) * 32 + lane / kLanes, tok = r / a.group, hd = r - tok * a.group;
+      const __nv_bfloat16* q = a.q + (int64_t)c.info.row0 * a.ld_q + (int64_t)c.kvh * a.group * D + ch * 8;
+      uint4 x[kSteps];
+#pragma unroll
+      for (int i = 0; i < kSteps; ++i) {
+        x[i] = make_uint4(0, 0, 0, 0);
+        if (r < rows) x[i] = __ldg(reinterpret_cast<const uint4*>(q + tok * a.ld_q + hd * D));
+        r += kRowsAt;
+        for (hd += kRowsAt; hd >= a.group; hd -= a.group) ++tok;
+      }
+      // fp16 holds the rows as they are if every piece of eight channels has an element between 2^-6 and 2^15; otherwise each row is
+      // brought there by a power of two
+      __nv_bfloat162 least = as_bf162(0x7f807f80u), most = as_bf162(0u);
+      int rr = (warp & 3) * 32 + lane / kLanes;
+#pragma unroll
+      for (int i = 0; i < kSteps; ++i) {
+        const __nv_bfloat162 big = __hmax2_nan(__hmax2_nan(__habs2(as_bf162(x[i].x)), __habs2(as_bf162(x[i].y))), __hmax2_nan(__habs2(as_bf162(x[i].z)), __habs2(as_bf162(x[i].w))));
+        most = __hmax2_nan(most, big);
+        if (r0 + rr + i * kRowsAt < rows) least = __hmin2_nan(least, big);
+      }
+      const float low = fminf(__low2float(least), __high2float(least));
+      const bool plain = __all_sync(0xffffffffu, __low2float(most) < 32768.f && __high2float(most) < 32768.f && low >= 0.015625f);  // (false for NaN)
+#pragma unroll
+      for (int i = 0; i < kSteps; ++i, rr += kRowsAt) {
+        float f[8] = {__uint_as_float(x[i].x << 16), __uint_as_float(x[i].x & 0xffff0000u), __uint_as_float(x[i].y << 16), __uint_as_float(x[i].y & 0xffff0000u),
+                      __uint_as_float(x[i].z << 16), __uint_as_float(x[i].z & 0xffff0000u), __uint_as_float(x[i].w << 16), __uint_as_float(x[i].w & 0xffff0000u)};
+        int e = 0;
+        if (!plain) {
+          float big = 0.f;
+#pragma unroll
+          for (int k = 0; k < 8; ++k) big = fmaxf(big, fabsf(f[k]));
+#pragma unroll
+          for (int d = 1; d < kLanes; d <<= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, d));
+          // largest element at 2^13 .. 2^14 (not of a row of zeros, or one with an infinity)
+          e = big > 0.f && big < INFINITY ? max((int)(__float_as_uint(big) >> 23), 27) - 127 - 13 : 0;
+          const float up = __uint_as_float((uint32_t)(127 - e) << 23);
+#pragma unroll
+          for (int k = 0; k < 8; ++k) f[k] *= up;
+        }
+        if (ch == 0) row_scale[h * 128 + rr] = __uint_as_float((uint32_t)(127 + e) << 23);
+        sts_v4(base + M::kQ + h * M::kHalf + (ch >> 3) * (128 * 128) + rr * 128 + (((ch & 7) ^ (rr & 7)) << 4),
+               make_uint4(pack_f16x2(f[0], f[4]), pack_f16x2(f[1], f[5]), pack_f16x2(f[2], f[6]), pack_f16x2(f[3], f[7])));
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(kQFull + h));
+      r = r0 + row;
+      tok = r / a.group;
+      b.there = r < rows;
+      b.out = a.out + (int64_t)(c.info.row0 + tok) * a.ld_out + (int64_t)(c.kvh * a.group + r - tok * a.group) * D;
+      b.back = row_scale[h * 128 + row];
+      // rows behind the last one have q = 0 and are not written, whatever they see
+      b.limit = b.lowest = b.there ? c.info.len - c.info.rows + tok + 1 : 0x7fffffff;
+#pragma unroll
+      for (int d = 16; d; d >>= 1) b.lowest = min(b.lowest, __shfl_xor_sync(0xffffffffu, b.lowest, d));
+      if (left > 0) next_block<L>(a, c);
+      return true;
+    };
+    const bool wide_out = !(reinterpret_cast<uintptr_t>(a.out) & 31) && a.ld_out % 16 == 0;  // whole 32-byte sectors
+    Block b, next;
+    b.n = 0;
+    float m = 0.f, sum = 0.f;
+    for (;;) {
+      // --- the next row block's Q (all products with this one's are done), while the last product with V runs
+      const bool more = enter(next);
+      if (b.n > 0) {
+        if (!(ok = wait_warp(kOFull + h, o_ph))) break;
+        o_ph ^= 1;
+        tc_fence_after();
+        // --- out, or a partial result; columns (0, 4, 1, 5, 2, 6, 3, 7) of eight are the channels in order
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;  // a row that sees nothing is 0
+        const int rr = h * 128 + row;
+        float* part = partial_of<L, D>(a, blockIdx.x, b.first == 0);
+#pragma unroll 1
+        for (int d = 0; d < D; d += 32) {
+          uint32_t v[32];
+          tmem_ld32_issue(o_at + d, v);
+          tmem_ld_done(v);
+          const auto at = [&](int i) { return __uint_as_float(v[i]); };
+          if (b.there && b.whole) {
+#pragma unroll
+            for (int i = 0; i < 32; i += 16) {
+              uint32_t y[8];
+#pragma unroll
+              for (int k = 0; k < 2; ++k) {
+                const int o = i + 8 * k;
+                y[4 * k] = pack_bf16x2(at(o) * inv, at(o + 2) * inv);
+                y[4 * k + 1] = pack_bf16x2(at(o + 4) * inv, at(o + 6) * inv);
+                y[4 * k + 2] = pack_bf16x2(at(o + 1) * inv, at(o + 3) * inv);
+                y[4 * k + 3] = pack_bf16x2(at(o + 5) * inv, at(o + 7) * inv);
+              }
+              if (wide_out) {
+                st_global_32(b.out + d + i, y);
+              } else {
+                *reinterpret_cast<uint4*>(b.out + d + i) = make_uint4(y[0], y[1], y[2], y[3]);
+                *reinterpret_cast<uint4*>(b.out + d + i + 8) = make_uint4(y[4], y[5], y[6], y[7]);
+              }
+            }
+          } else if (b.there) {
+#pragma unroll
+            for (int i = 0; i < 32; i += 8) {
+              *reinterpret_cast<float4*>(part + rr * D + d + i) = make_float4(at(i), at(i + 2), at(i + 4), at(i + 6));
+              *reinterpret_cast<float4*>(part + rr * D + d + i + 4) = make_float4(at(i + 1), at(i + 3), at(i + 5), at(i + 7));
+            }
+          }
+        }
+        if (!b.whole) {
+          part[L::R * D + rr] = m * b.back;
+          part[L::R * D + L::R + rr] = sum;
+        }
+        tc_fence_before();
+      }
+      if (!more) break;
+      b = next;
+      const float scale = a.scale * b.back;
+      m = -INFINITY;
+      sum = 0.f;
+      for (int j = 0; j < b.n; ++j, ++tile) {
+        const uint32_t buf = tile & 1;
+        if (!(ok = wait_warp(kSFull + 2 * h + buf, s_ph >> buf & 1))) break;
+        s_ph ^= 1u << buf;
+        tc_fence_after();
+        const uint32_t s_at = tmem + 128 * h + 64 * buf + lanes;
+        const int key0 = (b.first + j) * L::kKeys, bad = tile_bad[tile & 7];
+        const int see = bad ? 0 : b.limit - key0;  // keys of the tile before this one are seen
+        const bool mask = key0 + L::kKeys > b.lowest || bad;
+        uint32_t p[32];
+        float add[2], best;
+        if (mask) {  // hidden scores become -infinity in place: the tiles that need none pay nothing
+#pragma unroll 1
+          for (int d = 0; d < L::kKeys; d += 32) {
+            tmem_ld32_issue(s_at + d, p);
+            tmem_ld_done(p);
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if (d + i >= see) p[i] = 0xff800000u;
+            tmem_st32(s_at + d, p);
+          }
+        }
+        for (int again = j == 0 ? 0 : 1;; ++again) {  // (the first tile: once for its maximum alone)
+          uint32_t v[2][32];
+          tmem_ld32_issue(s_at, v[0]);
+          tmem_ld32_issue(s_at + 32, v[1]);
+          tmem_ld_done(v[0]);
+          tmem_ld_done(v[1]);
+          float t[4] = {m, m, m, m};
+#pragma unroll
+          for (int i = 0; i < 64; i += 2) t[i >> 1 & 3] = max3(t[i >> 1 & 3], __uint_as_float(v[i >> 5][i & 31]), __uint_as_float(v[i >> 5][(i & 31) + 1]));
+          best = max3(max3(t[0], t[1], t[2]), t[3], t[3]);
+          if (again == 0) {
+            m = best;
+            continue;
+          }
+          // weights by the maximum so far, the tile's maximum beside them
+          const float shift = m == -INFINITY ? 0.f : -m * scale;
+          uint64_t sums[2] = {0, 0};
+          const uint64_t scale2 = pack_f32x2(scale, scale), shift2 = pack_f32x2(shift, shift);
+#pragma unroll
+          for (int i = 0; i < 32; ++i) {
+            float x0, x1;
+            unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(v[i >> 4][2 * (i & 15)]), __uint_as_float(v[i >> 4][2 * (i & 15) + 1])), scale2, shift2), x0, x1);
+            x0 = ex2(x0);
+            x1 = ex2(x1);
+            sums[i & 1] = add_f32x2(sums[i & 1], pack_f32x2(x0, x1));
+            p[i] = pack_f16x2(x0, x1);
+          }
+          unpack_f32x2(add_f32x2(sums[0], sums[1]), add[0], add[1]);
+          // the maximum moves only when a score is 2^6 above it (weights stay below 2^6): seldom, and then the tile is done again
+          if (!__any_sync(0xffffffffu, best * scale > m * scale + 6.f)) break;
+          // O holds the tiles before this one: their products end before those with the K of the next tile, or (there is none) signal
+          if (!(ok = j + 1 < b.n ? wait_warp(kSFull + 2 * h + (buf ^ 1), s_ph >> (buf ^ 1) & 1) : wait_warp(kOFull + h, o_ph))) break;
+          tc_fence_after();
+          const float f = best == m ? 1.f : ex2((m - best) * scale);
+          m = best;
+          sum *= f;
+#pragma unroll 1
+          for (int d = 0; d < D; d += 32) {
+            tmem_ld32_issue(o_at + d, p);
+            tmem_ld_done(p);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) p[i] = __float_as_uint(__uint_as_float(p[i]) * f);
+            tmem_st32(o_at + d, p);
+          }
+        }
+        if (!ok) break;
+        sum += add[0] + add[1];
+        tmem_st32(s_at, p);
+        if (j > 0 && j + 1 == b.n) {  // the last two products with V signal: the first of them is seen before the second can start
+          if (!(ok = wait_warp(kOFull + h, o_ph))) break;
+          o_ph ^= 1;
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(kPFull + 2 * h + buf));
+      }
+      if (!ok) break;
+    }
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+    if (warp == kCopyWarp) {  // ------------------------------------------------------------------ pages -> shared memory
+      if (lane == 0) {
+        int slot = 0, filled = 0;
+        uint32_t phase = 0;
+        bool ok = true;
+        while (ok && left > 0) {
+          const int stop = (int)min((long long)c.tiles, c.tile + left);
+          left -= stop - c.tile;
+          const int pages = (c.info.len + kPageTokens - 1) / kPageTokens;
+          const int32_t* row = a.v.table + (int64_t)max(c.info.slot, 0) * a.v.max_pages;
+          if (c.info.slot < 0) cache_fault(a.status);
+          {  // the row block's part of q into L2, a key tile or more before the softmax warps ask for it
+            const int t0 = c.rb * L::R / a.group, t1 = min(c.info.rows, (c.rb * L::R + L::R + a.group - 1) / a.group);
+            for (int t = t0; t < t1; ++t) prefetch_l2(a.q + (int64_t)(c.info.row0 + t) * a.ld_q + (int64_t)c.kvh * a.group * D, a.group * D * 2);
+          }
+          for (int p = c.tile; p < stop; ++p) {
+            if (filled >= kRaw && !wait(kRawEmpty + slot, phase ^ 1)) { ok = false; break; }
+            const int page = p < pages ? __ldg(row + p) : -1;
+            const bool there = page >= 0 && page < a.v.num_pages;
+            if (!there && p < pages) cache_fault(a.status);
+            raw_bad[slot] = !there;
+            if (there) {
+              mbar_expect_tx(bar(kRawFull + slot), M::kRun);
+              bulk_load(base + M::kRawAt + slot * M::kRun, a.v.pages + page * a.v.page_bytes + (int64_t)c.kvh * M::kRun, M::kRun, bar(kRawFull + slot));
+            } else {
+              mbar_arrive(bar(kRawFull + slot));
+            }
+            ++filled;
+            if (++slot == kRaw) { slot = 0; phase ^= 1; }
+          }
+          if (left > 0) next_block<L>(a, c);
+        }
+        if (!ok) drain_ring(bar(kRawFull), kRaw, filled);
+      }
+    } else if (warp == kMmaWarp) {  // ------------------------------------------------------------ MMAs
+      // (few instructions between two MMAs: what the issuing thread does there delays them)
+      if (elect_one()) {
+        constexpr uint32_t kQk = f16_idesc(64, false), kPv = f16_idesc(D, true);
+        const uint32_t q_lo = (base + M::kQ) >> 4, k_lo = (base + M::kK) >> 4, v_lo = ((base + M::kV) >> 4) | (uint32_t)(M::kSub >> 4) << 16;
+        uint32_t q_ph = 0, p_ph = 0;    // a bit per half; per half and buffer
+        uint32_t k_at = 0, v_at = 0;    // key tiles of the run whose products with K / V have been issued
+        bool ok = true;
+        const auto qk = [&](int h) {
+          const uint32_t d = tmem + 128 * h + 64 * (k_at & 1), q0 = q_lo + h * (M::kHalf >> 4), k0 = k_lo + k_at % kRing * (M::kTile >> 4);
+#pragma unroll
+          for (int i = 0; i < D / 16; ++i)
+            umma_bf16(d, desc_of(q0 + (((i / 4) * 128 * 128 + (i % 4) * 32) >> 4)), desc_of(k0 + (((i / 4) * M::kSub + (i % 4) * 32) >> 4)), kQk, i > 0);
+          umma_commit(bar(kSFull + 2 * h + (k_at & 1)));
+        };
+        while (ok && left > 0) {
+          const int stop = (int)min((long long)c.tiles, c.tile + left), n = stop - c.tile;
+          const int halves = c.info.rows * a.group - c.rb * L::R > 128 ? 2 : 1;
+          left -= n;
+          // Products with K run two tiles ahead: the scores of a half's next tile are there when its softmax has finished one.
+          for (int j = 0; ok && j < min(n, 2); ++j, ++k_at) {
+            if (!(ok = wait(kTileFull + k_at % kRing, k_at / kRing & 1))) break;
+            for (int h = 0; h < halves; ++h) {
+              if (j == 0) {
+                if (!(ok = wait(kQFull + h, q_ph >> h & 1))) break;
+                q_ph ^= 1u << h;
+              }
+              tc_fence_after();
+              qk(h);
+            }
+          }
+          for (int j = 0; ok && j < n; ++j, ++v_at) {
+            const bool more = j + 2 < n;
+            for (int h = 0; h < halves; ++h) {
+              const uint32_t at = 2 * h + (v_at & 1);
+              if (!(ok = wait(kPFull + at, p_ph >> at & 1))) break;
+              p_ph ^= 1u << at;
+              tc_fence_after();
+              const uint32_t d = tmem + 256 + D * h, p0 = tmem + 128 * h + 64 * (v_at & 1), v0 = v_lo + v_at % kRing * (M::kTile >> 4);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) umma_bf16_ts(d, p0 + 8 * i, desc_of(v0 + i * (2048 >> 4)), kPv, i > 0 || j > 0);
+              if (!more) {
+                umma_commit(bar(kOFull + h));
+                continue;
+              }
+              if (h == 0 && !(ok = wait(kTileFull + k_at % kRing, k_at / kRing & 1))) break;
+              qk(h);
+            }
+            if (!ok) break;
+            // V of this tile, and K of every tile up to it, have been used
+            umma_commit(bar(kTileEmpty + v_at % kRing));
+            if (more) ++k_at;
+          }
+          if (left > 0) next_block<L>(a, c);
+        }
+        if (!ok) {  // MMAs in flight finish (a bounded wait) before tensor memory is given back
+          umma_commit(bar(kDone));
+          const long long t0 = clock64();
+          while (!mbar_try_wait(bar(kDone), 0) && clock64() - t0 < kWaitLimitCycles / 16) {}
+        }
+      }
+      __syncwarp();
+    } else if (warp < kMmaWarp) {  // ---------------------------------------------------------- pages -> operands
+      const int wt = tid - kSoftWarps * 32;
+      const int token = wt & 63, part = wt >> 6;       // D = 128: a 64-channel group each; D = 64: half a group each
+      constexpr int kWords = D / 16;                   // 32-bit words of codes per thread: 8 or 4
+      const int group = D == 128 ? part : 0, word0 = D == 128 ? 0 : part * 4;
+      int slot = 0, tile = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      while (ok && left > 0) {
+        const int stop = (int)min((long long)c.tiles, c.tile + left);
+        left -= stop - c.tile;
+        for (int j = c.tile; j < stop; ++j, ++tile) {
+          const int st = tile % kRing;
+          const uint32_t reuse = (tile / kRing & 1) ^ 1;
+          const uint32_t k_dst = base + M::kK + st * M::kTile + group * M::kSub + token * 128, v_dst = k_dst + M::kV - M::kK;
+          if (!(ok = wait_warp(kRawFull + slot, phase))) break;
+          const uint32_t raw = base + M::kRawAt + slot * M::kRun;
+          const bool bad = raw_bad[slot] != 0;
+          const bool in = !bad && j * kPageTokens + token < c.info.len;
+          const uint32_t sw = (uint32_t)(token & 7);
+          float2 mk = lds_half2(raw + 64 * D + (group * kPageTokens + token) * 4), mv = lds_half2(raw + 68 * D + (group * kPageTokens + token) * 4);
+          uint4 ck[kWords / 4], cv[kWords / 4];
+#pragma unroll
+          for (int i = 0; i < kWords / 4; ++i) {
+            const uint32_t at = raw + (D == 128 ? group * 2 + i : part) * 1024 + token * 16;
+            ck[i] = lds_v4(at);
+            cv[i] = lds_v4(at + 32 * D);
+          }
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(kRawEmpty + slot));
+          if (++slot == kRaw) { slot = 0; phase ^= 1; }
+          if (tile >= kRing && !(ok = wait_warp(kTileEmpty + st, reuse))) break;
+          if (wt == 0) tile_bad[tile & 7] = bad;
+          __half2 ms, mc;
+          if (!in) mk = make_float2(0.f, 0.f);
+          scale_of(mk, ms, mc);
+#pragma unroll
+          for (int i = 0; i < kWords; ++i) {
+            const uint32_t w = in ? (&ck[i / 4].x)[i % 4] : 0x88888888u;
+            sts_v4(k_dst + (((word0 + i) ^ sw) << 4), widen(w, ms, mc));
+          }
+          // a token that is not finite has made its scores NaN: here it must not reach the rows that do not see it
+          if (!in || mv.y != mv.y) mv = make_float2(0.f, 0.f);
+          scale_of(mv, ms, mc);
+#pragma unroll
+          for (int i = 0; i < kWords; ++i) {
+            const uint32_t w = in ? (&cv[i / 4].x)[i % 4] : 0x88888888u;
+            sts_v4(v_dst + (((word0 + i) ^ sw) << 4), widen(w, ms, mc));
+          }
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(kTileFull + st));
+        }
+        if (ok && left > 0) next_block<L>(a, c);
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == kMmaWarp) tmem_dealloc(tmem, 512);
+}
+
+template <int D>
+int32_t launch(essa_ctx* ctx, const AttendArgs& a, cudaStream_t stream) {
+  constexpr int smem = Mem<D>::kBytes + 1024;
+  cudaError_t e = cudaFuncSetAttribute(attend_tiles_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e != cudaSuccess) return check_cuda(ctx, e, "cudaFuncSetAttribute (attend tiles)");
+  attend_tiles_kernel<D><<<ctx->sm_count, kThreads, smem, stream>>>(a);
+  e = cudaGetLastError();
+  if (e != cudaSuccess) return check_cuda(ctx, e, "attend tiles launch");
+  ++ctx->launches;
+  return launch_join<TileList, D>(ctx, a, ctx->sm_count, 8, stream);
+}
+
+}  // namespace
+
+int64_t attend_tiles_workspace(int head_dim, int sm_count) { return (int64_t)sm_count * 2 * TileList::R * (head_dim + 2) * 4; }
+
+int32_t launch_attend_tiles(essa_ctx* ctx, const AttendArgs& a, cudaStream_t stream) {
+  return a.v.head_dim == 64 ? launch<64>(ctx, a, stream) : launch<128>(ctx, a, stream);
+}
+
+}  // namespace essa

@@ -79,32 +79,36 @@ class Pair:
             assert got.shape == want.shape
 
 
-def attend_bound(q, v, codes, scale, out, p, softmax_scale, k=None):
-    """How far a row of essa_cache_attend may be from the fp64 result, element by element; one entry, all heads.
+def attend_bound(q, v, codes, scale, out, p, softmax_scale, k):
+    """How far a row of essa_cache_attend may be from the fp64 result, element by element; one entry, all heads.  It holds for both kernels.
 
     * out is rounded to bf16 once: 2^-8 |out|;
-    * a weight times the value's scale is rounded to bf16 before it meets (code - 8): 2^-8 sum_k p_k s_k |c_k - 8|;
-    * a score is wrong by at most `d` and moves the weights by a factor e^(+-2 d) at most: (e^(2 d) - 1) sum_k p_k |v_k|.  The tensor core adds
-      64 products of q (128 + code) <= 143 |q| in fp32 (taken as 16 roundings of 2^-23), the scales and the second term
-      (minimum - 128 scale) sum(q) come on top with 2^-22 of terms of the same size: d = scale * 2^-18 * 143 * sum_g max_k(s_g) sum|q_g|
-      + 2^-21 max|score| for the final product and exponent (and, with k, the rounding of k to bf16 in the
-      tile kernel: eight standard deviations of a sum of independent errors of at most 2^-8 |q_i k_i| each).
+    * few rows: a weight times the value's scale is rounded to bf16 before it meets (code - 8): 2^-8 sum_k p_k s_k |c_k - 8|;
+      many rows: V and P are fp16, V's offset (minimum + 8 scale) too: 2^-11 sum_k p_k (2 |v_k| + |offset_k|), weights below
+      2^-14 of the largest to 2^-25 absolutely: 2^-25 sum_k |v_k| (the sum of the weights is at least 1);
+    * a score is wrong by at most `err` and moves the weights by a factor e^(+-2 err) at most: (e^(2 err) - 1) sum_k p_k |v_k|.  The tensor
+      core adds 64 products of q (128 + code) <= 143 |q| in fp32 (taken as 16 roundings of 2^-23), the scales and the second term
+      (minimum - 128 scale) sum(q) come on top with 2^-22 of terms of the same size: scale * 2^-18 * 143 * sum_g max_k(s_g) sum|q_g|, and
+      2^-21 max|score| for the final product and exponent.  Many rows: K is (code - 8) scale + offset with the offset and the result
+      rounded to fp16: 2^-11 |offset| |sum q| per group, as it is the same for the whole group, and eight standard deviations of a
+      sum of independent errors of at most 2^-11 |q_i k_i| each;
     * fp32 sums of weights: 2^-16 sum_k p_k |v_k|."""
     rows, heads, d = q.shape
-    kvh = v.shape[0]
-    group = heads // kvh
+    group = heads // v.shape[0]
+    q = q.astype(np.float64)
     tol = np.zeros_like(out)
     for h in range(heads):
         c = h // group
-        centred = np.abs(codes[c, 1].astype(np.float64) - 8) * np.repeat(scale[c, 1].astype(np.float64), co.GROUP, -1)
-        qa = np.abs(q[:, h].astype(np.float64))
-        smax = scale[c, 0].astype(np.float64).max(0, initial=0.0)  # per group
-        err = softmax_scale * 2.0 ** -18 * 143 * (qa.reshape(rows, -1, co.GROUP).sum(-1) * smax).sum(-1)
-        if k is not None and k.shape[1]:
-            e2 = np.max((qa ** 2) @ (np.abs(k[c]) ** 2).T, axis=1)
-            err = err + softmax_scale * 8 * 2.0 ** -8 / np.sqrt(3) * np.sqrt(e2)
-        big = np.max(np.abs(q[:, h].astype(np.float64) @ (k[c] if k is not None else v[c]).T), axis=1, initial=0.0) * softmax_scale
-        err = err + 2.0 ** -21 * big
-        spread = p[:, h] @ np.abs(v[c])
-        tol[:, h] = 2.0 ** -8 * np.abs(out[:, h]) + 2.0 ** -8 * (p[:, h] @ centred) + (np.expm1(2 * err)[:, None] + 2.0 ** -16) * spread + 1e-30
+        s = scale[c].astype(np.float64)                                      # [2, keys, groups]
+        centred = (codes[c].astype(np.float64) - 8) * np.repeat(s, co.GROUP, -1)
+        offset = np.stack([k[c], v[c]]) - centred
+        qh, vh = q[:, h], np.abs(v[c])
+        err = softmax_scale * 2.0 ** -18 * 143 * (np.abs(qh).reshape(rows, -1, co.GROUP).sum(-1) * s[0].max(0, initial=0.0)).sum(-1)
+        err = err + 2.0 ** -21 * softmax_scale * np.max(np.abs(qh @ k[c].T), axis=1, initial=0.0)
+        shared = sum(np.abs(qh[:, g:g + co.GROUP] @ offset[0][:, g:g + co.GROUP].T) for g in range(0, d, co.GROUP))
+        alone = 8 / np.sqrt(3) * np.sqrt((qh ** 2) @ (k[c] ** 2).T)
+        err = err + softmax_scale * 2.0 ** -11 * np.max(shared + alone, axis=1, initial=0.0)
+        ph = p[:, h]
+        tol[:, h] = (2.0 ** -8 * np.abs(out[:, h]) + 2.0 ** -8 * (ph @ np.abs(centred[1])) + 2.0 ** -11 * (ph @ (2 * vh + np.abs(offset[1])))
+                     + 2.0 ** -25 * (ph > 0).astype(float) @ vh + (np.expm1(2 * err)[:, None] + 2.0 ** -16) * (ph @ vh) + 1e-30)
     return tol
