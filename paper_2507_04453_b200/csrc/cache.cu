@@ -669,6 +669,7 @@ int32_t essa_cache_attend(essa_ctx* ctx, const essa_cache_desc* cache, int32_t l
   a.ld_q = ld_q;
   a.ld_out = ld_out;
   a.group = (int32_t)group;
+  a.by_group = Divisor::of((uint32_t)group);
   a.scale = scale * 1.4426950408889634f;
   a.ws = static_cast<float*>(workspace);
   a.status = ctx->d_status;

@@ -25,9 +25,9 @@ constexpr int kThreads = kWarps * 32 + 32;    // + one copying warp
 // Row blocks of R rows; every row block of an entry walks all its pages (the few rows of an entry see nearly the same ones).
 template <int ROWS>
 struct DecodeList {
-  static constexpr int R = ROWS, kMinRun = 2;
-  __device__ static int tiles(const EntryInfo& e, int, int) { return max((e.len + kPageTokens - 1) / kPageTokens, 1); }
-  __device__ static long long per_head(const EntryInfo& e, int group) { return (long long)row_blocks(e, group, R) * tiles(e, group, 0); }
+  static constexpr int R = ROWS, kMinRun = 2, kSetup = 2;
+  __device__ static int tiles(const EntryInfo& e, const AttendArgs&, int) { return max((e.len + kPageTokens - 1) / kPageTokens, 1); }
+  __device__ static long long per_head(const EntryInfo& e, const AttendArgs& a) { return (long long)row_blocks(e, a.group, R) * (tiles(e, a, 0) + kSetup); }
 };
 
 __device__ __forceinline__ void ldmatrix_x4(uint32_t addr, uint32_t (&r)[4]) {
@@ -107,13 +107,13 @@ __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_
     uint32_t phase = 0;
     bool ok = true;
     while (ok && left > 0) {
-      const int stop = (int)min((long long)c.tiles, c.tile + left);
-      left -= stop - c.tile;
+      int tile, stop;
+      take_block<L>(c, left, tile, stop);
       const int32_t* row = a.v.table + (int64_t)max(c.info.slot, 0) * a.v.max_pages;
       const bool none = c.info.len == 0;
-      for (; c.tile < stop; ++c.tile) {
+      for (; tile < stop; ++tile) {
         if (filled >= S::kStages && !mbar_wait(empty + 8 * st, phase ^ 1, &abort_flag, a.status)) { ok = false; break; }
-        const int page = none ? -1 : __ldg(row + c.tile);
+        const int page = none ? -1 : __ldg(row + tile);
         const bool there = page >= 0 && page < a.v.num_pages;
         if (!there && (!none || c.info.slot < 0)) cache_fault(a.status);
         bad_page[st] = !there;
@@ -139,7 +139,10 @@ __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_
   int st = 0;
   uint32_t phase = 0;
   bool dead = false;  // a wait ran out: the warp goes through the barriers with the others and does nothing else
-  while (left > 0) {
+  for (; left > 0; next_block<L>(a, c)) {
+    int first, stop;
+    take_block<L>(c, left, first, stop);
+    if (first == stop) break;  // (the run ends before the row block's first tile)
     const int rows = c.info.rows * a.group;  // (fits: T * group is checked on the host)
     const int r0 = c.rb * R;
     // --- query operand: lane (g, t) holds channels 32 h + 8 t .. + 7 of column g, in the order that the nibbles come in
@@ -149,7 +152,7 @@ __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       const int r = r0 + nt * 8 + g;
-      const int j = r / a.group, hd = r - j * a.group;
+      const int j = a.by_group(r), hd = r - j * a.group;
       const bool there = r < rows;
       const uint4* src = reinterpret_cast<const uint4*>(a.q + (int64_t)(c.info.row0 + (there ? j : 0)) * a.ld_q + (int64_t)(c.kvh * a.group + hd) * D) + t;
       float sum[G];
@@ -175,7 +178,7 @@ __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_
 #pragma unroll
       for (int x = 0; x < 2; ++x) {  // tokens that column 2 t + x sees
         const int rc = r0 + nt * 8 + 2 * t + x;
-        limit[nt][x] = rc < rows ? c.info.len - c.info.rows + rc / a.group + 1 : 0;
+        limit[nt][x] = rc < rows ? c.info.len - c.info.rows + a.by_group(rc) + 1 : 0;
       }
     }
     float o[NT][CH][2][4];
@@ -194,7 +197,6 @@ __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_
         for (int i = 0; i < G; ++i) om[nt][i][x] = 0.f;
       }
     }
-    const int first = c.tile, stop = (int)min((long long)c.tiles, c.tile + left);
     for (int tile = first; tile < stop; ++tile) {
       if (!dead) dead = !__all_sync(0xffffffffu, mbar_wait(full + 8 * st, phase, &abort_flag, a.status));
       if (dead) continue;
@@ -320,7 +322,6 @@ __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_
       if (lane == 0) mbar_arrive(empty + 8 * st);
       if (++st == S::kStages) { st = 0; phase ^= 1; }
     }
-    left -= stop - first;
 
     // --- join the four warps: each leaves O, maximum and sum of its tokens in shared memory
     float* mine = join + warp * S::kPart;
@@ -367,7 +368,7 @@ __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_
         if (d4 == 0) { part[R * D + col] = m; part[R * D + R + col] = sum; }
       } else if (r < rows) {
         const float inv = sum == 0.f ? 0.f : 1.f / sum;  // a row that sees nothing is 0
-        const int j = r / a.group, hd = r - j * a.group;
+        const int j = a.by_group(r), hd = r - j * a.group;
         uint2 y;
         y.x = pack_bf16x2(v.x * inv, v.y * inv);
         y.y = pack_bf16x2(v.z * inv, v.w * inv);
@@ -375,7 +376,7 @@ __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_
       }
     }
     epi_bar_sync();
-    if (left > 0) next_block<L>(a, c);
+    if (left <= 0) break;
   }
 }
 

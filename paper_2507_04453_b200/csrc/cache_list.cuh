@@ -3,15 +3,31 @@
 // results (O, maximum, sum per row, fp32) in the workspace, two slots per run at most, and attend_join_kernel adds them in
 // run order.  Ragged lengths, causal prompts and single long sequences balance alike, results do not depend on timing, and
 // the workspace is bounded by the grid.
+// A row block also costs its queries' way in and its results' way out, so it stands in the list as kSetup elements without work,
+// followed by its key tiles; a cut between those leaves it whole to the run behind the cut.
 //
-// A list policy L gives R (query rows of a row block), tiles(info, group, rb) >= 1 (key tiles of a row block, so that rows that
-// see nothing are still written) and per_head(info, group) (their sum over an entry's row blocks).
+// A list policy L gives R (query rows of a row block), tiles(info, args, rb) >= 1 (key tiles of a row block, so that rows that
+// see nothing are still written), per_head(info, args) (the elements of all row blocks of an entry), kSetup and kMinRun.
 #pragma once
 
 #include "cache.cuh"
 #include "tc_ptx.cuh"
 
 namespace essa {
+
+// Division by the number of heads of a group (rows are token * group + head) as a multiplication: for n < 2^31,
+// n / d = (umulhi(mul, n) + n) >> shift with shift = ceil(log2 d), mul = floor(2^32 (2^shift - d) / d) + 1.
+struct Divisor {
+  uint32_t d, mul, shift;
+  static Divisor of(uint32_t d) {
+    uint32_t s = 0;
+    while ((1ull << s) < d) ++s;
+    return {d, (uint32_t)(((1ull << 32) * ((1ull << s) - d)) / d + 1), s};
+  }
+#ifdef __CUDACC__
+  __device__ __forceinline__ int operator()(int n) const { return (int)((__umulhi(mul, (uint32_t)n) + (uint32_t)n) >> shift); }
+#endif
+};
 
 struct AttendArgs {
   CacheView v;
@@ -20,6 +36,7 @@ struct AttendArgs {
   __nv_bfloat16* out;
   int64_t ld_q, ld_out;
   int32_t group;
+  Divisor by_group;
   float scale;  // softmax scale * log2(e)
   float* ws;
   int32_t* status;
@@ -34,11 +51,12 @@ __device__ __forceinline__ float ex2(float x) {
 }
 
 struct Cursor {  // a place in the list
-  int entry, kvh, rb, tile, blocks, tiles;
+  int entry, kvh, rb, at, blocks, tiles;  // at: element of the row block
   EntryInfo info;
 };
 
-__device__ __forceinline__ int row_blocks(const EntryInfo& e, int group, int R) { return (int)(((int64_t)e.rows * group + R - 1) / R); }
+// (rows * group < 2^31 is checked on the host)
+__device__ __forceinline__ int row_blocks(const EntryInfo& e, int group, int R) { return (int)(((uint32_t)e.rows * (uint32_t)group + R - 1) / R); }
 
 // Elements of the list; all threads of the block.  sm: shared [33].
 template <class L>
@@ -47,7 +65,7 @@ __device__ long long list_total(const AttendArgs& a, long long* sm) {
   for (int base = 0; base < a.e.n; base += blockDim.x) {
     const int i = base + threadIdx.x;
     long long w = 0, t;
-    if (i < a.e.n) w = L::per_head(load_entry(a.v, a.e, i), a.group) * a.v.kv_heads;
+    if (i < a.e.n) w = L::per_head(load_entry(a.v, a.e, i), a) * a.v.kv_heads;
     block_scan(w, &t, sm);
     total += t;
   }
@@ -61,7 +79,7 @@ __device__ void list_seek(const AttendArgs& a, long long at, Cursor& c, long lon
   for (int base = 0; base < a.e.n; base += blockDim.x) {
     const int i = base + threadIdx.x;
     long long w = 0, t;
-    if (i < a.e.n) w = L::per_head(load_entry(a.v, a.e, i), a.group) * a.v.kv_heads;
+    if (i < a.e.n) w = L::per_head(load_entry(a.v, a.e, i), a) * a.v.kv_heads;
     const long long pre = before + block_scan(w, &t, sm);
     if (w > 0 && at >= pre && at < pre + w) {
       found[0] = i;
@@ -74,17 +92,26 @@ __device__ void list_seek(const AttendArgs& a, long long at, Cursor& c, long lon
   c.entry = (int)found[0];
   c.info = load_entry(a.v, a.e, c.entry);
   c.blocks = row_blocks(c.info, a.group, L::R);
-  const long long per = L::per_head(c.info, a.group);
+  const long long per = L::per_head(c.info, a);
   c.kvh = (int)(found[1] / per);
   long long rest = found[1] % per;
-  for (c.rb = 0; (c.tiles = L::tiles(c.info, a.group, c.rb)) <= rest; ++c.rb) rest -= c.tiles;
-  c.tile = (int)rest;
+  for (c.rb = 0; (c.tiles = L::tiles(c.info, a, c.rb)) + L::kSetup <= rest; ++c.rb) rest -= c.tiles + L::kSetup;
+  c.at = (int)rest;
 }
 
+// Takes what is left of c's row block from a run that has `left` elements to go: key tiles first .. stop - 1 (none, if the run ends
+// before the first) are the run's.
+template <class L>
+__device__ __forceinline__ void take_block(const Cursor& c, long long& left, int& first, int& stop) {
+  const int n = (int)min((long long)(c.tiles + L::kSetup - c.at), left);
+  first = max(c.at - L::kSetup, 0);
+  stop = max(c.at + n - L::kSetup, 0);
+  left -= n;
+}
 // The row block after c's; must not be called at the end of the list.
 template <class L>
 __device__ __forceinline__ void next_block(const AttendArgs& a, Cursor& c) {
-  c.tile = 0;
+  c.at = 0;
   if (++c.rb >= c.blocks) {
     c.rb = 0;
     if (++c.kvh >= a.v.kv_heads) {
@@ -96,7 +123,7 @@ __device__ __forceinline__ void next_block(const AttendArgs& a, Cursor& c) {
       } while (c.blocks == 0);
     }
   }
-  c.tiles = L::tiles(c.info, a.group, c.rb);
+  c.tiles = L::tiles(c.info, a, c.rb);
 }
 
 __device__ __forceinline__ long long run_start(long long total, int runs, int c) { return total * c / runs; }
@@ -117,7 +144,7 @@ __device__ __forceinline__ float* partial_of(const AttendArgs& a, int run, bool 
 }
 
 // Joins the row blocks that run boundaries cut.  Thread blocks (c, *) look at the boundary between runs c and c + 1 and work if it
-// is the first one inside its row block; gridDim.y of them share its rows.  Launched to start beside the attention kernel: it finds
+// is the first one between key tiles of its row block; gridDim.y of them share its rows.  Launched to start beside the attention kernel: it finds
 // its row block meanwhile and waits for the partial results.
 template <class L, int D>
 __global__ void __launch_bounds__(128) attend_join_kernel(AttendArgs a, int grid) {
@@ -133,19 +160,21 @@ __global__ void __launch_bounds__(128) attend_join_kernel(AttendArgs a, int grid
   if (work) {
     const long long edge = run_start(total, runs, run + 1);
     list_seek<L>(a, edge, c, scan_sm, found);
-    first = edge - c.tile;  // the row block's first element
-    work = c.tile > 0 && first >= run_start(total, runs, run);
+    first = edge - c.at;  // the row block's first element
+    work = c.at > L::kSetup && first + L::kSetup >= run_start(total, runs, run);
   }
   grid_dep_wait();
   if (!work) return;
-  const long long stop = first + c.tiles;
+  const long long stop = first + L::kSetup + c.tiles;
   const int rows = c.info.rows * a.group, r0 = c.rb * R;
+  int last = run;  // the runs run .. last have a part of the row block
+  while (last + 1 < runs && run_start(total, runs, last + 1) < stop) ++last;
   for (int x = blockIdx.y * 128 + threadIdx.x; x < R * (D / 4); x += gridDim.y * 128) {
     const int row = x / (D / 4), d4 = (x % (D / 4)) * 4, r = r0 + row;
     if (r >= rows) break;
     float m = -INFINITY, sum = 0.f;
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int k = run; k < runs && run_start(total, runs, k) < stop; ++k) {
+    for (int k = run; k <= last; ++k) {
       const float* p = partial_of<L, D>(a, k, k == run);
       const float pm = p[R * D + row], mn = fmaxf(m, pm);
       const float f0 = m == -INFINITY ? 0.f : ex2((m - mn) * a.scale), f1 = pm == -INFINITY ? 0.f : ex2((pm - mn) * a.scale);
@@ -158,7 +187,7 @@ __global__ void __launch_bounds__(128) attend_join_kernel(AttendArgs a, int grid
       m = mn;
     }
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    const int j = r / a.group, hd = r - j * a.group;
+    const int j = a.by_group(r), hd = r - j * a.group;
     uint2 y;
     y.x = pack_bf16x2(v.x * inv, v.y * inv);
     y.y = pack_bf16x2(v.z * inv, v.w * inv);

@@ -22,16 +22,16 @@ namespace essa {
 namespace {
 
 struct TileList {
-  static constexpr int R = 256, kKeys = kPageTokens, kMinRun = 2;
+  static constexpr int R = 256, kKeys = kPageTokens, kMinRun = 2, kSetup = 6;
   // keys that the last row of the row block sees, in tiles
-  __device__ static int tiles(const EntryInfo& e, int group, int rb) {
-    const int last = (int)min((int64_t)e.rows - 1, ((int64_t)rb * R + R - 1) / group);
+  __device__ static int tiles(const EntryInfo& e, const AttendArgs& a, int rb) {
+    const int last = min(e.rows - 1, a.by_group(min(rb * R, 0x7fffffff - R) + R - 1));
     return max((e.len - e.rows + last + 1 + kKeys - 1) / kKeys, 1);
   }
-  __device__ static long long per_head(const EntryInfo& e, int group) {
+  __device__ static long long per_head(const EntryInfo& e, const AttendArgs& a) {
     long long sum = 0;
-    const int blocks = row_blocks(e, group, R);
-    for (int rb = 0; rb < blocks; ++rb) sum += tiles(e, group, rb);
+    const int blocks = row_blocks(e, a.group, R);
+    for (int rb = 0; rb < blocks; ++rb) sum += tiles(e, a, rb) + kSetup;
     return sum;
   }
 };
@@ -39,8 +39,8 @@ struct TileList {
 constexpr int kSoftWarps = 8, kWidenWarps = 4;
 constexpr int kMmaWarp = kSoftWarps + kWidenWarps, kCopyWarp = kMmaWarp + 1;
 constexpr int kThreads = 512;  // four warpgroups; the last two warps only give registers away
-// Registers per thread: launched with 128, of which the softmax takes more.  2 * 152 + 2 * 104 = 4 * 128.
-constexpr int kSoftRegs = 152, kOtherRegs = 104;
+// Registers per thread: launched with 128, of which the softmax takes more.  2 * 136 + 2 * 120 = 4 * 128.
+constexpr int kSoftRegs = 136, kOtherRegs = 120;
 constexpr int kRaw = 3;  // pages in flight
 
 constexpr int kRing = 4;  // key tiles of K and of V
@@ -125,15 +125,22 @@ __device__ __forceinline__ uint64_t desc_of(uint32_t lo) {
   return (uint64_t)hi << 32 | lo;
 }
 
+// (w & mask) | magic in one instruction (left to the compiler it becomes two).
+template <uint32_t MASK>
+__device__ __forceinline__ __half2 masked(uint32_t w, uint32_t magic) {
+  uint32_t r;
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(w), "n"(MASK), "r"(magic));
+  return as_half2(r);
+}
 // Eight codes -> fp16 (code - 8) * s + c in the order (0, 4, 1, 5, 2, 6, 3, 7).
-__device__ __forceinline__ uint4 widen(uint32_t w, __half2 s, __half2 c) {
+__device__ __forceinline__ uint4 widen(uint32_t w, __half2 s, __half2 c, uint32_t magic /* 0x64006400 */) {
   const __half2 o = as_half2(0x64086408u), sixteenth = as_half2(0x2c002c00u), o16 = as_half2(0xd480d480u);  // 1032; 1 / 16; -72
   uint32_t y[4];
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
     const uint32_t x = w >> (8 * j);
-    y[2 * j] = bits(__hfma2(__hsub2(as_half2((x & 0x000f000fu) | 0x64006400u), o), s, c));                    // 1024 + code
-    y[2 * j + 1] = bits(__hfma2(__hfma2(as_half2((x & 0x00f000f0u) | 0x64006400u), sixteenth, o16), s, c));  // 1024 + 16 code
+    y[2 * j] = bits(__hfma2(__hsub2(masked<0x000f000fu>(x, magic), o), s, c));                    // 1024 + code
+    y[2 * j + 1] = bits(__hfma2(__hfma2(masked<0x00f000f0u>(x, magic), sixteenth, o16), s, c));  // 1024 + 16 code
   }
   return make_uint4(y[0], y[1], y[2], y[3]);
 }
@@ -213,11 +220,11 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
     const auto enter = [&](Block& b) {
       for (;; next_block<L>(a, c)) {
         if (left <= 0) return false;
-        const int stop = (int)min((long long)c.tiles, c.tile + left);
-        b.first = c.tile;
-        b.n = stop - c.tile;
-        b.whole = c.tile == 0 && stop == c.tiles;
-        left -= b.n;
+        int stop;
+        take_block<L>(c, left, b.first, stop);
+        b.n = stop - b.first;
+        if (b.n == 0) return false;  // (the run ends before the row block's first tile)
+        b.whole = b.first == 0 && stop == c.tiles;
         if (c.rb * L::R + h * 128 < c.info.rows * a.group) break;
         tile += b.n;
         if (left <= 0) return false;
@@ -225,15 +232,13 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
       const int rows = c.info.rows * a.group, r0 = c.rb * L::R + h * 128;
       constexpr int kLanes = D / 8, kRowsAt = 32 / kLanes, kSteps = 32 / kRowsAt;
       const int ch = lane % kLanes;
-      int r = r0 + (warp & 3) * 32 + lane / kLanes, tok = r / a.group, hd = r - tok * a.group;
       const __nv_bfloat16* q = a.q + (int64_t)c.info.row0 * a.ld_q + (int64_t)c.kvh * a.group * D + ch * 8;
       uint4 x[kSteps];
 #pragma unroll
       for (int i = 0; i < kSteps; ++i) {
+        const int r = r0 + (warp & 3) * 32 + i * kRowsAt + lane / kLanes, tok = a.by_group(r);
         x[i] = make_uint4(0, 0, 0, 0);
-        if (r < rows) x[i] = __ldg(reinterpret_cast<const uint4*>(q + tok * a.ld_q + hd * D));
-        r += kRowsAt;
-        for (hd += kRowsAt; hd >= a.group; hd -= a.group) ++tok;
+        if (r < rows) x[i] = __ldg(reinterpret_cast<const uint4*>(q + tok * a.ld_q + (r - tok * a.group) * D));
       }
       // fp16 holds the rows as they are if every piece of eight channels has an element between 2^-6 and 2^15; otherwise each row is
       // brought there by a power of two
@@ -271,15 +276,13 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(kQFull + h));
-      r = r0 + row;
-      tok = r / a.group;
+      const int r = r0 + row, tok = a.by_group(r);
       b.there = r < rows;
       b.out = a.out + (int64_t)(c.info.row0 + tok) * a.ld_out + (int64_t)(c.kvh * a.group + r - tok * a.group) * D;
       b.back = row_scale[h * 128 + row];
       // rows behind the last one have q = 0 and are not written, whatever they see
-      b.limit = b.lowest = b.there ? c.info.len - c.info.rows + tok + 1 : 0x7fffffff;
-#pragma unroll
-      for (int d = 16; d; d >>= 1) b.lowest = min(b.lowest, __shfl_xor_sync(0xffffffffu, b.lowest, d));
+      b.limit = b.there ? c.info.len - c.info.rows + tok + 1 : 0x7fffffff;
+      b.lowest = __shfl_sync(0xffffffffu, b.limit, 0);
       if (left > 0) next_block<L>(a, c);
       return true;
     };
@@ -342,46 +345,67 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
       const float scale = a.scale * b.back;
       m = -INFINITY;
       sum = 0.f;
-      for (int j = 0; j < b.n; ++j, ++tile) {
-        const uint32_t buf = tile & 1;
-        if (!(ok = wait_warp(kSFull + 2 * h + buf, s_ph >> buf & 1))) break;
-        s_ph ^= 1u << buf;
+      const auto scores_at = [&](int t) { return tmem + 128 * h + 64 * (t & 1) + lanes; };
+      // Scores of the block's tile j, the run's tile t: waits for them; hidden ones become -infinity in place (the tiles that hide none
+      // pay nothing for it).
+      const auto arrived = [&](int j, int t) {
+        if (!(ok = wait_warp(kSFull + 2 * h + (t & 1), s_ph >> (t & 1) & 1))) return;
+        s_ph ^= 1u << (t & 1);
         tc_fence_after();
-        const uint32_t s_at = tmem + 128 * h + 64 * buf + lanes;
-        const int key0 = (b.first + j) * L::kKeys, bad = tile_bad[tile & 7];
-        const int see = bad ? 0 : b.limit - key0;  // keys of the tile before this one are seen
-        const bool mask = key0 + L::kKeys > b.lowest || bad;
-        uint32_t p[32];
-        float add[2], best;
-        if (mask) {  // hidden scores become -infinity in place: the tiles that need none pay nothing
+        const int key0 = (b.first + j) * L::kKeys, bad = tile_bad[t & 7];
+        if (key0 + L::kKeys > b.lowest || bad) {
+          const int see = bad ? 0 : b.limit - key0;  // keys of the tile before this one are seen
 #pragma unroll 1
           for (int d = 0; d < L::kKeys; d += 32) {
-            tmem_ld32_issue(s_at + d, p);
-            tmem_ld_done(p);
+            uint32_t v[32];
+            tmem_ld32_issue(scores_at(t) + d, v);
+            tmem_ld_done(v);
 #pragma unroll
             for (int i = 0; i < 32; ++i)
-              if (d + i >= see) p[i] = 0xff800000u;
-            tmem_st32(s_at + d, p);
+              if (d + i >= see) v[i] = 0xff800000u;
+            tmem_st32(scores_at(t) + d, v);
           }
         }
-        for (int again = j == 0 ? 0 : 1;; ++again) {  // (the first tile: once for its maximum alone)
+      };
+      const uint64_t scale2 = pack_f32x2(scale, scale);
+      for (int j = 0; j < b.n; ++j, ++tile) {
+        arrived(j, tile);
+        if (!ok) break;
+        const uint32_t s_at = scores_at(tile);
+        uint32_t p[32];
+        float s0, s1;
+        bool look = j == 0;  // for the maximum, before the weights: in the first tile, and where the weights by the one so far turn out too large
+        for (;;) {
           uint32_t v[2][32];
           tmem_ld32_issue(s_at, v[0]);
           tmem_ld32_issue(s_at + 32, v[1]);
           tmem_ld_done(v[0]);
           tmem_ld_done(v[1]);
-          float t[4] = {m, m, m, m};
+          if (look) {
+            float t[4] = {m, m, m, m};
 #pragma unroll
-          for (int i = 0; i < 64; i += 2) t[i >> 1 & 3] = max3(t[i >> 1 & 3], __uint_as_float(v[i >> 5][i & 31]), __uint_as_float(v[i >> 5][(i & 31) + 1]));
-          best = max3(max3(t[0], t[1], t[2]), t[3], t[3]);
-          if (again == 0) {
-            m = best;
-            continue;
+            for (int i = 0; i < 64; i += 2) t[i >> 1 & 3] = max3(t[i >> 1 & 3], __uint_as_float(v[i >> 5][i & 31]), __uint_as_float(v[i >> 5][(i & 31) + 1]));
+            const float top = max3(max3(t[0], t[1], t[2]), t[3], t[3]);
+            if (j > 0) {
+              // O holds the tiles before this one: their products end before those with the K of the next tile, or (there is none) signal
+              if (!(ok = j + 1 < b.n ? wait_warp(kSFull + 2 * h + (~tile & 1), s_ph >> (~tile & 1) & 1) : wait_warp(kOFull + h, o_ph))) break;
+              tc_fence_after();
+              const float f = top == m ? 1.f : ex2((m - top) * scale);
+              sum *= f;
+#pragma unroll 1
+              for (int d = 0; d < D; d += 32) {
+                tmem_ld32_issue(o_at + d, p);
+                tmem_ld_done(p);
+#pragma unroll
+                for (int i = 0; i < 32; ++i) p[i] = __float_as_uint(__uint_as_float(p[i]) * f);
+                tmem_st32(o_at + d, p);
+              }
+            }
+            m = top;
           }
-          // weights by the maximum so far, the tile's maximum beside them
           const float shift = m == -INFINITY ? 0.f : -m * scale;
+          const uint64_t shift2 = pack_f32x2(shift, shift);
           uint64_t sums[2] = {0, 0};
-          const uint64_t scale2 = pack_f32x2(scale, scale), shift2 = pack_f32x2(shift, shift);
 #pragma unroll
           for (int i = 0; i < 32; ++i) {
             float x0, x1;
@@ -391,26 +415,15 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
             sums[i & 1] = add_f32x2(sums[i & 1], pack_f32x2(x0, x1));
             p[i] = pack_f16x2(x0, x1);
           }
-          unpack_f32x2(add_f32x2(sums[0], sums[1]), add[0], add[1]);
-          // the maximum moves only when a score is 2^6 above it (weights stay below 2^6): seldom, and then the tile is done again
-          if (!__any_sync(0xffffffffu, best * scale > m * scale + 6.f)) break;
-          // O holds the tiles before this one: their products end before those with the K of the next tile, or (there is none) signal
-          if (!(ok = j + 1 < b.n ? wait_warp(kSFull + 2 * h + (buf ^ 1), s_ph >> (buf ^ 1) & 1) : wait_warp(kOFull + h, o_ph))) break;
-          tc_fence_after();
-          const float f = best == m ? 1.f : ex2((m - best) * scale);
-          m = best;
-          sum *= f;
-#pragma unroll 1
-          for (int d = 0; d < D; d += 32) {
-            tmem_ld32_issue(o_at + d, p);
-            tmem_ld_done(p);
-#pragma unroll
-            for (int i = 0; i < 32; ++i) p[i] = __float_as_uint(__uint_as_float(p[i]) * f);
-            tmem_st32(o_at + d, p);
-          }
+          unpack_f32x2(add_f32x2(sums[0], sums[1]), s0, s1);
+          s0 += s1;
+          // No running maximum: the tile's sum says whether a weight can be too large for fp16 (a score 2^14 above the maximum so far in
+          // the softmax; seldom).  Then the maximum is looked for, O and the sum are scaled, and the tile is done again.
+          if (look || !__any_sync(0xffffffffu, s0 > 16384.f || (m == -INFINITY && s0 > 0.f))) break;
+          look = true;
         }
         if (!ok) break;
-        sum += add[0] + add[1];
+        sum += s0;
         tmem_st32(s_at, p);
         if (j > 0 && j + 1 == b.n) {  // the last two products with V signal: the first of them is seen before the second can start
           if (!(ok = wait_warp(kOFull + h, o_ph))) break;
@@ -418,7 +431,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
         }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(bar(kPFull + 2 * h + buf));
+        if (lane == 0) mbar_arrive(bar(kPFull + 2 * h + (tile & 1)));
       }
       if (!ok) break;
     }
@@ -430,16 +443,17 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
         uint32_t phase = 0;
         bool ok = true;
         while (ok && left > 0) {
-          const int stop = (int)min((long long)c.tiles, c.tile + left);
-          left -= stop - c.tile;
+          int first, stop;
+          take_block<L>(c, left, first, stop);
+          if (first == stop) break;  // (the run ends before the row block's first tile)
           const int pages = (c.info.len + kPageTokens - 1) / kPageTokens;
           const int32_t* row = a.v.table + (int64_t)max(c.info.slot, 0) * a.v.max_pages;
           if (c.info.slot < 0) cache_fault(a.status);
           {  // the row block's part of q into L2, a key tile or more before the softmax warps ask for it
-            const int t0 = c.rb * L::R / a.group, t1 = min(c.info.rows, (c.rb * L::R + L::R + a.group - 1) / a.group);
+            const int t0 = a.by_group(c.rb * L::R), t1 = min(c.info.rows, a.by_group(min(c.rb * L::R, 0x7fffffff - L::R) + L::R - 1) + 1);
             for (int t = t0; t < t1; ++t) prefetch_l2(a.q + (int64_t)(c.info.row0 + t) * a.ld_q + (int64_t)c.kvh * a.group * D, a.group * D * 2);
           }
-          for (int p = c.tile; p < stop; ++p) {
+          for (int p = first; p < stop; ++p) {
             if (filled >= kRaw && !wait(kRawEmpty + slot, phase ^ 1)) { ok = false; break; }
             const int page = p < pages ? __ldg(row + p) : -1;
             const bool there = page >= 0 && page < a.v.num_pages;
@@ -474,9 +488,10 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
           umma_commit(bar(kSFull + 2 * h + (k_at & 1)));
         };
         while (ok && left > 0) {
-          const int stop = (int)min((long long)c.tiles, c.tile + left), n = stop - c.tile;
-          const int halves = c.info.rows * a.group - c.rb * L::R > 128 ? 2 : 1;
-          left -= n;
+          int first, stop;
+          take_block<L>(c, left, first, stop);
+          const int n = stop - first, halves = c.info.rows * a.group - c.rb * L::R > 128 ? 2 : 1;
+          if (n == 0) break;
           // Products with K run two tiles ahead: the scores of a half's next tile are there when its softmax has finished one.
           for (int j = 0; ok && j < min(n, 2); ++j, ++k_at) {
             if (!(ok = wait(kTileFull + k_at % kRing, k_at / kRing & 1))) break;
@@ -523,15 +538,17 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
     } else if (warp < kMmaWarp) {  // ---------------------------------------------------------- pages -> operands
       const int wt = tid - kSoftWarps * 32;
       const int token = wt & 63, part = wt >> 6;       // D = 128: a 64-channel group each; D = 64: half a group each
+      uint32_t magic = 0x64006400u;
+      asm volatile("" : "+r"(magic));  // in a register
       constexpr int kWords = D / 16;                   // 32-bit words of codes per thread: 8 or 4
       const int group = D == 128 ? part : 0, word0 = D == 128 ? 0 : part * 4;
       int slot = 0, tile = 0;
       uint32_t phase = 0;
       bool ok = true;
       while (ok && left > 0) {
-        const int stop = (int)min((long long)c.tiles, c.tile + left);
-        left -= stop - c.tile;
-        for (int j = c.tile; j < stop; ++j, ++tile) {
+        int first, stop;
+        take_block<L>(c, left, first, stop);
+        for (int j = first; j < stop; ++j, ++tile) {
           const int st = tile % kRing;
           const uint32_t reuse = (tile / kRing & 1) ^ 1;
           const uint32_t k_dst = base + M::kK + st * M::kTile + group * M::kSub + token * 128, v_dst = k_dst + M::kV - M::kK;
@@ -559,7 +576,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
 #pragma unroll
           for (int i = 0; i < kWords; ++i) {
             const uint32_t w = in ? (&ck[i / 4].x)[i % 4] : 0x88888888u;
-            sts_v4(k_dst + (((word0 + i) ^ sw) << 4), widen(w, ms, mc));
+            sts_v4(k_dst + (((word0 + i) ^ sw) << 4), widen(w, ms, mc, magic));
           }
           // a token that is not finite has made its scores NaN: here it must not reach the rows that do not see it
           if (!in || mv.y != mv.y) mv = make_float2(0.f, 0.f);
@@ -567,7 +584,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
 #pragma unroll
           for (int i = 0; i < kWords; ++i) {
             const uint32_t w = in ? (&cv[i / 4].x)[i % 4] : 0x88888888u;
-            sts_v4(v_dst + (((word0 + i) ^ sw) << 4), widen(w, ms, mc));
+            sts_v4(v_dst + (((word0 + i) ^ sw) << 4), widen(w, ms, mc, magic));
           }
           fence_proxy_async_smem();
           __syncwarp();
