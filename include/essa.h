@@ -450,9 +450,10 @@ int32_t essa_cache_read(essa_ctx* ctx, const essa_cache_desc* cache, int32_t lay
  *   multiple of kv_heads; scale > 0, finite.
  *   max_new >= 1: the most rows an entry is expected to have.  It only chooses the schedule (1 for decode steps); any value
  *   gives right results.
- * Scores, maximum, sums and the accumulators are fp32; out is rounded to bf16 once.  Up to 16 query rows per (entry, kv head), by
- * max_new: the products work on the codes themselves and a weight times its value's scale is rounded to bf16 once.  More rows: K,
- * V and the weights are fp16 operands (2^-11); stored values beyond +-65440 are taken as +-65440. */
+ * Scores, maximum, sums and the accumulators are fp32; out is rounded to bf16 once; operands of the products are fp16, each rounded
+ * once (2^-11).  Up to 16 query rows per (entry, kv head), by max_new, the products work on the codes themselves, and a weight times its
+ * value's scale is the rounded operand; with more rows they are K, V and the weights, and stored values beyond +-65440 are taken
+ * as +-65440. */
 int32_t essa_cache_attend(essa_ctx* ctx, const essa_cache_desc* cache, int32_t layer, const void* q, int64_t ld_q, int32_t q_heads, int32_t T,
                           const int32_t* slots, const int32_t* tok_offsets, int32_t n, int32_t max_new, float scale, void* out, int64_t ld_out,
                           void* workspace, int64_t workspace_bytes, void* stream);

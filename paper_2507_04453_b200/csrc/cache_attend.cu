@@ -2,14 +2,17 @@
 // K = code * scale + minimum per token and group of 64 channels.
 //
 // What bounds it: the cache is read once and each byte carries two values, so a B200 streams ~46 codes per clock and SM
-// from HBM; what the kernel has to keep up with is widening them.  The mathematics is arranged so that a code needs only
-// (shift, and-or) for K and one subtraction more for V:
-//   S = sum_g s_g (q_g . c_g) + min_g sum(q_g).  The tensor core multiplies q by the bf16 numbers 128 + c (a code dropped
-//   into the mantissa of 128); with acc_g = q_g . (128 + c_g) in fp32, S = sum_g s_g acc_g + (min_g - 128 s_g) sum(q_g).
-//   O = sum_k p_k (s_k (c_k - 8) + (min_k + 8 s_k)): p_k s_k is rounded to bf16 (one rounding, 2^-8 of a centred value at most: with the
-//   codes not centred it would be 2^-8 of a number 2.6 times as large), the second term stays on the CUDA cores in fp32.
-//   (Leaving the 128 in and subtracting 136 sum(p s) at the end loses the result in fp32: |128 s| against averages of
-//   thousands of values.)
+// from HBM; what the kernel has to keep up with is widening them.  The mathematics is arranged so that a code needs little more than an
+// and-or.  A nibble dropped into the mantissa of the fp16 number 1024 is 1024 + c, or 1024 + 16 c one nibble further up, so
+// that a word of eight codes needs one shift.
+//   S = sum_g s_g (q_g . c_g) + min_g sum(q_g).  The tensor core multiplies q, or q / 16, by those numbers as they are and starts from
+//   minus what the 1024 will add (a sum over q), so that in fp32 the offset has gone when it has finished.
+//   O = sum_k p_k (s_k (c_k - 8) + (min_k + 8 s_k)): one operation more takes a number to c - 8; the weight times the scale is rounded to
+//   fp16 (2^-11 of a centred value; with the codes not centred it would be 2^-11 of a number 2.6 times as large), the second term stays
+//   on the CUDA cores in fp32.  (Leaving the 1024 in and subtracting it from the sum at the end loses the result in fp32.)
+// fp16 holds what it has to: a query row is brought to a largest element of 2^13 .. 2^14 by a power of two, and scales are taken
+// relative to a power of two near the largest that the warp has met (products 2^-14 below it lose bits).
+// (The first version had bf16 operands: three shifts and twice the roundings per word of codes, 289 us for 910 MB of cache.)
 // K and V are the M = 16 operand of mma.m16n8k16, the query rows (heads of the group x tokens) are the N = 8 columns: a
 // group of up to eight heads fills the tensor core's tile, where q as the M operand would leave half of it empty.
 //
@@ -41,23 +44,12 @@ __device__ __forceinline__ uint32_t movmatrix_trans(uint32_t v) {
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
   return r;
 }
-__device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+__device__ __forceinline__ void mma_f16(float (&d)[4], __half2 a0, __half2 a1, __half2 a2, __half2 a3, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+      : "r"(half2_bits(a0)), "r"(half2_bits(a1)), "r"(half2_bits(a2)), "r"(half2_bits(a3)), "r"(b0), "r"(b1));
 }
-// Nibble j of both halves of w as the bf16 pair (128 + low, 128 + high).
-template <int J>
-__device__ __forceinline__ uint32_t nibbles(uint32_t w) {
-  return ((w >> (4 * J)) & 0x000f000fu) | 0x43004300u;
-}
-// ... centred: (code - 8), exact.
-template <int J>
-__device__ __forceinline__ uint32_t nibbles_centred(uint32_t w) {
-  const uint32_t x = nibbles<J>(w), o = 0x43084308u;  // 136
-  const __nv_bfloat162 r = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&x), *reinterpret_cast<const __nv_bfloat162*>(&o));
-  return *reinterpret_cast<const uint32_t*>(&r);
-}
+
 template <int D, int NT>
 struct Shape {
   static constexpr int R = 8 * NT;             // query rows of a row block
@@ -138,6 +130,8 @@ __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_
   const uint32_t k_lane = (uint32_t)(key0 + (lane & 15)) * 16 + (uint32_t)(lane >> 4) * 1024;  // ldmatrix row addresses: (tokens 0-7, 8-15) x two chunks
   int st = 0;
   uint32_t phase = 0;
+  uint32_t magic = 0x64006400u;
+  asm volatile("" : "+r"(magic));  // (in a register, where the and-or can take it)
   bool dead = false;  // a wait ran out: the warp goes through the barriers with the others and does nothing else
   for (; left > 0; next_block<L>(a, c)) {
     int first, stop;
@@ -145,44 +139,80 @@ __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_
     if (first == stop) break;  // (the run ends before the row block's first tile)
     const int rows = c.info.rows * a.group;  // (fits: T * group is checked on the host)
     const int r0 = c.rb * R;
-    // --- query operand: lane (g, t) holds channels 32 h + 8 t .. + 7 of column g, in the order that the nibbles come in
+    // --- query operand: lane (g, t) holds channels 32 h + 8 t .. + 7 of column g, in the order that the nibbles come in:
+    // (0, 4), (1, 5) / 16, (2, 6), (3, 7) / 16
     uint32_t qf[NT][CH][4];
-    float qsum[NT][G][2];
-    int limit[NT][2];
+    float qsum[NT][G][2], start[NT][G][2];  // per group: the sum of q; minus what the 1024 in the codes' numbers adds
+    float sc[NT][2], back[NT][2];           // softmax scale in the units of the row; what the row was divided by
+    int limit[NT][2], lowest = 0x7fffffff;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       const int r = r0 + nt * 8 + g;
       const int j = a.by_group(r), hd = r - j * a.group;
       const bool there = r < rows;
       const uint4* src = reinterpret_cast<const uint4*>(a.q + (int64_t)(c.info.row0 + (there ? j : 0)) * a.ld_q + (int64_t)(c.kvh * a.group + hd) * D) + t;
-      float sum[G];
+      uint4 u[CH];
+      float big = 0.f;
 #pragma unroll
-      for (int i = 0; i < G; ++i) sum[i] = 0.f;
+      for (int h = 0; h < CH; ++h) u[h] = there ? __ldg(src + h * 4) : make_uint4(0, 0, 0, 0);
+      const auto at = [&](int h, int x) {
+        const uint32_t w = x < 2 ? u[h].x : x < 4 ? u[h].y : x < 6 ? u[h].z : u[h].w;
+        return __uint_as_float(x & 1 ? w & 0xffff0000u : w << 16);
+      };
 #pragma unroll
-      for (int h = 0; h < CH; ++h) {
-        const uint4 u = there ? __ldg(src + h * 4) : make_uint4(0, 0, 0, 0);
-        qf[nt][h][0] = __byte_perm(u.x, u.z, 0x5410);
-        qf[nt][h][1] = __byte_perm(u.x, u.z, 0x7632);
-        qf[nt][h][2] = __byte_perm(u.y, u.w, 0x5410);
-        qf[nt][h][3] = __byte_perm(u.y, u.w, 0x7632);
+      for (int h = 0; h < CH; ++h)
 #pragma unroll
-        for (int x = 0; x < 4; ++x) sum[h / 2] += __uint_as_float(qf[nt][h][x] << 16) + __uint_as_float(qf[nt][h][x] & 0xffff0000u);
-      }
+        for (int x = 0; x < 8; ++x) big = fmaxf(big, fabsf(at(h, x)));
+      big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
+      big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
+      // a power of two (1 for a row of zeros, or one with an infinity)
+      const int e = big > 0.f && big < INFINITY ? max((int)(__float_as_uint(big) >> 23), 27) - 127 - 13 : 0;
+      const float up = __uint_as_float((uint32_t)(127 - e) << 23), down = __uint_as_float((uint32_t)(127 + e) << 23);
+      float even[G], odd[G];
+#pragma unroll
+      for (int i = 0; i < G; ++i) even[i] = odd[i] = 0.f;
+#pragma unroll
+      for (int h = 0; h < CH; ++h)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const float f = x & 1 ? up * 0.0625f : up;
+          const __half2 v = __floats2half2_rn(at(h, x) * f, at(h, x + 4) * f);
+          qf[nt][h][x] = half2_bits(v);
+          (x & 1 ? odd : even)[h / 2] += __low2float(v) + __high2float(v);
+        }
 #pragma unroll
       for (int i = 0; i < G; ++i) {
-        sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], 1);
-        sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], 2);
-        qsum[nt][i][0] = __shfl_sync(0xffffffffu, sum[i], 8 * t);
-        qsum[nt][i][1] = __shfl_sync(0xffffffffu, sum[i], 8 * t + 4);
+        even[i] += __shfl_xor_sync(0xffffffffu, even[i], 1);
+        even[i] += __shfl_xor_sync(0xffffffffu, even[i], 2);
+        odd[i] += __shfl_xor_sync(0xffffffffu, odd[i], 1);
+        odd[i] += __shfl_xor_sync(0xffffffffu, odd[i], 2);
+        const float all = fmaf(16.f, odd[i], even[i]), off = -1024.f * (even[i] + odd[i]);
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          qsum[nt][i][x] = __shfl_sync(0xffffffffu, all, 8 * t + 4 * x);
+          start[nt][i][x] = __shfl_sync(0xffffffffu, off, 8 * t + 4 * x);
+        }
       }
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {  // tokens that column 2 t + x sees
-        const int rc = r0 + nt * 8 + 2 * t + x;
-        limit[nt][x] = rc < rows ? c.info.len - c.info.rows + a.by_group(rc) + 1 : 0;
+      for (int x = 0; x < 2; ++x) {
+        back[nt][x] = __shfl_sync(0xffffffffu, down, 8 * t + 4 * x);
+        sc[nt][x] = a.scale * back[nt][x];
+        const int rc = r0 + nt * 8 + 2 * t + x;  // tokens that column 2 t + x sees; a column without a row sees all and is not written
+        limit[nt][x] = rc < rows ? c.info.len - c.info.rows + a.by_group(rc) + 1 : 0x7fffffff;
+        lowest = min(lowest, limit[nt][x]);
       }
     }
+    lowest = min(lowest, __shfl_xor_sync(0xffffffffu, lowest, 1));
+    lowest = min(lowest, __shfl_xor_sync(0xffffffffu, lowest, 2));
     float o[NT][CH][2][4];
-    float mx[NT][2], l[NT][2], om[NT][G][2];
+    // running maximum, the score that moves it, the exponent's shift; sum of weights; second term of O
+    float mx[NT][2], high[NT][2], shift[NT][2], l[NT][2], om[NT][G][2];
+    float unit[G], per_unit[G];  // scales relative to a power of two: o is in `unit`s; before the first scale any makes a new one
+#pragma unroll
+    for (int i = 0; i < G; ++i) {
+      unit[i] = 0x1p-40f;
+      per_unit[i] = 0x1p40f;
+    }
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
@@ -191,8 +221,8 @@ __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_
         for (int x = 0; x < 8; ++x) o[nt][h][x >> 2][x & 3] = 0.f;
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        mx[nt][x] = -INFINITY;
-        l[nt][x] = 0.f;
+        mx[nt][x] = high[nt][x] = -INFINITY;
+        shift[nt][x] = l[nt][x] = 0.f;
 #pragma unroll
         for (int i = 0; i < G; ++i) om[nt][i][x] = 0.f;
       }
@@ -201,10 +231,8 @@ __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_
       if (!dead) dead = !__all_sync(0xffffffffu, mbar_wait(full + 8 * st, phase, &abort_flag, a.status));
       if (dead) continue;
       const uint32_t blk = ring + st * S::kBytes;
-      const int pos = tile * kPageTokens + key0 + g;  // tokens of this lane's scores: pos, pos + 8
-      const bool bad = bad_page[st] != 0;
-      const bool in0 = !bad && pos < c.info.len, in1 = !bad && pos + 8 < c.info.len;
-      if (!bad && tile * kPageTokens + key0 < c.info.len) {
+      const int pos0 = tile * kPageTokens + key0, pos = pos0 + g;  // tokens of this lane's scores: pos, pos + 8
+      if (!bad_page[st] && pos0 < c.info.len) {
         // --- scores
         float s[NT][4];
 #pragma unroll
@@ -217,43 +245,75 @@ __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int x = 0; x < 4; ++x) acc[nt][x] = 0.f;
+            for (int x = 0; x < 4; ++x) acc[nt][x] = start[nt][i][x & 1];
           uint32_t w[4];  // chunk 2i: tokens g, g + 8; chunk 2i + 1: tokens g, g + 8
           ldmatrix_x4(blk + k_lane + i * 2048, w);
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            const uint32_t a00 = nibbles<0>(w[2 * h]), a01 = nibbles<0>(w[2 * h + 1]), a02 = nibbles<1>(w[2 * h]), a03 = nibbles<1>(w[2 * h + 1]);
-            const uint32_t a10 = nibbles<2>(w[2 * h]), a11 = nibbles<2>(w[2 * h + 1]), a12 = nibbles<3>(w[2 * h]), a13 = nibbles<3>(w[2 * h + 1]);
+            const uint32_t u0 = w[2 * h], u1 = w[2 * h + 1], v0 = u0 >> 8, v1 = u1 >> 8;
+            const __half2 a00 = nibble_half2<0x000f000fu>(u0, magic), a01 = nibble_half2<0x000f000fu>(u1, magic), a02 = nibble_half2<0x00f000f0u>(u0, magic),
+                          a03 = nibble_half2<0x00f000f0u>(u1, magic);
+            const __half2 a10 = nibble_half2<0x000f000fu>(v0, magic), a11 = nibble_half2<0x000f000fu>(v1, magic), a12 = nibble_half2<0x00f000f0u>(v0, magic),
+                          a13 = nibble_half2<0x00f000f0u>(v1, magic);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-              mma_bf16(acc[nt], a00, a01, a02, a03, qf[nt][2 * i + h][0], qf[nt][2 * i + h][1]);
-              mma_bf16(acc[nt], a10, a11, a12, a13, qf[nt][2 * i + h][2], qf[nt][2 * i + h][3]);
+              mma_f16(acc[nt], a00, a01, a02, a03, qf[nt][2 * i + h][0], qf[nt][2 * i + h][1]);
+              mma_f16(acc[nt], a10, a11, a12, a13, qf[nt][2 * i + h][2], qf[nt][2 * i + h][3]);
             }
           }
           const uint32_t meta = blk + 64 * D + (i * kPageTokens + key0 + g) * 4;
           const float2 m0 = lds_half2(meta), m1 = lds_half2(meta + 32);
-          const float z0 = fmaf(-128.f, m0.x, m0.y), z1 = fmaf(-128.f, m1.x, m1.y);
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
+          for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
-              s[nt][x] = fmaf(m0.x, acc[nt][x], fmaf(z0, qsum[nt][i][x], s[nt][x]));
-              s[nt][2 + x] = fmaf(m1.x, acc[nt][2 + x], fmaf(z1, qsum[nt][i][x], s[nt][2 + x]));
+              s[nt][x] = fmaf(m0.x, acc[nt][x], fmaf(m0.y, qsum[nt][i][x], s[nt][x]));
+              s[nt][2 + x] = fmaf(m1.x, acc[nt][2 + x], fmaf(m1.y, qsum[nt][i][x], s[nt][2 + x]));
             }
+        }
+        // --- the values' scales and minima: (scale, minimum + 8 scale)
+        float2 m0[G], m1[G];
+        bool grow = false;
+#pragma unroll
+        for (int i = 0; i < G; ++i) {
+          const uint32_t meta = blk + 64 * D + 4 * D + (i * kPageTokens + key0 + g) * 4;
+          m0[i] = lds_half2(meta);
+          m1[i] = lds_half2(meta + 32);
+        }
+        if (pos0 + 16 > lowest || pos0 + 16 > c.info.len) {
+          // hidden tokens (whatever their scores are, NaN too); behind the sequence's end the page holds anything
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+              if (pos >= min(limit[nt][x], c.info.len)) s[nt][x] = -INFINITY;
+              if (pos + 8 >= min(limit[nt][x], c.info.len)) s[nt][2 + x] = -INFINITY;
+            }
+#pragma unroll
+          for (int i = 0; i < G; ++i) {
+            if (pos >= c.info.len) m0[i] = make_float2(0.f, 0.f);
+            if (pos + 8 >= c.info.len) m1[i] = make_float2(0.f, 0.f);
           }
         }
-        // --- mask (whatever a hidden token's score is, NaN too), running maximum
-        bool grow = false;
+#pragma unroll
+        for (int i = 0; i < G; ++i) {
+          // (a token that is not finite has made its scores NaN, and must not reach the columns that do not see it)
+          m0[i].y = fmaf(8.f, m0[i].x, m0[i].y);
+          m1[i].y = fmaf(8.f, m1[i].x, m1[i].y);
+          if (m0[i].y != m0[i].y) m0[i].y = 0.f;
+          if (m1[i].y != m1[i].y) m1[i].y = 0.f;
+          m0[i].x *= per_unit[i];
+          m1[i].x *= per_unit[i];
+          grow |= fmaxf(m0[i].x, m1[i].x) > 16.f;
+        }
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            if (!in0 || pos >= limit[nt][x]) s[nt][x] = -INFINITY;
-            if (!in1 || pos + 8 >= limit[nt][x]) s[nt][2 + x] = -INFINITY;
-            // the maximum moves only when a score is 2^6 above it in the softmax: until then weights stay below 2^6
-            grow |= fmaxf(s[nt][x], s[nt][2 + x]) * a.scale > mx[nt][x] * a.scale + 6.f;
-          }
+          for (int x = 0; x < 2; ++x) grow |= fmaxf(s[nt][x], s[nt][2 + x]) > high[nt][x];
         if (__any_sync(0xffffffffu, grow)) {
+          // The maximum moves only when a score is 2^6 above it in the softmax, the unit of the scales when one is 2^4 above it
+          // (weights stay below 2^6, their products with scales below 2^10): seldom.
+          float f[NT][2];
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -262,58 +322,70 @@ __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_
               m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
               m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
               m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
-              const float f = m == mx[nt][x] ? 1.f : ex2((mx[nt][x] - m) * a.scale);
+              f[nt][x] = m == mx[nt][x] ? 1.f : ex2((mx[nt][x] - m) * sc[nt][x]);
               mx[nt][x] = m;
-              l[nt][x] *= f;
+              shift[nt][x] = m == -INFINITY ? 0.f : -m * sc[nt][x];  // (a column that sees nothing yet: all weights 0)
+              high[nt][x] = m == -INFINITY ? m : m + 6.f / sc[nt][x];
+              l[nt][x] *= f[nt][x];
 #pragma unroll
-              for (int i = 0; i < G; ++i) om[nt][i][x] *= f;
-#pragma unroll
-              for (int h = 0; h < CH; ++h)
-#pragma unroll
-                for (int jj = 0; jj < 2; ++jj) { o[nt][h][jj][x] *= f; o[nt][h][jj][2 + x] *= f; }
+              for (int i = 0; i < G; ++i) om[nt][i][x] *= f[nt][x];
             }
+#pragma unroll
+          for (int i = 0; i < G; ++i) {
+            float top = fmaxf(m0[i].x, m1[i].x);
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
+            float by = 1.f;
+            if (top > 1.f) by = __uint_as_float((254u << 23) - (__float_as_uint(top) & 0x7f800000u));  // the power of two that brings it to 1 .. 2
+            m0[i].x *= by;
+            m1[i].x *= by;
+            per_unit[i] *= by;
+            unit[i] = 1.f / per_unit[i];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int h = 2 * i; h < 2 * i + 2; ++h)
+#pragma unroll
+                  for (int jj = 0; jj < 2; ++jj) {
+                    o[nt][h][jj][x] *= f[nt][x] * by;
+                    o[nt][h][jj][2 + x] *= f[nt][x] * by;
+                  }
+          }
         }
         // --- weights
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
-            const float base = mx[nt][x] == -INFINITY ? 0.f : mx[nt][x] * a.scale;  // a column that sees nothing yet: all weights 0
-            s[nt][x] = ex2(fmaf(s[nt][x], a.scale, -base));
-            s[nt][2 + x] = ex2(fmaf(s[nt][2 + x], a.scale, -base));
+            s[nt][x] = ex2(fmaf(s[nt][x], sc[nt][x], shift[nt][x]));
+            s[nt][2 + x] = ex2(fmaf(s[nt][2 + x], sc[nt][x], shift[nt][x]));
             l[nt][x] += s[nt][x] + s[nt][2 + x];
           }
         // --- values
 #pragma unroll
         for (int i = 0; i < G; ++i) {
-          const uint32_t meta = blk + 64 * D + 4 * D + (i * kPageTokens + key0 + g) * 4;
-          float2 m0 = lds_half2(meta), m1 = lds_half2(meta + 32);
-          // tokens behind the sequence's end hold anything; a token that is not finite has already made its scores NaN
-          if (!in0) m0 = make_float2(0.f, 0.f);
-          if (!in1) m1 = make_float2(0.f, 0.f);
-          float c0 = fmaf(8.f, m0.x, m0.y), c1 = fmaf(8.f, m1.x, m1.y);
-          if (c0 != c0) c0 = 0.f;
-          if (c1 != c1) c1 = 0.f;
           uint32_t p0[NT], p1[NT];
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
-            for (int x = 0; x < 2; ++x) om[nt][i][x] = fmaf(s[nt][x], c0, fmaf(s[nt][2 + x], c1, om[nt][i][x]));
-            p0[nt] = movmatrix_trans(pack_bf16x2(s[nt][0] * m0.x, s[nt][1] * m0.x));
-            p1[nt] = movmatrix_trans(pack_bf16x2(s[nt][2] * m1.x, s[nt][3] * m1.x));
+            for (int x = 0; x < 2; ++x) om[nt][i][x] = fmaf(s[nt][x], m0[i].y, fmaf(s[nt][2 + x], m1[i].y, om[nt][i][x]));
+            p0[nt] = movmatrix_trans(half2_bits(__floats2half2_rn(s[nt][0] * m0[i].x, s[nt][1] * m0[i].x)));
+            p1[nt] = movmatrix_trans(half2_bits(__floats2half2_rn(s[nt][2] * m1[i].x, s[nt][3] * m1[i].x)));
           }
           uint32_t w[4];
           ldmatrix_x4_trans(blk + 32 * D + k_lane + i * 2048, w);
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            const uint32_t a00 = nibbles_centred<0>(w[2 * h]), a01 = nibbles_centred<1>(w[2 * h]), a02 = nibbles_centred<0>(w[2 * h + 1]),
-                           a03 = nibbles_centred<1>(w[2 * h + 1]);
-            const uint32_t a10 = nibbles_centred<2>(w[2 * h]), a11 = nibbles_centred<3>(w[2 * h]), a12 = nibbles_centred<2>(w[2 * h + 1]),
-                           a13 = nibbles_centred<3>(w[2 * h + 1]);
+            const uint32_t u0 = w[2 * h], u1 = w[2 * h + 1], v0 = u0 >> 8, v1 = u1 >> 8;
+            const __half2 a00 = centred_low(u0, magic), a01 = centred_high(u0, magic), a02 = centred_low(u1, magic), a03 = centred_high(u1, magic);
+            const __half2 a10 = centred_low(v0, magic), a11 = centred_high(v0, magic), a12 = centred_low(v1, magic), a13 = centred_high(v1, magic);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-              mma_bf16(o[nt][2 * i + h][0], a00, a01, a02, a03, p0[nt], p1[nt]);
-              mma_bf16(o[nt][2 * i + h][1], a10, a11, a12, a13, p0[nt], p1[nt]);
+              mma_f16(o[nt][2 * i + h][0], a00, a01, a02, a03, p0[nt], p1[nt]);
+              mma_f16(o[nt][2 * i + h][1], a10, a11, a12, a13, p0[nt], p1[nt]);
             }
           }
         }
@@ -341,10 +413,12 @@ __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_
         }
         const int col = nt * 8 + 2 * t + x;
 #pragma unroll
-        for (int h = 0; h < CH; ++h)
+        for (int h = 0; h < CH; ++h) {
+          const auto value = [&](float v) { return fmaf(v, unit[h / 2], add[h / 2]); };
           *reinterpret_cast<float4*>(mine + col * D + 32 * h + 4 * g) =
-              make_float4(o[nt][h][0][x] + add[h / 2], o[nt][h][0][2 + x] + add[h / 2], o[nt][h][1][x] + add[h / 2], o[nt][h][1][2 + x] + add[h / 2]);
-        if (g == 0) { mine[R * D + col] = mx[nt][x]; mine[R * D + R + col] = sum; }
+              make_float4(value(o[nt][h][0][x]), value(o[nt][h][0][2 + x]), value(o[nt][h][1][x]), value(o[nt][h][1][2 + x]));
+        }
+        if (g == 0) { mine[R * D + col] = mx[nt][x] * back[nt][x]; mine[R * D + R + col] = sum; }
       }
     epi_bar_sync();
     const bool whole = first == 0 && stop == c.tiles;

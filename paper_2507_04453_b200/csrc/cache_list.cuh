@@ -50,6 +50,22 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 
+__device__ __forceinline__ uint32_t half2_bits(__half2 v) { return *reinterpret_cast<uint32_t*>(&v); }
+__device__ __forceinline__ __half2 as_half2(uint32_t v) { return *reinterpret_cast<__half2*>(&v); }
+// Two codes as fp16 numbers: (w & MASK) | magic, magic = 0x64006400, is 1024 + code for the nibbles 0 and 4 of w (MASK 0x000f000f) and
+// 1024 + 16 code for the nibbles 1 and 5 (MASK 0x00f000f0).  One instruction; left to the compiler it becomes two.
+template <uint32_t MASK>
+__device__ __forceinline__ __half2 nibble_half2(uint32_t w, uint32_t magic) {
+  uint32_t r;
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(w), "n"(MASK), "r"(magic));
+  return as_half2(r);
+}
+// code - 8 of the nibbles 0 and 4, and of the nibbles 1 and 5: exact.
+__device__ __forceinline__ __half2 centred_low(uint32_t w, uint32_t magic) { return __hsub2(nibble_half2<0x000f000fu>(w, magic), as_half2(0x64086408u) /* 1032 */); }
+__device__ __forceinline__ __half2 centred_high(uint32_t w, uint32_t magic) {
+  return __hfma2(nibble_half2<0x00f000f0u>(w, magic), as_half2(0x2c002c00u) /* 1 / 16 */, as_half2(0xd480d480u) /* -72 */);
+}
+
 struct Cursor {  // a place in the list
   int entry, kvh, rb, at, blocks, tiles;  // at: element of the row block
   EntryInfo info;

@@ -67,8 +67,6 @@ __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
   const __half2 v = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&v);
 }
-__device__ __forceinline__ uint32_t bits(__half2 v) { return *reinterpret_cast<uint32_t*>(&v); }
-__device__ __forceinline__ __half2 as_half2(uint32_t v) { return *reinterpret_cast<__half2*>(&v); }
 __device__ __forceinline__ __nv_bfloat162 as_bf162(uint32_t v) { return *reinterpret_cast<__nv_bfloat162*>(&v); }
 
 // Operands in shared memory are 128-byte rows under the 128-byte swizzle.  Q and K: a row is 64 channels of a row / key (K contiguous).
@@ -125,24 +123,11 @@ __device__ __forceinline__ uint64_t desc_of(uint32_t lo) {
   return (uint64_t)hi << 32 | lo;
 }
 
-// (w & mask) | magic in one instruction (left to the compiler it becomes two).
-template <uint32_t MASK>
-__device__ __forceinline__ __half2 masked(uint32_t w, uint32_t magic) {
-  uint32_t r;
-  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(w), "n"(MASK), "r"(magic));
-  return as_half2(r);
-}
 // Eight codes -> fp16 (code - 8) * s + c in the order (0, 4, 1, 5, 2, 6, 3, 7).
 __device__ __forceinline__ uint4 widen(uint32_t w, __half2 s, __half2 c, uint32_t magic /* 0x64006400 */) {
-  const __half2 o = as_half2(0x64086408u), sixteenth = as_half2(0x2c002c00u), o16 = as_half2(0xd480d480u);  // 1032; 1 / 16; -72
-  uint32_t y[4];
-#pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    const uint32_t x = w >> (8 * j);
-    y[2 * j] = bits(__hfma2(__hsub2(masked<0x000f000fu>(x, magic), o), s, c));                    // 1024 + code
-    y[2 * j + 1] = bits(__hfma2(__hfma2(masked<0x00f000f0u>(x, magic), sixteenth, o16), s, c));  // 1024 + 16 code
-  }
-  return make_uint4(y[0], y[1], y[2], y[3]);
+  const uint32_t x = w >> 8;
+  return make_uint4(half2_bits(__hfma2(centred_low(w, magic), s, c)), half2_bits(__hfma2(centred_high(w, magic), s, c)),
+                    half2_bits(__hfma2(centred_low(x, magic), s, c)), half2_bits(__hfma2(centred_high(x, magic), s, c)));
 }
 // Scale and centre of a token's group, (scale, minimum) = m.  Values beyond +-65440 are brought there: what fp16 rounds them to
 // has to stay finite.

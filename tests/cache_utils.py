@@ -83,15 +83,16 @@ def attend_bound(q, v, codes, scale, out, p, softmax_scale, k):
     """How far a row of essa_cache_attend may be from the fp64 result, element by element; one entry, all heads.  It holds for both kernels.
 
     * out is rounded to bf16 once: 2^-8 |out|;
-    * few rows: a weight times the value's scale is rounded to bf16 before it meets (code - 8): 2^-8 sum_k p_k s_k |c_k - 8|;
+    * few rows: a weight times the value's scale is rounded to fp16 before it meets (code - 8): 2^-11 sum_k p_k s_k |c_k - 8|, and where the
+      product is 2^-14 below the unit (at most twice the largest scale of a group; the weights' sum is at least 1) 2^-24 max(s) absolutely;
       many rows: V and P are fp16, V's offset (minimum + 8 scale) too: 2^-11 sum_k p_k (2 |v_k| + |offset_k|), weights below
-      2^-14 of the largest to 2^-25 absolutely: 2^-25 sum_k |v_k| (the sum of the weights is at least 1);
-    * a score is wrong by at most `err` and moves the weights by a factor e^(+-2 err) at most: (e^(2 err) - 1) sum_k p_k |v_k|.  The tensor
-      core adds 64 products of q (128 + code) <= 143 |q| in fp32 (taken as 16 roundings of 2^-23), the scales and the second term
-      (minimum - 128 scale) sum(q) come on top with 2^-22 of terms of the same size: scale * 2^-18 * 143 * sum_g max_k(s_g) sum|q_g|, and
-      2^-21 max|score| for the final product and exponent.  Many rows: K is (code - 8) scale + offset with the offset and the result
-      rounded to fp16: 2^-11 |offset| |sum q| per group, as it is the same for the whole group, and eight standard deviations of a
-      sum of independent errors of at most 2^-11 |q_i k_i| each;
+      2^-14 of the largest to 2^-25 absolutely: 2^-25 sum_k |v_k|;
+    * a score is wrong by at most `err` and moves the weights by a factor e^(+-2 err) at most: (e^(2 err) - 1) sum_k p_k |v_k|.  Few rows: the
+      tensor core adds 64 products of q (1024 + code), or q / 16 (1024 + 16 code), at most 1039 |q| each, in fp32 (taken as 16 roundings of
+      2^-23); the scales and the second term minimum sum(q) come on top with 2^-22 of terms of the same size: scale * 2^-18 * 1039 *
+      sum_g max_k(s_g) sum|q_g|, and 2^-21 max|score| for the final product and exponent.  Many rows: K is (code - 8) scale + offset
+      with the offset and the result rounded to fp16: 2^-11 |offset| |sum q| per group, as it is the same for the whole group, and
+      eight standard deviations of a sum of independent errors of at most 2^-11 |q_i k_i| each;
     * fp32 sums of weights: 2^-16 sum_k p_k |v_k|."""
     rows, heads, d = q.shape
     group = heads // v.shape[0]
@@ -103,12 +104,12 @@ def attend_bound(q, v, codes, scale, out, p, softmax_scale, k):
         centred = (codes[c].astype(np.float64) - 8) * np.repeat(s, co.GROUP, -1)
         offset = np.stack([k[c], v[c]]) - centred
         qh, vh = q[:, h], np.abs(v[c])
-        err = softmax_scale * 2.0 ** -18 * 143 * (np.abs(qh).reshape(rows, -1, co.GROUP).sum(-1) * s[0].max(0, initial=0.0)).sum(-1)
+        err = softmax_scale * 2.0 ** -18 * 1039 * (np.abs(qh).reshape(rows, -1, co.GROUP).sum(-1) * s[0].max(0, initial=0.0)).sum(-1)
         err = err + 2.0 ** -21 * softmax_scale * np.max(np.abs(qh @ k[c].T), axis=1, initial=0.0)
         shared = sum(np.abs(qh[:, g:g + co.GROUP] @ offset[0][:, g:g + co.GROUP].T) for g in range(0, d, co.GROUP))
         alone = 8 / np.sqrt(3) * np.sqrt((qh ** 2) @ (k[c] ** 2).T)
         err = err + softmax_scale * 2.0 ** -11 * np.max(shared + alone, axis=1, initial=0.0)
         ph = p[:, h]
-        tol[:, h] = (2.0 ** -8 * np.abs(out[:, h]) + 2.0 ** -8 * (ph @ np.abs(centred[1])) + 2.0 ** -11 * (ph @ (2 * vh + np.abs(offset[1])))
-                     + 2.0 ** -25 * (ph > 0).astype(float) @ vh + (np.expm1(2 * err)[:, None] + 2.0 ** -16) * (ph @ vh) + 1e-30)
+        tol[:, h] = (2.0 ** -8 * np.abs(out[:, h]) + 2.0 ** -11 * (ph @ np.abs(centred[1])) + 2.0 ** -11 * (ph @ (2 * vh + np.abs(offset[1])))
+                     + 2.0 ** -24 * 8 * ((ph > 0).sum(-1) * s[1].max(initial=0.0))[:, None] + 2.0 ** -25 * (ph > 0).astype(float) @ vh + (np.expm1(2 * err)[:, None] + 2.0 ** -16) * (ph @ vh) + 1e-30)
     return tol
