@@ -379,8 +379,8 @@ int32_t essa_apply_projection_simt(essa_ctx* ctx, const essa_adapter* adapter, c
  * Storage.  Keys and values of one token and kv head are cut into groups of ESSA_CACHE_GROUP channels.  With min and max
  * over a group: minimum = fp16(min), scale = fp16((max - minimum) / 15), code = rint((x - minimum) / scale) in 0 .. 15
  * (0 where scale is 0), in fp32; a stored value stands for code * scale + minimum.  A token of a kv head whose keys or
- * values hold a NaN or an infinity, or whose minimum or scale does not fit fp16, is stored as NaN: every query row that sees it
- * becomes NaN (rows that do not see it are not touched).
+ * values hold a NaN or an infinity, or whose minimum or scale does not fit fp16, is stored as keys of NaN (scale 0, minimum NaN in every
+ * group) and values of 0, and read back as NaN: every query row that sees it becomes NaN (rows that do not see it are not touched).
  * A page holds ESSA_CACHE_PAGE_TOKENS tokens of one layer: for each kv head one run of 72 * head_dim bytes,
  *   codes of K, then of V:            [head_dim / 32][64 tokens][16 bytes], two codes per byte, low nibble = even channel;
  *   (scale, minimum) of K, then of V: [head_dim / 64][64 tokens][2] fp16.

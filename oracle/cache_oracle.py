@@ -27,15 +27,15 @@ def quantize(x):
 
 
 def quantize_tokens(k, v):
-    """Both halves of tokens [T, kv_heads, d]; a token whose keys or values do not fit is NaN in both."""
+    """Both halves of tokens [T, kv_heads, d]; a token whose keys or values do not fit has keys of NaN and values of 0."""
     out = []
     bad = np.zeros(k.shape[:-1], bool)
     for x in (k, v):
         codes, scale, low = quantize(x)
         bad |= ~(np.isfinite(x).all(-1) & np.isfinite(scale).all(-1) & np.isfinite(low).all(-1))
         out.append([codes, scale, low])
-    for codes, scale, low in out:
-        codes[bad], scale[bad], low[bad] = 0, 0, np.nan
+    for (codes, scale, low), stored in zip(out, (np.nan, 0)):
+        codes[bad], scale[bad], low[bad] = 0, 0, stored
     return out
 
 

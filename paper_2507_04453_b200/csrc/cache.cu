@@ -114,8 +114,8 @@ __global__ void __launch_bounds__(256) append_kernel(CacheView v, CacheEntries e
   if (page < 0) return;
   if (misfits) {
     pk.codes = pv.codes = 0;
-    pk.scale = pv.scale = __ushort_as_half(0);
-    pk.low = pv.low = __ushort_as_half(0x7e00);
+    pk.scale = pv.scale = pv.low = __ushort_as_half(0);  // (V 0: it meets weights 0 in the rows that do not see the token)
+    pk.low = __ushort_as_half(0x7e00);
   }
   uint8_t* run = v.pages + page * v.page_bytes + (int64_t)h * 72 * D;
   uint8_t* code = run + (lane >> 2) * 1024 + offset * 16 + (lane & 3) * 4;
@@ -142,6 +142,8 @@ __global__ void __launch_bounds__(256) read_kernel(CacheView v, CacheEntries e, 
   if (page == -2) cache_fault(status);
   const uint8_t* run = v.pages + (int64_t)max(page, 0) * v.page_bytes + (int64_t)h * 72 * D;
   const int64_t at = ((int64_t)t * v.kv_heads + h) * D + lane * 8;
+  // (a token that did not fit has NaN keys only)
+  const bool nan = page >= 0 && __hisnan(*reinterpret_cast<const __half*>(run + 64 * D + offset * 4 + 2));
 #pragma unroll
   for (int which = 0; which < 2; ++which) {
     __nv_bfloat16* out = which ? v_out : k_out;
@@ -151,6 +153,7 @@ __global__ void __launch_bounds__(256) read_kernel(CacheView v, CacheEntries e, 
     if (page >= 0) {
       w = *reinterpret_cast<const uint32_t*>(run + which * 32 * D + (lane >> 2) * 1024 + offset * 16 + (lane & 3) * 4);
       m = __half22float2(*reinterpret_cast<const __half2*>(run + 64 * D + which * 4 * D + ((lane >> 3) * kPageTokens + offset) * 4));
+      if (nan) m.y = __int_as_float(0x7fffffff);
     }
     uint32_t y[4];
 #pragma unroll

@@ -22,7 +22,8 @@
 namespace essa {
 namespace {
 
-constexpr int kWarps = 4;                     // consuming warps: 16 tokens of a page each
+constexpr int kWarps = 4;                     // consuming warps: two share a page (32 tokens each), pages go to the pairs in turn
+constexpr int KS = 2;                         // slices of 16 tokens per warp: independent chains of products that hide one another's latency
 constexpr int kThreads = kWarps * 32 + 32;    // + one copying warp
 
 // Row blocks of R rows; every row block of an entry walks all its pages (the few rows of an entry see nearly the same ones).
@@ -50,6 +51,27 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], __half2 a0, __half2 a1, _
       : "r"(half2_bits(a0)), "r"(half2_bits(a1)), "r"(half2_bits(a2)), "r"(half2_bits(a3)), "r"(b0), "r"(b1));
 }
 
+// mbar_wait for the warp that fills a deep ring: it sleeps between probes and leaves the issue slots to the warps that compute.
+__device__ __forceinline__ bool wait_napping(uint32_t bar, uint32_t parity, volatile int* abort_flag, int32_t* status) {
+  const long long t0 = clock64();
+  while (!mbar_test_wait(bar, parity)) {
+    __nanosleep(64);
+    if (*abort_flag) return false;
+    if (clock64() - t0 > kWaitLimitCycles) {
+      *abort_flag = 1;
+      atomicCAS(status, 0, ESSA_ERR_DEVICE_TIMEOUT);
+      return false;
+    }
+  }
+  return true;
+}
+// mma_f16 with the accumulator's start in registers of its own (they stay).
+__device__ __forceinline__ void mma_f16_from(float (&d)[4], const float (&c)[4], __half2 a0, __half2 a1, __half2 a2, __half2 a3, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %12, %13};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(half2_bits(a0)), "r"(half2_bits(a1)), "r"(half2_bits(a2)), "r"(half2_bits(a3)), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]), "f"(c[2]), "f"(c[3]));
+}
+
 template <int D, int NT>
 struct Shape {
   static constexpr int R = 8 * NT;             // query rows of a row block
@@ -57,6 +79,7 @@ struct Shape {
   static constexpr int kStages = (D == 128 ? 6 : 10);
   static constexpr int kPart = Partial<DecodeList<R>, D>::kFloats;
   static constexpr int kJoin = kWarps * R * (D + 2) * 4;
+  static_assert(kStages % 2 == 0, "");
   static constexpr int kSmem = kStages * kBytes + kJoin + 256;
 };
 
@@ -80,7 +103,7 @@ __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_
   grid_dep_launch();
   if (tid == 0) {
     abort_flag = 0;
-    for (int s = 0; s < S::kStages; ++s) { mbar_init(full + 8 * s, 1); mbar_init(empty + 8 * s, kWarps); }
+    for (int s = 0; s < S::kStages; ++s) { mbar_init(full + 8 * s, 1); mbar_init(empty + 8 * s, 2); }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   __syncthreads();
@@ -104,7 +127,7 @@ __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_
       const int32_t* row = a.v.table + (int64_t)max(c.info.slot, 0) * a.v.max_pages;
       const bool none = c.info.len == 0;
       for (; tile < stop; ++tile) {
-        if (filled >= S::kStages && !mbar_wait(empty + 8 * st, phase ^ 1, &abort_flag, a.status)) { ok = false; break; }
+        if (filled >= S::kStages && !wait_napping(empty + 8 * st, phase ^ 1, &abort_flag, a.status)) { ok = false; break; }
         const int page = none ? -1 : __ldg(row + tile);
         const bool there = page >= 0 && page < a.v.num_pages;
         if (!there && (!none || c.info.slot < 0)) cache_fault(a.status);
@@ -126,10 +149,11 @@ __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_
 
   // ----------------------------------------------------------------------------------------- consuming warps
   const int g = lane >> 2, t = lane & 3;
-  const int key0 = warp * 16;                                                 // this warp's tokens of a page
+  const int key0 = (warp & 1) * 32;                                           // this warp's tokens of a page
   const uint32_t k_lane = (uint32_t)(key0 + (lane & 15)) * 16 + (uint32_t)(lane >> 4) * 1024;  // ldmatrix row addresses: (tokens 0-7, 8-15) x two chunks
-  int st = 0;
+  int st = warp >> 1;  // (an even number of stages: a pair's pages stay in its stages)
   uint32_t phase = 0;
+  int mine_at = warp >> 1;  // the pair's first tile of a row block, counted from the run's first tile of it
   uint32_t magic = 0x64006400u;
   asm volatile("" : "+r"(magic));  // (in a register, where the and-or can take it)
   bool dead = false;  // a wait ran out: the warp goes through the barriers with the others and does nothing else
@@ -142,7 +166,7 @@ __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_
     // --- query operand: lane (g, t) holds channels 32 h + 8 t .. + 7 of column g, in the order that the nibbles come in:
     // (0, 4), (1, 5) / 16, (2, 6), (3, 7) / 16
     uint32_t qf[NT][CH][4];
-    float qsum[NT][G][2], start[NT][G][2];  // per group: the sum of q; minus what the 1024 in the codes' numbers adds
+    float qsum[NT][G][2], start[NT][G][4];  // per group: the sum of q; minus what the 1024 in the codes' numbers adds
     float sc[NT][2], back[NT][2];           // softmax scale in the units of the row; what the row was divided by
     int limit[NT][2], lowest = 0x7fffffff;
 #pragma unroll
@@ -190,7 +214,7 @@ __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
           qsum[nt][i][x] = __shfl_sync(0xffffffffu, all, 8 * t + 4 * x);
-          start[nt][i][x] = __shfl_sync(0xffffffffu, off, 8 * t + 4 * x);
+          start[nt][i][x] = start[nt][i][2 + x] = __shfl_sync(0xffffffffu, off, 8 * t + 4 * x);
         }
       }
 #pragma unroll
@@ -207,12 +231,9 @@ __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_
     float o[NT][CH][2][4];
     // running maximum, the score that moves it, the exponent's shift; sum of weights; second term of O
     float mx[NT][2], high[NT][2], shift[NT][2], l[NT][2], om[NT][G][2];
-    float unit[G], per_unit[G];  // scales relative to a power of two: o is in `unit`s; before the first scale any makes a new one
+    float per_unit[G];  // scales are relative to a power of two, the unit of o: this is its inverse; before the first scale any makes a new one
 #pragma unroll
-    for (int i = 0; i < G; ++i) {
-      unit[i] = 0x1p-40f;
-      per_unit[i] = 0x1p40f;
-    }
+    for (int i = 0; i < G; ++i) per_unit[i] = 0x1p40f;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
@@ -227,89 +248,104 @@ __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_
         for (int i = 0; i < G; ++i) om[nt][i][x] = 0.f;
       }
     }
-    for (int tile = first; tile < stop; ++tile) {
+    for (int tile = first + mine_at; tile < stop; tile += 2) {
       if (!dead) dead = !__all_sync(0xffffffffu, mbar_wait(full + 8 * st, phase, &abort_flag, a.status));
       if (dead) continue;
       const uint32_t blk = ring + st * S::kBytes;
-      const int pos0 = tile * kPageTokens + key0, pos = pos0 + g;  // tokens of this lane's scores: pos, pos + 8
+      const __half2* meta = reinterpret_cast<const __half2*>(smem + st * S::kBytes + 64 * D) + key0 + g;  // (scale, minimum) of K, then of V
+      const int pos0 = tile * kPageTokens + key0, pos = pos0 + g;  // tokens of this lane's scores: pos + 8 n, n < 2 KS
       if (!bad_page[st] && pos0 < c.info.len) {
-        // --- scores
-        float s[NT][4];
+        // --- scores; of slice k: token pos + 16 k in [0..1], + 8 in [2..3]
+        float s[KS][NT][4];
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+        for (int k = 0; k < KS; ++k)
 #pragma unroll
-          for (int x = 0; x < 4; ++x) s[nt][x] = 0.f;
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) s[k][nt][x] = 0.f;
 #pragma unroll
         for (int i = 0; i < G; ++i) {
-          float acc[NT][4];
+          float acc[KS][NT][4];
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
+          for (int k = 0; k < KS; ++k) {
+            uint32_t w[4];  // chunk 2i: tokens g, g + 8; chunk 2i + 1: tokens g, g + 8
+            ldmatrix_x4(blk + k_lane + i * 2048 + k * 256, w);
 #pragma unroll
-            for (int x = 0; x < 4; ++x) acc[nt][x] = start[nt][i][x & 1];
-          uint32_t w[4];  // chunk 2i: tokens g, g + 8; chunk 2i + 1: tokens g, g + 8
-          ldmatrix_x4(blk + k_lane + i * 2048, w);
+            for (int h = 0; h < 2; ++h) {
+              const uint32_t u0 = w[2 * h], u1 = w[2 * h + 1], v0 = u0 >> 8, v1 = u1 >> 8;
+              const __half2 a00 = nibble_half2<0x000f000fu>(u0, magic), a01 = nibble_half2<0x000f000fu>(u1, magic), a02 = nibble_half2<0x00f000f0u>(u0, magic),
+                            a03 = nibble_half2<0x00f000f0u>(u1, magic);
+              const __half2 a10 = nibble_half2<0x000f000fu>(v0, magic), a11 = nibble_half2<0x000f000fu>(v1, magic), a12 = nibble_half2<0x00f000f0u>(v0, magic),
+                            a13 = nibble_half2<0x00f000f0u>(v1, magic);
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const uint32_t u0 = w[2 * h], u1 = w[2 * h + 1], v0 = u0 >> 8, v1 = u1 >> 8;
-            const __half2 a00 = nibble_half2<0x000f000fu>(u0, magic), a01 = nibble_half2<0x000f000fu>(u1, magic), a02 = nibble_half2<0x00f000f0u>(u0, magic),
-                          a03 = nibble_half2<0x00f000f0u>(u1, magic);
-            const __half2 a10 = nibble_half2<0x000f000fu>(v0, magic), a11 = nibble_half2<0x000f000fu>(v1, magic), a12 = nibble_half2<0x00f000f0u>(v0, magic),
-                          a13 = nibble_half2<0x00f000f0u>(v1, magic);
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-              mma_f16(acc[nt], a00, a01, a02, a03, qf[nt][2 * i + h][0], qf[nt][2 * i + h][1]);
-              mma_f16(acc[nt], a10, a11, a12, a13, qf[nt][2 * i + h][2], qf[nt][2 * i + h][3]);
+              for (int nt = 0; nt < NT; ++nt) {
+                if (h == 0) mma_f16_from(acc[k][nt], start[nt][i], a00, a01, a02, a03, qf[nt][2 * i][0], qf[nt][2 * i][1]);
+                else mma_f16(acc[k][nt], a00, a01, a02, a03, qf[nt][2 * i + 1][0], qf[nt][2 * i + 1][1]);
+                mma_f16(acc[k][nt], a10, a11, a12, a13, qf[nt][2 * i + h][2], qf[nt][2 * i + h][3]);
+              }
             }
           }
-          const uint32_t meta = blk + 64 * D + (i * kPageTokens + key0 + g) * 4;
-          const float2 m0 = lds_half2(meta), m1 = lds_half2(meta + 32);
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
+          for (int k = 0; k < KS; ++k) {
+            const float2 m0 = __half22float2(meta[i * kPageTokens + 16 * k]), m1 = __half22float2(meta[i * kPageTokens + 16 * k + 8]);
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {
-              s[nt][x] = fmaf(m0.x, acc[nt][x], fmaf(m0.y, qsum[nt][i][x], s[nt][x]));
-              s[nt][2 + x] = fmaf(m1.x, acc[nt][2 + x], fmaf(m1.y, qsum[nt][i][x], s[nt][2 + x]));
-            }
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int x = 0; x < 2; ++x) {
+                s[k][nt][x] = fmaf(m0.x, acc[k][nt][x], fmaf(m0.y, qsum[nt][i][x], s[k][nt][x]));
+                s[k][nt][2 + x] = fmaf(m1.x, acc[k][nt][2 + x], fmaf(m1.y, qsum[nt][i][x], s[k][nt][2 + x]));
+              }
+          }
         }
         // --- the values' scales and minima: (scale, minimum + 8 scale)
-        float2 m0[G], m1[G];
+        float2 mv[KS][2][G];
         bool grow = false;
 #pragma unroll
-        for (int i = 0; i < G; ++i) {
-          const uint32_t meta = blk + 64 * D + 4 * D + (i * kPageTokens + key0 + g) * 4;
-          m0[i] = lds_half2(meta);
-          m1[i] = lds_half2(meta + 32);
-        }
-        if (pos0 + 16 > lowest || pos0 + 16 > c.info.len) {
+        for (int k = 0; k < KS; ++k)
+#pragma unroll
+          for (int y = 0; y < 2; ++y)
+#pragma unroll
+            for (int i = 0; i < G; ++i) mv[k][y][i] = __half22float2(meta[(G + i) * kPageTokens + 16 * k + 8 * y]);
+        if (pos0 + 16 * KS > lowest || pos0 + 16 * KS > c.info.len) {
           // hidden tokens (whatever their scores are, NaN too); behind the sequence's end the page holds anything
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
+          for (int k = 0; k < KS; ++k)
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {
-              if (pos >= min(limit[nt][x], c.info.len)) s[nt][x] = -INFINITY;
-              if (pos + 8 >= min(limit[nt][x], c.info.len)) s[nt][2 + x] = -INFINITY;
+            for (int y = 0; y < 2; ++y) {
+              const int at = pos + 16 * k + 8 * y;
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+                  if (at >= min(limit[nt][x], c.info.len)) s[k][nt][2 * y + x] = -INFINITY;
+#pragma unroll
+              for (int i = 0; i < G; ++i)
+                if (at >= c.info.len) mv[k][y][i] = make_float2(0.f, 0.f);
             }
-#pragma unroll
-          for (int i = 0; i < G; ++i) {
-            if (pos >= c.info.len) m0[i] = make_float2(0.f, 0.f);
-            if (pos + 8 >= c.info.len) m1[i] = make_float2(0.f, 0.f);
-          }
         }
 #pragma unroll
         for (int i = 0; i < G; ++i) {
-          // (a token that is not finite has made its scores NaN, and must not reach the columns that do not see it)
-          m0[i].y = fmaf(8.f, m0[i].x, m0[i].y);
-          m1[i].y = fmaf(8.f, m1[i].x, m1[i].y);
-          if (m0[i].y != m0[i].y) m0[i].y = 0.f;
-          if (m1[i].y != m1[i].y) m1[i].y = 0.f;
-          m0[i].x *= per_unit[i];
-          m1[i].x *= per_unit[i];
-          grow |= fmaxf(m0[i].x, m1[i].x) > 16.f;
+          float top = 0.f;
+#pragma unroll
+          for (int k = 0; k < KS; ++k)
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+              float2& m = mv[k][y][i];
+              m.y = fmaf(8.f, m.x, m.y);
+              m.x *= per_unit[i];
+              top = fmaxf(top, m.x);
+            }
+          grow |= top > 16.f;
         }
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int x = 0; x < 2; ++x) grow |= fmaxf(s[nt][x], s[nt][2 + x]) > high[nt][x];
+          for (int x = 0; x < 2; ++x) {
+            float top = -INFINITY;
+#pragma unroll
+            for (int k = 0; k < KS; ++k) top = fmaxf(top, fmaxf(s[k][nt][x], s[k][nt][2 + x]));
+            grow |= top > high[nt][x];
+          }
         if (__any_sync(0xffffffffu, grow)) {
           // The maximum moves only when a score is 2^6 above it in the softmax, the unit of the scales when one is 2^4 above it
           // (weights stay below 2^6, their products with scales below 2^10): seldom.
@@ -318,7 +354,9 @@ __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
-              float m = fmaxf(mx[nt][x], fmaxf(s[nt][x], s[nt][2 + x]));
+              float m = mx[nt][x];
+#pragma unroll
+              for (int k = 0; k < KS; ++k) m = fmaxf(m, fmaxf(s[k][nt][x], s[k][nt][2 + x]));
               m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
               m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
               m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
@@ -332,16 +370,20 @@ __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_
             }
 #pragma unroll
           for (int i = 0; i < G; ++i) {
-            float top = fmaxf(m0[i].x, m1[i].x);
+            float top = 0.f;
+#pragma unroll
+            for (int k = 0; k < KS; ++k) top = fmaxf(top, fmaxf(mv[k][0][i].x, mv[k][1][i].x));
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
             float by = 1.f;
             if (top > 1.f) by = __uint_as_float((254u << 23) - (__float_as_uint(top) & 0x7f800000u));  // the power of two that brings it to 1 .. 2
-            m0[i].x *= by;
-            m1[i].x *= by;
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+              mv[k][0][i].x *= by;
+              mv[k][1][i].x *= by;
+            }
             per_unit[i] *= by;
-            unit[i] = 1.f / per_unit[i];
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -357,43 +399,50 @@ __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_
         }
         // --- weights
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+        for (int k = 0; k < KS; ++k)
 #pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            s[nt][x] = ex2(fmaf(s[nt][x], sc[nt][x], shift[nt][x]));
-            s[nt][2 + x] = ex2(fmaf(s[nt][2 + x], sc[nt][x], shift[nt][x]));
-            l[nt][x] += s[nt][x] + s[nt][2 + x];
-          }
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+              s[k][nt][x] = ex2(fmaf(s[k][nt][x], sc[nt][x], shift[nt][x]));
+              s[k][nt][2 + x] = ex2(fmaf(s[k][nt][2 + x], sc[nt][x], shift[nt][x]));
+              l[nt][x] += s[k][nt][x] + s[k][nt][2 + x];
+            }
         // --- values
 #pragma unroll
-        for (int i = 0; i < G; ++i) {
-          uint32_t p0[NT], p1[NT];
+        for (int i = 0; i < G; ++i)
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-            for (int x = 0; x < 2; ++x) om[nt][i][x] = fmaf(s[nt][x], m0[i].y, fmaf(s[nt][2 + x], m1[i].y, om[nt][i][x]));
-            p0[nt] = movmatrix_trans(half2_bits(__floats2half2_rn(s[nt][0] * m0[i].x, s[nt][1] * m0[i].x)));
-            p1[nt] = movmatrix_trans(half2_bits(__floats2half2_rn(s[nt][2] * m1[i].x, s[nt][3] * m1[i].x)));
-          }
-          uint32_t w[4];
-          ldmatrix_x4_trans(blk + 32 * D + k_lane + i * 2048, w);
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const uint32_t u0 = w[2 * h], u1 = w[2 * h + 1], v0 = u0 >> 8, v1 = u1 >> 8;
-            const __half2 a00 = centred_low(u0, magic), a01 = centred_high(u0, magic), a02 = centred_low(u1, magic), a03 = centred_high(u1, magic);
-            const __half2 a10 = centred_low(v0, magic), a11 = centred_high(v0, magic), a12 = centred_low(v1, magic), a13 = centred_high(v1, magic);
+          for (int k = 0; k < KS; ++k) {
+            const float2 m0 = mv[k][0][i], m1 = mv[k][1][i];
+            uint32_t p0[NT], p1[NT];
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-              mma_f16(o[nt][2 * i + h][0], a00, a01, a02, a03, p0[nt], p1[nt]);
-              mma_f16(o[nt][2 * i + h][1], a10, a11, a12, a13, p0[nt], p1[nt]);
+#pragma unroll
+              for (int x = 0; x < 2; ++x) om[nt][i][x] = fmaf(s[k][nt][x], m0.y, fmaf(s[k][nt][2 + x], m1.y, om[nt][i][x]));
+              p0[nt] = movmatrix_trans(half2_bits(__floats2half2_rn(s[k][nt][0] * m0.x, s[k][nt][1] * m0.x)));
+              p1[nt] = movmatrix_trans(half2_bits(__floats2half2_rn(s[k][nt][2] * m1.x, s[k][nt][3] * m1.x)));
+            }
+            uint32_t w[4];
+            ldmatrix_x4_trans(blk + 32 * D + k_lane + i * 2048 + k * 256, w);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const uint32_t u0 = w[2 * h], u1 = w[2 * h + 1], v0 = u0 >> 8, v1 = u1 >> 8;
+              const __half2 a00 = centred_low(u0, magic), a01 = centred_high(u0, magic), a02 = centred_low(u1, magic), a03 = centred_high(u1, magic);
+              const __half2 a10 = centred_low(v0, magic), a11 = centred_high(v0, magic), a12 = centred_low(v1, magic), a13 = centred_high(v1, magic);
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) {
+                mma_f16(o[nt][2 * i + h][0], a00, a01, a02, a03, p0[nt], p1[nt]);
+                mma_f16(o[nt][2 * i + h][1], a10, a11, a12, a13, p0[nt], p1[nt]);
+              }
             }
           }
-        }
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(empty + 8 * st);
-      if (++st == S::kStages) { st = 0; phase ^= 1; }
+      st += 2;
+      if (st >= S::kStages) { st -= S::kStages; phase ^= 1; }
     }
+    mine_at = (mine_at + stop - first) & 1;  // (the pairs take turns over the whole run)
 
     // --- join the four warps: each leaves O, maximum and sum of its tokens in shared memory
     float* mine = join + warp * S::kPart;
@@ -414,7 +463,7 @@ __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_
         const int col = nt * 8 + 2 * t + x;
 #pragma unroll
         for (int h = 0; h < CH; ++h) {
-          const auto value = [&](float v) { return fmaf(v, unit[h / 2], add[h / 2]); };
+          const auto value = [&](float v) { return fmaf(v, 1.f / per_unit[h / 2], add[h / 2]); };
           *reinterpret_cast<float4*>(mine + col * D + 32 * h + 4 * g) =
               make_float4(value(o[nt][h][0][x]), value(o[nt][h][0][2 + x]), value(o[nt][h][1][x]), value(o[nt][h][1][2 + x]));
         }

@@ -563,8 +563,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
             const uint32_t w = in ? (&ck[i / 4].x)[i % 4] : 0x88888888u;
             sts_v4(k_dst + (((word0 + i) ^ sw) << 4), widen(w, ms, mc, magic));
           }
-          // a token that is not finite has made its scores NaN: here it must not reach the rows that do not see it
-          if (!in || mv.y != mv.y) mv = make_float2(0.f, 0.f);
+          if (!in) mv = make_float2(0.f, 0.f);
           scale_of(mv, ms, mc);
 #pragma unroll
           for (int i = 0; i < kWords; ++i) {

@@ -39,8 +39,8 @@ def test_constant_groups_and_tokens_that_do_not_fit():
     assert scale[0, 0, 0] == 0 and np.all(codes == 0) and np.all(co.dequantize(codes, scale, low) == 1.25)
     k, v = np.zeros((4, 1, 64), np.float32), np.zeros((4, 1, 64), np.float32)
     k[1, 0, 3], v[2, 0, 9], k[3, 0, 0] = np.inf, np.nan, -1e5
-    for codes, scale, low in co.quantize_tokens(k, v):
-        assert np.isnan(low[1:]).all() and (scale[1:] == 0).all() and np.isfinite(low[0]).all()
+    (kc, ks, kl), (vc, vs, vl) = co.quantize_tokens(k, v)
+    assert np.isnan(kl[1:]).all() and (vl[1:] == 0).all() and (ks[1:] == 0).all() and (vs[1:] == 0).all() and np.isfinite(kl[0]).all()
 
 
 def test_bytes_of_a_page():
