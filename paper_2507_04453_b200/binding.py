@@ -378,7 +378,8 @@ class KvCache:
 
     pages [layers, num_pages, page_bytes] uint8, table [max_seqs, max_pages], lengths [max_seqs], refs [num_pages] int32.
     Index and count arguments are int32 tensors on the cache's device.  ``stream``: a torch.cuda.Stream; None = the current
-    stream of the cache's device.  Workspaces and outputs come from torch's allocator, on that stream."""
+    stream of the cache's device.  Workspaces and outputs come from torch's allocator, on that
+    stream.  Not thread-safe, as its context."""
 
     def __init__(self, ctx, layers, num_pages, kv_heads, head_dim, max_seqs, max_pages, pages=None, table=None, lengths=None, refs=None):
         torch = ctx.torch
@@ -411,80 +412,105 @@ class KvCache:
         self._pages_ws = need.value
         self._sms = torch.cuda.get_device_properties(self.device).multi_processor_count
         self._attend_ws = {}  # (q_heads, max_new) -> bytes
+        self._ws = {}         # cudaStream_t -> workspace
+        self._lib, self._h, self._ref, self._index = ctx.lib, ctx.handle, C.byref(self.desc), self.device.index
+        self._int32, self._bf16, self._scale = torch.int32, torch.bfloat16, head_dim ** -0.5
+        self._current_stream = torch._C._cuda_getCurrentRawStream
         if fresh:
             self.reset()
 
-    # -- plumbing
-    def _on(self, stream):
-        """(stream to enqueue on, context manager under which torch allocates for it)"""
-        torch = self.ctx.torch
-        return (torch.cuda.current_stream(self.device), contextlib.nullcontext()) if stream is None else (stream, torch.cuda.stream(stream))
+    # -- plumbing (a decode step makes these calls once per layer: they take a few microseconds each, so the checks are terse)
+    def _raw(self, stream):
+        """The cudaStream_t to enqueue on (None: torch's current stream of the cache's device)."""
+        return (self._current_stream(self._index) if stream is None else stream.cuda_stream) or None
+
+    def _fail(self, name, what):
+        raise EssaError(ESSA_ERR_INVALID_ARG, f"kv_cache: {name} must be {what} on {self.device}")
 
     def _ints(self, name, t, n=None):
         """Checks an int32 index tensor; its pointer (None for None)."""
         if t is None:
             return None
-        if t.dtype != self.ctx.torch.int32 or t.dim() != 1 or not t.is_contiguous() or t.device != self.device or (n is not None and t.numel() != n):
-            raise EssaError(ESSA_ERR_INVALID_ARG, f"kv_cache: {name} must be a contiguous int32 vector on {self.device}" + ("" if n is None else f" of {n} elements"))
-        return t.data_ptr() if t.numel() else None
+        if t.dtype is not self._int32 or t.dim() != 1 or t.get_device() != self._index or not t.is_contiguous() or (n is not None and t.shape[0] != n):
+            self._fail(name, "a contiguous int32 vector" + ("" if n is None else f" of {n} elements"))
+        return t.data_ptr() or None
 
     def _entries(self, T, slots, tok_offsets):
-        n = T if tok_offsets is None else tok_offsets.numel() - 1
+        n = T if tok_offsets is None else tok_offsets.shape[0] - 1
         if n < 0:
             raise EssaError(ESSA_ERR_INVALID_ARG, "kv_cache: tok_offsets is empty")
         return self._ints("slots", slots, n), self._ints("tok_offsets", tok_offsets), n
 
     def _rows(self, name, t, heads):
         """Checks a token-major [T, heads, head_dim] or [T, heads * head_dim] bf16 tensor; (pointer, elements between rows)."""
-        ok = t.dtype == self.ctx.torch.bfloat16 and t.device == self.device
-        if ok and t.dim() == 3:
-            ok = t.shape[1:] == (heads, self.head_dim) and (t.numel() == 0 or (t.stride(2) == 1 and (heads == 1 or t.stride(1) == self.head_dim)))
+        shape, d = t.shape, self.head_dim
+        width = heads * d
+        ok = t.dtype is self._bf16 and t.get_device() == self._index
+        if ok and len(shape) == 3:
+            ok = shape[1] == heads and shape[2] == d
         elif ok:
-            ok = t.dim() == 2 and t.shape[1] == heads * self.head_dim and (t.numel() == 0 or t.stride(1) == 1)
-        if not ok:
-            raise EssaError(ESSA_ERR_INVALID_ARG, f"kv_cache: {name} must be a bf16 tensor [T, {heads}, {self.head_dim}] on {self.device} whose rows are contiguous")
-        T = t.shape[0]
-        return (t.data_ptr() if T else None), (t.stride(0) if T > 1 else heads * self.head_dim)
+            ok = len(shape) == 2 and shape[1] == width
+        if ok and t.is_contiguous():
+            return t.data_ptr() or None, width
+        if ok and shape[0]:
+            stride = t.stride()
+            if stride[-1] == 1 and (len(shape) == 2 or heads == 1 or stride[1] == d):
+                return t.data_ptr(), (stride[0] if shape[0] > 1 else width)
+        self._fail(name, f"a bf16 tensor [T, {heads}, {d}] whose rows are contiguous")
 
-    def _space(self, bytes_):
-        return self.ctx.torch.empty(bytes_, dtype=self.ctx.torch.uint8, device=self.device)
+    def _workspace(self, bytes_, raw, stream):
+        """A workspace for a call on stream `raw`: one buffer per stream serves its calls in turn.  A call that is being captured
+        gets its own, from the graph's pool: the graph may be replayed beside later calls on the stream it was captured on."""
+        torch = self.ctx.torch
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return self._workspace(bytes_, raw, None)
+        if torch.cuda.is_current_stream_capturing():
+            return torch.empty(bytes_, dtype=torch.uint8, device=self.device)
+        ws = self._ws.get(raw)
+        if ws is None or ws.shape[0] < bytes_:
+            ws = self._ws[raw] = torch.empty(bytes_, dtype=torch.uint8, device=self.device)
+        return ws
+
+    def _empty(self, shape, stream):
+        torch = self.ctx.torch
+        if stream is None:
+            return torch.empty(shape, dtype=torch.bfloat16, device=self.device)
+        with torch.cuda.stream(stream):
+            return torch.empty(shape, dtype=torch.bfloat16, device=self.device)
+
+    def _check(self, st):
+        if st != ESSA_OK:
+            self.ctx._check(st)
 
     # -- pages
     def reset(self, stream=None):
         """essa_cache_reset: all sequences empty, all pages free."""
-        s, _ = self._on(stream)
-        self.ctx._check(self.ctx.lib.essa_cache_reset(self.ctx.handle, C.byref(self.desc), s.cuda_stream or None))
+        self._check(self._lib.essa_cache_reset(self._h, self._ref, self._raw(stream)))
 
     def grow(self, slots, counts, stream=None):
         """essa_cache_grow: sequence slots[i] (None: i) becomes counts[i] tokens longer."""
-        n = counts.numel()
-        a, b = self._ints("slots", slots, n), self._ints("counts", counts)
-        s, alloc = self._on(stream)
-        with alloc:
-            ws = self._space(self._pages_ws)
-        self.ctx._check(self.ctx.lib.essa_cache_grow(self.ctx.handle, C.byref(self.desc), a, b, n, ws.data_ptr(), self._pages_ws, s.cuda_stream or None))
+        n = counts.shape[0]
+        a, b, raw = self._ints("slots", slots, n), self._ints("counts", counts), self._raw(stream)
+        ws = self._workspace(self._pages_ws, raw, stream)
+        self._check(self._lib.essa_cache_grow(self._h, self._ref, a, b, n, ws.data_ptr(), ws.shape[0], raw))
 
     def fork(self, src, dst, lens=None, stream=None):
         """essa_cache_fork: sequence dst[i] becomes a copy of the first lens[i] (None: all) tokens of src[i]."""
-        n = src.numel()
-        a, b, c = self._ints("src", src), self._ints("dst", dst, n), self._ints("lens", lens, n)
-        s, alloc = self._on(stream)
-        with alloc:
-            ws = self._space(self._pages_ws)
-        self.ctx._check(self.ctx.lib.essa_cache_fork(self.ctx.handle, C.byref(self.desc), a, b, c, n, ws.data_ptr(), self._pages_ws, s.cuda_stream or None))
+        n = src.shape[0]
+        a, b, c, raw = self._ints("src", src), self._ints("dst", dst, n), self._ints("lens", lens, n), self._raw(stream)
+        ws = self._workspace(self._pages_ws, raw, stream)
+        self._check(self._lib.essa_cache_fork(self._h, self._ref, a, b, c, n, ws.data_ptr(), ws.shape[0], raw))
 
     def free(self, slots, stream=None):
         """essa_cache_free: the sequences become empty."""
-        s, _ = self._on(stream)
-        self.ctx._check(self.ctx.lib.essa_cache_free(self.ctx.handle, C.byref(self.desc), self._ints("slots", slots), slots.numel(), s.cuda_stream or None))
+        self._check(self._lib.essa_cache_free(self._h, self._ref, self._ints("slots", slots), slots.shape[0], self._raw(stream)))
 
     def compact(self, used=None, stream=None):
         """essa_cache_compact: the pages in use become 0 .. U - 1; used (int32, one element) receives U."""
-        u = self._ints("used", used, 1)
-        s, alloc = self._on(stream)
-        with alloc:
-            ws = self._space(self._pages_ws)
-        self.ctx._check(self.ctx.lib.essa_cache_compact(self.ctx.handle, C.byref(self.desc), u, ws.data_ptr(), self._pages_ws, s.cuda_stream or None))
+        u, raw = self._ints("used", used, 1), self._raw(stream)
+        ws = self._workspace(self._pages_ws, raw, stream)
+        self._check(self._lib.essa_cache_compact(self._h, self._ref, u, ws.data_ptr(), ws.shape[0], raw))
 
     # -- tokens
     def append(self, layer: int, k, v, tok_offsets=None, slots=None, stream=None):
@@ -495,51 +521,43 @@ class KvCache:
         pk, ldk = self._rows("k", k, self.kv_heads)
         pv, ldv = self._rows("v", v, self.kv_heads)
         a, b, n = self._entries(T, slots, tok_offsets)
-        s, _ = self._on(stream)
-        self.ctx._check(self.ctx.lib.essa_cache_append(self.ctx.handle, C.byref(self.desc), layer, pk, ldk, pv, ldv, T, a, b, n, s.cuda_stream or None))
+        self._check(self._lib.essa_cache_append(self._h, self._ref, layer, pk, ldk, pv, ldv, T, a, b, n, self._raw(stream)))
 
     def read(self, layer: int, tok_offsets, T: int, slots=None, k_out=None, v_out=None, stream=None):
         """essa_cache_read: (k, v) [T, kv_heads, head_dim] bf16, the last tokens of the entries' sequences as they are stored."""
-        torch = self.ctx.torch
         a, b, n = self._entries(T, slots, tok_offsets)
-        s, alloc = self._on(stream)
-        with alloc:
-            shape = (T, self.kv_heads, self.head_dim)
-            k_out = torch.empty(shape, dtype=torch.bfloat16, device=self.device) if k_out is None else k_out
-            v_out = torch.empty(shape, dtype=torch.bfloat16, device=self.device) if v_out is None else v_out
-        for name, t in (("k_out", k_out), ("v_out", v_out)):
-            self._rows(name, t, self.kv_heads)
-            if t.shape[0] != T or not t.is_contiguous():
-                raise EssaError(ESSA_ERR_INVALID_ARG, f"kv_cache: {name} must be contiguous with T rows")
-        self.ctx._check(self.ctx.lib.essa_cache_read(self.ctx.handle, C.byref(self.desc), layer, k_out.data_ptr() if T else None,
-                                                     v_out.data_ptr() if T else None, T, a, b, n, s.cuda_stream or None))
+        shape = (T, self.kv_heads, self.head_dim)
+        k_out = self._empty(shape, stream) if k_out is None else k_out
+        v_out = self._empty(shape, stream) if v_out is None else v_out
+        pk, pv = self._rows("k_out", k_out, self.kv_heads)[0], self._rows("v_out", v_out, self.kv_heads)[0]
+        if k_out.shape[0] != T or v_out.shape[0] != T or not (k_out.is_contiguous() and v_out.is_contiguous()):
+            self._fail("k_out and v_out", f"contiguous tensors of {T} rows")
+        self._check(self._lib.essa_cache_read(self._h, self._ref, layer, pk, pv, T, a, b, n, self._raw(stream)))
         return k_out, v_out
 
     def attend(self, layer: int, q, tok_offsets=None, slots=None, max_new: int = 1, scale=None, out=None, stream=None):
         """essa_cache_attend: q [T, heads, head_dim] (or [T, heads * head_dim]) bf16 over the cached tokens; the result has q's
         shape.  max_new: the most rows an entry is expected to have (chooses the schedule only); scale: None = head_dim ** -0.5."""
-        torch = self.ctx.torch
-        T = q.shape[0]
-        heads = q.shape[1] if q.dim() == 3 else q.shape[-1] // self.head_dim
+        shape = q.shape
+        heads = shape[1] if len(shape) == 3 else shape[-1] // self.head_dim
         pq, ldq = self._rows("q", q, heads)
-        a, b, n = self._entries(T, slots, tok_offsets)
-        key = (heads, max_new)
-        need = self._attend_ws.get(key)
+        a, b, n = self._entries(shape[0], slots, tok_offsets)
+        need = self._attend_ws.get((heads, max_new))
         if need is None:
             got = C.c_int64(0)
-            st = self.ctx.lib.essa_cache_attend_workspace(C.byref(self.desc), heads, max_new, self._sms, C.byref(got))
+            st = self._lib.essa_cache_attend_workspace(self._ref, heads, max_new, self._sms, C.byref(got))
             if st != ESSA_OK:
                 raise EssaError(st, "kv_cache: the number of query heads must be a multiple of kv_heads and max_new at least 1")
-            need = self._attend_ws[key] = got.value
-        s, alloc = self._on(stream)
-        with alloc:
-            out = torch.empty(q.shape, dtype=q.dtype, device=self.device) if out is None else out
-            ws = self._space(need)
-        if out.shape != q.shape:
+            need = self._attend_ws[(heads, max_new)] = got.value
+        if out is None:
+            out = self._empty(shape, stream)
+        elif out.shape != shape:
             raise EssaError(ESSA_ERR_INVALID_ARG, "kv_cache: out must have q's shape")
         po, ldo = self._rows("out", out, heads)
-        self.ctx._check(self.ctx.lib.essa_cache_attend(self.ctx.handle, C.byref(self.desc), layer, pq, ldq, heads, T, a, b, n, max_new,
-                                                       self.head_dim ** -0.5 if scale is None else scale, po, ldo, ws.data_ptr(), need, s.cuda_stream or None))
+        raw = self._raw(stream)
+        ws = self._workspace(need, raw, stream)
+        self._check(self._lib.essa_cache_attend(self._h, self._ref, layer, pq, ldq, heads, shape[0], a, b, n, max_new, self._scale if scale is None else scale,
+                                                po, ldo, ws.data_ptr(), ws.shape[0], raw))
         return out
 
 

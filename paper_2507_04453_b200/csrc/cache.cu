@@ -9,17 +9,34 @@ namespace {
 constexpr int kPlanThreads = 1024;
 
 // ------------------------------------------------------------------------------------------------ tokens
+constexpr int kOffsetsMax = 2048;  // offsets that a thread block searches in shared memory
+
+// The offsets of a call in shared memory, if they fit (all threads of the block; a search of dependent loads from L2 would take
+// longer than the rest of a decode step's append).
+__device__ __forceinline__ void stage_offsets(const CacheEntries& e, int32_t* sm) {
+  if (!e.off || e.n >= kOffsetsMax) return;
+  for (int i = threadIdx.x; i <= e.n; i += blockDim.x) sm[i] = __ldg(e.off + i);
+  __syncthreads();
+}
 // The entry that row t belongs to (off[i] <= t < off[i + 1]); -1 if none.
-__device__ __forceinline__ int entry_of(const CacheEntries& e, int t) {
+__device__ __forceinline__ int entry_of(const CacheEntries& e, const int32_t* sm, int t) {
   if (!e.off) return t;
-  if (e.n == 0 || t < __ldg(e.off) || t >= __ldg(e.off + e.n)) return -1;
-  return find_candidate(e.off, e.n, t);
+  if (e.n == 0) return -1;
+  if (e.n >= kOffsetsMax) return t < __ldg(e.off) || t >= __ldg(e.off + e.n) ? -1 : find_candidate(e.off, e.n, t);
+  if (t < sm[0] || t >= sm[e.n]) return -1;
+  int lo = 0, hi = e.n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (sm[mid] <= t) lo = mid; else hi = mid;
+  }
+  return lo;
 }
 
 // Where row t of the call is cached: page (>= 0) and offset in it; -1 if the row belongs to no entry, -2 if it should be in
 // the cache and is not.
-__device__ __forceinline__ int locate_token(const CacheView& v, const CacheEntries& e, int t, int* offset) {
-  const int i = entry_of(e, t);
+__device__ __forceinline__ int locate_token(const CacheView& v, const CacheEntries& e, const int32_t* sm, int t, int* offset, int* end) {
+  *end = t + 1;  // (rows up to here follow in the same entry and page)
+  const int i = entry_of(e, sm, t);
   if (i < 0) return -1;
   const EntryInfo info = load_entry(v, e, i);
   const int pos = info.len - info.rows + (t - info.row0);
@@ -27,104 +44,116 @@ __device__ __forceinline__ int locate_token(const CacheView& v, const CacheEntri
   const int page = __ldg(v.table + (int64_t)info.slot * v.max_pages + pos / kPageTokens);
   if (page < 0 || page >= v.num_pages) return -2;
   *offset = pos % kPageTokens;
+  *end = min(t + kPageTokens - *offset, info.row0 + info.rows);
   return page;
 }
 
+// Eight channels of a group of 64; the other seven neighbours (lanes of an aligned group of eight) hold the rest.
+struct Piece {
+  uint4 raw;  // bf16
+  __device__ __forceinline__ float value(int i) const {
+    const uint32_t w = i < 2 ? raw.x : i < 4 ? raw.y : i < 6 ? raw.z : raw.w;
+    return __uint_as_float(i & 1 ? w & 0xffff0000u : w << 16);
+  }
+};
 struct Packed {
   uint32_t codes;
   __half scale, low;
+  bool fits;
 };
+__device__ __forceinline__ __nv_bfloat162 as_bf162(uint32_t v) { return *reinterpret_cast<__nv_bfloat162*>(&v); }
 
-// 4-bit storage of a group of 64 channels of which this thread holds eight, the other seven neighbours (lanes of an aligned
-// group of eight) the rest.
-__device__ __forceinline__ void group_stats(const float (&x)[8], float& low, float& high, bool& finite) {
-  low = x[0];
-  high = x[0];
-  float probe = 0.f;
+// 4-bit storage of the group.  The minimum and maximum are found on bf16 pairs (exact, NaN stays NaN); one shuffle a step carries
+// (max, -min).
+__device__ __forceinline__ Packed pack_group(const Piece& x) {
+  const __nv_bfloat162 a = as_bf162(x.raw.x), b = as_bf162(x.raw.y), c = as_bf162(x.raw.z), d = as_bf162(x.raw.w);
+  const __nv_bfloat162 top = __hmax2_nan(__hmax2_nan(a, b), __hmax2_nan(c, d)), low = __hneg2(__hmin2_nan(__hmin2_nan(a, b), __hmin2_nan(c, d)));
+  __nv_bfloat162 both = __hmax2_nan(__lows2bfloat162(top, low), __highs2bfloat162(top, low));
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    low = fminf(low, x[i]);
-    high = fmaxf(high, x[i]);
-    probe = fmaf(x[i], 0.f, probe);  // NaN if any is NaN or infinite
-  }
-  finite = probe == 0.f;
-#pragma unroll
-  for (int d = 1; d < 8; d <<= 1) {
-    low = fminf(low, __shfl_xor_sync(0xffffffffu, low, d));
-    high = fmaxf(high, __shfl_xor_sync(0xffffffffu, high, d));
-  }
-}
-__device__ __forceinline__ Packed pack_group(const float (&x)[8], float low, float high) {
+  for (int step = 1; step < 8; step <<= 1) both = __hmax2_nan(both, __shfl_xor_sync(0xffffffffu, both, step));
+  const float high = __low2float(both);
   Packed p;
-  p.low = __float2half_rn(low);
+  p.low = __float2half_rn(-__high2float(both));
   const float base = __half2float(p.low);
-  p.scale = __float2half_rn(__fdiv_rn(high - base, 15.f));
+  // (high - base) / 15, correctly rounded (Markstein: a quotient from the rounded reciprocal, corrected by its exact remainder)
+  const float range = high - base, q0 = range * (1.f / 15.f);
+  p.scale = __float2half_rn(fmaf(fmaf(-15.f, q0, range), 1.f / 15.f, q0));
   const float s = __half2float(p.scale);
+  p.fits = s < INFINITY && fabsf(base) < INFINITY;  // (false for NaN)
   p.codes = 0;
   if (s > 0.f) {
+    // rint((x - base) / s): times 1 / s it is off by a few units of 2^-23, which matters next to a half only; then the division is made.
+    // (The division, the rounding and the conversion of every value kept the kernel at a quarter of the memory's rate: 128 us for 32 thousand
+    // tokens of 8 heads of 128, 209 MB.)
+    float inv;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));
+    const float magic = 12582912.f;  // 1.5 * 2^23: what is added to it is rounded to an integer, ties to even
+    float far = 0.f, c8[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float c = fminf(fmaxf(rintf(__fdiv_rn(x[i] - base, s)), 0.f), 15.f);
-      p.codes |= (uint32_t)c << (4 * i);
+      const float q = fminf(fmaxf((x.value(i) - base) * inv, 0.f), 15.f);
+      c8[i] = q + magic;
+      far = fmaxf(far, fabsf(q - (c8[i] - magic)));
     }
+    if (far > 0.4999f) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) c8[i] = fminf(fmaxf(__fdiv_rn(x.value(i) - base, s), 0.f), 15.f) + magic;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) p.codes |= (__float_as_uint(c8[i]) & 15u) << (4 * i);
   }
   return p;
 }
-__device__ __forceinline__ void unpack8(const __nv_bfloat16* src, float (&x)[8]) {
-  const uint4 u = *reinterpret_cast<const uint4*>(src);
-  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x[2 * i] = __uint_as_float(w[i] << 16);
-    x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-  }
-}
 
-// One thread per eight channels of K and of V of one (token, kv head): D / 8 neighbouring lanes per token, tokens innermost so
-// that the 16-byte pieces of neighbouring tokens (adjacent in a page) meet in one sector.  Bound by HBM: 4 * D bytes in and
-// 1.125 * D out per (token, kv head).
-template <int D>
+// D / 8 neighbouring lanes take a token of a kv head, eight channels of K and of V each, kTokens tokens in turn; a thread block has
+// consecutive tokens of a head, so that the 16-byte pieces of neighbouring tokens (adjacent in a page) meet in one sector.  Bound by
+// HBM: 4 * D bytes in and 1.125 * D out per (token, kv head).
+template <int D, int kTokens>
 __global__ void __launch_bounds__(256) append_kernel(CacheView v, CacheEntries e, const __nv_bfloat16* k, int64_t ld_k, const __nv_bfloat16* val, int64_t ld_v,
                                                      int32_t* status) {
   constexpr int L = D / 8;  // lanes per token
-  const int64_t unit = ((int64_t)blockIdx.x * 256 + threadIdx.x) / L;
-  const int lane = threadIdx.x % L;
-  const int t = (int)(unit % e.T), h = (int)(unit / e.T);
-  const bool in = h < v.kv_heads;
-  int offset = 0;
-  int page = in ? locate_token(v, e, t, &offset) : -1;
-  if (page >= 0 && __ldg(v.refs + page) != 1) page = -2;  // shared (or free): not this sequence's to write
-  if (page == -2) cache_fault(status);
-  float xk[8], xv[8];
-  if (page >= 0) {
-    unpack8(k + t * ld_k + h * D + lane * 8, xk);
-    unpack8(val + t * ld_v + h * D + lane * 8, xv);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) xk[i] = xv[i] = 0.f;
-  }
-  float lk, hk, lv, hv;
-  bool fk, fv;
-  group_stats(xk, lk, hk, fk);
-  group_stats(xv, lv, hv, fv);
-  Packed pk = pack_group(xk, lk, hk), pv = pack_group(xv, lv, hv);
-  const bool fits = fk && fv && !__hisinf(pk.low) && !__hisinf(pk.scale) && !__hisinf(pv.low) && !__hisinf(pv.scale);
-  // one lane that does not fit makes the token (its L lanes) NaN
-  const uint32_t misfits = __ballot_sync(0xffffffffu, !fits) >> ((threadIdx.x & 31) / L * L) & ((1u << L) - 1);
-  if (page < 0) return;
-  if (misfits) {
-    pk.codes = pv.codes = 0;
-    pk.scale = pv.scale = pv.low = __ushort_as_half(0);  // (V 0: it meets weights 0 in the rows that do not see the token)
-    pk.low = __ushort_as_half(0x7e00);
-  }
-  uint8_t* run = v.pages + page * v.page_bytes + (int64_t)h * 72 * D;
-  uint8_t* code = run + (lane >> 2) * 1024 + offset * 16 + (lane & 3) * 4;
-  *reinterpret_cast<uint32_t*>(code) = pk.codes;
-  *reinterpret_cast<uint32_t*>(code + 32 * D) = pv.codes;
-  if ((lane & 7) == 0) {
-    __half2* meta = reinterpret_cast<__half2*>(run + 64 * D + ((lane >> 3) * kPageTokens + offset) * 4);
-    meta[0] = __halves2half2(pk.scale, pk.low);
-    meta[D] = __halves2half2(pv.scale, pv.low);
+  __shared__ int32_t offsets[kOffsetsMax];
+  stage_offsets(e, offsets);
+  // (heads innermost: thread blocks that run together read the whole rows of their tokens)
+  const int h = (int)(blockIdx.x % (uint32_t)v.kv_heads), lane = threadIdx.x % L;
+  const int64_t unit = (int64_t)(blockIdx.x / (uint32_t)v.kv_heads) * (256 / L) + threadIdx.x / L;
+  int end = -1, page = -1, offset = 0;  // the tokens before `end` follow the last one located in its entry and page
+#pragma unroll 1
+  for (int j = 0; j < kTokens; ++j) {
+    const int64_t at = unit * kTokens + j;
+    const bool in = at < e.T;
+    const int t = in ? (int)at : 0;
+    Piece xk, xv;
+    xk.raw = xv.raw = make_uint4(0, 0, 0, 0);
+    if (in) {  // (before the look-up: its loads and these need not wait for one another)
+      xk.raw = *reinterpret_cast<const uint4*>(k + t * ld_k + h * D + lane * 8);
+      xv.raw = *reinterpret_cast<const uint4*>(val + t * ld_v + h * D + lane * 8);
+    }
+    if (in && t < end) {
+      ++offset;
+    } else if (in) {
+      page = locate_token(v, e, offsets, t, &offset, &end);
+      if (page >= 0 && __ldg(v.refs + page) != 1) page = -2;  // shared (or free): not this sequence's to write
+      if (page == -2) cache_fault(status);
+    }
+    Packed pk = pack_group(xk), pv = pack_group(xv);
+    // one lane that does not fit makes the token (its L lanes) NaN
+    const uint32_t misfits = __ballot_sync(0xffffffffu, !(pk.fits && pv.fits)) >> ((threadIdx.x & 31) / L * L) & ((1u << L) - 1);
+    if (misfits) {
+      pk.codes = pv.codes = 0;
+      pk.scale = pv.scale = pv.low = __ushort_as_half(0);  // (V 0: it meets weights 0 in the rows that do not see the token)
+      pk.low = __ushort_as_half(0x7e00);
+    }
+    if (!in || page < 0) continue;
+    uint8_t* run = v.pages + page * v.page_bytes + (int64_t)h * 72 * D;
+    uint8_t* code = run + (lane >> 2) * 1024 + offset * 16 + (lane & 3) * 4;
+    *reinterpret_cast<uint32_t*>(code) = pk.codes;
+    *reinterpret_cast<uint32_t*>(code + 32 * D) = pv.codes;
+    if ((lane & 7) == 0) {
+      __half2* meta = reinterpret_cast<__half2*>(run + 64 * D + ((lane >> 3) * kPageTokens + offset) * 4);
+      meta[0] = __halves2half2(pk.scale, pk.low);
+      meta[D] = __halves2half2(pv.scale, pv.low);
+    }
   }
 }
 
@@ -132,12 +161,15 @@ __global__ void __launch_bounds__(256) append_kernel(CacheView v, CacheEntries e
 template <int D>
 __global__ void __launch_bounds__(256) read_kernel(CacheView v, CacheEntries e, __nv_bfloat16* k_out, __nv_bfloat16* v_out, int32_t* status) {
   constexpr int L = D / 8;
-  const int64_t unit = ((int64_t)blockIdx.x * 256 + threadIdx.x) / L;
-  const int lane = threadIdx.x % L;
-  const int t = (int)(unit % e.T), h = (int)(unit / e.T);
-  if (h >= v.kv_heads) return;
-  int offset = 0;
-  const int page = locate_token(v, e, t, &offset);
+  __shared__ int32_t offsets[kOffsetsMax];
+  stage_offsets(e, offsets);
+  // (heads innermost: thread blocks that run together read the whole rows of their tokens)
+  const int h = (int)(blockIdx.x % (uint32_t)v.kv_heads), lane = threadIdx.x % L;
+  const int64_t unit = (int64_t)(blockIdx.x / (uint32_t)v.kv_heads) * (256 / L) + threadIdx.x / L;
+  const int t = (int)min(unit, (int64_t)e.T);
+  if (t >= e.T) return;
+  int offset = 0, end;
+  const int page = locate_token(v, e, offsets, t, &offset, &end);
   if (page == -1) return;
   if (page == -2) cache_fault(status);
   const uint8_t* run = v.pages + (int64_t)max(page, 0) * v.page_bytes + (int64_t)h * 72 * D;
@@ -543,6 +575,11 @@ int32_t launched(essa_ctx* ctx, const char* what, int kernels) {
 // the 256-row tiles of tcgen05 re-use a widened page often enough.
 bool few_rows(int64_t rows) { return rows <= 16; }
 size_t seen_bytes(const CacheView& v) { return (size_t)(v.max_seqs + 31) / 32 * 4; }
+// Thread blocks of append and read: 256 / (head_dim / 8) times `per` tokens of one head each.
+int64_t token_blocks(int32_t T, const CacheView& v, int per) {
+  const int64_t tokens = (int64_t)256 / (v.head_dim / 8) * per;
+  return (T + tokens - 1) / tokens * v.kv_heads;
+}
 int copy_grid(const essa_ctx* ctx) { return ctx->sm_count * 8; }
 
 }  // namespace
@@ -616,12 +653,16 @@ int32_t essa_cache_append(essa_ctx* ctx, const essa_cache_desc* cache, int32_t l
   ESSA_TRY(check_rows(ctx, "cache_append", "k", k, ld_k, (int64_t)v.kv_heads * v.head_dim));
   ESSA_TRY(check_rows(ctx, "cache_append", "v", val, ld_v, (int64_t)v.kv_heads * v.head_dim));
   DeviceGuard guard(ctx->device);
-  const int64_t blocks = ((int64_t)T * v.kv_heads * (v.head_dim / 8) + 255) / 256;
-  if (blocks > 0x7fffffff) return fail(ctx, ESSA_ERR_UNSUPPORTED_SHAPE, "cache_append: too many tokens");
+  // Four tokens per thread share a look-up; a call that would leave SMs without work that way (fewer than four thread blocks each) takes one
+  // (32 thousand tokens of 8 heads: @ against @ us; 256 tokens of 4 heads: @ against @).
+  const bool four = token_blocks(T, v, 4) >= 4 * ctx->sm_count;
+  const int64_t grid = token_blocks(T, v, four ? 4 : 1);
+  if (grid > 0x7fffffff) return fail(ctx, ESSA_ERR_UNSUPPORTED_SHAPE, "cache_append: too many tokens");
   const auto *kk = static_cast<const __nv_bfloat16*>(k), *vv = static_cast<const __nv_bfloat16*>(val);
   cudaStream_t stream = static_cast<cudaStream_t>(stream_v);
-  if (v.head_dim == 64) append_kernel<64><<<(unsigned)blocks, 256, 0, stream>>>(v, e, kk, ld_k, vv, ld_v, ctx->d_status);
-  else append_kernel<128><<<(unsigned)blocks, 256, 0, stream>>>(v, e, kk, ld_k, vv, ld_v, ctx->d_status);
+  const auto run = [&](auto kernel) { kernel<<<(unsigned)grid, 256, 0, stream>>>(v, e, kk, ld_k, vv, ld_v, ctx->d_status); };
+  if (v.head_dim == 64) four ? run(append_kernel<64, 4>) : run(append_kernel<64, 1>);
+  else four ? run(append_kernel<128, 4>) : run(append_kernel<128, 1>);
   return launched(ctx, "cache_append", 1);
 }
 
@@ -636,12 +677,12 @@ int32_t essa_cache_read(essa_ctx* ctx, const essa_cache_desc* cache, int32_t lay
   if (k_out) ESSA_TRY(check_rows(ctx, "cache_read", "k_out", k_out, width, width));
   if (v_out) ESSA_TRY(check_rows(ctx, "cache_read", "v_out", v_out, width, width));
   DeviceGuard guard(ctx->device);
-  const int64_t blocks = ((int64_t)T * v.kv_heads * (v.head_dim / 8) + 255) / 256;
-  if (blocks > 0x7fffffff) return fail(ctx, ESSA_ERR_UNSUPPORTED_SHAPE, "cache_read: too many tokens");
+  const int64_t grid = token_blocks(T, v, 1);
+  if (grid > 0x7fffffff) return fail(ctx, ESSA_ERR_UNSUPPORTED_SHAPE, "cache_read: too many tokens");
   auto *kk = static_cast<__nv_bfloat16*>(k_out), *vv = static_cast<__nv_bfloat16*>(v_out);
   cudaStream_t stream = static_cast<cudaStream_t>(stream_v);
-  if (v.head_dim == 64) read_kernel<64><<<(unsigned)blocks, 256, 0, stream>>>(v, e, kk, vv, ctx->d_status);
-  else read_kernel<128><<<(unsigned)blocks, 256, 0, stream>>>(v, e, kk, vv, ctx->d_status);
+  if (v.head_dim == 64) read_kernel<64><<<(unsigned)grid, 256, 0, stream>>>(v, e, kk, vv, ctx->d_status);
+  else read_kernel<128><<<(unsigned)grid, 256, 0, stream>>>(v, e, kk, vv, ctx->d_status);
   return launched(ctx, "cache_read", 1);
 }
 

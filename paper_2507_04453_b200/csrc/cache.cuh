@@ -41,9 +41,9 @@ struct AttendArgs;  // cache_list.cuh
 // cache_attend.cu (few query rows per sequence) and cache_tiles.cu (many): rows_hint = most query rows (tokens x heads of a group)
 // that an entry is expected to have; both are right for any number.
 int64_t attend_decode_workspace(int head_dim, int64_t rows_hint, int sm_count);
-int32_t launch_attend_decode(essa_ctx* ctx, const AttendArgs& a, int64_t rows_hint, cudaStream_t stream);
+int32_t launch_attend_decode(essa_ctx* ctx, AttendArgs& a, int64_t rows_hint, cudaStream_t stream);
 int64_t attend_tiles_workspace(int head_dim, int sm_count);
-int32_t launch_attend_tiles(essa_ctx* ctx, const AttendArgs& a, cudaStream_t stream);
+int32_t launch_attend_tiles(essa_ctx* ctx, AttendArgs& a, cudaStream_t stream);
 
 #ifdef __CUDACC__
 __device__ __forceinline__ EntryInfo load_entry(const CacheView& v, const CacheEntries& e, int i) {

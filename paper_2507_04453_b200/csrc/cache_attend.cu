@@ -92,8 +92,7 @@ __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_
   constexpr int R = S::R, G = D / kCacheGroup, CH = D / 32;
   using L = DecodeList<R>;
   extern __shared__ __align__(128) uint8_t smem[];
-  __shared__ long long scan_sm[33];
-  __shared__ long long found[2];
+  __shared__ RunShared run_sm;
   __shared__ volatile int abort_flag;
   __shared__ int bad_page[S::kStages];
   __shared__ __align__(8) uint64_t bars[2 * S::kStages];
@@ -107,14 +106,9 @@ __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   __syncthreads();
-  const long long total = list_total<L>(a, scan_sm);
-  if (total == 0) return;
-  const int runs = run_count<L>(total, gridDim.x);
-  if ((int)blockIdx.x >= runs) return;
-  const long long begin = run_start(total, runs, blockIdx.x), end = run_start(total, runs, blockIdx.x + 1);
   Cursor c;
-  list_seek<L>(a, begin, c, scan_sm, found);
-  long long left = end - begin;
+  long long left = find_run<L>(a, c, run_sm);
+  if (left == 0) return;
 
   if (warp == kWarps) {  // ---------------------------------------------------------------- copying warp
     if (lane != 0) return;
@@ -504,16 +498,17 @@ __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_
 }
 
 template <int D, int NT>
-int32_t launch(essa_ctx* ctx, const AttendArgs& a, cudaStream_t stream) {
+int32_t launch(essa_ctx* ctx, AttendArgs& a, cudaStream_t stream) {
   using S = Shape<D, NT>;
-  cudaError_t e = cudaFuncSetAttribute(attend_decode_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
-  if (e != cudaSuccess) return check_cuda(ctx, e, "cudaFuncSetAttribute (attend)");
   const int grid = ctx->sm_count * attend_blocks_per_sm(D, NT);
+  a.partials_at = partials_at(grid);
+  cudaError_t e = allow_shared<attend_decode_kernel<D, NT>>(S::kSmem, ctx->device);
+  if (e != cudaSuccess) return check_cuda(ctx, e, "cudaFuncSetAttribute (attend)");
   attend_decode_kernel<D, NT><<<grid, kThreads, S::kSmem, stream>>>(a);
   e = cudaGetLastError();
   if (e != cudaSuccess) return check_cuda(ctx, e, "attend launch");
   ++ctx->launches;
-  return launch_join<DecodeList<S::R>, D>(ctx, a, grid, 1, stream);
+  return launch_join<DecodeList<S::R>, D>(ctx, a, grid, S::R / 4, stream);
 }
 
 }  // namespace
@@ -523,10 +518,10 @@ static int attend_nt(int64_t rows_hint) { return rows_hint > 8 ? 2 : 1; }
 
 int64_t attend_decode_workspace(int head_dim, int64_t rows_hint, int sm_count) {
   const int nt = attend_nt(rows_hint);
-  return (int64_t)sm_count * attend_blocks_per_sm(head_dim, nt) * 2 * (8 * nt) * (head_dim + 2) * 4;
+  return attend_workspace(sm_count * attend_blocks_per_sm(head_dim, nt), (int64_t)(8 * nt) * (head_dim + 2));
 }
 
-int32_t launch_attend_decode(essa_ctx* ctx, const AttendArgs& a, int64_t rows_hint, cudaStream_t stream) {
+int32_t launch_attend_decode(essa_ctx* ctx, AttendArgs& a, int64_t rows_hint, cudaStream_t stream) {
   const int nt = attend_nt(rows_hint);
   if (a.v.head_dim == 64) return nt == 1 ? launch<64, 1>(ctx, a, stream) : launch<64, 2>(ctx, a, stream);
   return nt == 1 ? launch<128, 1>(ctx, a, stream) : launch<128, 2>(ctx, a, stream);

@@ -10,6 +10,8 @@
 // see nothing are still written), per_head(info, args) (the elements of all row blocks of an entry), kSetup and kMinRun.
 #pragma once
 
+#include <atomic>
+
 #include "cache.cuh"
 #include "tc_ptx.cuh"
 
@@ -39,8 +41,14 @@ struct AttendArgs {
   Divisor by_group;
   float scale;  // softmax scale * log2(e)
   float* ws;
+  int64_t partials_at;  // floats before the partial results
   int32_t* status;
 };
+
+// Bytes of the workspace for `grid` thread blocks, two partial results of `floats` each; the partial results begin after the run places.
+constexpr int64_t kRunPlaceBytes = 40;
+inline int64_t partials_at(int grid) { return (kRunPlaceBytes * grid + 255) / 256 * 64; }
+inline int64_t attend_workspace(int grid, int64_t floats) { return (partials_at(grid) + (int64_t)grid * 2 * floats) * 4; }
 
 #ifdef __CUDACC__
 // 2^x by the special function unit (results below the normal range are 0, which no weight notices).
@@ -66,6 +74,14 @@ __device__ __forceinline__ __half2 centred_high(uint32_t w, uint32_t magic) {
   return __hfma2(nibble_half2<0x00f000f0u>(w, magic), as_half2(0x2c002c00u) /* 1 / 16 */, as_half2(0xd480d480u) /* -72 */);
 }
 
+// Where a run begins, as its thread block has found it (the workspace's first part, one for each thread block).
+struct RunPlace {
+  long long total;
+  int runs, entry, kvh, rb, at, tiles, row0, rows;
+};
+static_assert(sizeof(RunPlace) == kRunPlaceBytes, "");
+__device__ __forceinline__ RunPlace* run_places(const AttendArgs& a) { return reinterpret_cast<RunPlace*>(a.ws); }
+
 struct Cursor {  // a place in the list
   int entry, kvh, rb, at, blocks, tiles;  // at: element of the row block
   EntryInfo info;
@@ -74,45 +90,68 @@ struct Cursor {  // a place in the list
 // (rows * group < 2^31 is checked on the host)
 __device__ __forceinline__ int row_blocks(const EntryInfo& e, int group, int R) { return (int)(((uint32_t)e.rows * (uint32_t)group + R - 1) / R); }
 
-// Elements of the list; all threads of the block.  sm: shared [33].
+__device__ __forceinline__ long long run_start(long long total, int runs, int c) { return total * c / runs; }
+// Runs that share the list: L::kMinRun elements each at least (a shorter one would pay its fixed cost and a join for little).
 template <class L>
-__device__ long long list_total(const AttendArgs& a, long long* sm) {
-  long long total = 0;
-  for (int base = 0; base < a.e.n; base += blockDim.x) {
-    const int i = base + threadIdx.x;
-    long long w = 0, t;
-    if (i < a.e.n) w = L::per_head(load_entry(a.v, a.e, i), a) * a.v.kv_heads;
-    block_scan(w, &t, sm);
-    total += t;
-  }
-  return total;
+__device__ __forceinline__ int run_count(long long total, int grid) {
+  return (int)max(1LL, min((long long)grid, (total + L::kMinRun - 1) / L::kMinRun));
 }
 
-// The place of element `at` < total; all threads of the block.  found: shared [2].
+struct RunShared {
+  long long scan[33];
+  long long rest;
+  int entry;
+};
+// This thread block's run: its first element's place and its length (0: none); all threads of the block.  Every thread sums a stretch
+// of the entries; the one whose stretch holds the place walks it again.
 template <class L>
-__device__ void list_seek(const AttendArgs& a, long long at, Cursor& c, long long* sm, long long* found) {
-  long long before = 0;
-  for (int base = 0; base < a.e.n; base += blockDim.x) {
-    const int i = base + threadIdx.x;
-    long long w = 0, t;
-    if (i < a.e.n) w = L::per_head(load_entry(a.v, a.e, i), a) * a.v.kv_heads;
-    const long long pre = before + block_scan(w, &t, sm);
-    if (w > 0 && at >= pre && at < pre + w) {
-      found[0] = i;
-      found[1] = at - pre;
-    }
-    before += t;
-    __syncthreads();
-    if (at < before) break;
+__device__ long long find_run(const AttendArgs& a, Cursor& c, RunShared& sm) {
+  const int per = (a.e.n + blockDim.x - 1) / blockDim.x, lo = min((int)threadIdx.x * per, a.e.n), hi = min(lo + per, a.e.n);
+  long long sum = 0, total;
+  for (int i = lo; i < hi; ++i) sum += L::per_head(load_entry(a.v, a.e, i), a) * a.v.kv_heads;
+  const long long pre = block_scan(sum, &total, sm.scan);
+  if (total == 0) {
+    if (blockIdx.x == 0 && threadIdx.x == 0) run_places(a)[0].runs = 0;
+    return 0;
   }
-  c.entry = (int)found[0];
+  const int runs = run_count<L>(total, gridDim.x);
+  if ((int)blockIdx.x >= runs) return 0;
+  const long long begin = run_start(total, runs, blockIdx.x), end = run_start(total, runs, blockIdx.x + 1);
+  if (begin >= pre && begin < pre + sum) {
+    long long rest = begin - pre;
+    for (int i = lo; i < hi; ++i) {
+      const long long w = L::per_head(load_entry(a.v, a.e, i), a) * a.v.kv_heads;
+      if (rest < w) {
+        sm.entry = i;
+        sm.rest = rest;
+        break;
+      }
+      rest -= w;
+    }
+  }
+  __syncthreads();
+  c.entry = sm.entry;
   c.info = load_entry(a.v, a.e, c.entry);
   c.blocks = row_blocks(c.info, a.group, L::R);
-  const long long per = L::per_head(c.info, a);
-  c.kvh = (int)(found[1] / per);
-  long long rest = found[1] % per;
+  const long long per_head = L::per_head(c.info, a);
+  c.kvh = (int)(sm.rest / per_head);
+  long long rest = sm.rest % per_head;
   for (c.rb = 0; (c.tiles = L::tiles(c.info, a, c.rb)) + L::kSetup <= rest; ++c.rb) rest -= c.tiles + L::kSetup;
   c.at = (int)rest;
+  if (threadIdx.x == 0) {  // for attend_join_kernel
+    RunPlace p;
+    p.total = total;
+    p.runs = runs;
+    p.entry = c.entry;
+    p.kvh = c.kvh;
+    p.rb = c.rb;
+    p.at = c.at;
+    p.tiles = c.tiles;
+    p.row0 = c.info.row0;
+    p.rows = c.info.rows;
+    run_places(a)[blockIdx.x] = p;
+  }
+  return end - begin;
 }
 
 // Takes what is left of c's row block from a run that has `left` elements to go: key tiles first .. stop - 1 (none, if the run ends
@@ -142,13 +181,6 @@ __device__ __forceinline__ void next_block(const AttendArgs& a, Cursor& c) {
   c.tiles = L::tiles(c.info, a, c.rb);
 }
 
-__device__ __forceinline__ long long run_start(long long total, int runs, int c) { return total * c / runs; }
-// Runs that share the list: L::kMinRun elements each at least (a shorter one would pay its fixed cost and a join for little).
-template <class L>
-__device__ __forceinline__ int run_count(long long total, int grid) {
-  return (int)max(1LL, min((long long)grid, (total + L::kMinRun - 1) / L::kMinRun));
-}
-
 template <class L, int D>
 struct Partial {
   static constexpr int kFloats = L::R * (D + 2);  // O [R][D], maximum [R], sum [R]
@@ -156,59 +188,77 @@ struct Partial {
 // Slot of the partial result that run `run` leaves for a row block: 1 if the row block begins in this run, else 0.
 template <class L, int D>
 __device__ __forceinline__ float* partial_of(const AttendArgs& a, int run, bool begins) {
-  return a.ws + ((int64_t)run * 2 + (begins ? 1 : 0)) * Partial<L, D>::kFloats;
+  return a.ws + a.partials_at + ((int64_t)run * 2 + (begins ? 1 : 0)) * Partial<L, D>::kFloats;
 }
 
 // Joins the row blocks that run boundaries cut.  Thread blocks (c, *) look at the boundary between runs c and c + 1 and work if it
-// is the first one between key tiles of its row block; gridDim.y of them share its rows.  Launched to start beside the attention kernel: it finds
-// its row block meanwhile and waits for the partial results.
+// is the first one between key tiles of its row block; gridDim.y of them share its rows.  A warp takes a row; its partial results are
+// read eight at a time (they come from L2, one after the other they would cost its latency each) and added in run order.
 template <class L, int D>
-__global__ void __launch_bounds__(128) attend_join_kernel(AttendArgs a, int grid) {
-  constexpr int R = L::R;
-  __shared__ long long scan_sm[33];
-  __shared__ long long found[2];
-  const long long total = list_total<L>(a, scan_sm);
-  const int runs = total ? run_count<L>(total, grid) : 0;
-  Cursor c;
-  long long first = 0;
-  const int run = blockIdx.x;
-  bool work = run + 1 < runs;
-  if (work) {
-    const long long edge = run_start(total, runs, run + 1);
-    list_seek<L>(a, edge, c, scan_sm, found);
-    first = edge - c.at;  // the row block's first element
-    work = c.at > L::kSetup && first + L::kSetup >= run_start(total, runs, run);
-  }
+__global__ void __launch_bounds__(128) attend_join_kernel(AttendArgs a) {
+  constexpr int R = L::R, V = D / 32;  // V floats of a row per lane
   grid_dep_wait();
-  if (!work) return;
-  const long long stop = first + L::kSetup + c.tiles;
-  const int rows = c.info.rows * a.group, r0 = c.rb * R;
-  int last = run;  // the runs run .. last have a part of the row block
-  while (last + 1 < runs && run_start(total, runs, last + 1) < stop) ++last;
-  for (int x = blockIdx.y * 128 + threadIdx.x; x < R * (D / 4); x += gridDim.y * 128) {
-    const int row = x / (D / 4), d4 = (x % (D / 4)) * 4, r = r0 + row;
+  const int run = blockIdx.x;
+  const int runs = run_places(a)[0].runs;  // (0: no entry has a row)
+  if (run + 1 >= runs) return;
+  const RunPlace p = run_places(a)[run + 1];
+  const long long edge = run_start(p.total, runs, run + 1), first = edge - p.at, begin = run_start(p.total, runs, run);
+  if (p.at <= L::kSetup || first + L::kSetup < begin) return;
+  const long long stop = first + L::kSetup + p.tiles;
+  // the runs run .. last have a part of the row block: floor(total k / runs) < stop for k < stop * runs / total
+  const int last = (int)min((long long)runs - 1, (stop * runs + p.total - 1) / p.total - 1);
+  const int rows = p.rows * a.group, r0 = p.rb * R, lane = threadIdx.x & 31;
+  for (int row = blockIdx.y * 4 + (threadIdx.x >> 5); row < R; row += gridDim.y * 4) {
+    const int r = r0 + row;
     if (r >= rows) break;
-    float m = -INFINITY, sum = 0.f;
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int k = run; k <= last; ++k) {
-      const float* p = partial_of<L, D>(a, k, k == run);
-      const float pm = p[R * D + row], mn = fmaxf(m, pm);
-      const float f0 = m == -INFINITY ? 0.f : ex2((m - mn) * a.scale), f1 = pm == -INFINITY ? 0.f : ex2((pm - mn) * a.scale);
-      const float4 y = *reinterpret_cast<const float4*>(p + row * D + d4);
-      sum = fmaf(f0, sum, f1 * p[R * D + R + row]);
-      v.x = fmaf(f0, v.x, f1 * y.x);
-      v.y = fmaf(f0, v.y, f1 * y.y);
-      v.z = fmaf(f0, v.z, f1 * y.z);
-      v.w = fmaf(f0, v.w, f1 * y.w);
-      m = mn;
+    float m = -INFINITY, sum = 0.f, v[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = 0.f;
+    for (int k0 = run; k0 <= last; k0 += 8) {
+      float pm[8], ps[8], pv[8][V];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int at = min(k0 + k, last);  // (behind the last one: read again and given no weight)
+        const float* q = partial_of<L, D>(a, at, at == run);
+        // (volatile loads: the compiler would move each to where it is used, behind the one before)
+        pm[k] = ld_cg_f32(q + R * D + row);
+        ps[k] = ld_cg_f32(q + R * D + R + row);
+        if constexpr (V == 4) {
+          const float4 x = ld_cg_f32x4(q + row * D + lane * 4);
+          pv[k][0] = x.x, pv[k][1] = x.y, pv[k][2] = x.z, pv[k][3] = x.w;
+        } else {
+          pv[k][0] = ld_cg_f32(q + row * D + lane * 2);
+          pv[k][1] = ld_cg_f32(q + row * D + lane * 2 + 1);
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        if (k0 + k > last) break;
+        const float mn = fmaxf(m, pm[k]);
+        const float f0 = m == -INFINITY ? 0.f : ex2((m - mn) * a.scale), f1 = pm[k] == -INFINITY ? 0.f : ex2((pm[k] - mn) * a.scale);
+        sum = fmaf(f0, sum, f1 * ps[k]);
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = fmaf(f0, v[i], f1 * pv[k][i]);
+        m = mn;
+      }
     }
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
     const int j = a.by_group(r), hd = r - j * a.group;
-    uint2 y;
-    y.x = pack_bf16x2(v.x * inv, v.y * inv);
-    y.y = pack_bf16x2(v.z * inv, v.w * inv);
-    *reinterpret_cast<uint2*>(a.out + (int64_t)(c.info.row0 + j) * a.ld_out + (int64_t)(c.kvh * a.group + hd) * D + d4) = y;
+    uint32_t* out = reinterpret_cast<uint32_t*>(a.out + (int64_t)(p.row0 + j) * a.ld_out + (int64_t)(p.kvh * a.group + hd) * D + lane * V);
+#pragma unroll
+    for (int i = 0; i < V; i += 2) out[i / 2] = pack_bf16x2(v[i] * inv, v[i + 1] * inv);
   }
+}
+
+// A kernel's dynamic shared memory allowance, raised on its first launch on a device (the call costs about a microsecond).
+template <auto kKernel>
+cudaError_t allow_shared(int bytes, int device) {
+  static std::atomic<uint64_t> done{0};  // a bit per device
+  const uint64_t bit = device < 64 ? 1ull << device : 0;
+  if (done.load(std::memory_order_relaxed) & bit) return cudaSuccess;
+  const cudaError_t e = cudaFuncSetAttribute(kKernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+  return e;
 }
 
 template <class L, int D>
@@ -223,7 +273,7 @@ int32_t launch_join(essa_ctx* ctx, const AttendArgs& a, int grid, int row_split,
   attr.val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, attend_join_kernel<L, D>, a, grid);
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, attend_join_kernel<L, D>, a);
   if (e != cudaSuccess) return check_cuda(ctx, e, "attend join launch");
   ++ctx->launches;
   return ESSA_OK;

@@ -143,8 +143,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
   using M = Mem<D>;
   using L = TileList;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ long long scan_sm[33];
-  __shared__ long long found[2];
+  __shared__ RunShared run_sm;
   __shared__ volatile int abort_flag;
   __shared__ int raw_bad[kRaw];
   __shared__ int tile_bad[8];  // the key tile's page is not there
@@ -165,14 +164,9 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   __syncthreads();
-  const long long total = list_total<L>(a, scan_sm);
-  if (total == 0) return;
-  const int runs = run_count<L>(total, gridDim.x);
-  if ((int)blockIdx.x >= runs) return;
-  const long long begin = run_start(total, runs, blockIdx.x);
-  long long left = run_start(total, runs, blockIdx.x + 1) - begin;
   Cursor c;
-  list_seek<L>(a, begin, c, scan_sm, found);
+  long long left = find_run<L>(a, c, run_sm);
+  if (left == 0) return;
   if (warp == kMmaWarp) {
     tmem_alloc(smem_u32(&tmem_slot), 512);
     tmem_relinquish();
@@ -585,22 +579,23 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
 }
 
 template <int D>
-int32_t launch(essa_ctx* ctx, const AttendArgs& a, cudaStream_t stream) {
+int32_t launch(essa_ctx* ctx, AttendArgs& a, cudaStream_t stream) {
   constexpr int smem = Mem<D>::kBytes + 1024;
-  cudaError_t e = cudaFuncSetAttribute(attend_tiles_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  a.partials_at = partials_at(ctx->sm_count);
+  cudaError_t e = allow_shared<attend_tiles_kernel<D>>(smem, ctx->device);
   if (e != cudaSuccess) return check_cuda(ctx, e, "cudaFuncSetAttribute (attend tiles)");
   attend_tiles_kernel<D><<<ctx->sm_count, kThreads, smem, stream>>>(a);
   e = cudaGetLastError();
   if (e != cudaSuccess) return check_cuda(ctx, e, "attend tiles launch");
   ++ctx->launches;
-  return launch_join<TileList, D>(ctx, a, ctx->sm_count, 8, stream);
+  return launch_join<TileList, D>(ctx, a, ctx->sm_count, 16, stream);
 }
 
 }  // namespace
 
-int64_t attend_tiles_workspace(int head_dim, int sm_count) { return (int64_t)sm_count * 2 * TileList::R * (head_dim + 2) * 4; }
+int64_t attend_tiles_workspace(int head_dim, int sm_count) { return attend_workspace(sm_count, (int64_t)TileList::R * (head_dim + 2)); }
 
-int32_t launch_attend_tiles(essa_ctx* ctx, const AttendArgs& a, cudaStream_t stream) {
+int32_t launch_attend_tiles(essa_ctx* ctx, AttendArgs& a, cudaStream_t stream) {
   return a.v.head_dim == 64 ? launch<64>(ctx, a, stream) : launch<128>(ctx, a, stream);
 }
 
