@@ -192,8 +192,8 @@ __device__ __forceinline__ float* partial_of(const AttendArgs& a, int run, bool 
 }
 
 // Joins the row blocks that run boundaries cut.  Thread blocks (c, *) look at the boundary between runs c and c + 1 and work if it
-// is the first one between key tiles of its row block; gridDim.y of them share its rows.  A warp takes a row; its partial results are
-// read eight at a time (they come from L2, one after the other they would cost its latency each) and added in run order.
+// is the first one between key tiles of its row block; gridDim.y of them share its rows.  A warp takes a row and adds its parts
+// in run order.
 template <class L, int D>
 __global__ void __launch_bounds__(128) attend_join_kernel(AttendArgs a) {
   constexpr int R = L::R, V = D / 32;  // V floats of a row per lane
@@ -214,32 +214,44 @@ __global__ void __launch_bounds__(128) attend_join_kernel(AttendArgs a) {
     float m = -INFINITY, sum = 0.f, v[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) v[i] = 0.f;
-    for (int k0 = run; k0 <= last; k0 += 8) {
-      float pm[8], ps[8], pv[8][V];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const int at = min(k0 + k, last);  // (behind the last one: read again and given no weight)
-        const float* q = partial_of<L, D>(a, at, at == run);
-        // (volatile loads: the compiler would move each to where it is used, behind the one before)
-        pm[k] = ld_cg_f32(q + R * D + row);
-        ps[k] = ld_cg_f32(q + R * D + R + row);
-        if constexpr (V == 4) {
-          const float4 x = ld_cg_f32x4(q + row * D + lane * 4);
-          pv[k][0] = x.x, pv[k][1] = x.y, pv[k][2] = x.z, pv[k][3] = x.w;
-        } else {
-          pv[k][0] = ld_cg_f32(q + row * D + lane * 2);
-          pv[k][1] = ld_cg_f32(q + row * D + lane * 2 + 1);
-        }
+    for (int k0 = run; k0 <= last; k0 += 32) {  // a lane has the maximum and the sum of a run's part
+      const int n = min(last + 1 - k0, 32);
+      float pm = -INFINITY, ps = 0.f;
+      if (lane < n) {
+        const float* q = partial_of<L, D>(a, k0 + lane, k0 + lane == run) + R * D + row;
+        pm = q[0];
+        ps = q[R];
       }
+      float top = fmaxf(m, pm);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        if (k0 + k > last) break;
-        const float mn = fmaxf(m, pm[k]);
-        const float f0 = m == -INFINITY ? 0.f : ex2((m - mn) * a.scale), f1 = pm[k] == -INFINITY ? 0.f : ex2((pm[k] - mn) * a.scale);
-        sum = fmaf(f0, sum, f1 * ps[k]);
+      for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+      const float f0 = m == -INFINITY ? 0.f : ex2((m - top) * a.scale), f = pm == -INFINITY ? 0.f : ex2((pm - top) * a.scale);
+      float add = f * ps;  // (NaN where a part has seen nothing but NaN)
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = fmaf(f0, v[i], f1 * pv[k][i]);
-        m = mn;
+      for (int d = 16; d; d >>= 1) add += __shfl_xor_sync(0xffffffffu, add, d);
+      sum = fmaf(f0, sum, add);
+      m = top;
+#pragma unroll
+      for (int i = 0; i < V; ++i) v[i] *= f0;
+      for (int k = 0; k < n; k += 8) {  // eight parts' loads are on their way together: L2's latency, not its rate, is what a row would wait for
+        float x[8][V];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          const int at = k0 + min(k + u, n - 1);
+          const float* q = partial_of<L, D>(a, at, at == run) + row * D + lane * V;
+#pragma unroll
+          for (int i = 0; i < V; i += 2) {
+            const float2 y = *reinterpret_cast<const float2*>(q + i);
+            x[u][i] = y.x;
+            x[u][i + 1] = y.y;
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          const float w = __shfl_sync(0xffffffffu, f, min(k + u, n - 1));
+#pragma unroll
+          for (int i = 0; i < V; ++i) v[i] = fmaf(k + u < n ? w : 0.f, x[u][i], v[i]);
+        }
       }
     }
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
