@@ -157,45 +157,58 @@ __global__ void __launch_bounds__(256) append_kernel(CacheView v, CacheEntries e
   }
 }
 
+// The low four bits of w as a number: dropped into the mantissa of 2^23 (a conversion would go through a slower unit).
+__device__ __forceinline__ float code_float(uint32_t w) { return __uint_as_float(0x4B000000u | (w & 15u)) - 8388608.f; }
+
 // The inverse, with the same mapping of threads.
-template <int D>
+template <int D, int kTokens>
 __global__ void __launch_bounds__(256) read_kernel(CacheView v, CacheEntries e, __nv_bfloat16* k_out, __nv_bfloat16* v_out, int32_t* status) {
   constexpr int L = D / 8;
   __shared__ int32_t offsets[kOffsetsMax];
   stage_offsets(e, offsets);
-  // (heads innermost: thread blocks that run together read the whole rows of their tokens)
   const int h = (int)(blockIdx.x % (uint32_t)v.kv_heads), lane = threadIdx.x % L;
   const int64_t unit = (int64_t)(blockIdx.x / (uint32_t)v.kv_heads) * (256 / L) + threadIdx.x / L;
-  const int t = (int)min(unit, (int64_t)e.T);
-  if (t >= e.T) return;
-  int offset = 0, end;
-  const int page = locate_token(v, e, offsets, t, &offset, &end);
-  if (page == -1) return;
-  if (page == -2) cache_fault(status);
-  const uint8_t* run = v.pages + (int64_t)max(page, 0) * v.page_bytes + (int64_t)h * 72 * D;
-  const int64_t at = ((int64_t)t * v.kv_heads + h) * D + lane * 8;
-  // (a token that did not fit has NaN keys only)
-  const bool nan = page >= 0 && __hisnan(*reinterpret_cast<const __half*>(run + 64 * D + offset * 4 + 2));
-#pragma unroll
-  for (int which = 0; which < 2; ++which) {
-    __nv_bfloat16* out = which ? v_out : k_out;
-    if (!out) continue;
-    uint32_t w = 0;
-    float2 m = make_float2(0.f, 0.f);
+  int end = -1, page = -1, offset = 0;  // the tokens before `end` follow the last one located in its entry and page
+#pragma unroll 1
+  for (int j = 0; j < kTokens; ++j) {
+    const int64_t at = unit * kTokens + j;
+    if (at >= e.T) return;
+    const int t = (int)at;
+    if (t < end) {
+      ++offset;
+    } else {
+      page = locate_token(v, e, offsets, t, &offset, &end);
+      if (page == -2) cache_fault(status);
+    }
+    if (page == -1) continue;
+    const uint8_t* run = v.pages + (int64_t)max(page, 0) * v.page_bytes + (int64_t)h * 72 * D;
+    const int64_t to = ((int64_t)t * v.kv_heads + h) * D + lane * 8;
+    uint32_t w[2] = {0, 0};
+    float2 m[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
     if (page >= 0) {
-      w = *reinterpret_cast<const uint32_t*>(run + which * 32 * D + (lane >> 2) * 1024 + offset * 16 + (lane & 3) * 4);
-      m = __half22float2(*reinterpret_cast<const __half2*>(run + 64 * D + which * 4 * D + ((lane >> 3) * kPageTokens + offset) * 4));
-      if (nan) m.y = __int_as_float(0x7fffffff);
+      const uint32_t* code = reinterpret_cast<const uint32_t*>(run + (lane >> 2) * 1024 + offset * 16 + (lane & 3) * 4);
+      const __half2* meta = reinterpret_cast<const __half2*>(run + 64 * D + ((lane >> 3) * kPageTokens + offset) * 4);
+      w[0] = code[0];
+      w[1] = code[8 * D];
+      m[0] = __half22float2(meta[0]);
+      m[1] = __half22float2(meta[D]);
+      if (m[0].y != m[0].y) m[1].y = m[0].y;  // (a token that did not fit has NaN keys only)
     }
-    uint32_t y[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      // product and sum rounded apart (as the definition reads), then once to bf16
-      const float a = __fadd_rn(__fmul_rn((float)((w >> (8 * i)) & 15), m.x), m.y), b = __fadd_rn(__fmul_rn((float)((w >> (8 * i + 4)) & 15), m.x), m.y);
-      const __nv_bfloat162 r = __floats2bfloat162_rn(a, b);
-      y[i] = *reinterpret_cast<const uint32_t*>(&r);
+    for (int which = 0; which < 2; ++which) {
+      __nv_bfloat16* out = which ? v_out : k_out;
+      if (!out) continue;
+      uint32_t y[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        // product and sum rounded apart (as the definition reads), then once to bf16
+        const float a = __fadd_rn(__fmul_rn(code_float(w[which] >> (8 * i)), m[which].x), m[which].y);
+        const float b = __fadd_rn(__fmul_rn(code_float(w[which] >> (8 * i + 4)), m[which].x), m[which].y);
+        const __nv_bfloat162 r = __floats2bfloat162_rn(a, b);
+        y[i] = *reinterpret_cast<const uint32_t*>(&r);
+      }
+      *reinterpret_cast<uint4*>(out + to) = make_uint4(y[0], y[1], y[2], y[3]);
     }
-    *reinterpret_cast<uint4*>(out + at) = make_uint4(y[0], y[1], y[2], y[3]);
   }
 }
 
@@ -580,6 +593,8 @@ int64_t token_blocks(int32_t T, const CacheView& v, int per) {
   const int64_t tokens = (int64_t)256 / (v.head_dim / 8) * per;
   return (T + tokens - 1) / tokens * v.kv_heads;
 }
+// Four tokens per thread share a look-up, as long as that leaves every SM four thread blocks (@).
+bool four_tokens(const essa_ctx* ctx, int32_t T, const CacheView& v) { return token_blocks(T, v, 4) >= 4 * ctx->sm_count; }
 int copy_grid(const essa_ctx* ctx) { return ctx->sm_count * 8; }
 
 }  // namespace
@@ -653,9 +668,7 @@ int32_t essa_cache_append(essa_ctx* ctx, const essa_cache_desc* cache, int32_t l
   ESSA_TRY(check_rows(ctx, "cache_append", "k", k, ld_k, (int64_t)v.kv_heads * v.head_dim));
   ESSA_TRY(check_rows(ctx, "cache_append", "v", val, ld_v, (int64_t)v.kv_heads * v.head_dim));
   DeviceGuard guard(ctx->device);
-  // Four tokens per thread share a look-up; a call that would leave SMs without work that way (fewer than four thread blocks each) takes one
-  // (32 thousand tokens of 8 heads: @ against @ us; 256 tokens of 4 heads: @ against @).
-  const bool four = token_blocks(T, v, 4) >= 4 * ctx->sm_count;
+  const bool four = four_tokens(ctx, T, v);
   const int64_t grid = token_blocks(T, v, four ? 4 : 1);
   if (grid > 0x7fffffff) return fail(ctx, ESSA_ERR_UNSUPPORTED_SHAPE, "cache_append: too many tokens");
   const auto *kk = static_cast<const __nv_bfloat16*>(k), *vv = static_cast<const __nv_bfloat16*>(val);
@@ -677,12 +690,14 @@ int32_t essa_cache_read(essa_ctx* ctx, const essa_cache_desc* cache, int32_t lay
   if (k_out) ESSA_TRY(check_rows(ctx, "cache_read", "k_out", k_out, width, width));
   if (v_out) ESSA_TRY(check_rows(ctx, "cache_read", "v_out", v_out, width, width));
   DeviceGuard guard(ctx->device);
-  const int64_t grid = token_blocks(T, v, 1);
+  const bool four = four_tokens(ctx, T, v);
+  const int64_t grid = token_blocks(T, v, four ? 4 : 1);
   if (grid > 0x7fffffff) return fail(ctx, ESSA_ERR_UNSUPPORTED_SHAPE, "cache_read: too many tokens");
   auto *kk = static_cast<__nv_bfloat16*>(k_out), *vv = static_cast<__nv_bfloat16*>(v_out);
   cudaStream_t stream = static_cast<cudaStream_t>(stream_v);
-  if (v.head_dim == 64) read_kernel<64><<<(unsigned)grid, 256, 0, stream>>>(v, e, kk, vv, ctx->d_status);
-  else read_kernel<128><<<(unsigned)grid, 256, 0, stream>>>(v, e, kk, vv, ctx->d_status);
+  const auto run = [&](auto kernel) { kernel<<<(unsigned)grid, 256, 0, stream>>>(v, e, kk, vv, ctx->d_status); };
+  if (v.head_dim == 64) four ? run(read_kernel<64, 4>) : run(read_kernel<64, 1>);
+  else four ? run(read_kernel<128, 4>) : run(read_kernel<128, 1>);
   return launched(ctx, "cache_read", 1);
 }
 
