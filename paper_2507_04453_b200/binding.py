@@ -413,7 +413,7 @@ class KvCache:
         self._sms = torch.cuda.get_device_properties(self.device).multi_processor_count
         self._attend_ws = {}  # (q_heads, max_new) -> bytes
         self._ws = {}         # cudaStream_t -> workspace
-        self._lib, self._h, self._ref, self._index = ctx.lib, ctx.handle, C.byref(self.desc), self.device.index
+        self._lib, self._ref, self._index = ctx.lib, C.byref(self.desc), self.device.index
         self._int32, self._bf16, self._scale = torch.int32, torch.bfloat16, head_dim ** -0.5
         self._current_stream = torch._C._cuda_getCurrentRawStream
         if fresh:
@@ -486,31 +486,31 @@ class KvCache:
     # -- pages
     def reset(self, stream=None):
         """essa_cache_reset: all sequences empty, all pages free."""
-        self._check(self._lib.essa_cache_reset(self._h, self._ref, self._raw(stream)))
+        self._check(self._lib.essa_cache_reset(self.ctx.handle, self._ref, self._raw(stream)))
 
     def grow(self, slots, counts, stream=None):
         """essa_cache_grow: sequence slots[i] (None: i) becomes counts[i] tokens longer."""
         n = counts.shape[0]
         a, b, raw = self._ints("slots", slots, n), self._ints("counts", counts), self._raw(stream)
         ws = self._workspace(self._pages_ws, raw, stream)
-        self._check(self._lib.essa_cache_grow(self._h, self._ref, a, b, n, ws.data_ptr(), ws.shape[0], raw))
+        self._check(self._lib.essa_cache_grow(self.ctx.handle, self._ref, a, b, n, ws.data_ptr(), ws.shape[0], raw))
 
     def fork(self, src, dst, lens=None, stream=None):
         """essa_cache_fork: sequence dst[i] becomes a copy of the first lens[i] (None: all) tokens of src[i]."""
         n = src.shape[0]
         a, b, c, raw = self._ints("src", src), self._ints("dst", dst, n), self._ints("lens", lens, n), self._raw(stream)
         ws = self._workspace(self._pages_ws, raw, stream)
-        self._check(self._lib.essa_cache_fork(self._h, self._ref, a, b, c, n, ws.data_ptr(), ws.shape[0], raw))
+        self._check(self._lib.essa_cache_fork(self.ctx.handle, self._ref, a, b, c, n, ws.data_ptr(), ws.shape[0], raw))
 
     def free(self, slots, stream=None):
         """essa_cache_free: the sequences become empty."""
-        self._check(self._lib.essa_cache_free(self._h, self._ref, self._ints("slots", slots), slots.shape[0], self._raw(stream)))
+        self._check(self._lib.essa_cache_free(self.ctx.handle, self._ref, self._ints("slots", slots), slots.shape[0], self._raw(stream)))
 
     def compact(self, used=None, stream=None):
         """essa_cache_compact: the pages in use become 0 .. U - 1; used (int32, one element) receives U."""
         u, raw = self._ints("used", used, 1), self._raw(stream)
         ws = self._workspace(self._pages_ws, raw, stream)
-        self._check(self._lib.essa_cache_compact(self._h, self._ref, u, ws.data_ptr(), ws.shape[0], raw))
+        self._check(self._lib.essa_cache_compact(self.ctx.handle, self._ref, u, ws.data_ptr(), ws.shape[0], raw))
 
     # -- tokens
     def append(self, layer: int, k, v, tok_offsets=None, slots=None, stream=None):
@@ -521,7 +521,7 @@ class KvCache:
         pk, ldk = self._rows("k", k, self.kv_heads)
         pv, ldv = self._rows("v", v, self.kv_heads)
         a, b, n = self._entries(T, slots, tok_offsets)
-        self._check(self._lib.essa_cache_append(self._h, self._ref, layer, pk, ldk, pv, ldv, T, a, b, n, self._raw(stream)))
+        self._check(self._lib.essa_cache_append(self.ctx.handle, self._ref, layer, pk, ldk, pv, ldv, T, a, b, n, self._raw(stream)))
 
     def read(self, layer: int, tok_offsets, T: int, slots=None, k_out=None, v_out=None, stream=None):
         """essa_cache_read: (k, v) [T, kv_heads, head_dim] bf16, the last tokens of the entries' sequences as they are stored."""
@@ -532,7 +532,7 @@ class KvCache:
         pk, pv = self._rows("k_out", k_out, self.kv_heads)[0], self._rows("v_out", v_out, self.kv_heads)[0]
         if k_out.shape[0] != T or v_out.shape[0] != T or not (k_out.is_contiguous() and v_out.is_contiguous()):
             self._fail("k_out and v_out", f"contiguous tensors of {T} rows")
-        self._check(self._lib.essa_cache_read(self._h, self._ref, layer, pk, pv, T, a, b, n, self._raw(stream)))
+        self._check(self._lib.essa_cache_read(self.ctx.handle, self._ref, layer, pk, pv, T, a, b, n, self._raw(stream)))
         return k_out, v_out
 
     def attend(self, layer: int, q, tok_offsets=None, slots=None, max_new: int = 1, scale=None, out=None, stream=None):
@@ -556,7 +556,7 @@ class KvCache:
         po, ldo = self._rows("out", out, heads)
         raw = self._raw(stream)
         ws = self._workspace(need, raw, stream)
-        self._check(self._lib.essa_cache_attend(self._h, self._ref, layer, pq, ldq, heads, shape[0], a, b, n, max_new, self._scale if scale is None else scale,
+        self._check(self._lib.essa_cache_attend(self.ctx.handle, self._ref, layer, pq, ldq, heads, shape[0], a, b, n, max_new, self._scale if scale is None else scale,
                                                 po, ldo, ws.data_ptr(), ws.shape[0], raw))
         return out
 

@@ -29,7 +29,7 @@ constexpr int kThreads = kWarps * 32 + 32;    // + one copying warp
 // Row blocks of R rows; every row block of an entry walks all its pages (the few rows of an entry see nearly the same ones).
 template <int ROWS>
 struct DecodeList {
-  static constexpr int R = ROWS, kMinRun = 2, kSetup = 2;
+  static constexpr int R = ROWS, kMinRun = 2, kSetup = 5;
   __device__ static int tiles(const EntryInfo& e, const AttendArgs&, int) { return max((e.len + kPageTokens - 1) / kPageTokens, 1); }
   __device__ static long long per_head(const EntryInfo& e, const AttendArgs& a) { return (long long)row_blocks(e, a.group, R) * (tiles(e, a, 0) + kSetup); }
 };
@@ -77,8 +77,9 @@ struct Shape {
   static constexpr int R = 8 * NT;             // query rows of a row block
   static constexpr int kBytes = 72 * D;        // a (page, kv head) run
   static constexpr int kStages = (D == 128 ? 6 : 10);
-  static constexpr int kPart = Partial<DecodeList<R>, D>::kFloats;
-  static constexpr int kJoin = kWarps * R * (D + 2) * 4;
+  static constexpr int kCol = D + 4;           // floats of a column's O in the join (padded: the lanes of a store have columns of their own)
+  static constexpr int kWarpJoin = R * (kCol + 2);
+  static constexpr int kJoin = kWarps * kWarpJoin * 4;
   static_assert(kStages % 2 == 0, "");
   static constexpr int kSmem = kStages * kBytes + kJoin + 256;
 };
@@ -439,7 +440,7 @@ __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_
     mine_at = (mine_at + stop - first) & 1;  // (the pairs take turns over the whole run)
 
     // --- join the four warps: each leaves O, maximum and sum of its tokens in shared memory
-    float* mine = join + warp * S::kPart;
+    float* mine = join + warp * S::kWarpJoin;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -458,10 +459,10 @@ __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_
 #pragma unroll
         for (int h = 0; h < CH; ++h) {
           const auto value = [&](float v) { return fmaf(v, 1.f / per_unit[h / 2], add[h / 2]); };
-          *reinterpret_cast<float4*>(mine + col * D + 32 * h + 4 * g) =
+          *reinterpret_cast<float4*>(mine + col * S::kCol + 32 * h + 4 * g) =
               make_float4(value(o[nt][h][0][x]), value(o[nt][h][0][2 + x]), value(o[nt][h][1][x]), value(o[nt][h][1][2 + x]));
         }
-        if (g == 0) { mine[R * D + col] = mx[nt][x] * back[nt][x]; mine[R * D + R + col] = sum; }
+        if (g == 0) { mine[R * S::kCol + col] = mx[nt][x] * back[nt][x]; mine[R * S::kCol + R + col] = sum; }
       }
     epi_bar_sync();
     const bool whole = first == 0 && stop == c.tiles;
@@ -470,14 +471,14 @@ __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_
       const int col = x / (D / 4), d4 = (x % (D / 4)) * 4, r = r0 + col;
       float m = -INFINITY, sum = 0.f;
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) m = fmaxf(m, join[w * S::kPart + R * D + col]);
+      for (int w = 0; w < kWarps; ++w) m = fmaxf(m, join[w * S::kWarpJoin + R * S::kCol + col]);
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (int w = 0; w < kWarps; ++w) {
-        const float* p = join + w * S::kPart;
-        const float pm = p[R * D + col], f = pm == -INFINITY ? 0.f : ex2((pm - m) * a.scale);
-        const float4 y = *reinterpret_cast<const float4*>(p + col * D + d4);
-        sum = fmaf(f, p[R * D + R + col], sum);
+        const float* p = join + w * S::kWarpJoin;
+        const float pm = p[R * S::kCol + col], f = pm == -INFINITY ? 0.f : ex2((pm - m) * a.scale);
+        const float4 y = *reinterpret_cast<const float4*>(p + col * S::kCol + d4);
+        sum = fmaf(f, p[R * S::kCol + R + col], sum);
         v.x = fmaf(f, y.x, v.x); v.y = fmaf(f, y.y, v.y); v.z = fmaf(f, y.z, v.z); v.w = fmaf(f, y.w, v.w);
       }
       if (!whole) {
