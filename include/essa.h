@@ -436,7 +436,8 @@ int32_t essa_cache_reset(essa_ctx* ctx, const essa_cache_desc* cache, void* stre
 int32_t essa_cache_grow(essa_ctx* ctx, const essa_cache_desc* cache, const int32_t* slots, const int32_t* counts, int32_t n, void* workspace,
                         int64_t workspace_bytes, void* stream);
 /* Store k and v ([T] rows of kv_heads * head_dim bf16, ld_k / ld_v elements apart: multiples of 8; 16-byte aligned) of the
- * entries' tokens in layer `layer`.  Tokens on a page that another sequence shares are skipped (ESSA_ERR_CACHE). */
+ * entries' tokens in layer `layer`.  Tokens on a page that another sequence shares are skipped (ESSA_ERR_CACHE).  The entries'
+ * sequences are distinct (if one is named twice, which of the rows are stored is not defined). */
 int32_t essa_cache_append(essa_ctx* ctx, const essa_cache_desc* cache, int32_t layer, const void* k, int64_t ld_k, const void* v, int64_t ld_v, int32_t T,
                           const int32_t* slots, const int32_t* tok_offsets, int32_t n, void* stream);
 /* The inverse: the entries' tokens of layer `layer` as dense bf16 [T][kv_heads][head_dim] (k_out, v_out; either may be
@@ -447,7 +448,7 @@ int32_t essa_cache_read(essa_ctx* ctx, const essa_cache_desc* cache, int32_t lay
  *   out[r][h] = sum_s p_s v_s,  p = softmax over s <= pos of scale * (q[r][h] . k_s),  kv head h / (q_heads / kv_heads),
  * over the tokens 0 .. pos of the row's sequence (its own included: append comes first).  A row that sees no token is 0.
  *   q, out [T] rows of q_heads * head_dim bf16, ld_q / ld_out elements apart (multiples of 8; 16-byte aligned); q_heads a
- *   multiple of kv_heads; scale > 0, finite.
+ *   multiple of kv_heads; 0 < scale <= 2^127.  out does not overlap q.  A sequence may be named by several entries.
  *   max_new >= 1: the most rows an entry is expected to have.  It only chooses the schedule (1 for decode steps); any value
  *   gives right results.
  * Scores, maximum, sums and the accumulators are fp32; out is rounded to bf16 once; operands of the products are fp16, each rounded

@@ -1,6 +1,4 @@
 // Paged 4-bit key / value cache: storing and reading tokens, page management, and the C entry points of include/essa.h.
-#include <cmath>
-
 #include "cache_list.cuh"
 
 namespace essa {
@@ -106,8 +104,9 @@ __device__ __forceinline__ Packed pack_group(const Piece& x) {
 }
 
 // D / 8 neighbouring lanes take a token of a kv head, eight channels of K and of V each, kTokens tokens in turn; a thread block has
-// consecutive tokens of a head, so that the 16-byte pieces of neighbouring tokens (adjacent in a page) meet in one sector.  Bound by
-// HBM: 4 * D bytes in and 1.125 * D out per (token, kv head).
+// consecutive tokens of a head, so that the 16-byte pieces of neighbouring tokens (adjacent in a page) meet in one sector.  Bytes: 4 * D in
+// and 1.125 * D out per (token, kv head).  32 thousand tokens of 8 heads of 128: 64 us, 2.7 TB/s; what it waits for is issue slots (some 20
+// instructions a value between conversion, comparison and packing).
 template <int D, int kTokens>
 __global__ void __launch_bounds__(256) append_kernel(CacheView v, CacheEntries e, const __nv_bfloat16* k, int64_t ld_k, const __nv_bfloat16* val, int64_t ld_v,
                                                      int32_t* status) {
@@ -160,7 +159,7 @@ __global__ void __launch_bounds__(256) append_kernel(CacheView v, CacheEntries e
 // The low four bits of w as a number: dropped into the mantissa of 2^23 (a conversion would go through a slower unit).
 __device__ __forceinline__ float code_float(uint32_t w) { return __uint_as_float(0x4B000000u | (w & 15u)) - 8388608.f; }
 
-// The inverse, with the same mapping of threads.
+// The inverse, with the same mapping of threads: 1.125 * D bytes in and 4 * D out.  32 thousand tokens of 8 heads of 128: 36 us, 4.8 TB/s.
 template <int D, int kTokens>
 __global__ void __launch_bounds__(256) read_kernel(CacheView v, CacheEntries e, __nv_bfloat16* k_out, __nv_bfloat16* v_out, int32_t* status) {
   constexpr int L = D / 8;
@@ -309,10 +308,21 @@ __global__ void __launch_bounds__(kPlanThreads) grow_kernel(CacheView v, const i
     }
     const long long at = before + block_scan(need, &total, scan_sm);
     before += total;
-    for (int j = 0; j < need; ++j) {
-      const int page = ws.from[at + j];
-      v.table[(int64_t)slot * v.max_pages + pages_of(len) + j] = page;
+    // A few pages each (decode steps): every thread writes its entry's.  Many (long prompts): the warp writes them, an entry after the
+    // other, 32 pages at a time; a thread alone would wait for memory once a page (one sequence of 100 thousand tokens: 64 us, so 14).
+    const auto give = [&](int to, int first, int64_t from, int j) {
+      const int page = ws.from[from + j];
+      v.table[(int64_t)to * v.max_pages + first + j] = page;
       v.refs[page] = 1;
+    };
+    if (__reduce_max_sync(0xffffffffu, (int)need) <= __reduce_add_sync(0xffffffffu, (int)(need + 31) / 32)) {
+      for (int j = 0; j < need; ++j) give(slot, pages_of(len), at, j);
+    } else {
+      for (int u = 0; u < 32; ++u) {
+        const int pages = __shfl_sync(0xffffffffu, (int)need, u), to = __shfl_sync(0xffffffffu, slot, u), first = __shfl_sync(0xffffffffu, pages_of(len), u);
+        const long long from = __shfl_sync(0xffffffffu, at, u);
+        for (int j = threadIdx.x & 31; j < pages; j += 32) give(to, first, from, j);
+      }
     }
     if (i < n) v.lengths[slot] = len + add;
   }
@@ -414,7 +424,8 @@ __global__ void __launch_bounds__(kPlanThreads) fork_plan_kernel(CacheView v, co
   }
 }
 
-// Page copies from[i] -> to[i], i < copies, in every layer: units of 256 threads x 4 x 16 bytes over the whole grid.
+// Page copies from[i] -> to[i], i < copies, in every layer: units of 256 threads x 4 x 16 bytes over the whole grid.  Bound by HBM: 900
+// pages of 288 KB (2 x 265 MB) take 80 us, 6.6 TB/s.
 __device__ __forceinline__ void copy_pages(const CacheView& v, const PlanSpace& ws, int copies) {
   constexpr int kPer = 4;
   const int per_page = (int)(v.page_bytes / 16);  // 16-byte words (a multiple of 288)
@@ -584,8 +595,9 @@ int32_t launched(essa_ctx* ctx, const char* what, int kernels) {
   ctx->launches += kernels;
   return check_cuda(ctx, cudaGetLastError(), what);
 }
-// Which attention kernel: up to 16 query rows per (entry, kv head) fit the one that widens codes straight into mma operands; from there on
-// the 256-row tiles of tcgen05 re-use a widened page often enough.
+// Which attention kernel: up to 16 query rows per (entry, kv head) take the one that widens codes straight into mma operands; with more the
+// 256-row tiles of tcgen05 re-use a widened page often enough.  Few rows / tiles, us, heads of 128 channels: 32 sequences of 4096 tokens, 8 kv
+// heads: 8 rows 47 / 133, 16 rows 79 / 134, 24 rows 137 / 134, 64 rows 256 / 138; one of 30000 tokens: 16 rows 29 / 41, 24 rows 42 / 41.
 bool few_rows(int64_t rows) { return rows <= 16; }
 size_t seen_bytes(const CacheView& v) { return (size_t)(v.max_seqs + 31) / 32 * 4; }
 // Thread blocks of append and read: 256 / (head_dim / 8) times `per` tokens of one head each.
@@ -593,7 +605,8 @@ int64_t token_blocks(int32_t T, const CacheView& v, int per) {
   const int64_t tokens = (int64_t)256 / (v.head_dim / 8) * per;
   return (T + tokens - 1) / tokens * v.kv_heads;
 }
-// Four tokens per thread share a look-up, as long as that leaves every SM four thread blocks (@).
+// Four tokens per thread share a look-up, as long as that leaves every SM four thread blocks.  32 thousand tokens of 8 heads, stored and read
+// back: 124 us, with one token per thread 159; 256 tokens (too few for the rule): 45 us with either.
 bool four_tokens(const essa_ctx* ctx, int32_t T, const CacheView& v) { return token_blocks(T, v, 4) >= 4 * ctx->sm_count; }
 int copy_grid(const essa_ctx* ctx) { return ctx->sm_count * 8; }
 
@@ -710,7 +723,7 @@ int32_t essa_cache_attend(essa_ctx* ctx, const essa_cache_desc* cache, int32_t l
   ESSA_TRY(check_entries(ctx, "cache_attend", e));
   if (q_heads < 1 || q_heads % v.kv_heads) return fail(ctx, ESSA_ERR_INVALID_ARG, "cache_attend: q_heads must be a multiple of kv_heads");
   if (max_new < 1) return fail(ctx, ESSA_ERR_INVALID_ARG, "cache_attend: max_new must be at least 1");
-  if (!(scale > 0.f) || !std::isfinite(scale)) return fail(ctx, ESSA_ERR_INVALID_ARG, "cache_attend: scale must be positive and finite");
+  if (!(scale > 0.f && scale <= 0x1p127f)) return fail(ctx, ESSA_ERR_INVALID_ARG, "cache_attend: scale must be positive and at most 2^127");
   const int64_t group = q_heads / v.kv_heads;
   if (group * T > 0x7fffffff) return fail(ctx, ESSA_ERR_UNSUPPORTED_SHAPE, "cache_attend: T * (q_heads / kv_heads) must be below 2^31");
   if (T == 0 || n == 0) return ESSA_OK;

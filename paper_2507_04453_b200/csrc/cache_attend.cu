@@ -17,6 +17,8 @@
 // group of up to eight heads fills the tensor core's tile, where q as the M operand would leave half of it empty.
 //
 // Work split: cache_list.cuh, with row blocks of 8 or 16 query rows and key tiles of one page.
+#include <cfloat>
+
 #include "cache_list.cuh"
 
 namespace essa {
@@ -215,7 +217,7 @@ __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         back[nt][x] = __shfl_sync(0xffffffffu, down, 8 * t + 4 * x);
-        sc[nt][x] = a.scale * back[nt][x];
+        sc[nt][x] = fmaxf(a.scale * back[nt][x], FLT_MIN);  // (hidden scores are -infinity, and 0 times that is NaN)
         const int rc = r0 + nt * 8 + 2 * t + x;  // tokens that column 2 t + x sees; a column without a row sees all and is not written
         limit[nt][x] = rc < rows ? c.info.len - c.info.rows + a.by_group(rc) + 1 : 0x7fffffff;
         lowest = min(lowest, limit[nt][x]);

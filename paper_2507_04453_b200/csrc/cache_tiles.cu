@@ -16,6 +16,8 @@
 // the result alone.  S, the running maximum, the sums and O are fp32.
 // Channel order inside a group of eight channels is (0, 4, 1, 5, 2, 6, 3, 7), what masking nibbles out of a word gives: Q is stored in
 // the same order, and O's columns are put back on the way out.
+#include <cfloat>
+
 #include "cache_list.cuh"
 
 namespace essa {
@@ -321,7 +323,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
       }
       if (!more) break;
       b = next;
-      const float scale = a.scale * b.back;
+      const float scale = fmaxf(a.scale * b.back, FLT_MIN);  // (hidden scores are -infinity, and 0 times that is NaN)
       m = -INFINITY;
       sum = 0.f;
       const auto scores_at = [&](int t) { return tmem + 128 * h + 64 * (t & 1) + lanes; };

@@ -488,3 +488,209 @@ def test_host_side_refusals(torch, ctx):
     g.fork(ints([]), ints([]))
     g.free(ints([]))
     assert ctx.get_status() == 0
+
+
+# ------------------------------------------------------------------------------------------------ sizes, extremes, ways of calling
+def check_rows(p, got, q, slot, scale, extra=0.0, length=None):
+    """Rows `got` for the queries `q` of the last tokens of a sequence against the model; `extra` is added to the bound."""
+    k, v, codes, sc = p.cpu.sequence(0, slot)
+    want, w = co.attend(q, k, v, int(p.cpu.lengths[slot]), scale)
+    with np.errstate(over="ignore"):  # (a bound may be infinite where scores are large)
+        tol = attend_bound(q, v, codes, sc, want, w, scale, k) + extra
+    err = np.abs(got - want)
+    assert np.isfinite(got).all() and (err <= tol).all(), (slot, float(np.max(err / tol)))
+
+
+def test_one_sequence_grows_by_many_pages_beside_short_ones(torch, ctx):
+    """A prompt of thousands of pages in the same call as sequences that get one, none, or two."""
+    p = Pair(torch, ctx, 1, 3000, 1, 64, 70, 2100)
+    counts = np.random.default_rng(1).integers(0, 130, 70)
+    counts[[3, 40]] = 64 * 2000 + 5, 64 * 600
+    for _ in range(2):
+        p.gpu.grow(None, p.ints(counts))
+        p.cpu.grow(range(70), counts)
+        assert ctx.get_status() == 0
+        p.assert_same(pages=False)
+        counts = np.minimum(counts, 70)
+
+
+def test_more_entries_than_a_thread_block_has_offsets_for(torch, ctx):
+    rng = np.random.default_rng(14)
+    n = 2600
+    p = Pair(torch, ctx, 1, 4000, 1, 64, n, 3)
+    p.place(rng.integers(0, 100, n), rng)
+    rows = np.minimum(rng.integers(0, 4, n), p.cpu.lengths)
+    slots = rng.permutation(n)
+    off = np.concatenate([[0], np.cumsum(rows[slots])])
+    T = int(off[-1])
+    k, v = (bf16(rng, (T, 1, 64)) for _ in range(2))
+    p.gpu.append(0, p.bf(k), p.bf(v), p.ints(off), slots=p.ints(slots))
+    p.cpu.append(0, k, v, off, slots)
+    p.assert_same()
+    ko, vo = p.gpu.read(0, p.ints(off), T, slots=p.ints(slots))
+    for got, x in ((ko, k), (vo, v)):
+        want = co.dequantize(*co.quantize(x))
+        np.testing.assert_array_equal(got.float().cpu().numpy(), wl.round_to_bf16(want.astype(np.float32)))
+    q = bf16(rng, (T, 3, 64))
+    for hint in (1, 100):
+        got = p.gpu.attend(0, p.bf(q), p.ints(off), slots=p.ints(slots), max_new=hint).float().cpu().numpy()
+        for i in rng.permutation(n)[:200]:
+            if rows[slots[i]]:
+                check_rows(p, got[off[i]:off[i + 1]], q[off[i]:off[i + 1]], slots[i], 64 ** -0.5)
+    assert ctx.get_status() == 0
+
+
+@pytest.mark.parametrize("hint", [1, 100])
+@pytest.mark.parametrize("d", [64, 128])
+def test_queries_of_very_different_size(torch, ctx, hint, d):
+    """Rows between 2^-110 and 2^6 side by side, rows of zeros, rows whose channels lie far apart, and a scale that takes them below fp32's range."""
+    rng = np.random.default_rng(15)
+    p = Pair(torch, ctx, 1, 30, 2, d, 3, 6)
+    p.place([300, 64, 7], rng)
+    rows = [40, 30, 7]
+    off = np.concatenate([[0], np.cumsum(rows)])
+    T = int(off[-1])
+    q = bf16(rng, (T, 6, d))
+    q *= np.float32(2.0) ** rng.integers(-110, 7, (T, 6, 1)).astype(np.float32)
+    q[::7] = 0
+    q[1::7, :, ::2] *= np.float32(2.0 ** -20)
+    for scale in (d ** -0.5, 1e-12, 1e-38):
+        got = p.gpu.attend(0, p.bf(q), p.ints(off), max_new=hint, scale=scale).float().cpu().numpy()
+        for i in range(3):
+            check_rows(p, got[off[i]:off[i + 1]], q[off[i]:off[i + 1]], i, scale)
+    assert ctx.get_status() == 0
+
+
+@pytest.mark.parametrize("hint", [1, 100])
+@pytest.mark.parametrize("size_k,size_v", [(1.0, 14000.0), (14000.0, 1.0), (1.0, 1e-6), (1.0, 0.0)])
+def test_keys_and_values_of_extreme_size(torch, ctx, hint, size_k, size_v):
+    """Up to fp16's end, and down to values that its subnormal numbers hold."""
+    rng = np.random.default_rng(16)
+    p = Pair(torch, ctx, 1, 30, 1, 128, 2, 6)
+    p.place([300, 65], rng)
+    for s in range(2):
+        n = int(p.cpu.lengths[s])
+        k, v = (np.clip(bf16(rng, (n, 1, 128)), -4, 4) * np.float32(size) for size in (size_k, size_v))
+        p.cpu.append(0, wl.round_to_bf16(k), wl.round_to_bf16(v), [0, n], [s])
+    p.push()
+    off, q = [0, 30, 60], bf16(rng, (60, 5, 128))
+    scale = 128 ** -0.5 / size_k
+    got = p.gpu.attend(0, p.bf(q), p.ints(off), max_new=hint, scale=scale).float().cpu().numpy()
+    assert ctx.get_status() == 0
+    # many rows: a value's offset and the value itself are rounded to fp16, below its normal range to 2^-25 absolutely each; weights sum to 1
+    for s in range(2):
+        check_rows(p, got[off[s]:off[s + 1]], q[off[s]:off[s + 1]], s, scale, extra=2.0 ** -24)
+
+
+@pytest.mark.parametrize("hint", [1, 100])
+def test_a_token_that_did_not_fit_reaches_only_the_rows_that_see_it(torch, ctx, hint):
+    rng = np.random.default_rng(17)
+    p = Pair(torch, ctx, 1, 8, 1, 64, 2, 4)
+    p.place([200, 60], rng)
+    k, v = bf16(rng, (40, 1, 64)), bf16(rng, (40, 1, 64))
+    v[25, 0, 3] = np.inf
+    k[33, 0, 60] = np.nan
+    p.gpu.append(0, p.bf(k), p.bf(v), p.ints([0, 40]), slots=p.ints([0]))
+    p.cpu.append(0, k, v, [0, 40], [0])
+    p.assert_same()
+    q = bf16(rng, (60, 4, 64))
+    got = p.gpu.attend(0, p.bf(q), p.ints([0, 40, 60]), max_new=hint).float().cpu().numpy()
+    assert ctx.get_status() == 0
+    assert np.isnan(got[25:40]).all()
+    p.cpu.lengths[0] = 160 + 25  # what the rows before it see
+    check_rows(p, got[:25], q[:25], 0, 64 ** -0.5)
+    check_rows(p, got[40:], q[40:], 1, 64 ** -0.5)
+
+
+@pytest.mark.parametrize("hint", [1, 100])
+def test_two_entries_on_one_sequence(torch, ctx, hint):
+    """attend and read may name a sequence as often as they like."""
+    rng = np.random.default_rng(18)
+    p = Pair(torch, ctx, 1, 8, 2, 64, 2, 4)
+    p.place([130, 60], rng)
+    q = bf16(rng, (5, 4, 64))
+    off, slots = p.ints([0, 2, 5]), p.ints([0, 0])
+    got = p.gpu.attend(0, p.bf(q), off, slots=slots, max_new=hint).float().cpu().numpy()
+    check_rows(p, got[:2], q[:2], 0, 64 ** -0.5)
+    check_rows(p, got[2:], q[2:], 0, 64 ** -0.5)
+    ko, _ = p.gpu.read(0, off, 5, slots=slots)
+    assert torch.equal(ko[:2], ko[3:]) and ctx.get_status() == 0
+
+
+def test_graphs_of_two_calls_replayed_beside_one_another(torch, ctx):
+    """Two captured calls of each kernel hold workspaces of their own: replays that overlap give what the calls alone give."""
+    rng = np.random.default_rng(19)
+    p = Pair(torch, ctx, 1, 200, 2, 128, 3, 180)
+    p.place([11000, 300, 64], rng)
+    for hint in (1, 100):
+        q = [p.bf(bf16(rng, (3, 8, 128))) for _ in range(2)]
+        want = [p.gpu.attend(0, x, max_new=hint) for x in q]
+        outs, graphs = [torch.empty_like(x) for x in q], [torch.cuda.CUDAGraph() for _ in q]
+        torch.cuda.synchronize()
+        for x, out, graph in zip(q, outs, graphs):
+            with torch.cuda.graph(graph):
+                p.gpu.attend(0, x, max_new=hint, out=out)
+        streams = [torch.cuda.Stream() for _ in q]
+        for _ in range(20):
+            for out in outs:
+                out.fill_(7.0)
+            torch.cuda.synchronize()
+            for _ in range(3):
+                for graph, s in zip(graphs, streams):
+                    with torch.cuda.stream(s):
+                        graph.replay()
+                eager = p.gpu.attend(0, q[0], max_new=hint)
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(outs, want)) and torch.equal(eager, want[0])
+    assert ctx.get_status() == 0
+
+
+def test_a_step_on_a_stream_of_its_own(torch, ctx):
+    """Every call with `stream`: nothing of it depends on the current stream, which is busy with other work."""
+    rng = np.random.default_rng(20)
+    p = Pair(torch, ctx, 1, 20, 2, 64, 4, 4)
+    p.place([62, 0, 127, 64], rng)
+    k, v = (bf16(rng, (4, 2, 64)) for _ in range(2))
+    q = bf16(rng, (2, 4, 64))
+    dk, dv, dq, one, src, dst, off = p.bf(k), p.bf(v), p.bf(q), p.ints([1] * 4), p.ints([0]), p.ints([1]), p.ints([0, 1])
+    pair = p.ints([0, 2])
+    busy = torch.zeros(64 << 20, device="cuda")
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    for _ in range(20):
+        busy += 1
+    p.gpu.grow(None, one, stream=s)
+    p.gpu.append(0, dk, dv, stream=s)
+    out = p.gpu.attend(0, dq, slots=pair, stream=s)
+    p.gpu.fork(src, dst, stream=s)
+    ko, vo = p.gpu.read(0, off, 1, slots=dst, stream=s)
+    p.gpu.compact(stream=s)
+    s.synchronize()
+    p.cpu.grow(range(4), [1] * 4)
+    p.cpu.append(0, k, v, [0, 1, 2, 3, 4], range(4))
+    for i, slot in enumerate((0, 2)):
+        check_rows(p, out[i:i + 1].float().cpu().numpy(), q[i:i + 1], slot, 64 ** -0.5)
+    p.cpu.fork([0], [1])
+    p.cpu.compact()
+    p.assert_same()
+    want = co.dequantize(*co.quantize(k[:1]))
+    np.testing.assert_array_equal(ko.float().cpu().numpy(), wl.round_to_bf16(want.astype(np.float32)))
+    assert ctx.get_status() == 0
+
+
+def test_scales_out_of_range_empty_offsets_and_a_closed_context_are_refused(torch):
+    c = binding.Context(0)
+    g = c.kv_cache(1, 4, 2, 64, 2, 2)
+    q = torch.zeros((1, 4, 64), dtype=torch.bfloat16, device="cuda")
+    none = torch.empty(0, dtype=torch.int32, device="cuda")
+    for call in (lambda: g.attend(0, q, scale=float("inf")), lambda: g.attend(0, q, scale=3e38), lambda: g.attend(0, q, scale=-1.0), lambda: g.attend(0, q, none),
+                 lambda: g.attend(0, q[0]), lambda: g.attend(0, q.expand(2, 4, 64))):
+        with pytest.raises((binding.EssaError, RuntimeError)):
+            call()
+    assert c.get_status() == 0
+    g.attend(0, q)
+    torch.cuda.synchronize()
+    c.close()
+    for call in (lambda: g.attend(0, q), lambda: g.reset(), lambda: g.append(0, q[:, :2], q[:, :2]), lambda: c.kv_cache(1, 4, 2, 64, 2, 2)):
+        with pytest.raises(binding.EssaError):
+            call()
