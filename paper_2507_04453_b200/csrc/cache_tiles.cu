@@ -24,7 +24,7 @@ namespace essa {
 namespace {
 
 struct TileList {
-  static constexpr int R = 256, kKeys = kPageTokens, kMinRun = 2, kSetup = 6;
+  static constexpr int R = 256, kKeys = kPageTokens, kMinRun = 2, kSetup = 4;
   // keys that the last row of the row block sees, in tiles
   __device__ static int tiles(const EntryInfo& e, const AttendArgs& a, int rb) {
     const int last = min(e.rows - 1, a.by_group(min(rb * R, 0x7fffffff - R) + R - 1));
@@ -38,11 +38,11 @@ struct TileList {
   }
 };
 
-constexpr int kSoftWarps = 8, kWidenWarps = 4;
+constexpr int kSoftWarps = 16, kWidenWarps = 4;
 constexpr int kMmaWarp = kSoftWarps + kWidenWarps, kCopyWarp = kMmaWarp + 1;
-constexpr int kThreads = 512;  // four warpgroups; the last two warps only give registers away
-// Registers per thread: launched with 128, of which the softmax takes more.  2 * 136 + 2 * 120 = 4 * 128.
-constexpr int kSoftRegs = 136, kOtherRegs = 120;
+constexpr int kThreads = 768;  // six warpgroups; the last two warps only give registers away
+// Registers per thread: launched with 80, of which the softmax takes more.  4 * 88 + 2 * 64 = 6 * 80.
+constexpr int kSoftRegs = 88, kOtherRegs = 64;
 constexpr int kRaw = 3;  // pages in flight
 
 constexpr int kRing = 4;  // key tiles of K and of V
@@ -110,6 +110,20 @@ __device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b) {
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
 }
+// 16 consecutive columns of the warp's lanes (with the wait).
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&v)[16]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr), "r"(v[0]), "r"(v[1]),
+               "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
+               : "memory");
+  asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+}
+// Barrier of two warps, and whether a predicate holds for any of their threads.
+__device__ __forceinline__ void pair_sync(int id) { asm volatile("bar.sync %0, 64;" ::"r"(id) : "memory"); }
+__device__ __forceinline__ bool pair_any(int id, bool x) {
+  uint32_t r;
+  asm volatile("{\n.reg .pred p, q;\nsetp.ne.u32 p, %2, 0;\nbar.red.or.pred q, %1, 64, p;\nselp.u32 %0, 1, 0, q;\n}\n" : "=r"(r) : "r"(id), "r"((uint32_t)x) : "memory");
+  return r != 0;
+}
 // One lane of the (converged) warp, the same one every time.
 __device__ __forceinline__ bool elect_one() {
   uint32_t p;
@@ -150,7 +164,15 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
   __shared__ int raw_bad[kRaw];
   __shared__ int tile_bad[8];  // the key tile's page is not there
   __shared__ uint32_t tmem_slot;
-  __shared__ float row_scale[L::R];  // what a row of Q was divided by
+  __shared__ float row_scale[L::R];           // what a row of Q was divided by
+  __shared__ float of_part[2][L::R];   // maximum, then sum, of the keys that a row's two threads look at
+  // Where the softmax and the widening warps are in the list, between row blocks (in registers it would cost their loops spills).
+  struct Place {
+    Cursor c;
+    long long left;
+  };
+  __shared__ Place places[kSoftWarps + kWidenWarps];
+  __shared__ int out_of[kSoftWarps][2][3];  // a softmax warp's present and next row block: first row of q, kv head, row of the group
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const uint32_t bars = base + M::kBars;
   const auto bar = [&](int i) { return bars + 8 * i; };
@@ -160,8 +182,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
     abort_flag = 0;
     for (int i = 0; i < kRaw; ++i) { mbar_init(bar(kRawFull + i), 1); mbar_init(bar(kRawEmpty + i), kWidenWarps); }
     for (int i = 0; i < kRing; ++i) { mbar_init(bar(kTileFull + i), kWidenWarps); mbar_init(bar(kTileEmpty + i), 1); }
-    for (int i = 0; i < 2; ++i) { mbar_init(bar(kQFull + i), 4); mbar_init(bar(kOFull + i), 1); }
-    for (int i = 0; i < 4; ++i) { mbar_init(bar(kSFull + i), 1); mbar_init(bar(kPFull + i), 4); }
+    for (int i = 0; i < 2; ++i) { mbar_init(bar(kQFull + i), kSoftWarps / 2); mbar_init(bar(kOFull + i), 1); }
+    for (int i = 0; i < 4; ++i) { mbar_init(bar(kSFull + i), 1); mbar_init(bar(kPFull + i), kSoftWarps / 2); }
     mbar_init(bar(kDone), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -177,54 +199,78 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = tmem_slot;
+  const auto keep_place = [&](const Cursor& at, long long rest) {
+    __syncwarp();
+    if (lane == 0) places[warp] = Place{at, rest};
+    __syncwarp();
+  };
+  if (warp < kSoftWarps + kWidenWarps) keep_place(c, left);
   const auto wait = [&](int b, uint32_t parity) { return mbar_wait(bar(b), parity, &abort_flag, a.status); };
   const auto wait_warp = [&](int b, uint32_t parity) { return __all_sync(0xffffffffu, wait(b, parity)) != 0; };
 
-  if (warp < kSoftWarps) {  // ------------------------------------------------------------------ softmax, a thread per row
+  if (warp < kSoftWarps) {  // ------------------------------------------------------------------ softmax, two threads per row
+    // (32 of a tile's 64 keys each, and half of O's channels; the two warps that share 32 rows keep in step by a barrier of their own)
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
-    const int h = warp >> 2, row = (warp & 3) * 32 + lane;
-    const uint32_t lanes = (uint32_t)(warp & 3) * 32u << 16;
-    const uint32_t o_at = tmem + 256 + D * h + lanes;
+    const int h = warp >> 3, part = warp >> 2 & 1, quad = warp & 3, row = quad * 32 + lane, pair = 1 + 4 * h + quad;
+    const uint32_t lanes = (uint32_t)quad * 32u << 16;
+    const uint32_t o_at = tmem + 256 + D * h + D / 2 * part + lanes;
     int tile = 0;  // key tiles of the run so far
     uint32_t s_ph = 0, o_ph = 0;  // s_ph: a bit per buffer
-    bool ok = true;
+    bool dead = false;  // a wait ran out: the warp goes on through the barriers with the other one, and waits for nothing else
+    const auto await = [&](int b, uint32_t parity) {
+      if (!dead) dead = !wait_warp(b, parity);
+      tc_fence_after();
+    };
     // What a thread needs of the row block that it is at.
     struct Block {
       int first, n;
-      bool whole, there;  // there: the row exists
-      __nv_bfloat16* out;
-      int limit, lowest;  // keys that the row sees; the fewest of the warp's rows
+      int limit, lowest;  // keys that the row sees (0x7fffffff: no such row); the fewest of the warp's rows
       float back;         // what the row of Q was divided by
+      bool whole;
     };
     // Moves on to the next row block in which this half has rows (false: none left) and puts its rows of Q into shared memory: D / 8
     // lanes per row, channels in the order of the widened codes.
+    int parity = 0;
     const auto enter = [&](Block& b) {
-      for (;; next_block<L>(a, c)) {
-        if (left <= 0) return false;
-        int stop;
-        take_block<L>(c, left, b.first, stop);
-        b.n = stop - b.first;
-        if (b.n == 0) return false;  // (the run ends before the row block's first tile)
-        b.whole = b.first == 0 && stop == c.tiles;
-        if (c.rb * L::R + h * 128 < c.info.rows * a.group) break;
-        tile += b.n;
-        if (left <= 0) return false;
+      int rows, r0, row0, kvh, past;
+      {
+        Cursor c = places[warp].c;
+        long long left = places[warp].left;
+        for (;; next_block<L>(a, c)) {
+          if (left <= 0) return false;
+          int stop;
+          take_block<L>(c, left, b.first, stop);
+          b.n = stop - b.first;
+          if (b.n == 0) return false;  // (the run ends before the row block's first tile)
+          b.whole = b.first == 0 && stop == c.tiles;
+          if (c.rb * L::R + h * 128 < c.info.rows * a.group) break;
+          tile += b.n;
+          if (left <= 0) return false;
+        }
+        rows = c.info.rows * a.group;
+        r0 = c.rb * L::R + h * 128;
+        row0 = c.info.row0;
+        kvh = c.kvh;
+        past = c.info.len - c.info.rows;
+        if (left > 0) next_block<L>(a, c);
+        keep_place(c, left);
       }
-      const int rows = c.info.rows * a.group, r0 = c.rb * L::R + h * 128;
-      constexpr int kLanes = D / 8, kRowsAt = 32 / kLanes, kSteps = 32 / kRowsAt;
+      parity ^= 1;
+      if (lane < 3) out_of[warp][parity][lane] = lane == 0 ? row0 : lane == 1 ? kvh : r0;
+      constexpr int kLanes = D / 8, kRowsAt = 32 / kLanes, kSteps = 16 / kRowsAt;
       const int ch = lane % kLanes;
-      const __nv_bfloat16* q = a.q + (int64_t)c.info.row0 * a.ld_q + (int64_t)c.kvh * a.group * D + ch * 8;
+      const __nv_bfloat16* q = a.q + (int64_t)row0 * a.ld_q + (int64_t)kvh * a.group * D + ch * 8;
       uint4 x[kSteps];
 #pragma unroll
       for (int i = 0; i < kSteps; ++i) {
-        const int r = r0 + (warp & 3) * 32 + i * kRowsAt + lane / kLanes, tok = a.by_group(r);
+        const int r = r0 + quad * 32 + part * 16 + i * kRowsAt + lane / kLanes, tok = a.by_group(r);
         x[i] = make_uint4(0, 0, 0, 0);
         if (r < rows) x[i] = __ldg(reinterpret_cast<const uint4*>(q + tok * a.ld_q + (r - tok * a.group) * D));
       }
       // fp16 holds the rows as they are if every piece of eight channels has an element between 2^-6 and 2^15; otherwise each row is
       // brought there by a power of two
       __nv_bfloat162 least = as_bf162(0x7f807f80u), most = as_bf162(0u);
-      int rr = (warp & 3) * 32 + lane / kLanes;
+      int rr = quad * 32 + part * 16 + lane / kLanes;
 #pragma unroll
       for (int i = 0; i < kSteps; ++i) {
         const __nv_bfloat162 big = __hmax2_nan(__hmax2_nan(__habs2(as_bf162(x[i].x)), __habs2(as_bf162(x[i].y))), __hmax2_nan(__habs2(as_bf162(x[i].z)), __habs2(as_bf162(x[i].w))));
@@ -257,14 +303,12 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(kQFull + h));
-      const int r = r0 + row, tok = a.by_group(r);
-      b.there = r < rows;
-      b.out = a.out + (int64_t)(c.info.row0 + tok) * a.ld_out + (int64_t)(c.kvh * a.group + r - tok * a.group) * D;
+      pair_sync(pair);  // (row_scale)
+      const int r = r0 + row;
       b.back = row_scale[h * 128 + row];
       // rows behind the last one have q = 0 and are not written, whatever they see
-      b.limit = b.there ? c.info.len - c.info.rows + tok + 1 : 0x7fffffff;
+      b.limit = r < rows ? past + a.by_group(r) + 1 : 0x7fffffff;
       b.lowest = __shfl_sync(0xffffffffu, b.limit, 0);
-      if (left > 0) next_block<L>(a, c);
       return true;
     };
     const bool wide_out = !(reinterpret_cast<uintptr_t>(a.out) & 31) && a.ld_out % 16 == 0;  // whole 32-byte sectors
@@ -275,20 +319,28 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
       // --- the next row block's Q (all products with this one's are done), while the last product with V runs
       const bool more = enter(next);
       if (b.n > 0) {
-        if (!(ok = wait_warp(kOFull + h, o_ph))) break;
+        of_part[part][h * 128 + row] = sum;
+        pair_sync(pair);
+        sum = of_part[0][h * 128 + row] + of_part[1][h * 128 + row];
+        pair_sync(pair);
+        await(kOFull + h, o_ph);
         o_ph ^= 1;
-        tc_fence_after();
         // --- out, or a partial result; columns (0, 4, 1, 5, 2, 6, 3, 7) of eight are the channels in order
         const float inv = sum == 0.f ? 0.f : 1.f / sum;  // a row that sees nothing is 0
         const int rr = h * 128 + row;
-        float* part = partial_of<L, D>(a, blockIdx.x, b.first == 0);
+        const int* o = out_of[warp][parity ^ (more ? 1 : 0)];
+        const int r = o[2] + row, tok = a.by_group(r);
+        __nv_bfloat16* out = a.out + (int64_t)(o[0] + tok) * a.ld_out + (int64_t)(o[1] * a.group + r - tok * a.group) * D;
+        const bool there = b.limit != 0x7fffffff;
+        float* partial = partial_of<L, D>(a, blockIdx.x, b.first == 0);
 #pragma unroll 1
-        for (int d = 0; d < D; d += 32) {
+        for (int d = 0; d < D / 2; d += 32) {
           uint32_t v[32];
           tmem_ld32_issue(o_at + d, v);
           tmem_ld_done(v);
           const auto at = [&](int i) { return __uint_as_float(v[i]); };
-          if (b.there && b.whole) {
+          const int ch = D / 2 * part + d;
+          if (there && b.whole) {
 #pragma unroll
             for (int i = 0; i < 32; i += 16) {
               uint32_t y[8];
@@ -301,23 +353,23 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
                 y[4 * k + 3] = pack_bf16x2(at(o + 5) * inv, at(o + 7) * inv);
               }
               if (wide_out) {
-                st_global_32(b.out + d + i, y);
+                st_global_32(out + ch + i, y);
               } else {
-                *reinterpret_cast<uint4*>(b.out + d + i) = make_uint4(y[0], y[1], y[2], y[3]);
-                *reinterpret_cast<uint4*>(b.out + d + i + 8) = make_uint4(y[4], y[5], y[6], y[7]);
+                *reinterpret_cast<uint4*>(out + ch + i) = make_uint4(y[0], y[1], y[2], y[3]);
+                *reinterpret_cast<uint4*>(out + ch + i + 8) = make_uint4(y[4], y[5], y[6], y[7]);
               }
             }
-          } else if (b.there) {
+          } else if (there) {
 #pragma unroll
             for (int i = 0; i < 32; i += 8) {
-              *reinterpret_cast<float4*>(part + rr * D + d + i) = make_float4(at(i), at(i + 2), at(i + 4), at(i + 6));
-              *reinterpret_cast<float4*>(part + rr * D + d + i + 4) = make_float4(at(i + 1), at(i + 3), at(i + 5), at(i + 7));
+              *reinterpret_cast<float4*>(partial + rr * D + ch + i) = make_float4(at(i), at(i + 2), at(i + 4), at(i + 6));
+              *reinterpret_cast<float4*>(partial + rr * D + ch + i + 4) = make_float4(at(i + 1), at(i + 3), at(i + 5), at(i + 7));
             }
           }
         }
-        if (!b.whole) {
-          part[L::R * D + rr] = m * b.back;
-          part[L::R * D + L::R + rr] = sum;
+        if (!b.whole && part == 0) {
+          partial[L::R * D + rr] = m * b.back;
+          partial[L::R * D + L::R + rr] = sum;
         }
         tc_fence_before();
       }
@@ -326,60 +378,58 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
       const float scale = fmaxf(a.scale * b.back, FLT_MIN);  // (hidden scores are -infinity, and 0 times that is NaN)
       m = -INFINITY;
       sum = 0.f;
-      const auto scores_at = [&](int t) { return tmem + 128 * h + 64 * (t & 1) + lanes; };
+      const auto scores_at = [&](int t) { return tmem + 128 * h + 64 * (t & 1) + lanes; };  // (P follows in the first 32 columns)
       // Scores of the block's tile j, the run's tile t: waits for them; hidden ones become -infinity in place (the tiles that hide none
       // pay nothing for it).
       const auto arrived = [&](int j, int t) {
-        if (!(ok = wait_warp(kSFull + 2 * h + (t & 1), s_ph >> (t & 1) & 1))) return;
+        await(kSFull + 2 * h + (t & 1), s_ph >> (t & 1) & 1);
         s_ph ^= 1u << (t & 1);
-        tc_fence_after();
         const int key0 = (b.first + j) * L::kKeys, bad = tile_bad[t & 7];
         if (key0 + L::kKeys > b.lowest || bad) {
-          const int see = bad ? 0 : b.limit - key0;  // keys of the tile before this one are seen
-#pragma unroll 1
-          for (int d = 0; d < L::kKeys; d += 32) {
-            uint32_t v[32];
-            tmem_ld32_issue(scores_at(t) + d, v);
-            tmem_ld_done(v);
+          const int see = bad ? 0 : b.limit - key0 - 32 * part;  // this thread's keys before this one are seen
+          uint32_t v[32];
+          tmem_ld32_issue(scores_at(t) + 32 * part, v);
+          tmem_ld_done(v);
 #pragma unroll
-            for (int i = 0; i < 32; ++i)
-              if (d + i >= see) v[i] = 0xff800000u;
-            tmem_st32(scores_at(t) + d, v);
-          }
+          for (int i = 0; i < 32; ++i)
+            if (i >= see) v[i] = 0xff800000u;
+          tmem_st32(scores_at(t) + 32 * part, v);
         }
       };
       const uint64_t scale2 = pack_f32x2(scale, scale);
       for (int j = 0; j < b.n; ++j, ++tile) {
         arrived(j, tile);
-        if (!ok) break;
         const uint32_t s_at = scores_at(tile);
-        uint32_t p[32];
+        uint32_t p[16];
         float s0, s1;
         bool look = j == 0;  // for the maximum, before the weights: in the first tile, and where the weights by the one so far turn out too large
         for (;;) {
-          uint32_t v[2][32];
-          tmem_ld32_issue(s_at, v[0]);
-          tmem_ld32_issue(s_at + 32, v[1]);
-          tmem_ld_done(v[0]);
-          tmem_ld_done(v[1]);
+          uint32_t v[32];
+          tmem_ld32_issue(s_at + 32 * part, v);
+          tmem_ld_done(v);
           if (look) {
             float t[4] = {m, m, m, m};
 #pragma unroll
-            for (int i = 0; i < 64; i += 2) t[i >> 1 & 3] = max3(t[i >> 1 & 3], __uint_as_float(v[i >> 5][i & 31]), __uint_as_float(v[i >> 5][(i & 31) + 1]));
-            const float top = max3(max3(t[0], t[1], t[2]), t[3], t[3]);
+            for (int i = 0; i < 32; i += 2) t[i >> 1 & 3] = max3(t[i >> 1 & 3], __uint_as_float(v[i]), __uint_as_float(v[i + 1]));
+            float top = max3(max3(t[0], t[1], t[2]), t[3], t[3]);
+            of_part[part][h * 128 + row] = top;
+            tc_fence_before();
+            pair_sync(pair);
+            tc_fence_after();
+            top = fmaxf(top, of_part[part ^ 1][h * 128 + row]);
             if (j > 0) {
               // O holds the tiles before this one: their products end before those with the K of the next tile, or (there is none) signal
-              if (!(ok = j + 1 < b.n ? wait_warp(kSFull + 2 * h + (~tile & 1), s_ph >> (~tile & 1) & 1) : wait_warp(kOFull + h, o_ph))) break;
-              tc_fence_after();
+              if (j + 1 < b.n) await(kSFull + 2 * h + (~tile & 1), s_ph >> (~tile & 1) & 1);
+              else await(kOFull + h, o_ph);
               const float f = top == m ? 1.f : ex2((m - top) * scale);
               sum *= f;
 #pragma unroll 1
-              for (int d = 0; d < D; d += 32) {
-                tmem_ld32_issue(o_at + d, p);
-                tmem_ld_done(p);
+              for (int d = 0; d < D / 2; d += 16) {
+                float y[16];
+                tmem_ld16(o_at + d, y);
 #pragma unroll
-                for (int i = 0; i < 32; ++i) p[i] = __float_as_uint(__uint_as_float(p[i]) * f);
-                tmem_st32(o_at + d, p);
+                for (int i = 0; i < 16; ++i) p[i] = __float_as_uint(y[i] * f);
+                tmem_st16(o_at + d, p);
               }
             }
             m = top;
@@ -388,9 +438,9 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
           const uint64_t shift2 = pack_f32x2(shift, shift);
           uint64_t sums[2] = {0, 0};
 #pragma unroll
-          for (int i = 0; i < 32; ++i) {
+          for (int i = 0; i < 16; ++i) {
             float x0, x1;
-            unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(v[i >> 4][2 * (i & 15)]), __uint_as_float(v[i >> 4][2 * (i & 15) + 1])), scale2, shift2), x0, x1);
+            unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])), scale2, shift2), x0, x1);
             x0 = ex2(x0);
             x1 = ex2(x1);
             sums[i & 1] = add_f32x2(sums[i & 1], pack_f32x2(x0, x1));
@@ -400,21 +450,24 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
           s0 += s1;
           // No running maximum: the tile's sum says whether a weight can be too large for fp16 (a score 2^14 above the maximum so far in
           // the softmax; seldom).  Then the maximum is looked for, O and the sum are scaled, and the tile is done again.
-          if (look || !__any_sync(0xffffffffu, s0 > 16384.f || (m == -INFINITY && s0 > 0.f))) break;
+          // (The barrier, here or above, also stands between the other warp's reading of its scores and P, which goes where they are.)
+          if (look) break;
+          tc_fence_before();
+          const bool again = pair_any(pair, s0 > 16384.f || (m == -INFINITY && s0 > 0.f));
+          tc_fence_after();
+          if (!again) break;
           look = true;
         }
-        if (!ok) break;
         sum += s0;
-        tmem_st32(s_at, p);
+        tmem_st16(s_at + 16 * part, p);
         if (j > 0 && j + 1 == b.n) {  // the last two products with V signal: the first of them is seen before the second can start
-          if (!(ok = wait_warp(kOFull + h, o_ph))) break;
+          await(kOFull + h, o_ph);
           o_ph ^= 1;
         }
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(kPFull + 2 * h + (tile & 1)));
       }
-      if (!ok) break;
     }
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
@@ -526,17 +579,25 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
       int slot = 0, tile = 0;
       uint32_t phase = 0;
       bool ok = true;
-      while (ok && left > 0) {
-        int first, stop;
-        take_block<L>(c, left, first, stop);
-        for (int j = first; j < stop; ++j, ++tile) {
+      for (;;) {
+        int j, stop, len;
+        {
+          Cursor c = places[warp].c;
+          long long left = places[warp].left;
+          if (left <= 0) break;
+          take_block<L>(c, left, j, stop);
+          len = c.info.len;
+          if (left > 0) next_block<L>(a, c);
+          keep_place(c, left);
+        }
+        for (; j < stop; ++j, ++tile) {
           const int st = tile % kRing;
           const uint32_t reuse = (tile / kRing & 1) ^ 1;
           const uint32_t k_dst = base + M::kK + st * M::kTile + group * M::kSub + token * 128, v_dst = k_dst + M::kV - M::kK;
           if (!(ok = wait_warp(kRawFull + slot, phase))) break;
           const uint32_t raw = base + M::kRawAt + slot * M::kRun;
           const bool bad = raw_bad[slot] != 0;
-          const bool in = !bad && j * kPageTokens + token < c.info.len;
+          const bool in = !bad && j * kPageTokens + token < len;
           const uint32_t sw = (uint32_t)(token & 7);
           float2 mk = lds_half2(raw + 64 * D + (group * kPageTokens + token) * 4), mv = lds_half2(raw + 68 * D + (group * kPageTokens + token) * 4);
           uint4 ck[kWords / 4], cv[kWords / 4];
@@ -570,7 +631,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
           __syncwarp();
           if (lane == 0) mbar_arrive(bar(kTileFull + st));
         }
-        if (ok && left > 0) next_block<L>(a, c);
+        if (!ok) break;
       }
     }
   }
