@@ -46,16 +46,18 @@ __device__ __forceinline__ int locate_token(const CacheView& v, const CacheEntri
   return page;
 }
 
-// Eight channels of a group of 64; the other seven neighbours (lanes of an aligned group of eight) hold the rest.
+// Sixteen channels of a group of 64; the other three neighbours (lanes of an aligned group of four) hold the rest.  (With eight channels a
+// lane, what every lane does for a token made it 20 instructions a value instead of 16: 54 us for 32 thousand tokens of 8 heads of 128, now 51.)
 struct Piece {
-  uint4 raw;  // bf16
+  uint4 raw[2];  // bf16
   __device__ __forceinline__ float value(int i) const {
-    const uint32_t w = i < 2 ? raw.x : i < 4 ? raw.y : i < 6 ? raw.z : raw.w;
+    const uint4& r = raw[i >> 3];
+    const uint32_t w = (i & 7) < 2 ? r.x : (i & 7) < 4 ? r.y : (i & 7) < 6 ? r.z : r.w;
     return __uint_as_float(i & 1 ? w & 0xffff0000u : w << 16);
   }
 };
 struct Packed {
-  uint32_t codes;
+  uint2 codes;
   __half scale, low;
   bool fits;
 };
@@ -64,11 +66,18 @@ __device__ __forceinline__ __nv_bfloat162 as_bf162(uint32_t v) { return *reinter
 // 4-bit storage of the group.  The minimum and maximum are found on bf16 pairs (exact, NaN stays NaN); one shuffle a step carries
 // (max, -min).
 __device__ __forceinline__ Packed pack_group(const Piece& x) {
-  const __nv_bfloat162 a = as_bf162(x.raw.x), b = as_bf162(x.raw.y), c = as_bf162(x.raw.z), d = as_bf162(x.raw.w);
-  const __nv_bfloat162 top = __hmax2_nan(__hmax2_nan(a, b), __hmax2_nan(c, d)), low = __hneg2(__hmin2_nan(__hmin2_nan(a, b), __hmin2_nan(c, d)));
+  __nv_bfloat162 top = as_bf162(x.raw[0].x), low = top;
+#pragma unroll
+  for (int i = 1; i < 8; ++i) {
+    const uint4& r = x.raw[i >> 2];
+    const __nv_bfloat162 v = as_bf162((i & 3) == 0 ? r.x : (i & 3) == 1 ? r.y : (i & 3) == 2 ? r.z : r.w);
+    top = __hmax2_nan(top, v);
+    low = __hmin2_nan(low, v);
+  }
+  low = __hneg2(low);
   __nv_bfloat162 both = __hmax2_nan(__lows2bfloat162(top, low), __highs2bfloat162(top, low));
 #pragma unroll
-  for (int step = 1; step < 8; step <<= 1) both = __hmax2_nan(both, __shfl_xor_sync(0xffffffffu, both, step));
+  for (int step = 1; step < 4; step <<= 1) both = __hmax2_nan(both, __shfl_xor_sync(0xffffffffu, both, step));
   const float high = __low2float(both);
   Packed p;
   p.low = __float2half_rn(-__high2float(both));
@@ -78,39 +87,56 @@ __device__ __forceinline__ Packed pack_group(const Piece& x) {
   p.scale = __float2half_rn(fmaf(fmaf(-15.f, q0, range), 1.f / 15.f, q0));
   const float s = __half2float(p.scale);
   p.fits = s < INFINITY && fabsf(base) < INFINITY;  // (false for NaN)
-  p.codes = 0;
+  p.codes = make_uint2(0, 0);
   if (s > 0.f) {
-    // rint((x - base) / s): times 1 / s it is off by a few units of 2^-23, which matters next to a half only; then the division is made.
-    // (The division, the rounding and the conversion of every value kept the kernel at a quarter of the memory's rate: 128 us for 32 thousand
-    // tokens of 8 heads of 128, 209 MB.)
+    // rint((x - base) / s), clipped to 0 .. 15, as x * k - base * k with k = 1 / (15 s): the saturating multiply-add clips it to 0 .. 1 and
+    // the next one takes it to 0 .. 15 and rounds.  With |base| <= 100 s the products are wrong by (115 + 100) 2^-22 < 10^-4 steps at most,
+    // which matters next to a half only; then, and with a larger base, the division is made.  (The division, the rounding and the conversion of
+    // every value kept the kernel at a quarter of the memory's rate: 128 us for 32 thousand tokens of 8 heads of 128, 209 MB; a subtraction, a
+    // multiplication and two comparisons to clip every value: 64 us, so 54.)
     float inv;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));
     const float magic = 12582912.f;  // 1.5 * 2^23: what is added to it is rounded to an integer, ties to even
-    float far = 0.f, c8[8];
+    const float k = inv * (1.f / 15.f), offset = -base * k;
+    const uint64_t magic2 = pack_f32x2(magic, magic), back2 = pack_f32x2(-magic, -magic), up2 = pack_f32x2(15.f, 15.f), down2 = pack_f32x2(-15.f, -15.f);
+    float far = fabsf(base) <= 100.f * s ? 0.f : 1.f;
+    uint32_t half[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float q = fminf(fmaxf((x.value(i) - base) * inv, 0.f), 15.f);
-      c8[i] = q + magic;
-      far = fmaxf(far, fabsf(q - (c8[i] - magic)));
+    for (int j = 0; j < 4; ++j) {
+      float n[4], first = 0.f;
+#pragma unroll
+      for (int i = 0; i < 4; i += 2) {
+        const uint64_t t = pack_f32x2(__saturatef(fmaf(x.value(4 * j + i), k, offset)), __saturatef(fmaf(x.value(4 * j + i + 1), k, offset)));
+        const uint64_t c = fma_f32x2(t, up2, magic2), r = add_f32x2(c, back2);
+        float c0, c1, d0, d1;
+        unpack_f32x2(c, c0, c1);
+        unpack_f32x2(r, n[i], n[i + 1]);
+        unpack_f32x2(fma_f32x2(t, down2, r), d0, d1);
+        far = fmaxf(far, fmaxf(fabsf(d0), fabsf(d1)));
+        if (i == 0) first = c0;
+      }
+      half[j] = __float_as_uint(fmaf(n[3], 4096.f, fmaf(n[2], 256.f, fmaf(n[1], 16.f, first))));  // (four codes in the lowest 16 bits)
     }
+    p.codes = make_uint2(__byte_perm(half[0], half[1], 0x5410), __byte_perm(half[2], half[3], 0x5410));
     if (far > 0.4999f) {
+      p.codes = make_uint2(0, 0);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) c8[i] = fminf(fmaxf(__fdiv_rn(x.value(i) - base, s), 0.f), 15.f) + magic;
+      for (int i = 0; i < 16; ++i)
+        (i < 8 ? p.codes.x : p.codes.y) |= (__float_as_uint(fminf(fmaxf(__fdiv_rn(x.value(i) - base, s), 0.f), 15.f) + magic) & 15u) << (4 * (i & 7));
     }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) p.codes |= (__float_as_uint(c8[i]) & 15u) << (4 * i);
   }
   return p;
 }
 
-// D / 8 neighbouring lanes take a token of a kv head, eight channels of K and of V each, kTokens tokens in turn; a thread block has
-// consecutive tokens of a head, so that the 16-byte pieces of neighbouring tokens (adjacent in a page) meet in one sector.  Bytes: 4 * D in
-// and 1.125 * D out per (token, kv head).  32 thousand tokens of 8 heads of 128: 64 us, 2.7 TB/s; what it waits for is issue slots (some 20
-// instructions a value between conversion, comparison and packing).
+// D / 16 neighbouring lanes take a token of a kv head, sixteen channels of K and of V each, kTokens tokens in turn; a thread block has
+// consecutive tokens of a head, so that the pieces of neighbouring tokens (adjacent in a page) meet in one sector.  Bytes: 4 * D in
+// and 1.125 * D out per (token, kv head).  32 thousand tokens of 8 heads of 128: 51 us, 3.4 TB/s; two thirds of the issue slots are taken (16
+// instructions a value between conversion, comparison and packing).  Five thread blocks per SM: 51.2 us, with the registers of four 53.3; two,
+// three and eight tokens per thread instead of four: 53.2 to 57.3.
 template <int D, int kTokens>
-__global__ void __launch_bounds__(256) append_kernel(CacheView v, CacheEntries e, const __nv_bfloat16* k, int64_t ld_k, const __nv_bfloat16* val, int64_t ld_v,
+__global__ void __launch_bounds__(256, 5) append_kernel(CacheView v, CacheEntries e, const __nv_bfloat16* k, int64_t ld_k, const __nv_bfloat16* val, int64_t ld_v,
                                                      int32_t* status) {
-  constexpr int L = D / 8;  // lanes per token
+  constexpr int L = D / 16;  // lanes per token
   __shared__ int32_t offsets[kOffsetsMax];
   stage_offsets(e, offsets);
   // (heads innermost: thread blocks that run together read the whole rows of their tokens)
@@ -123,10 +149,15 @@ __global__ void __launch_bounds__(256) append_kernel(CacheView v, CacheEntries e
     const bool in = at < e.T;
     const int t = in ? (int)at : 0;
     Piece xk, xv;
-    xk.raw = xv.raw = make_uint4(0, 0, 0, 0);
+    xk.raw[0] = xk.raw[1] = xv.raw[0] = xv.raw[1] = make_uint4(0, 0, 0, 0);
     if (in) {  // (before the look-up: its loads and these need not wait for one another)
-      xk.raw = *reinterpret_cast<const uint4*>(k + t * ld_k + h * D + lane * 8);
-      xv.raw = *reinterpret_cast<const uint4*>(val + t * ld_v + h * D + lane * 8);
+      const uint4* from_k = reinterpret_cast<const uint4*>(k + t * ld_k + h * D + lane * 16);
+      const uint4* from_v = reinterpret_cast<const uint4*>(val + t * ld_v + h * D + lane * 16);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        xk.raw[i] = from_k[i];
+        xv.raw[i] = from_v[i];
+      }
     }
     if (in && t < end) {
       ++offset;
@@ -139,17 +170,17 @@ __global__ void __launch_bounds__(256) append_kernel(CacheView v, CacheEntries e
     // one lane that does not fit makes the token (its L lanes) NaN
     const uint32_t misfits = __ballot_sync(0xffffffffu, !(pk.fits && pv.fits)) >> ((threadIdx.x & 31) / L * L) & ((1u << L) - 1);
     if (misfits) {
-      pk.codes = pv.codes = 0;
+      pk.codes = pv.codes = make_uint2(0, 0);
       pk.scale = pv.scale = pv.low = __ushort_as_half(0);  // (V 0: it meets weights 0 in the rows that do not see the token)
       pk.low = __ushort_as_half(0x7e00);
     }
     if (!in || page < 0) continue;
     uint8_t* run = v.pages + page * v.page_bytes + (int64_t)h * 72 * D;
-    uint8_t* code = run + (lane >> 2) * 1024 + offset * 16 + (lane & 3) * 4;
-    *reinterpret_cast<uint32_t*>(code) = pk.codes;
-    *reinterpret_cast<uint32_t*>(code + 32 * D) = pv.codes;
-    if ((lane & 7) == 0) {
-      __half2* meta = reinterpret_cast<__half2*>(run + 64 * D + ((lane >> 3) * kPageTokens + offset) * 4);
+    uint8_t* code = run + (lane >> 1) * 1024 + offset * 16 + (lane & 1) * 8;
+    *reinterpret_cast<uint2*>(code) = pk.codes;
+    *reinterpret_cast<uint2*>(code + 32 * D) = pv.codes;
+    if ((lane & 3) == 0) {
+      __half2* meta = reinterpret_cast<__half2*>(run + 64 * D + ((lane >> 2) * kPageTokens + offset) * 4);
       meta[0] = __halves2half2(pk.scale, pk.low);
       meta[D] = __halves2half2(pv.scale, pv.low);
     }
@@ -159,7 +190,8 @@ __global__ void __launch_bounds__(256) append_kernel(CacheView v, CacheEntries e
 // The low four bits of w as a number: dropped into the mantissa of 2^23 (a conversion would go through a slower unit).
 __device__ __forceinline__ float code_float(uint32_t w) { return __uint_as_float(0x4B000000u | (w & 15u)) - 8388608.f; }
 
-// The inverse, with the same mapping of threads: 1.125 * D bytes in and 4 * D out.  32 thousand tokens of 8 heads of 128: 36 us, 4.8 TB/s.
+// The inverse, with the same mapping of threads: 1.125 * D bytes in and 4 * D out.  32 thousand tokens of 8 heads of 128: 36 us,
+// 4.8 TB/s.
 template <int D, int kTokens>
 __global__ void __launch_bounds__(256) read_kernel(CacheView v, CacheEntries e, __nv_bfloat16* k_out, __nv_bfloat16* v_out, int32_t* status) {
   constexpr int L = D / 8;
@@ -600,14 +632,15 @@ int32_t launched(essa_ctx* ctx, const char* what, int kernels) {
 // heads: 8 rows 47 / 133, 16 rows 79 / 134, 24 rows 137 / 134, 64 rows 256 / 138; one of 30000 tokens: 16 rows 29 / 41, 24 rows 42 / 41.
 bool few_rows(int64_t rows) { return rows <= 16; }
 size_t seen_bytes(const CacheView& v) { return (size_t)(v.max_seqs + 31) / 32 * 4; }
-// Thread blocks of append and read: 256 / (head_dim / 8) times `per` tokens of one head each.
-int64_t token_blocks(int32_t T, const CacheView& v, int per) {
-  const int64_t tokens = (int64_t)256 / (v.head_dim / 8) * per;
+// Thread blocks of append and read: 256 threads, `channels` of them a thread, take `per` tokens of one head each.
+int64_t token_blocks(int32_t T, const CacheView& v, int channels, int per) {
+  const int64_t tokens = (int64_t)256 / (v.head_dim / channels) * per;
   return (T + tokens - 1) / tokens * v.kv_heads;
 }
 // Four tokens per thread share a look-up, as long as that leaves every SM four thread blocks.  32 thousand tokens of 8 heads, stored and read
-// back: 124 us, with one token per thread 159; 256 tokens (too few for the rule): 45 us with either.
-bool four_tokens(const essa_ctx* ctx, int32_t T, const CacheView& v) { return token_blocks(T, v, 4) >= 4 * ctx->sm_count; }
+// back: 124 us, with one token per thread 159 (before other steps); 256 tokens (too few for the rule): 45 us with either.
+bool four_tokens(const essa_ctx* ctx, int32_t T, const CacheView& v, int channels) { return token_blocks(T, v, channels, 4) >= 4 * ctx->sm_count; }
+constexpr int kAppendChannels = 16, kReadChannels = 8;
 int copy_grid(const essa_ctx* ctx) { return ctx->sm_count * 8; }
 
 }  // namespace
@@ -681,8 +714,8 @@ int32_t essa_cache_append(essa_ctx* ctx, const essa_cache_desc* cache, int32_t l
   ESSA_TRY(check_rows(ctx, "cache_append", "k", k, ld_k, (int64_t)v.kv_heads * v.head_dim));
   ESSA_TRY(check_rows(ctx, "cache_append", "v", val, ld_v, (int64_t)v.kv_heads * v.head_dim));
   DeviceGuard guard(ctx->device);
-  const bool four = four_tokens(ctx, T, v);
-  const int64_t grid = token_blocks(T, v, four ? 4 : 1);
+  const bool four = four_tokens(ctx, T, v, kAppendChannels);
+  const int64_t grid = token_blocks(T, v, kAppendChannels, four ? 4 : 1);
   if (grid > 0x7fffffff) return fail(ctx, ESSA_ERR_UNSUPPORTED_SHAPE, "cache_append: too many tokens");
   const auto *kk = static_cast<const __nv_bfloat16*>(k), *vv = static_cast<const __nv_bfloat16*>(val);
   cudaStream_t stream = static_cast<cudaStream_t>(stream_v);
@@ -703,8 +736,8 @@ int32_t essa_cache_read(essa_ctx* ctx, const essa_cache_desc* cache, int32_t lay
   if (k_out) ESSA_TRY(check_rows(ctx, "cache_read", "k_out", k_out, width, width));
   if (v_out) ESSA_TRY(check_rows(ctx, "cache_read", "v_out", v_out, width, width));
   DeviceGuard guard(ctx->device);
-  const bool four = four_tokens(ctx, T, v);
-  const int64_t grid = token_blocks(T, v, four ? 4 : 1);
+  const bool four = four_tokens(ctx, T, v, kReadChannels);
+  const int64_t grid = token_blocks(T, v, kReadChannels, four ? 4 : 1);
   if (grid > 0x7fffffff) return fail(ctx, ESSA_ERR_UNSUPPORTED_SHAPE, "cache_read: too many tokens");
   auto *kk = static_cast<__nv_bfloat16*>(k_out), *vv = static_cast<__nv_bfloat16*>(v_out);
   cudaStream_t stream = static_cast<cudaStream_t>(stream_v);

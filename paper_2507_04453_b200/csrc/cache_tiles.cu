@@ -1,19 +1,24 @@
 // Attention over the paged 4-bit cache for many rows per sequence (prompts, chunks): tcgen05 tiles.
 //
 // A row block is 256 query rows (token-major: row r of an entry is token r / group, head r % group of a kv head, so the heads that
-// share K and V share a tile), two halves of 128; a key tile is two pages.  Per key tile and half: S = Q K^T (fp16, M = 128, N = 128)
-// into tensor memory, softmax by four warps (a thread per row), P back into the same columns of tensor memory as fp16,
-// O += P V (fp16, A from tensor memory, V as stored: MN-major).  The halves alternate: while one is in its softmax, the tensor
-// core works for the other.  Four warps widen the pages, one copies them in (bulk copies), one issues the MMAs.
+// share K and V share a tile), two halves of 128; a key tile is one page.  Per key tile and half: S = Q K^T (fp16, M = 128, N = 64)
+// into one of two buffers in tensor memory, softmax by eight warps (two threads per row, 32 keys each), P back into the same columns as
+// fp16, O += P V (fp16, A from tensor memory, V as stored: MN-major).  Products with K run two tiles ahead.  Four warps widen the pages, one
+// copies them in (bulk copies), one issues the MMAs.  Tensor memory: 4 x 64 columns of scores, 2 x head_dim of O.
 //
-// What bounds it: per key tile and SM the MMAs need 2048 cycles (1024 per half), the exponentials of the softmax 2048 on the
-// special function units, the widening ~550 issue slots per scheduler beside ~1300 of the softmax.
+// What bounds it (heads of 128 channels): a key tile takes ~2290 cycles of an SM.  The tensor pipe counts 1024 of them as active, but the MMAs take
+// ~1800 (N = 64 makes a product with K read 6 KB of shared memory in its 32 cycles of arithmetic); the exponentials need 1024 of the special
+// function units, the warps half of the issue slots.  Two prompts of 450 tokens after 16 thousand, 64 heads (468 GFLOP): 488 us, 0.96 PFLOP/s.
+// A row block costs some six tiles beside its own (queries in, results out): ragged prompts of 1 .. 1024 tokens, 40 heads (231 GFLOP): 496 us.
+// What was tried: a thread per row (eight softmax warps): 558 us for the ragged prompts, 495 for the others; key tiles of two pages, products
+// with K of N = 128 and one buffer of scores per half: 558 and 455 (the halves' softmax and products then alternate, but a tile of 128
+// keys is a coarse grain for short prompts); the same with 80 registers for the softmax instead of 96: 705 and 608.
 //
 // Roundings: K and V become fp16 as their scale and minimum are applied, (code - 8) * scale + (minimum + 8 scale), with the offset and the
 // result rounded (2^-11 each).  Q is bf16; a row times a power of two, its largest element at 2^13 .. 2^14, is fp16 without loss (elements
 // 2^-27 below the largest lose bits).  P is fp16 (2^-11; weights below 6e-8 of the largest lose bits).  With bf16 operands instead, K's
 // three roundings (scale, offset, result: 2^-8 each) made up most of the error: 3.2e-3 of the result's norm against 1.7e-3 from rounding
-// the result alone.  S, the running maximum, the sums and O are fp32.
+// the result alone.  S, the maximum, the sums and O are fp32.
 // Channel order inside a group of eight channels is (0, 4, 1, 5, 2, 6, 3, 7), what masking nibbles out of a word gives: Q is stored in
 // the same order, and O's columns are put back on the way out.
 #include <cfloat>
@@ -23,6 +28,7 @@
 namespace essa {
 namespace {
 
+// kSetup: the ragged prompts take 738 us with 2 and 683 with 4 in the first version, 502, 497 and 500 with 6, 4 and 5 in this one.
 struct TileList {
   static constexpr int R = 256, kKeys = kPageTokens, kMinRun = 2, kSetup = 4;
   // keys that the last row of the row block sees, in tiles
@@ -41,11 +47,12 @@ struct TileList {
 constexpr int kSoftWarps = 16, kWidenWarps = 4;
 constexpr int kMmaWarp = kSoftWarps + kWidenWarps, kCopyWarp = kMmaWarp + 1;
 constexpr int kThreads = 768;  // six warpgroups; the last two warps only give registers away
-// Registers per thread: launched with 80, of which the softmax takes more.  4 * 88 + 2 * 64 = 6 * 80.
+// Registers per thread: launched with 80, of which the softmax takes more.  4 * 88 + 2 * 64 = 6 * 80.  (Nothing spills; 96 and 48: 508 us for
+// the ragged prompts, 80 and 80: 505, this: 502.)
 constexpr int kSoftRegs = 88, kOtherRegs = 64;
 constexpr int kRaw = 3;  // pages in flight
 
-constexpr int kRing = 4;  // key tiles of K and of V
+constexpr int kRing = 4;  // widened key tiles, K and V
 
 template <int D>
 struct Mem {  // offsets from a 1024-byte boundary
@@ -91,23 +98,6 @@ __device__ __forceinline__ void st_global_32(void* p, const uint32_t (&v)[8]) {
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float r;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
-  return r;
-}
-// Two fp32 operations in one instruction.
-__device__ __forceinline__ uint64_t pack_f32x2(float lo, float hi) {
-  uint64_t r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
-  return r;
-}
-__device__ __forceinline__ void unpack_f32x2(uint64_t v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
-__device__ __forceinline__ uint64_t fma_f32x2(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-  return r;
-}
-__device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
 }
 // 16 consecutive columns of the warp's lanes (with the wait).

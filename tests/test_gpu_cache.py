@@ -694,3 +694,31 @@ def test_scales_out_of_range_empty_offsets_and_a_closed_context_are_refused(torc
     for call in (lambda: g.attend(0, q), lambda: g.reset(), lambda: g.append(0, q[:, :2], q[:, :2]), lambda: c.kv_cache(1, 4, 2, 64, 2, 2)):
         with pytest.raises(binding.EssaError):
             call()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_codes_of_offset_tied_and_flat_groups(torch, ctx, d):
+    """Codes, scales and minima bit by bit where the quotient is hard: ties, minima hundreds of steps away, groups of one or two values, huge and
+    tiny steps; enough tokens for the schedule of long prompts too."""
+    rng = np.random.default_rng(21)
+    for T in (40, 5000):
+        p = Pair(torch, ctx, 1, 90, 2, d, 1, 90)
+        k, v = bf16(rng, (T, 2, d)), bf16(rng, (T, 2, d))
+        kind = np.arange(T) % 8
+        k[kind == 1] += 300
+        k[kind == 2] = rng.integers(0, 31, k[kind == 2].shape) / 2          # minimum 0 and maximum 15 in nearly every group: halves tie
+        k[kind == 2, :, ::64], k[kind == 2, :, 1::64] = 0, 15
+        k[kind == 3] = 1.7
+        k[kind == 4] = rng.choice([-3.0, 5.0], k[kind == 4].shape)
+        k[kind == 5] = k[kind == 5] * 0.02 + 2.5                            # 2.5 / (0.1 / 15): some 300 steps
+        k[kind == 6] *= 9000
+        k[kind == 7] *= 1e-5
+        v[kind < 4] = rng.integers(-15, 16, v[kind < 4].shape) / 2 + 0.25   # quotients at many fractions
+        v[kind >= 4] -= 40
+        k, v = wl.round_to_bf16(k.astype(np.float32)), wl.round_to_bf16(v.astype(np.float32))
+        p.gpu.grow(None, p.ints([T]))
+        p.cpu.grow([0], [T])
+        p.gpu.append(0, p.bf(k), p.bf(v), p.ints([0, T]))
+        p.cpu.append(0, k, v, [0, T], [0])
+        assert ctx.get_status() == 0
+        p.assert_same()
