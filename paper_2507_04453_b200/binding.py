@@ -415,6 +415,8 @@ class KvCache:
         self._ws = {}         # cudaStream_t -> workspace
         self._lib, self._ref, self._index = ctx.lib, C.byref(self.desc), self.device.index
         self._int32, self._bf16, self._scale = torch.int32, torch.bfloat16, head_dim ** -0.5
+        self._none = torch.empty(0, dtype=torch.bfloat16, device=self.device)
+        self._empty_like = torch.empty_like
         self._current_stream = torch._C._cuda_getCurrentRawStream
         if fresh:
             self.reset()
@@ -473,11 +475,10 @@ class KvCache:
         return ws
 
     def _empty(self, shape, stream):
-        torch = self.ctx.torch
         if stream is None:
-            return torch.empty(shape, dtype=torch.bfloat16, device=self.device)
-        with torch.cuda.stream(stream):
-            return torch.empty(shape, dtype=torch.bfloat16, device=self.device)
+            return self._none.new_empty(shape)  # (half the time of torch.empty with its keywords)
+        with self.ctx.torch.cuda.stream(stream):
+            return self._none.new_empty(shape)
 
     def _check(self, st):
         if st != ESSA_OK:
@@ -550,7 +551,7 @@ class KvCache:
                 raise EssaError(st, "kv_cache: the number of query heads must be a multiple of kv_heads and max_new at least 1")
             need = self._attend_ws[(heads, max_new)] = got.value
         if out is None:
-            out = self._empty(shape, stream)
+            out = self._empty_like(q) if stream is None and q.is_contiguous() else self._empty(shape, stream)
         elif out.shape != shape:
             raise EssaError(ESSA_ERR_INVALID_ARG, "kv_cache: out must have q's shape")
         po, ldo = self._rows("out", out, heads)

@@ -629,7 +629,7 @@ int32_t launched(essa_ctx* ctx, const char* what, int kernels) {
 }
 // Which attention kernel: up to 16 query rows per (entry, kv head) take the one that widens codes straight into mma operands; with more the
 // 256-row tiles of tcgen05 re-use a widened page often enough.  Few rows / tiles, us, heads of 128 channels: 32 sequences of 4096 tokens, 8 kv
-// heads: 8 rows 47 / 133, 16 rows 79 / 134, 24 rows 137 / 134, 64 rows 256 / 138; one of 30000 tokens: 16 rows 29 / 41, 24 rows 42 / 41.
+// heads: 8 rows 47 / 121, 16 rows 79 / 121, 24 rows 138 / 123, 64 rows 258 / 127; one of 30000 tokens: 16 rows 30 / 39, 24 rows 39 / 39.
 bool few_rows(int64_t rows) { return rows <= 16; }
 size_t seen_bytes(const CacheView& v) { return (size_t)(v.max_seqs + 31) / 32 * 4; }
 // Thread blocks of append and read: 256 threads, `channels` of them a thread, take `per` tokens of one head each.
