@@ -187,11 +187,11 @@ __global__ void __launch_bounds__(256, 5) append_kernel(CacheView v, CacheEntrie
   }
 }
 
-// The low four bits of w as a number: dropped into the mantissa of 2^23 (a conversion would go through a slower unit).
-__device__ __forceinline__ float code_float(uint32_t w) { return __uint_as_float(0x4B000000u | (w & 15u)) - 8388608.f; }
+// 2^23 + the low four bits of w (a conversion would go through a slower unit).
+__device__ __forceinline__ float raised_code(uint32_t w) { return __uint_as_float(0x4B000000u | (w & 15u)); }
 
-// The inverse, with the same mapping of threads: 1.125 * D bytes in and 4 * D out.  32 thousand tokens of 8 heads of 128: 36 us,
-// 4.8 TB/s.
+// The inverse, eight channels a lane: 1.125 * D bytes in and 4 * D out.  32 thousand tokens of 8 heads of 128: 37 us, 4.7 TB/s
+// (a multiplication and an addition for every value: 43).
 template <int D, int kTokens>
 __global__ void __launch_bounds__(256) read_kernel(CacheView v, CacheEntries e, __nv_bfloat16* k_out, __nv_bfloat16* v_out, int32_t* status) {
   constexpr int L = D / 8;
@@ -229,14 +229,15 @@ __global__ void __launch_bounds__(256) read_kernel(CacheView v, CacheEntries e, 
     for (int which = 0; which < 2; ++which) {
       __nv_bfloat16* out = which ? v_out : k_out;
       if (!out) continue;
+      const uint64_t scale2 = pack_f32x2(m[which].x, m[which].x), low2 = pack_f32x2(m[which].y, m[which].y), back2 = pack_f32x2(-8388608.f, -8388608.f);
       uint32_t y[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        // product and sum rounded apart (as the definition reads), then once to bf16
-        const float a = __fadd_rn(__fmul_rn(code_float(w[which] >> (8 * i)), m[which].x), m[which].y);
-        const float b = __fadd_rn(__fmul_rn(code_float(w[which] >> (8 * i + 4)), m[which].x), m[which].y);
-        const __nv_bfloat162 r = __floats2bfloat162_rn(a, b);
-        y[i] = *reinterpret_cast<const uint32_t*>(&r);
+        // code * scale is exact in fp32 (4 bits by 11), the sum is rounded, then once more to bf16
+        float a, b;
+        const uint64_t codes = add_f32x2(pack_f32x2(raised_code(w[which] >> (8 * i)), raised_code(w[which] >> (8 * i + 4))), back2);
+        unpack_f32x2(fma_f32x2(codes, scale2, low2), a, b);
+        y[i] = pack_bf16x2(a, b);
       }
       *reinterpret_cast<uint4*>(out + to) = make_uint4(y[0], y[1], y[2], y[3]);
     }
