@@ -300,7 +300,7 @@ int32_t essa_apply_block(essa_ctx* ctx, const essa_block_item* items, int32_t n_
  * items holds n_layers x n_items entries, layer-major: items[l * n_items + i] is projection i of layer l with its own
  * adapter, activations x, output y and table columns; tokens, segments and the table are shared by all of them.  The
  * result is what n_layers calls of essa_apply_block give.  Every layer's activations are the caller's (whatever runs
- * between the projections of consecutive layers is outside this library), so they must all be final when the call is
+ * between the projections of consecutive layers is not part of this call), so they must all be final when the call is
  * made.  At decode sizes (T <= 256) each layer is one launch and the launches are chained WITHOUT waiting for one
  * another: a layer's thread blocks start wherever the layer before has released an SM, so launch gaps and the tail of
  * one layer overlap the weight streaming of the next; the launches still complete in order.  Larger calls, and layers
