@@ -12,7 +12,9 @@
 // A row block costs some six tiles beside its own (queries in, results out): ragged prompts of 1 .. 1024 tokens, 40 heads (231 GFLOP): 496 us.
 // What was tried: a thread per row (eight softmax warps): 558 us for the ragged prompts, 495 for the others; key tiles of two pages, products
 // with K of N = 128 and one buffer of scores per half: 558 and 455 (the halves' softmax and products then alternate, but a tile of 128
-// keys is a coarse grain for short prompts); the same with 80 registers for the softmax instead of 96: 705 and 608.
+// keys is a coarse grain for short prompts); the same with 80 registers for the softmax instead of 96: 705 and 608;
+// an eighth, a quarter or a half of the exponentials by a polynomial on the FMA pipe: 486, 498 and 535 (issue slots are as short as the
+// special function units).
 //
 // Roundings: K and V become fp16 as their scale and minimum are applied, (code - 8) * scale + (minimum + 8 scale), with the offset and the
 // result rounded (2^-11 each).  Q is bf16; a row times a power of two, its largest element at 2^13 .. 2^14, is fp16 without loss (elements

@@ -722,3 +722,29 @@ def test_codes_of_offset_tied_and_flat_groups(torch, ctx, d):
         p.cpu.append(0, k, v, [0, T], [0])
         assert ctx.get_status() == 0
         p.assert_same()
+
+
+@pytest.mark.parametrize("heads,kv_heads,d", [(300, 1, 64), (33, 3, 128), (32, 2, 64), (17, 17, 64)])
+def test_groups_of_unusual_size(torch, ctx, heads, kv_heads, d):
+    """More heads in a group than a row block has rows, groups of 11 and 16 heads, and 17 kv heads of one head each."""
+    rng = np.random.default_rng(heads)
+    p = Pair(torch, ctx, 1, 20, kv_heads, d, 3, 5)
+    p.place([300, 65, 2], rng)
+    for rows, hint in (([1, 1, 1], 1), ([3, 2, 2], 3), ([40, 65, 2], 65)):
+        run_attend(torch, ctx, p, rows, [0, 1, 2], heads, rng, hint)
+
+
+def test_second_cache_object_on_the_same_buffers(torch, ctx):
+    """A second cache object on the buffers of the first sees the same sequences."""
+    rng = np.random.default_rng(23)
+    p = Pair(torch, ctx, 2, 10, 2, 64, 3, 4)
+    p.place([100, 3, 64], rng)
+    g = p.gpu
+    other = ctx.kv_cache(2, 10, 2, 64, 3, 4, pages=g.pages, table=g.table, lengths=g.lengths, refs=g.refs)
+    q = p.bf(bf16(rng, (3, 4, 64)))
+    for layer in range(2):
+        assert torch.equal(other.attend(layer, q), g.attend(layer, q))
+    other.grow(None, p.ints([1, 1, 1]))
+    p.cpu.grow(range(3), [1, 1, 1])
+    assert ctx.get_status() == 0
+    p.assert_same(pages=False)
