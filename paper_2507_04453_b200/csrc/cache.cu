@@ -395,6 +395,7 @@ __device__ void count_rows(const CacheView& v, const int32_t* dst, int n, int by
 
 __global__ void __launch_bounds__(kPlanThreads) fork_plan_kernel(CacheView v, const int32_t* src, const int32_t* dst, const int32_t* lens, int n, PlanSpace ws,
                                                                  int32_t* status) {
+  grid_dep_launch();
   extern __shared__ uint32_t seen[];
   __shared__ long long scan_sm[33];
   bool ok = slots_distinct(dst, n, v.max_seqs, seen);
@@ -486,6 +487,7 @@ __device__ __forceinline__ void copy_pages(const CacheView& v, const PlanSpace& 
 }
 
 __global__ void __launch_bounds__(256) fork_kernel(CacheView v, const int32_t* src, const int32_t* dst, const int32_t* lens, int n, PlanSpace ws) {
+  grid_dep_wait();
   if (!ws.head->ok) return;
   for (int i = blockIdx.x; i < n; i += gridDim.x) {
     const int s = src[i], d = dst[i], len = lens ? lens[i] : v.lengths[s], full = len / kPageTokens, last = ws.extra[i];
@@ -502,6 +504,7 @@ __global__ void __launch_bounds__(256) fork_kernel(CacheView v, const int32_t* s
 }
 
 __global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(CacheView v, PlanSpace ws, int32_t* used_out) {
+  grid_dep_launch();
   __shared__ long long scan_sm[33];
   long long used = 0;
   for (int base = 0; base < v.num_pages; base += blockDim.x) {
@@ -537,6 +540,7 @@ __global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(CacheView v,
   }
 }
 __global__ void __launch_bounds__(256) compact_kernel(CacheView v, PlanSpace ws) {
+  grid_dep_wait();
   const int copies = ws.head->copies;
   if (copies == 0) return;
   const int64_t entries = (int64_t)v.max_seqs * v.max_pages;
@@ -642,7 +646,20 @@ int64_t token_blocks(int32_t T, const CacheView& v, int channels, int per) {
 // back: 124 us, with one token per thread 159 (before other steps); 256 tokens (too few for the rule): 45 us with either.
 bool four_tokens(const essa_ctx* ctx, int32_t T, const CacheView& v, int channels) { return token_blocks(T, v, channels, 4) >= 4 * ctx->sm_count; }
 constexpr int kAppendChannels = 16, kReadChannels = 8;
-int copy_grid(const essa_ctx* ctx) { return ctx->sm_count * 8; }
+// The kernel behind a plan: its thread blocks are on their SMs when the plan is ready (they wait for the end of the plan's launch).
+template <class... Args>
+cudaError_t launch_behind_plan(const essa_ctx* ctx, cudaStream_t stream, void (*kernel)(Args...), Args... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(ctx->sm_count * 8);
+  cfg.blockDim = dim3(256);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
 
 }  // namespace
 }  // namespace essa
@@ -796,8 +813,8 @@ int32_t essa_cache_fork(essa_ctx* ctx, const essa_cache_desc* cache, const int32
   const PlanSpace ws = plan_space(workspace, v);
   fork_plan_kernel<<<1, kPlanThreads, seen_bytes(v), stream>>>(v, src, dst, lens, n, ws, ctx->d_status);
   ESSA_TRY(launched(ctx, "cache_fork", 1));
-  fork_kernel<<<copy_grid(ctx), 256, 0, stream>>>(v, src, dst, lens, n, ws);
-  return launched(ctx, "cache_fork", 1);
+  ++ctx->launches;
+  return check_cuda(ctx, launch_behind_plan(ctx, stream, fork_kernel, v, src, dst, lens, (int)n, ws), "cache_fork");
 }
 
 int32_t essa_cache_free(essa_ctx* ctx, const essa_cache_desc* cache, const int32_t* slots, int32_t n, void* stream) {
@@ -820,8 +837,8 @@ int32_t essa_cache_compact(essa_ctx* ctx, const essa_cache_desc* cache, int32_t*
   const PlanSpace ws = plan_space(workspace, v);
   compact_plan_kernel<<<1, kPlanThreads, 0, stream>>>(v, ws, used);
   ESSA_TRY(launched(ctx, "cache_compact", 1));
-  compact_kernel<<<copy_grid(ctx), 256, 0, stream>>>(v, ws);
-  return launched(ctx, "cache_compact", 1);
+  ++ctx->launches;
+  return check_cuda(ctx, launch_behind_plan(ctx, stream, compact_kernel, v, ws), "cache_compact");
 }
 
 }  // extern "C"
