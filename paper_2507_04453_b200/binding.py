@@ -528,11 +528,15 @@ class KvCache:
         """essa_cache_read: (k, v) [T, kv_heads, head_dim] bf16, the last tokens of the entries' sequences as they are stored."""
         a, b, n = self._entries(T, slots, tok_offsets)
         shape = (T, self.kv_heads, self.head_dim)
-        k_out = self._empty(shape, stream) if k_out is None else k_out
-        v_out = self._empty(shape, stream) if v_out is None else v_out
-        pk, pv = self._rows("k_out", k_out, self.kv_heads)[0], self._rows("v_out", v_out, self.kv_heads)[0]
-        if k_out.shape[0] != T or v_out.shape[0] != T or not (k_out.is_contiguous() and v_out.is_contiguous()):
-            self._fail("k_out and v_out", f"contiguous tensors of {T} rows")
+        if k_out is None and v_out is None:
+            k_out, v_out = self._empty(shape, stream), self._empty(shape, stream)
+            pk, pv = k_out.data_ptr() or None, v_out.data_ptr() or None
+        else:
+            k_out = self._empty(shape, stream) if k_out is None else k_out
+            v_out = self._empty(shape, stream) if v_out is None else v_out
+            pk, pv = self._rows("k_out", k_out, self.kv_heads)[0], self._rows("v_out", v_out, self.kv_heads)[0]
+            if k_out.shape[0] != T or v_out.shape[0] != T or not (k_out.is_contiguous() and v_out.is_contiguous()):
+                self._fail("k_out and v_out", f"contiguous tensors of {T} rows")
         self._check(self._lib.essa_cache_read(self.ctx.handle, self._ref, layer, pk, pv, T, a, b, n, self._raw(stream)))
         return k_out, v_out
 
@@ -552,9 +556,11 @@ class KvCache:
             need = self._attend_ws[(heads, max_new)] = got.value
         if out is None:
             out = self._empty_like(q) if stream is None and q.is_contiguous() else self._empty(shape, stream)
-        elif out.shape != shape:
-            raise EssaError(ESSA_ERR_INVALID_ARG, "kv_cache: out must have q's shape")
-        po, ldo = self._rows("out", out, heads)
+            po, ldo = out.data_ptr() or None, heads * self.head_dim
+        else:
+            if out.shape != shape:
+                raise EssaError(ESSA_ERR_INVALID_ARG, "kv_cache: out must have q's shape")
+            po, ldo = self._rows("out", out, heads)
         raw = self._raw(stream)
         ws = self._workspace(need, raw, stream)
         self._check(self._lib.essa_cache_attend(self.ctx.handle, self._ref, layer, pq, ldq, heads, shape[0], a, b, n, max_new, self._scale if scale is None else scale,

@@ -123,7 +123,7 @@ __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_
     bool ok = true;
     while (ok && left > 0) {
       int tile, stop;
-      take_block<L>(c, left, tile, stop);
+      take_block<L>(a, c, left, tile, stop);
       const int32_t* row = a.v.table + (int64_t)max(c.info.slot, 0) * a.v.max_pages;
       const bool none = c.info.len == 0;
       for (; tile < stop; ++tile) {
@@ -159,7 +159,7 @@ __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_
   bool dead = false;  // a wait ran out: the warp goes through the barriers with the others and does nothing else
   for (; left > 0; next_block<L>(a, c)) {
     int first, stop;
-    take_block<L>(c, left, first, stop);
+    take_block<L>(a, c, left, first, stop);
     if (first == stop) break;  // (the run ends before the row block's first tile)
     const int rows = c.info.rows * a.group;  // (fits: T * group is checked on the host)
     const int r0 = c.rb * R;
@@ -508,6 +508,7 @@ int32_t launch(essa_ctx* ctx, AttendArgs& a, cudaStream_t stream) {
   using S = Shape<D, NT>;
   const int grid = ctx->sm_count * attend_blocks_per_sm(D, NT);
   a.partials_at = partials_at(grid);
+  a.whole = whole_blocks(a, S::R, grid);
   cudaError_t e = allow_shared<attend_decode_kernel<D, NT>>(S::kSmem, ctx->device);
   if (e != cudaSuccess) return check_cuda(ctx, e, "cudaFuncSetAttribute (attend)");
   attend_decode_kernel<D, NT><<<grid, kThreads, S::kSmem, stream>>>(a);

@@ -3,6 +3,7 @@
 // results (O, maximum, sum per row, fp32) in the workspace, two slots per run at most, and attend_join_kernel adds them in
 // run order.  Ragged lengths, causal prompts and single long sequences balance alike, results do not depend on timing, and
 // the workspace is bounded by the grid.
+// Where sequences are short and row blocks few (whole_blocks), cuts move to the row blocks' ends instead: nothing is left to join.
 // A row block also costs its queries' way in and its results' way out, so it stands in the list as kSetup elements without work,
 // followed by its key tiles; a cut between those leaves it whole to the run behind the cut.
 //
@@ -42,6 +43,7 @@ struct AttendArgs {
   float scale;  // softmax scale * log2(e)
   float* ws;
   int64_t partials_at;  // floats before the partial results
+  int32_t whole;        // a run has the row blocks that begin in it, to their ends
   int32_t* status;
 };
 
@@ -49,6 +51,16 @@ struct AttendArgs {
 constexpr int64_t kRunPlaceBytes = 40;
 inline int64_t partials_at(int grid) { return (kRunPlaceBytes * grid + 255) / 256 * 64; }
 inline int64_t attend_workspace(int grid, int64_t floats) { return (partials_at(grid) + (int64_t)grid * 2 * floats) * 4; }
+
+// Whether a call is divided between row blocks (of R rows) only: there are no more of them than thread blocks, and no sequence has more than
+// kWholePages pages.  Cut anywhere and joined / cut between row blocks, us in a graph: a token of 4 sequences, 2 kv heads of 64: 2 pages 7.6 / 4.8,
+// 8 pages 7.6 / 6.5, 16 pages 8.2 / 9.3; of 16 sequences, 4 heads of 128: 10 / 7, 11 / 9, 12.5 / 15; 30 tokens of 2 sequences, 8 heads of 128: 16 / 14,
+// 28 / 22, 29.5 / 31.5.  A launch less on the host, too (13 -> 10 us a call).
+constexpr int kWholePages = 8;
+inline bool whole_blocks(const AttendArgs& a, int R, int grid) {
+  const int64_t by_rows = (int64_t)a.e.T * ((a.group + R - 1) / R), by_entries = (int64_t)a.e.T * a.group / R + a.e.n;  // row blocks of a kv head: at most these
+  return a.v.max_pages <= kWholePages && (by_rows < by_entries ? by_rows : by_entries) * a.v.kv_heads <= grid;
+}
 
 #ifdef __CUDACC__
 // 2^x by the special function unit (results below the normal range are 0, which no weight notices).
@@ -123,6 +135,8 @@ struct RunShared {
 // This thread block's run: its first element's place and its length (0: none); all threads of the block.  Every thread sums a stretch
 // of the entries; the one whose stretch holds the place walks it again.
 template <class L>
+__device__ __forceinline__ void next_block(const AttendArgs& a, Cursor& c);
+template <class L>
 __device__ long long find_run(const AttendArgs& a, Cursor& c, RunShared& sm) {
   const int per = (a.e.n + blockDim.x - 1) / blockDim.x, lo = min((int)threadIdx.x * per, a.e.n), hi = min(lo + per, a.e.n);
   long long sum = 0, total;
@@ -156,6 +170,12 @@ __device__ long long find_run(const AttendArgs& a, Cursor& c, RunShared& sm) {
   long long rest = sm.rest % per_head;
   for (c.rb = 0; (c.tiles = L::tiles(c.info, a, c.rb)) + L::kSetup <= rest; ++c.rb) rest -= c.tiles + L::kSetup;
   c.at = (int)rest;
+  if (a.whole) {  // (attend_join_kernel does not run)
+    if (c.at == 0) return end - begin;
+    const long long left = end - begin - (c.tiles + L::kSetup - c.at);
+    if (left > 0) next_block<L>(a, c);
+    return max(left, 0LL);
+  }
   if (threadIdx.x == 0) {  // for attend_join_kernel
     RunPlace p;
     p.total = total;
@@ -175,8 +195,8 @@ __device__ long long find_run(const AttendArgs& a, Cursor& c, RunShared& sm) {
 // Takes what is left of c's row block from a run that has `left` elements to go: key tiles first .. stop - 1 (none, if the run ends
 // before the first) are the run's.
 template <class L>
-__device__ __forceinline__ void take_block(const Cursor& c, long long& left, int& first, int& stop) {
-  const int n = (int)min((long long)(c.tiles + L::kSetup - c.at), left);
+__device__ __forceinline__ void take_block(const AttendArgs& a, const Cursor& c, long long& left, int& first, int& stop) {
+  const int all = c.tiles + L::kSetup - c.at, n = a.whole ? all : (int)min((long long)all, left);
   first = max(c.at - L::kSetup, 0);
   stop = max(c.at + n - L::kSetup, 0);
   left -= n;
@@ -293,7 +313,7 @@ cudaError_t allow_shared(int bytes, int device) {
 
 template <class L, int D>
 int32_t launch_join(essa_ctx* ctx, const AttendArgs& a, int grid, int row_split, cudaStream_t stream) {
-  if (grid < 2) return ESSA_OK;
+  if (grid < 2 || a.whole) return ESSA_OK;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(grid - 1, row_split);
   cfg.blockDim = dim3(128);

@@ -231,7 +231,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
         for (;; next_block<L>(a, c)) {
           if (left <= 0) return false;
           int stop;
-          take_block<L>(c, left, b.first, stop);
+          take_block<L>(a, c, left, b.first, stop);
           b.n = stop - b.first;
           if (b.n == 0) return false;  // (the run ends before the row block's first tile)
           b.whole = b.first == 0 && stop == c.tiles;
@@ -470,7 +470,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
         bool ok = true;
         while (ok && left > 0) {
           int first, stop;
-          take_block<L>(c, left, first, stop);
+          take_block<L>(a, c, left, first, stop);
           if (first == stop) break;  // (the run ends before the row block's first tile)
           const int pages = (c.info.len + kPageTokens - 1) / kPageTokens;
           const int32_t* row = a.v.table + (int64_t)max(c.info.slot, 0) * a.v.max_pages;
@@ -515,7 +515,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
         };
         while (ok && left > 0) {
           int first, stop;
-          take_block<L>(c, left, first, stop);
+          take_block<L>(a, c, left, first, stop);
           const int n = stop - first, halves = c.info.rows * a.group - c.rb * L::R > 128 ? 2 : 1;
           if (n == 0) break;
           // Products with K run two tiles ahead: the scores of a half's next tile are there when its softmax has finished one.
@@ -577,7 +577,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
           Cursor c = places[warp].c;
           long long left = places[warp].left;
           if (left <= 0) break;
-          take_block<L>(c, left, j, stop);
+          take_block<L>(a, c, left, j, stop);
           len = c.info.len;
           if (left > 0) next_block<L>(a, c);
           keep_place(c, left);
@@ -637,6 +637,7 @@ template <int D>
 int32_t launch(essa_ctx* ctx, AttendArgs& a, cudaStream_t stream) {
   constexpr int smem = Mem<D>::kBytes + 1024;
   a.partials_at = partials_at(ctx->sm_count);
+  a.whole = whole_blocks(a, TileList::R, ctx->sm_count);
   cudaError_t e = allow_shared<attend_tiles_kernel<D>>(smem, ctx->device);
   if (e != cudaSuccess) return check_cuda(ctx, e, "cudaFuncSetAttribute (attend tiles)");
   attend_tiles_kernel<D><<<ctx->sm_count, kThreads, smem, stream>>>(a);
