@@ -508,7 +508,7 @@ int32_t launch(essa_ctx* ctx, AttendArgs& a, cudaStream_t stream) {
   using S = Shape<D, NT>;
   const int grid = ctx->sm_count * attend_blocks_per_sm(D, NT);
   a.partials_at = partials_at(grid);
-  a.whole = whole_blocks(a, S::R, grid);
+  a.whole = whole_blocks<DecodeList<S::R>>(a, grid);
   cudaError_t e = allow_shared<attend_decode_kernel<D, NT>>(S::kSmem, ctx->device);
   if (e != cudaSuccess) return check_cuda(ctx, e, "cudaFuncSetAttribute (attend)");
   attend_decode_kernel<D, NT><<<grid, kThreads, S::kSmem, stream>>>(a);

@@ -3,7 +3,7 @@
 // results (O, maximum, sum per row, fp32) in the workspace, two slots per run at most, and attend_join_kernel adds them in
 // run order.  Ragged lengths, causal prompts and single long sequences balance alike, results do not depend on timing, and
 // the workspace is bounded by the grid.
-// Where sequences are short and row blocks few (whole_blocks), cuts move to the row blocks' ends instead: nothing is left to join.
+// Where that is cheaper (whole_blocks), cuts move to the row blocks' ends instead: nothing is left to join.
 // A row block also costs its queries' way in and its results' way out, so it stands in the list as kSetup elements without work,
 // followed by its key tiles; a cut between those leaves it whole to the run behind the cut.
 //
@@ -52,14 +52,20 @@ constexpr int64_t kRunPlaceBytes = 40;
 inline int64_t partials_at(int grid) { return (kRunPlaceBytes * grid + 255) / 256 * 64; }
 inline int64_t attend_workspace(int grid, int64_t floats) { return (partials_at(grid) + (int64_t)grid * 2 * floats) * 4; }
 
-// Whether a call is divided between row blocks (of R rows) only: there are no more of them than thread blocks, and no sequence has more than
-// kWholePages pages.  Cut anywhere and joined / cut between row blocks, us in a graph: a token of 4 sequences, 2 kv heads of 64: 2 pages 7.6 / 4.8,
-// 8 pages 7.6 / 6.5, 16 pages 8.2 / 9.3; of 16 sequences, 4 heads of 128: 10 / 7, 11 / 9, 12.5 / 15; 30 tokens of 2 sequences, 8 heads of 128: 16 / 14,
-// 28 / 22, 29.5 / 31.5.  A launch less on the host, too (13 -> 10 us a call).
-constexpr int kWholePages = 8;
-inline bool whole_blocks(const AttendArgs& a, int R, int grid) {
-  const int64_t by_rows = (int64_t)a.e.T * ((a.group + R - 1) / R), by_entries = (int64_t)a.e.T * a.group / R + a.e.n;  // row blocks of a kv head: at most these
-  return a.v.max_pages <= kWholePages && (by_rows < by_entries ? by_rows : by_entries) * a.v.kv_heads <= grid;
+// Whether a call is divided between row blocks only.  Cut anywhere, all thread blocks end together, but partial results are written, read and
+// joined, which costs about as much as kJoin key tiles; cut between row blocks, the last round leaves some idle for a row block's length (for
+// many rounds, of lengths that vary, half of them).  Lengths are known on the host as an upper bound only, hence kWholePages.
+// Cut anywhere / between row blocks, us in a graph, heads of 128 channels: one token of 16 sequences, 4 kv heads: 2 pages 10 / 7, 8 pages 11 / 9,
+// 16 pages 12.5 / 15; of 50, 8 heads: 13.9 / 8.4, 19.1 / 13.4, 25.2 / 19.9; of 256, 4 heads: 19.8 / 16.6, 32.2 / 29.9, 49.2 / 49.5, 32 pages 79 / 83;
+// 64 tokens of 15 sequences, 8 kv heads of 5: 33 / 21, 55 / 34, 70 / 51, 96 / 83; prompts of 1 .. 1024 tokens of 64: 498 / 479.
+// (A launch less on the host, too: 13 -> 10 us a call.)
+constexpr int kWholePages = 32, kJoin = 16;
+template <class L>
+bool whole_blocks(const AttendArgs& a, int grid) {
+  const int64_t by_rows = (int64_t)a.e.T * ((a.group + L::R - 1) / L::R), by_entries = (int64_t)a.e.T * a.group / L::R + a.e.n;
+  const int64_t blocks = (by_rows < by_entries ? by_rows : by_entries) * a.v.kv_heads;  // at most
+  const int64_t idle = blocks > 4 * (int64_t)grid ? grid / 2 : (blocks + grid - 1) / grid * grid - blocks;
+  return a.v.max_pages <= kWholePages && idle * (a.v.max_pages + L::kSetup) <= (int64_t)kJoin * grid;
 }
 
 #ifdef __CUDACC__

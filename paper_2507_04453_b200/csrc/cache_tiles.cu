@@ -637,7 +637,7 @@ template <int D>
 int32_t launch(essa_ctx* ctx, AttendArgs& a, cudaStream_t stream) {
   constexpr int smem = Mem<D>::kBytes + 1024;
   a.partials_at = partials_at(ctx->sm_count);
-  a.whole = whole_blocks(a, TileList::R, ctx->sm_count);
+  a.whole = whole_blocks<TileList>(a, ctx->sm_count);
   cudaError_t e = allow_shared<attend_tiles_kernel<D>>(smem, ctx->device);
   if (e != cudaSuccess) return check_cuda(ctx, e, "cudaFuncSetAttribute (attend tiles)");
   attend_tiles_kernel<D><<<ctx->sm_count, kThreads, smem, stream>>>(a);
