@@ -31,7 +31,7 @@ constexpr int KS = 2;                         // slices of 16 tokens per warp: i
 constexpr int kThreads = kWarps * 32 + 32;    // + one copying warp
 
 // Row blocks of R rows; every row block of an entry walks all its pages (the few rows of an entry see nearly the same ones).
-// kSetup: 256 sequences of up to 1024 tokens take 43.3 us with 2, 40.2 with 3, 38.8 with 5, 38.6 with 7, 39.6 with 10.
+// kSetup: 256 sequences of up to 1024 tokens take 43.3 us with 2, 40.2 with 3, 38.8 with 5, 38.6 with 7, 39.6 with 10 (cut anywhere).
 template <int ROWS>
 struct DecodeList {
   static constexpr int R = ROWS, kMinRun = 2, kSetup = 5;

@@ -9,12 +9,12 @@
 // What bounds it (heads of 128 channels): a key tile takes ~2290 cycles of an SM.  The tensor pipe counts 1024 of them as active, but the MMAs take
 // ~1800 (N = 64 makes a product with K read 6 KB of shared memory in its 32 cycles of arithmetic); the exponentials need 1024 of the special
 // function units, the warps half of the issue slots.  Two prompts of 450 tokens after 16 thousand, 64 heads (468 GFLOP): 488 us, 0.96 PFLOP/s.
-// A row block costs some six tiles beside its own (queries in, results out): ragged prompts of 1 .. 1024 tokens, 40 heads (231 GFLOP): 496 us.
-// What was tried: a thread per row (eight softmax warps): 558 us for the ragged prompts, 495 for the others; key tiles of two pages, products
+// A row block costs some six tiles beside its own (queries in, results out): ragged prompts of 1 .. 1024 tokens, 40 heads (231 GFLOP): 479 us.
+// What was tried, when the ragged prompts stood at 496: a thread per row (eight softmax warps): 558 us, and 495 for the others; key tiles of two pages, products
 // with K of N = 128 and one buffer of scores per half: 558 and 455 (the halves' softmax and products then alternate, but a tile of 128
 // keys is a coarse grain for short prompts); the same with 80 registers for the softmax instead of 96: 705 and 608;
 // an eighth, a quarter or a half of the exponentials by a polynomial on the FMA pipe: 486, 498 and 535 (issue slots are as short as the
-// special function units).
+// special function units); O through shared memory, so that stores are whole rows: 502 and 481 (an SM stores 32 bytes a cycle either way).
 //
 // Roundings: K and V become fp16 as their scale and minimum are applied, (code - 8) * scale + (minimum + 8 scale), with the offset and the
 // result rounded (2^-11 each).  Q is bf16; a row times a power of two, its largest element at 2^13 .. 2^14, is fp16 without loss (elements
@@ -30,7 +30,7 @@
 namespace essa {
 namespace {
 
-// kSetup: the ragged prompts take 738 us with 2 and 683 with 4 in the first version, 502, 497 and 500 with 6, 4 and 5 in this one.
+// kSetup: the ragged prompts take 483 us with 3, 479 with 4, 483 with 5, 493 with 6.
 struct TileList {
   static constexpr int R = 256, kKeys = kPageTokens, kMinRun = 2, kSetup = 4;
   // keys that the last row of the row block sees, in tiles
