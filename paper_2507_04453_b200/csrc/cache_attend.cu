@@ -105,7 +105,7 @@ __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_
   float* join = reinterpret_cast<float*>(smem + S::kStages * S::kBytes);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t ring = smem_u32(smem), full = smem_u32(bars), empty = full + 8 * S::kStages;
-  grid_dep_launch();
+  if (!a.whole) grid_dep_launch();  // (else the launch that follows is not the join)
   if (tid == 0) {
     abort_flag = 0;
     for (int s = 0; s < S::kStages; ++s) { mbar_init(full + 8 * s, 1); mbar_init(empty + 8 * s, 2); }

@@ -169,7 +169,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
   const uint32_t bars = base + M::kBars;
   const auto bar = [&](int i) { return bars + 8 * i; };
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  grid_dep_launch();
+  if (!a.whole) grid_dep_launch();  // (else the launch that follows is not the join)
   if (tid == 0) {
     abort_flag = 0;
     for (int i = 0; i < kRaw; ++i) { mbar_init(bar(kRawFull + i), 1); mbar_init(bar(kRawEmpty + i), kWidenWarps); }
@@ -311,6 +311,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
       // --- the next row block's Q (all products with this one's are done), while the last product with V runs
       const bool more = enter(next);
       if (b.n > 0) {
+        if (!more) pair_sync(pair);  // (the other warp has read of_part's maxima; enter has a barrier too)
         of_part[part][h * 128 + row] = sum;
         pair_sync(pair);
         sum = of_part[0][h * 128 + row] + of_part[1][h * 128 + row];

@@ -748,3 +748,34 @@ def test_second_cache_object_on_the_same_buffers(torch, ctx):
     p.cpu.grow(range(3), [1, 1, 1])
     assert ctx.get_status() == 0
     p.assert_same(pages=False)
+
+
+def test_projections_of_several_layers_right_behind_an_attention(torch, ctx):
+    """apply_layers chains its launches loosely; what stands before it on the stream (an attention without a join, one with, a fork) has ended
+    all the same when they read its output."""
+    cfg = wl.scaled_config("3", d_model=256, d_kv=128, rank=8, P=3, seg_len=40)
+    rng = np.random.default_rng(24)
+    case = Case(torch, ctx, cfg)
+    seg = torch.tensor([0, 40, 80, 120], dtype=torch.int32, device="cuda")
+    for pages in (20, 60):
+        p = Pair(torch, ctx, 1, 120 * pages, 2, 64, 120, pages)
+        p.gpu.pages.random_(0, 60)  # (small scales and minima, whatever they are)
+        p.gpu.grow(None, p.ints([pages * 64 - 3] * 120))
+        outs = [torch.empty((120, 256), dtype=torch.bfloat16, device="cuda") for _ in range(3)]
+        a = torch.empty((120, 256), dtype=torch.bfloat16, device="cuda")
+
+        def step(q, wait):
+            a.fill_(3.0)
+            p.gpu.attend(0, q, out=a)
+            if wait:
+                torch.cuda.synchronize()
+            ctx.apply_layers([[(case.handles[3], a, cfg.sigma_cols(3), o)] for o in outs], seg, case.d_sigma)
+            torch.cuda.synchronize()
+            return [o.clone() for o in outs]
+
+        for _ in range(10):
+            q = p.bf(bf16(rng, (120, 256)))
+            for x, y in zip(step(q, False), step(q, True)):
+                assert torch.equal(x, y)
+    assert ctx.get_status() == 0
+    case.close()
