@@ -131,21 +131,27 @@ __device__ __forceinline__ uint64_t desc_of(uint32_t lo) {
   return (uint64_t)hi << 32 | lo;
 }
 
+constexpr float kFp16End = 65440.f;  // (65504 less what rounding the centre and the result can add)
+
 // Eight codes -> fp16 (code - 8) * s + c in the order (0, 4, 1, 5, 2, 6, 3, 7).
 __device__ __forceinline__ uint4 widen(uint32_t w, __half2 s, __half2 c, uint32_t magic /* 0x64006400 */) {
   const uint32_t x = w >> 8;
   return make_uint4(half2_bits(__hfma2(centred_low(w, magic), s, c)), half2_bits(__hfma2(centred_high(w, magic), s, c)),
                     half2_bits(__hfma2(centred_low(x, magic), s, c)), half2_bits(__hfma2(centred_high(x, magic), s, c)));
 }
-// Scale and centre of a token's group, (scale, minimum) = m.  Values beyond +-65440 are brought there: what fp16 rounds them to
-// has to stay finite.
-__device__ __forceinline__ void scale_of(float2 m, __half2& s, __half2& c) {
-  if (m.y < -65440.f) m.y = -65440.f;
-  if (fmaf(15.f, m.x, m.y) > 65440.f) m.x = (65440.f - m.y) * (1.f / 15.01f);
-  s = __float2half2_rn(m.x);
-  c = __float2half2_rn(fmaf(8.f, m.x, m.y));
+// Whether some code of a token's group, (scale, minimum) = m, stands for a value beyond +-65440 (false for a minimum of NaN).
+__device__ __forceinline__ bool beyond_fp16(float2 m) { return m.y < -kFp16End || fmaf(15.f, m.x, m.y) > kFp16End; }
+// The same order for such a group (seldom): every value for itself, in fp32, brought to +-65440, what fp16 rounds it to being finite there.
+// (The centre of such a group can lie outside fp16 as well.  Changing the scale or the minimum instead would move its other values.)
+__device__ __forceinline__ uint4 widen_clipped(uint32_t w, float2 m) {
+  uint32_t r[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float lo = fmaf((float)(w >> (4 * i) & 15u), m.x, m.y), hi = fmaf((float)(w >> (4 * i + 16) & 15u), m.x, m.y);
+    r[i] = pack_f16x2(fminf(fmaxf(lo, -kFp16End), kFp16End), fminf(fmaxf(hi, -kFp16End), kFp16End));
+  }
+  return make_uint4(r[0], r[1], r[2], r[3]);
 }
-
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a) {
   using M = Mem<D>;
@@ -605,20 +611,23 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
           if (++slot == kRaw) { slot = 0; phase ^= 1; }
           if (tile >= kRing && !(ok = wait_warp(kTileEmpty + st, reuse))) break;
           if (wt == 0) tile_bad[tile & 7] = bad;
-          __half2 ms, mc;
-          if (!in) mk = make_float2(0.f, 0.f);
-          scale_of(mk, ms, mc);
+          if (!in) mk = mv = make_float2(0.f, 0.f);
+          const auto put = [&](uint32_t dst, const uint4 (&codes)[kWords / 4], float2 m) {
+            const __half2 s = __float2half2_rn(m.x), c = __float2half2_rn(fmaf(8.f, m.x, m.y));
 #pragma unroll
-          for (int i = 0; i < kWords; ++i) {
-            const uint32_t w = in ? (&ck[i / 4].x)[i % 4] : 0x88888888u;
-            sts_v4(k_dst + (((word0 + i) ^ sw) << 4), widen(w, ms, mc, magic));
-          }
-          if (!in) mv = make_float2(0.f, 0.f);
-          scale_of(mv, ms, mc);
+            for (int i = 0; i < kWords; ++i) sts_v4(dst + (((word0 + i) ^ sw) << 4), widen(in ? (&codes[i / 4].x)[i % 4] : 0x88888888u, s, c, magic));
+          };
+          const auto put_clipped = [&](uint32_t dst, const uint4 (&codes)[kWords / 4], float2 m) {
 #pragma unroll
-          for (int i = 0; i < kWords; ++i) {
-            const uint32_t w = in ? (&cv[i / 4].x)[i % 4] : 0x88888888u;
-            sts_v4(v_dst + (((word0 + i) ^ sw) << 4), widen(w, ms, mc, magic));
+            for (int i = 0; i < kWords; ++i) sts_v4(dst + (((word0 + i) ^ sw) << 4), widen_clipped((&codes[i / 4].x)[i % 4], m));
+          };
+          const bool clip = __any_sync(0xffffffffu, beyond_fp16(mk) | beyond_fp16(mv));
+          put(k_dst, ck, mk);
+          put(v_dst, cv, mv);
+          // (written again, not instead, and by a vote: ragged prompts 488 us without this, 492 so, 497 with a branch per thread, 512 with one around `put`)
+          if (clip) {
+            if (beyond_fp16(mk)) put_clipped(k_dst, ck, mk);
+            if (beyond_fp16(mv)) put_clipped(v_dst, cv, mv);
           }
           fence_proxy_async_smem();
           __syncwarp();

@@ -113,3 +113,17 @@ def attend_bound(q, v, codes, scale, out, p, softmax_scale, k):
         tol[:, h] = (2.0 ** -8 * np.abs(out[:, h]) + 2.0 ** -11 * (ph @ np.abs(centred[1])) + 2.0 ** -11 * (ph @ (2 * vh + np.abs(offset[1])))
                      + 2.0 ** -24 * 8 * ((ph > 0).sum(-1) * s[1].max(initial=0.0))[:, None] + 2.0 ** -25 * (ph > 0).astype(float) @ vh + (np.expm1(2 * err)[:, None] + 2.0 ** -16) * (ph @ vh) + 1e-30)
     return tol
+
+
+# How far a row of one head may be from the fp64 result by norm, for keys, values and queries without a common direction (N(0, 1) and the like)
+# and scores of a few units.  out is rounded to bf16 once: 2^-8 of every element at most, so 2^-8 of the norm.  What else is rounded belongs to one
+# key each (its weight, its value, its score: 2^-11 of them, scores of a few units to less than 2^-11) and is as independent from key to key as
+# the keys' contributions to the result are: whatever their number, sqrt(3) 2^-11 of the norm, taken as 2^-10.  Unlike attend_bound, which adds
+# the worst cases, this does not grow with the number of keys: a page of 64 among n equal ones is sqrt(64 / n) of the norm.
+NORM_LIMIT = 2.0 ** -8 + 2.0 ** -10
+
+
+def norm_error(got, want):
+    """|got - want| / |want| of every row and head; a row that sees nothing (want 0) has to be 0."""
+    a, b = np.linalg.norm(got.astype(np.float64) - want, axis=-1), np.linalg.norm(want, axis=-1)
+    return np.where(b > 0, a / np.where(b > 0, b, 1), np.where(a > 0, np.inf, 0.0))

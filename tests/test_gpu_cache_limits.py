@@ -1,0 +1,63 @@
+"""GPU tests of the paged 4-bit key / value cache where its limits lie: stored values beyond fp16, tables that are damaged, long sequences."""
+import numpy as np
+import pytest
+
+from oracle import cache_oracle as co
+from paper_2507_04453_b200 import binding
+from tests.cache_utils import NORM_LIMIT, Pair, attend_bound, bf16, norm_error
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def torch():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.fail("CUDA device required for -m gpu tests")
+    return torch
+
+
+@pytest.fixture(scope="module")
+def ctx(torch):
+    c = binding.Context(0)
+    yield c
+    assert c.get_status() == 0
+    c.close()
+
+
+# ------------------------------------------------------------------------------------------------ values beyond fp16
+# (minimum, scale) on both sides of +-65440: inside, the largest inside, above it, far above it, below it, on both sides
+RANGES = [(-2.5, 0.3), (20000, 3028), (-60000, 12000), (0, 65504), (-65504, 4000), (-65504, 12000), (65504, 0), (65440, 0)]
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("hint", [1, 100])
+@pytest.mark.parametrize("where", ["k", "v", "both"])
+def test_stored_values_beyond_fp16(torch, ctx, where, hint, d):
+    """A value beyond +-65440 counts as it is (few rows) or as +-65440 (many rows); its neighbours in the group are what they are."""
+    rng = np.random.default_rng(30)
+    p = Pair(torch, ctx, 1, 8, 2, d, 2, 4)
+    p.place([200, 70], rng)
+    for half, name in enumerate("kv"):
+        if where not in (name, "both"):
+            continue
+        kind = rng.integers(0, len(RANGES), p.cpu.scale[:, :, :, half].shape)
+        stale = np.isnan(p.cpu.low[:, :, :, half])
+        for a, i in ((p.cpu.low, 0), (p.cpu.scale, 1)):
+            a[:, :, :, half] = np.where(stale, a[:, :, :, half], np.array(RANGES, np.float16)[kind, i])
+        p.cpu.codes[:, :, :, half] = rng.integers(0, 16, p.cpu.codes[:, :, :, half].shape)
+    p.push()
+    off, q = [0, 30, 60], bf16(rng, (60, 4, d))
+    scale = d ** -0.5 / (1 if where == "v" else 2e5)  # (scores of a few units)
+    got = p.gpu.attend(0, p.bf(q), p.ints(off), max_new=hint, scale=scale).float().cpu().numpy()
+    assert ctx.get_status() == 0 and np.isfinite(got).all()
+    for s in range(2):
+        k, v, codes, sc = p.cpu.sequence(0, s)
+        if hint > 1:
+            k, v = np.clip(k, -65440, 65440), np.clip(v, -65440, 65440)
+        mine, out = q[off[s]:off[s + 1]], got[off[s]:off[s + 1]]
+        want, w = co.attend(mine, k, v, int(p.cpu.lengths[s]), scale)
+        err = np.abs(out - want)
+        tol = attend_bound(mine, v, codes, sc, want, w, scale, k)
+        assert (err <= tol).all(), float(np.max(err / tol))
+        assert norm_error(out, want).max() <= NORM_LIMIT, float(norm_error(out, want).max())
