@@ -401,7 +401,10 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
         const uint32_t s_at = scores_at(tile);
         uint32_t p[16];
         float s0, s1;
-        bool look = j == 0;  // for the maximum, before the weights: in the first tile, and where the weights by the one so far turn out too large
+        // Whether to look for the maximum before the weights: in the first tile, and where the weights by the one so far turn out too large or
+        // there is none yet though the row sees the tile (the pages before are not there): weights by 0 could then all vanish.  (A row's two
+        // threads have the same m and limit, so the two warps decide alike.)
+        bool look = j == 0 || __any_sync(0xffffffffu, m == -INFINITY && b.limit > (b.first + j) * L::kKeys);
         for (;;) {
           uint32_t v[32];
           tmem_ld32_issue(s_at + 32 * part, v);
@@ -411,6 +414,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
 #pragma unroll
             for (int i = 0; i < 32; i += 2) t[i >> 1 & 3] = max3(t[i >> 1 & 3], __uint_as_float(v[i]), __uint_as_float(v[i + 1]));
             float top = max3(max3(t[0], t[1], t[2]), t[3], t[3]);
+            if (j > 0) pair_sync(pair);  // (the other warp has read what the tile before left in of_part)
             of_part[part][h * 128 + row] = top;
             tc_fence_before();
             pair_sync(pair);
@@ -452,7 +456,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
           // (The barrier, here or above, also stands between the other warp's reading of its scores and P, which goes where they are.)
           if (look) break;
           tc_fence_before();
-          const bool again = pair_any(pair, s0 > 16384.f || (m == -INFINITY && s0 > 0.f));
+          const bool again = pair_any(pair, s0 > 16384.f);
           tc_fence_after();
           if (!again) break;
           look = true;

@@ -61,3 +61,35 @@ def test_stored_values_beyond_fp16(torch, ctx, where, hint, d):
         tol = attend_bound(mine, v, codes, sc, want, w, scale, k)
         assert (err <= tol).all(), float(np.max(err / tol))
         assert norm_error(out, want).max() <= NORM_LIMIT, float(norm_error(out, want).max())
+
+
+# ------------------------------------------------------------------------------------------------ damaged tables
+@pytest.mark.parametrize("hint", [1, 100])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("rows,bad", [(1, [0]), (30, [0]), (30, [0, 1]), (20, [0, 2]), (70, [0])])
+def test_pages_that_are_not_there_before_scores_far_below_zero(torch, ctx, rows, bad, d, hint):
+    """A sequence whose first pages are missing and whose scores all lie where e^score is no fp32 number: the softmax of what is left.  Keys are
+    whole numbers and queries multiples of 1/4, so that the scores (-128 and a few units) are sums of numbers that the products hold exactly."""
+    rng = np.random.default_rng(31)
+    p = Pair(torch, ctx, 1, 20, 1, d, 2, 8)
+    p.place([340, 90], rng)
+    here = ~np.isnan(p.cpu.low[0, :, :, 0, :, 0])                    # tokens of the two sequences
+    codes = rng.integers(0, 16, p.cpu.codes[0, :, :, 0].shape)
+    codes[..., np.arange(d) % 64 < 32] = 0                            # half of every group is -8
+    p.cpu.codes[0, :, :, 0][here] = codes[here]
+    p.cpu.scale[0, :, :, 0][here], p.cpu.low[0, :, :, 0][here] = 1, -8
+    p.push()
+    p.gpu.table[0, p.ints(bad).long()] = 20
+    q = np.where(np.arange(d) % 64 < 32, 4.0, rng.integers(-2, 3, (2 * rows, 4, d)) / 4).astype(np.float32)
+    scale = 8 / d
+    got = p.gpu.attend(0, p.bf(q), p.ints([0, rows, 2 * rows]), max_new=hint, scale=scale).float().cpu().numpy()
+    assert ctx.get_status() == binding.ESSA_ERR_CACHE
+    for s, mine, out in ((0, q[:rows], got[:rows]), (1, q[rows:], got[rows:])):
+        k, v, codes, sc = p.cpu.sequence(0, s)
+        n = k.shape[1]
+        keep = np.array([i for i in range(n) if s or i // co.PAGE not in bad])
+        for j in range(rows):  # (row by row: the tokens that it sees are not a row's number away from a common end)
+            see = keep[keep < n - rows + j + 1]
+            want, w = co.attend(mine[j:j + 1], k[:, see], v[:, see], len(see), scale)
+            tol = attend_bound(mine[j:j + 1], v[:, see], codes[:, :, see], sc[:, :, see], want, w, scale, k[:, see])
+            assert (np.abs(out[j:j + 1] - want) <= tol).all() and norm_error(out[j:j + 1], want).max() <= NORM_LIMIT, (s, j)
