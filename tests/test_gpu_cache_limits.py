@@ -93,3 +93,58 @@ def test_pages_that_are_not_there_before_scores_far_below_zero(torch, ctx, rows,
             want, w = co.attend(mine[j:j + 1], k[:, see], v[:, see], len(see), scale)
             tol = attend_bound(mine[j:j + 1], v[:, see], codes[:, :, see], sc[:, :, see], want, w, scale, k[:, see])
             assert (np.abs(out[j:j + 1] - want) <= tol).all() and norm_error(out[j:j + 1], want).max() <= NORM_LIMIT, (s, j)
+
+
+def damaged(torch, ctx, entry):
+    """Five sequences, two of them on a shared page, and a table entry that names no page in use."""
+    p = Pair(torch, ctx, 2, 12, 1, 64, 6, 5)
+    p.place([70, 64 + 10, 64, 10, 1, 0], np.random.default_rng(32))
+    p.gpu.fork(p.ints([1]), p.ints([5]))
+    p.cpu.fork([1], [5])
+    free = int(np.flatnonzero(p.cpu.refs == 0)[-1])
+    value = {"behind": 12, "far-behind": 1 << 30, "negative": -2, "free": free, "far-negative": -(1 << 31)}[entry]
+    return p, value
+
+
+ENTRIES = ["behind", "far-behind", "negative", "far-negative", "free"]
+
+
+@pytest.mark.parametrize("entry", ENTRIES)
+@pytest.mark.parametrize("at", [(0, 1), (3, 0), (3, 4)])
+def test_free_of_a_damaged_row_changes_nothing(torch, ctx, entry, at):
+    p, value = damaged(torch, ctx, entry)
+    p.cpu.table[at] = value
+    p.push()
+    p.gpu.free(p.ints([5, 0, 1, 3]))
+    assert ctx.get_status() == binding.ESSA_ERR_CACHE
+    p.assert_same()
+    slots = [s for s in (5, 1, 4) if s != at[0]]  # the other sequences can still be freed
+    p.gpu.free(p.ints(slots))
+    p.cpu.free(slots)
+    assert ctx.get_status() == 0
+    p.assert_same()
+
+
+@pytest.mark.parametrize("n,max_pages", [(1, 1), (1, 5000), (40, 700), (1400, 9), (3000, 40)])
+def test_free_sees_damage_in_any_row(torch, ctx, n, max_pages):
+    """From one entry to more than the thread blocks look at in one round: refused for a bad entry at the start, in between, at the end; done without."""
+    p = Pair(torch, ctx, 1, 9000, 1, 64, n, max_pages)
+    rng = np.random.default_rng(n + max_pages)
+    counts = rng.integers(0, min(64 * max_pages, 64 * 8000 // n) + 1, n)
+    p.gpu.grow(None, p.ints(counts))
+    p.cpu.grow(range(n), counts)
+    assert ctx.get_status() == 0
+    slots = rng.permutation(n)
+    for i, j in ((0, 0), (n // 2, max_pages // 2), (n - 1, max_pages - 1), (int(rng.integers(n)), int(rng.integers(max_pages)))):
+        at = (slots[i], j)
+        keep, p.cpu.table[at] = p.cpu.table[at], 9000
+        p.gpu.table.copy_(torch.from_numpy(p.cpu.table))
+        p.gpu.free(p.ints(slots))
+        assert ctx.get_status() == binding.ESSA_ERR_CACHE
+        p.assert_same(pages=False)
+        p.cpu.table[at] = keep
+    p.gpu.table.copy_(torch.from_numpy(p.cpu.table))
+    p.gpu.free(p.ints(slots))
+    p.cpu.free(slots)
+    assert ctx.get_status() == 0
+    p.assert_same(pages=False)
