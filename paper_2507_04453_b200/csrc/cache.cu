@@ -477,12 +477,13 @@ __global__ void __launch_bounds__(kPlanThreads) fork_plan_kernel(CacheView v, co
       want += total;
     }
     ok = __syncthreads_and(fine);
-    if (ok) {  // every page that will be shared or copied is a page
+    if (ok) {  // every page that will be shared or copied, and every one that the destinations hold, is a page in use
       for (int i = threadIdx.x >> 5; i < n; i += blockDim.x >> 5) {
         const int32_t* row = v.table + (int64_t)src[i] * v.max_pages;
         const int pages = pages_of(lens ? lens[i] : v.lengths[src[i]]);
-        for (int j = threadIdx.x & 31; j < pages; j += 32) fine = fine && row[j] >= 0 && row[j] < v.num_pages;
+        for (int j = threadIdx.x & 31; j < pages; j += 32) fine &= holders(v, row[j]) > 0;
       }
+      fine &= rows_sound(v, dst, n, threadIdx.x, blockDim.x);
       ok = __syncthreads_and(fine) && want <= v.num_pages;
     }
   }

@@ -148,3 +148,35 @@ def test_free_sees_damage_in_any_row(torch, ctx, n, max_pages):
     p.cpu.free(slots)
     assert ctx.get_status() == 0
     p.assert_same(pages=False)
+
+
+@pytest.mark.parametrize("entry", ENTRIES)
+@pytest.mark.parametrize("at", [(0, 1), (3, 0), (3, 4), (4, 0)])
+def test_fork_between_damaged_rows_changes_nothing(torch, ctx, entry, at):
+    """A source's page (0, 1), a destination's page (3, 0) and what stands behind its pages (3, 4): refused; a row that the fork does not touch: done."""
+    p, value = damaged(torch, ctx, entry)
+    p.cpu.table[at] = value
+    p.push()
+    p.gpu.fork(p.ints([0, 1]), p.ints([3, 2]))
+    if at[0] == 4:
+        p.cpu.fork([0, 1], [3, 2])
+        assert ctx.get_status() == 0
+    else:
+        assert ctx.get_status() == binding.ESSA_ERR_CACHE
+    p.assert_same()
+
+
+def test_fork_looks_only_at_the_pages_that_it_takes(torch, ctx):
+    """Damage behind the tokens that are forked does not matter; in the last of them it does."""
+    for value in (12, -2):
+        p = Pair(torch, ctx, 1, 12, 1, 64, 3, 5)
+        p.place([200, 70, 0], np.random.default_rng(33))
+        p.cpu.table[0, 3] = value
+        p.push()
+        p.gpu.fork(p.ints([0]), p.ints([1]), p.ints([192]))
+        p.cpu.fork([0], [1], [192])
+        assert ctx.get_status() == 0
+        p.assert_same()
+        p.gpu.fork(p.ints([0]), p.ints([1]), p.ints([193]))
+        assert ctx.get_status() == binding.ESSA_ERR_CACHE
+        p.assert_same()
