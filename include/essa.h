@@ -391,10 +391,15 @@ int32_t essa_apply_projection_simt(essa_ctx* ctx, const essa_adapter* adapter, c
  * may read them at any time; they are device-resident, so that a whole decode step (grow, append, attend) can be captured
  * into a CUDA graph and replayed while the sequences grow.
  *
- * Errors that only the device can see (a slot outside the cache, the same slot twice, a length beyond the table, a page
- * outside the pool, too few free pages) are recorded as ESSA_ERR_CACHE in the status word that essa_get_status reads.
- * essa_cache_grow, _fork, _free and _compact then change nothing at all; _append and _read skip the tokens in
- * question; _attend treats tokens on a bad page as hidden.
+ * Errors that only the device can see are recorded as ESSA_ERR_CACHE in the status word that essa_get_status reads.  The calls on pages look at
+ * all that they use first, and then change nothing at all if a slot lies outside the cache or is named twice (a fork's sources may be), and
+ *   essa_cache_grow     if a count is negative, a length is negative or becomes longer than the table, or there are too few free pages;
+ *   essa_cache_fork     if a dst is a src, lens[i] is negative or more than the source holds, there are too few free pages, a page that a source
+ *                       shares or that is copied is not a page in use (one of the pool, with refs > 0), or a destination's table row holds
+ *                       anything but pages in use and -1;
+ *   essa_cache_free     if a row of the table holds anything but pages in use and -1;
+ *   essa_cache_compact  if any row does (*used is not written then).
+ * _append and _read skip the tokens whose slot or page is bad, _attend treats them as hidden; the other tokens are stored, read and seen as ever.
  *
  * Entries.  append, read and attend work on n entries: entry i stands for rows tok_offsets[i] .. tok_offsets[i + 1] - 1 of
  * the token-major buffers (T rows in all; tok_offsets NULL: n = T, one row each) and belongs to sequence slots[i] (slots

@@ -246,10 +246,14 @@ __global__ void __launch_bounds__(256) read_kernel(CacheView v, CacheEntries e, 
 
 // ------------------------------------------------------------------------------------------------ pages
 // The plan of a page operation, in the caller's workspace.
+constexpr int kCheckBlocks = 60;  // thread blocks that look at the table beside compact's plan, at most
 struct PlanHead {
   int32_t ok;      // 0: refused, nothing may change
   int32_t copies;  // pages to copy (from[i] -> to[i], in every layer)
+  int32_t used;    // compact: pages in use
+  int32_t sound[kCheckBlocks];  // compact: whether each of those thread blocks found its share of the table in order
 };
+static_assert(sizeof(PlanHead) <= 256, "");
 struct PlanSpace {
   PlanHead* head;
   int32_t *from, *to;  // [num_pages] each
@@ -562,8 +566,15 @@ __global__ void __launch_bounds__(256) fork_kernel(CacheView v, const int32_t* s
   copy_pages(v, ws, ws.head->copies);
 }
 
-__global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(CacheView v, PlanSpace ws, int32_t* used_out) {
+// Thread block 0 plans, from the counts of the pages; the others look at the table, so that the kernel behind this one can tell before it
+// changes anything whether an entry names no page in use (nothing is changed here).
+__global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(CacheView v, PlanSpace ws) {
   grid_dep_launch();
+  if (blockIdx.x > 0) {
+    const bool sound = __syncthreads_and(rows_sound(v, nullptr, v.max_seqs, (blockIdx.x - 1) * kPlanThreads + threadIdx.x, (gridDim.x - 1) * kPlanThreads));
+    if (threadIdx.x == 0) ws.head->sound[blockIdx.x - 1] = sound;
+    return;
+  }
   __shared__ long long scan_sm[33];
   long long used = 0;
   for (int base = 0; base < v.num_pages; base += blockDim.x) {
@@ -586,26 +597,31 @@ __global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(CacheView v,
     movers += total & 0xffffffff;
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < movers; i += blockDim.x) {
+  for (int i = threadIdx.x; i < movers; i += blockDim.x) ws.extra[ws.from[i]] = ws.to[i];
+  if (threadIdx.x == 0) {
+    ws.head->copies = (int)movers;
+    ws.head->used = (int)used;
+  }
+}
+__global__ void __launch_bounds__(256) compact_kernel(CacheView v, PlanSpace ws, int checks, int32_t* used_out, int32_t* status) {
+  grid_dep_wait();
+  if (!__syncthreads_and(threadIdx.x >= checks || ws.head->sound[threadIdx.x])) {
+    if (blockIdx.x == 0 && threadIdx.x == 0) cache_fault(status);
+    return;
+  }
+  if (used_out && blockIdx.x == 0 && threadIdx.x == 0) *used_out = ws.head->used;
+  const int copies = ws.head->copies;
+  if (copies == 0) return;
+  const int64_t first = (int64_t)blockIdx.x * 256 + threadIdx.x, step = (int64_t)gridDim.x * 256;
+  for (int64_t i = first; i < copies; i += step) {
     const int from = ws.from[i], to = ws.to[i];
-    ws.extra[from] = to;
     v.refs[to] = v.refs[from];
     v.refs[from] = 0;
   }
-  if (threadIdx.x == 0) {
-    ws.head->ok = 1;
-    ws.head->copies = (int)movers;
-    if (used_out) *used_out = (int)used;
-  }
-}
-__global__ void __launch_bounds__(256) compact_kernel(CacheView v, PlanSpace ws) {
-  grid_dep_wait();
-  const int copies = ws.head->copies;
-  if (copies == 0) return;
   const int64_t entries = (int64_t)v.max_seqs * v.max_pages;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < entries; i += (int64_t)gridDim.x * 256) {
+  for (int64_t i = first; i < entries; i += step) {
     const int page = v.table[i];
-    if (page >= 0 && page < v.num_pages) {
+    if (page >= 0) {
       const int to = ws.extra[page];
       if (to != page) v.table[i] = to;
     }
@@ -907,10 +923,13 @@ int32_t essa_cache_compact(essa_ctx* ctx, const essa_cache_desc* cache, int32_t*
   DeviceGuard guard(ctx->device);
   cudaStream_t stream = static_cast<cudaStream_t>(stream_v);
   const PlanSpace ws = plan_space(workspace, v);
-  compact_plan_kernel<<<1, kPlanThreads, 0, stream>>>(v, ws, used);
+  // four entries of the table for a thread, up to kCheckBlocks thread blocks
+  const int64_t want = ((int64_t)v.max_seqs * v.max_pages + 4 * kPlanThreads - 1) / (4 * kPlanThreads);
+  const int checks = want < kCheckBlocks ? (int)want : kCheckBlocks;
+  compact_plan_kernel<<<1 + checks, kPlanThreads, 0, stream>>>(v, ws);
   ESSA_TRY(launched(ctx, "cache_compact", 1));
   ++ctx->launches;
-  return check_cuda(ctx, launch_behind_plan(ctx, stream, compact_kernel, v, ws), "cache_compact");
+  return check_cuda(ctx, launch_behind_plan(ctx, stream, compact_kernel, v, ws, checks, used, ctx->d_status), "cache_compact");
 }
 
 }  // extern "C"

@@ -180,3 +180,42 @@ def test_fork_looks_only_at_the_pages_that_it_takes(torch, ctx):
         p.gpu.fork(p.ints([0]), p.ints([1]), p.ints([193]))
         assert ctx.get_status() == binding.ESSA_ERR_CACHE
         p.assert_same()
+
+
+@pytest.mark.parametrize("entry", ENTRIES)
+@pytest.mark.parametrize("at", [(0, 1), (3, 0), (3, 4), (5, 4)])
+def test_compact_of_a_damaged_table_changes_nothing(torch, ctx, entry, at):
+    p, value = damaged(torch, ctx, entry)
+    p.cpu.table[at] = value
+    p.push()
+    used = torch.full((1,), -7, dtype=torch.int32, device="cuda")
+    for u in (used, None):
+        p.gpu.compact(u)
+        assert ctx.get_status() == binding.ESSA_ERR_CACHE
+        p.assert_same()
+    assert int(used) == -7
+
+
+@pytest.mark.parametrize("n,max_pages", [(1, 1), (1, 5000), (1400, 9), (3000, 120)])
+def test_compact_sees_damage_anywhere_in_the_table(torch, ctx, n, max_pages):
+    p = Pair(torch, ctx, 1, 9000, 1, 64, n, max_pages)
+    rng = np.random.default_rng(n + max_pages)
+    counts = rng.integers(0, min(64 * max_pages, 64 * 8000 // n) + 1, n)
+    gone = rng.permutation(n)[:n // 2]
+    p.gpu.grow(None, p.ints(counts))
+    p.cpu.grow(range(n), counts)
+    p.gpu.free(p.ints(gone))
+    p.cpu.free(gone)
+    assert ctx.get_status() == 0
+    for at in ((0, 0), (n // 2, max_pages // 2), (n - 1, max_pages - 1), (int(rng.integers(n)), int(rng.integers(max_pages)))):
+        keep, p.cpu.table[at] = p.cpu.table[at], 9000
+        p.gpu.table.copy_(torch.from_numpy(p.cpu.table))
+        p.gpu.compact()
+        assert ctx.get_status() == binding.ESSA_ERR_CACHE
+        p.assert_same(pages=False)
+        p.cpu.table[at] = keep
+    p.gpu.table.copy_(torch.from_numpy(p.cpu.table))
+    used = torch.zeros(1, dtype=torch.int32, device="cuda")
+    p.gpu.compact(used)
+    assert int(used) == p.cpu.compact() and ctx.get_status() == 0
+    p.assert_same(pages=False)
