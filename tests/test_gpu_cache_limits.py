@@ -219,3 +219,23 @@ def test_compact_sees_damage_anywhere_in_the_table(torch, ctx, n, max_pages):
     p.gpu.compact(used)
     assert int(used) == p.cpu.compact() and ctx.get_status() == 0
     p.assert_same(pages=False)
+
+
+# ------------------------------------------------------------------------------------------------ long sequences
+@pytest.mark.parametrize("heads,kv_heads,d,lengths,rows,hint", [
+    (14, 2, 128, [24901, 77], [1, 1], 1), (14, 2, 128, [24901, 77], [2, 1], 2), (14, 2, 128, [24901, 77], [37, 1], 64), (16, 1, 64, [60001], [1], 1),
+    (8, 8, 64, [9000, 5000, 3], [1, 1, 1], 1), (10, 2, 128, [5000, 4999, 130], [90, 65, 130], 130), (5, 1, 64, [3000, 2000], [700, 1], 700)])
+def test_long_sequences_by_the_norm_of_the_error(torch, ctx, heads, kv_heads, d, lengths, rows, hint):
+    """Each row and head by itself: no part of a row block that several thread blocks share is lost, counted twice or taken from another's."""
+    rng = np.random.default_rng(len(lengths) * 1000 + heads)
+    p = Pair(torch, ctx, 1, sum(co.pages_of(n) for n in lengths) + 3, kv_heads, d, len(lengths), co.pages_of(max(lengths)) + 40)
+    p.place(lengths, rng)
+    off = np.concatenate([[0], np.cumsum(rows)])
+    q = bf16(rng, (int(off[-1]), heads, d))
+    got = p.gpu.attend(0, p.bf(q), p.ints(off), max_new=hint).float().cpu().numpy()
+    assert ctx.get_status() == 0
+    for s in range(len(lengths)):
+        k, v, _, _ = p.cpu.sequence(0, s)
+        want, _ = co.attend(q[off[s]:off[s + 1]], k, v, lengths[s], d ** -0.5)
+        err = norm_error(got[off[s]:off[s + 1]], want)
+        assert err.max() <= NORM_LIMIT, (s, float(err.max()))
