@@ -467,6 +467,9 @@ class KvCache:
         if stream is not None:
             with torch.cuda.stream(stream):
                 return self._workspace(bytes_, raw, None)
+        if torch.cuda.current_device() != self._index:  # (whose current stream is not the call's)
+            with torch.cuda.device(self._index):
+                return self._workspace(bytes_, raw, None)
         if torch.cuda.is_current_stream_capturing():
             return torch.empty(bytes_, dtype=torch.uint8, device=self.device)
         ws = self._ws.get(raw)
