@@ -456,6 +456,7 @@ int32_t essa_cache_read(essa_ctx* ctx, const essa_cache_desc* cache, int32_t lay
  *   multiple of kv_heads; 0 < scale <= 2^127.  out does not overlap q.  A sequence may be named by several entries.
  *   max_new >= 1: the most rows an entry is expected to have.  It only chooses the schedule (1 for decode steps); any value
  *   gives right results.
+ * The products q . k have to stay within fp32's range (3.4e38); what scale makes of them may be larger.
  * Scores, maximum, sums and the accumulators are fp32; out is rounded to bf16 once; operands of the products are fp16, each rounded
  * once (2^-11).  Up to 16 query rows per (entry, kv head), by max_new, the products work on the codes themselves, and a weight times its
  * value's scale is the rounded operand; with more rows they are K, V and the weights, and stored values beyond +-65440 are taken

@@ -19,8 +19,6 @@
 // group of up to eight heads fills the tensor core's tile, where q as the M operand would leave half of it empty.
 //
 // Work split: cache_list.cuh, with row blocks of 8 or 16 query rows and key tiles of one page.
-#include <cfloat>
-
 #include "cache_list.cuh"
 
 namespace essa {
@@ -220,7 +218,7 @@ __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         back[nt][x] = __shfl_sync(0xffffffffu, down, 8 * t + 4 * x);
-        sc[nt][x] = fmaxf(a.scale * back[nt][x], FLT_MIN);  // (hidden scores are -infinity, and 0 times that is NaN)
+        sc[nt][x] = softmax_scale(a.scale * back[nt][x]);
         const int rc = r0 + nt * 8 + 2 * t + x;  // tokens that column 2 t + x sees; a column without a row sees all and is not written
         limit[nt][x] = rc < rows ? c.info.len - c.info.rows + a.by_group(rc) + 1 : 0x7fffffff;
         lowest = min(lowest, limit[nt][x]);
@@ -229,8 +227,9 @@ __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_
     lowest = min(lowest, __shfl_xor_sync(0xffffffffu, lowest, 1));
     lowest = min(lowest, __shfl_xor_sync(0xffffffffu, lowest, 2));
     float o[NT][CH][2][4];
-    // running maximum, the score that moves it, the exponent's shift; sum of weights; second term of O
-    float mx[NT][2], high[NT][2], shift[NT][2], l[NT][2], om[NT][G][2];
+    // running maximum, the score that moves it, what weights are relative to (the maximum, or 0 before there is one); sum of weights; second
+    // term of O
+    float mx[NT][2], high[NT][2], ref[NT][2], l[NT][2], om[NT][G][2];
     float per_unit[G];  // scales are relative to a power of two, the unit of o: this is its inverse; before the first scale any makes a new one
 #pragma unroll
     for (int i = 0; i < G; ++i) per_unit[i] = 0x1p40f;
@@ -243,7 +242,7 @@ __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         mx[nt][x] = high[nt][x] = -INFINITY;
-        shift[nt][x] = l[nt][x] = 0.f;
+        ref[nt][x] = l[nt][x] = 0.f;
 #pragma unroll
         for (int i = 0; i < G; ++i) om[nt][i][x] = 0.f;
       }
@@ -362,7 +361,7 @@ __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_
               m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
               f[nt][x] = m == mx[nt][x] ? 1.f : ex2((mx[nt][x] - m) * sc[nt][x]);
               mx[nt][x] = m;
-              shift[nt][x] = m == -INFINITY ? 0.f : -m * sc[nt][x];  // (a column that sees nothing yet: all weights 0)
+              ref[nt][x] = m == -INFINITY ? 0.f : m;  // (a column that sees nothing yet: all weights 0)
               high[nt][x] = m == -INFINITY ? m : m + 6.f / sc[nt][x];
               l[nt][x] *= f[nt][x];
 #pragma unroll
@@ -397,15 +396,16 @@ __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_
                   }
           }
         }
-        // --- weights
+        // --- weights.  (The difference comes first.  A multiply-add with a rounded product of maximum and scale leaves 2^-24 of that in every
+        // exponent, a factor next to other runs' parts, and far out all weights are 0 or infinite: 200 us for the long sequences, this 202.)
 #pragma unroll
         for (int k = 0; k < KS; ++k)
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
-              s[k][nt][x] = ex2(fmaf(s[k][nt][x], sc[nt][x], shift[nt][x]));
-              s[k][nt][2 + x] = ex2(fmaf(s[k][nt][2 + x], sc[nt][x], shift[nt][x]));
+              s[k][nt][x] = ex2((s[k][nt][x] - ref[nt][x]) * sc[nt][x]);
+              s[k][nt][2 + x] = ex2((s[k][nt][2 + x] - ref[nt][x]) * sc[nt][x]);
               l[nt][x] += s[k][nt][x] + s[k][nt][2 + x];
             }
         // --- values

@@ -76,6 +76,11 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 
+// What a difference of scores is multiplied with to be an exponent of 2, kept away from 0 and infinity: hidden scores are -infinity and equal ones
+// 0 apart, either of which would make NaN of it.  Scores in units of 2^13 .. 2^14 of a row of q and fp16's smallest numbers of K differ by 2^-48
+// or not at all: from 2^80 on, and well before, every difference is a weight of 0.
+__device__ __forceinline__ float softmax_scale(float x) { return fminf(fmaxf(x, 0x1p-126f), 0x1p80f); }
+
 // Two fp32 operations in one instruction.
 __device__ __forceinline__ uint64_t pack_f32x2(float lo, float hi) {
   uint64_t r;

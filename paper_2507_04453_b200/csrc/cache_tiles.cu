@@ -23,8 +23,6 @@
 // the result alone.  S, the maximum, the sums and O are fp32.
 // Channel order inside a group of eight channels is (0, 4, 1, 5, 2, 6, 3, 7), what masking nibbles out of a word gives: Q is stored in
 // the same order, and O's columns are put back on the way out.
-#include <cfloat>
-
 #include "cache_list.cuh"
 
 namespace essa {
@@ -312,7 +310,11 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
     const bool wide_out = !(reinterpret_cast<uintptr_t>(a.out) & 31) && a.ld_out % 16 == 0;  // whole 32-byte sectors
     Block b, next;
     b.n = 0;
-    float m = 0.f, sum = 0.f;
+    // Maximum, sum of weights and softmax scale (in the units of the row).  Weights are 2^(s scale + shift) with shift = -m scale, rounded: 2^-25
+    // of the exponent away from being relative to m itself.  That changes nothing in a row's own result, but a partial result is taken back to m
+    // (a factor), and an exponent is kept below 2^27, where it is at most 2^4.
+    float m = 0.f, sum = 0.f, scale = 0.f;
+    const auto shift_of = [&](float top) { return top == -INFINITY ? 0.f : -top * scale; };  // (a row that sees nothing yet: all weights 0)
     for (;;) {
       // --- the next row block's Q (all products with this one's are done), while the last product with V runs
       const bool more = enter(next);
@@ -326,6 +328,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
         o_ph ^= 1;
         // --- out, or a partial result; columns (0, 4, 1, 5, 2, 6, 3, 7) of eight are the channels in order
         const float inv = sum == 0.f ? 0.f : 1.f / sum;  // a row that sees nothing is 0
+        const float fix = ex2(m == -INFINITY ? 0.f : -fmaf(m, scale, shift_of(m)));
         const int rr = h * 128 + row;
         const int* o = out_of[warp][parity ^ (more ? 1 : 0)];
         const int r = o[2] + row, tok = a.by_group(r);
@@ -361,20 +364,20 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
           } else if (there) {
 #pragma unroll
             for (int i = 0; i < 32; i += 8) {
-              *reinterpret_cast<float4*>(partial + rr * D + ch + i) = make_float4(at(i), at(i + 2), at(i + 4), at(i + 6));
-              *reinterpret_cast<float4*>(partial + rr * D + ch + i + 4) = make_float4(at(i + 1), at(i + 3), at(i + 5), at(i + 7));
+              *reinterpret_cast<float4*>(partial + rr * D + ch + i) = make_float4(at(i) * fix, at(i + 2) * fix, at(i + 4) * fix, at(i + 6) * fix);
+              *reinterpret_cast<float4*>(partial + rr * D + ch + i + 4) = make_float4(at(i + 1) * fix, at(i + 3) * fix, at(i + 5) * fix, at(i + 7) * fix);
             }
           }
         }
         if (!b.whole && part == 0) {
           partial[L::R * D + rr] = m * b.back;
-          partial[L::R * D + L::R + rr] = sum;
+          partial[L::R * D + L::R + rr] = sum * fix;
         }
         tc_fence_before();
       }
       if (!more) break;
       b = next;
-      const float scale = fmaxf(a.scale * b.back, FLT_MIN);  // (hidden scores are -infinity, and 0 times that is NaN)
+      scale = softmax_scale(a.scale * b.back);
       m = -INFINITY;
       sum = 0.f;
       const auto scores_at = [&](int t) { return tmem + 128 * h + 64 * (t & 1) + lanes; };  // (P follows in the first 32 columns)
@@ -395,7 +398,6 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
           tmem_st32(scores_at(t) + 32 * part, v);
         }
       };
-      const uint64_t scale2 = pack_f32x2(scale, scale);
       for (int j = 0; j < b.n; ++j, ++tile) {
         arrived(j, tile);
         const uint32_t s_at = scores_at(tile);
@@ -420,11 +422,14 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
             pair_sync(pair);
             tc_fence_after();
             top = fmaxf(top, of_part[part ^ 1][h * 128 + row]);
+            // Exponents beyond 2^27 (no model has such scores; the products know them to 2^-18 at best) shrink to that: keys whose scores differ
+            // by more than 2^-19 of the maximum keep weights of 0.
+            if (top != -INFINITY && fabsf(top * scale) > 0x1p27f) scale = 0x1p27f / fabsf(top);
             if (j > 0) {
               // O holds the tiles before this one: their products end before those with the K of the next tile, or (there is none) signal
               if (j + 1 < b.n) await(kSFull + 2 * h + (~tile & 1), s_ph >> (~tile & 1) & 1);
               else await(kOFull + h, o_ph);
-              const float f = top == m ? 1.f : ex2((m - top) * scale);
+              const float f = top == m ? 1.f : m == -INFINITY ? 0.f : ex2(shift_of(top) - shift_of(m));
               sum *= f;
 #pragma unroll 1
               for (int d = 0; d < D / 2; d += 16) {
@@ -437,8 +442,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
             }
             m = top;
           }
-          const float shift = m == -INFINITY ? 0.f : -m * scale;
-          const uint64_t shift2 = pack_f32x2(shift, shift);
+          const float shift = shift_of(m);
+          const uint64_t scale2 = pack_f32x2(scale, scale), shift2 = pack_f32x2(shift, shift);
           uint64_t sums[2] = {0, 0};
 #pragma unroll
           for (int i = 0; i < 16; ++i) {

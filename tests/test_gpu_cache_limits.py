@@ -239,3 +239,62 @@ def test_long_sequences_by_the_norm_of_the_error(torch, ctx, heads, kv_heads, d,
         want, _ = co.attend(q[off[s]:off[s + 1]], k, v, lengths[s], d ** -0.5)
         err = norm_error(got[off[s]:off[s + 1]], want)
         assert err.max() <= NORM_LIMIT, (s, float(err.max()))
+
+
+# ------------------------------------------------------------------------------------------------ scores beyond fp32
+@pytest.mark.parametrize("hint", [1, 100])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("up,scale", [(0, 2.0 ** 127), (0, 2.0 ** 60), (60, 2.0 ** 80), (100, 2.0 ** 20), (-100, 2.0 ** 127)])
+@pytest.mark.parametrize("width", [30, 40])  # pages of the table: row blocks in one piece, and divided between thread blocks
+def test_scores_beyond_fp32_leave_the_largest(torch, ctx, up, scale, d, hint, width):
+    """Products of q and k that fp32 holds, and a scale that takes them out of its range (or far enough for one key to have all the weight): the
+    values of the keys with the largest product.  Keys are whole numbers and queries multiples of 1/4 times a power of two: products are exact, and
+    equal ones are equal."""
+    rng = np.random.default_rng(34)
+    p = Pair(torch, ctx, 1, 40, 1, d, 2, width)
+    p.place([340, 1500], rng)
+    here = ~np.isnan(p.cpu.low[0, :, :, 0, :, 0])
+    p.cpu.codes[0, :, :, 0][here] = rng.integers(0, 16, p.cpu.codes[0, :, :, 0].shape)[here]
+    p.cpu.scale[0, :, :, 0][here], p.cpu.low[0, :, :, 0][here] = 1, -8
+    p.push()
+    q = (rng.integers(-2, 3, (40, 4, d)) / 4 * 2.0 ** up).astype(np.float32)
+    got = p.gpu.attend(0, p.bf(q), p.ints([0, 20, 40]), max_new=hint, scale=scale).float().cpu().numpy()
+    assert ctx.get_status() == 0 and np.isfinite(got).all()
+    for s in range(2):
+        k, v, _, _ = p.cpu.sequence(0, s)
+        want, _ = co.attend(q[20 * s:20 * s + 20], k, v, k.shape[1], scale)
+        err = norm_error(got[20 * s:20 * s + 20], want)
+        assert err.max() <= NORM_LIMIT, (s, float(err.max()))
+
+
+# ------------------------------------------------------------------------------------------------ graphs
+def test_page_operations_captured_into_a_graph(torch, ctx):
+    """free, fork, grow and compact in one graph, replayed: each replay is the model's next round, and one that is refused changes nothing."""
+    rng = np.random.default_rng(35)
+    p = Pair(torch, ctx, 2, 60, 1, 64, 8, 6)
+    p.place([200, 70, 64, 10, 130, 0, 300, 1], rng)
+    src, dst, gone, more = p.ints([0, 1, 0]), p.ints([3, 4, 5]), p.ints([6]), p.ints([20] * 8)
+    used = p.ints([0])
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        p.gpu.free(gone)
+        p.gpu.fork(src, dst)
+        p.gpu.grow(None, more)
+        p.gpu.compact(used)
+    p.push()
+    for step in range(4):
+        graph.replay()
+        p.cpu.free([6])
+        p.cpu.fork([0, 1, 0], [3, 4, 5])
+        p.cpu.grow(range(8), [20] * 8)
+        assert p.cpu.compact() == int(used) and ctx.get_status() == 0
+        p.assert_same()
+    p.cpu.table[7, 5] = 60
+    p.push()
+    gone.fill_(7)
+    graph.replay()  # the free and the compact of row 7 are refused, the fork and the growth between them are not
+    p.cpu.fork([0, 1, 0], [3, 4, 5])
+    p.cpu.grow(range(8), [20] * 8)
+    assert ctx.get_status() == binding.ESSA_ERR_CACHE
+    p.assert_same()
