@@ -6,14 +6,16 @@
 // and-or.  A nibble dropped into the mantissa of the fp16 number 1024 is 1024 + c, or 1024 + 16 c one nibble further up, so
 // that a word of eight codes needs one shift.
 //   S = sum_g s_g (q_g . c_g) + min_g sum(q_g).  The tensor core multiplies q, or q / 16, by those numbers as they are and starts from
-//   minus what the 1024 will add (a sum over q), so that in fp32 the offset has gone when it has finished.
+//   minus what the 1024 will add (a sum over q), so that the offset has gone when it has finished.  (On the way the sum is up to 1024 sum |q|,
+//   whose last place in fp32 takes up to ten bits of the score's: some 10^-4 of a score's unit for 128 channels of N(0, 1).)
 //   O = sum_k p_k (s_k (c_k - 8) + (min_k + 8 s_k)): one operation more takes a number to c - 8; the weight times the scale is rounded to
 //   fp16 (2^-11 of a centred value; with the codes not centred it would be 2^-11 of a number 2.6 times as large), the second term stays
 //   on the CUDA cores in fp32.  (Leaving the 1024 in and subtracting it from the sum at the end loses the result in fp32.)
 // fp16 holds what it has to: a query row is brought to a largest element of 2^13 .. 2^14 by a power of two, and scales are taken
 // relative to a power of two near the largest that the warp has met (products 2^-14 below it lose bits).
-// 910 MB of cache (128 sequences of 4 to 8 thousand tokens, 8 kv heads, 8 query heads each): 196 us, 4.7 TB/s; ALU ~50 % and issue slots ~60 %
-// busy, tensor ~25 %.  The first version, with bf16 operands (three shifts and twice the roundings per word of codes): 289 us.  Tried and no faster:
+// 910 MB of cache (128 sequences of 4 to 8 thousand tokens, 8 kv heads, 8 query heads each): 200 to 219 us (by clocks), 4.2 to 4.6 TB/s; ALU 47 % and
+// issue slots 60 % busy, HBM 55 %, tensor 24 %: none is full; 3.4 warps per scheduler leave fixed latencies uncovered, and their 128 registers spill 64 bytes.  The first
+// version, with bf16 operands (three shifts and twice the roundings per word of codes): 289 us.  Tried and no faster:
 // four consuming warps that copy for themselves in four thread blocks per SM, one slice of 16 tokens per warp.
 // K and V are the M = 16 operand of mma.m16n8k16, the query rows (heads of the group x tokens) are the N = 8 columns: a
 // group of up to eight heads fills the tensor core's tile, where q as the M operand would leave half of it empty.

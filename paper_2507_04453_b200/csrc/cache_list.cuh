@@ -18,7 +18,8 @@
 
 namespace essa {
 
-// Division by the number of heads of a group (rows are token * group + head) as a multiplication: for n < 2^31,
+// Division by the number of heads of a group (rows are token * group + head) as a multiplication (T. Granlund and P. Montgomery, Division by
+// invariant integers using multiplication, 1994): for n < 2^31,
 // n / d = (umulhi(mul, n) + n) >> shift with shift = ceil(log2 d), mul = floor(2^32 (2^shift - d) / d) + 1.
 struct Divisor {
   uint32_t d, mul, shift;
@@ -101,7 +102,8 @@ __device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b) {
 
 __device__ __forceinline__ uint32_t half2_bits(__half2 v) { return *reinterpret_cast<uint32_t*>(&v); }
 __device__ __forceinline__ __half2 as_half2(uint32_t v) { return *reinterpret_cast<__half2*>(&v); }
-// Two codes as fp16 numbers: (w & MASK) | magic, magic = 0x64006400, is 1024 + code for the nibbles 0 and 4 of w (MASK 0x000f000f) and
+// Two codes as fp16 numbers (a published technique for 4-bit weights; the last place of an fp16 number from 1024 on is 1, so that a code
+// dropped into its mantissa is added to it): (w & MASK) | magic, magic = 0x64006400, is 1024 + code for the nibbles 0 and 4 of w (MASK 0x000f000f) and
 // 1024 + 16 code for the nibbles 1 and 5 (MASK 0x00f000f0).  One instruction; left to the compiler it becomes two.
 template <uint32_t MASK>
 __device__ __forceinline__ __half2 nibble_half2(uint32_t w, uint32_t magic) {

@@ -8,8 +8,9 @@
 //
 // What bounds it (heads of 128 channels): a key tile takes ~2290 cycles of an SM.  The tensor pipe counts 1024 of them as active, but the MMAs take
 // ~1800 (N = 64 makes a product with K read 6 KB of shared memory in its 32 cycles of arithmetic); the exponentials need 1024 of the special
-// function units, the warps half of the issue slots.  Two prompts of 450 tokens after 16 thousand, 64 heads (468 GFLOP): 488 us, 0.96 PFLOP/s.
-// A row block costs some six tiles beside its own (queries in, results out): ragged prompts of 1 .. 1024 tokens, 40 heads (231 GFLOP): 479 us.
+// function units, the warps half of the issue slots.  Two prompts of 450 tokens after 16 thousand, 64 heads (468 GFLOP): 500 to 550 us (by
+// clocks), 0.85 to 0.94 PFLOP/s.  A row block costs some six tiles beside its own (queries in, results out): ragged prompts of 1 .. 1024 tokens, 40 heads (231
+// GFLOP): 495 to 509 us.
 // What was tried, when the ragged prompts stood at 496: a thread per row (eight softmax warps): 558 us, and 495 for the others; key tiles of two pages, products
 // with K of N = 128 and one buffer of scores per half: 558 and 455 (the halves' softmax and products then alternate, but a tile of 128
 // keys is a coarse grain for short prompts); the same with 80 registers for the softmax instead of 96: 705 and 608;
