@@ -402,22 +402,19 @@ __device__ bool rows_sound(const CacheView& v, const int32_t* slots, int n, int 
 
 // Frees the sequences, or does nothing if a slot or an entry of their table rows is bad.  One cluster, whose thread blocks look at a share of the
 // entries each and tell one another before any of them changes something: thread blocks of a larger grid would need a workspace to come to one
-// verdict.  Between events, with the launch: 16 rows of 32 pages 9.1 us, 240 rows 11.1, 1000 rows of 64 13.2, 4096 rows of 256 58 (without
+// verdict.  Between events, with the launch: 16 rows of 32 pages 9 to 10 us, 240 rows 11 to 12, 1000 rows of 64 13, 4096 rows of 256 59 (without
 // a look at the rows, in a grid of any size: 7.0, 7.1, 8.2, 13).
 constexpr int kFreeCluster = 8, kFreeThreads = 1024;
 __global__ void __launch_bounds__(kFreeThreads) free_kernel(CacheView v, const int32_t* slots, int n, int32_t* status) {
   extern __shared__ uint32_t seen[];
   __shared__ uint32_t verdict;
   const int blocks = gridDim.x, threads = blocks * kFreeThreads, thread = blockIdx.x * kFreeThreads + threadIdx.x;
-  bool ok = slots_distinct(slots, n, v.max_seqs, seen);  // (the same in every thread block)
-  if (ok) {
-    ok = __syncthreads_and(rows_sound(v, slots, n, thread, threads));
-    if (threadIdx.x == 0) verdict = ok;
-    cluster_sync_all();
-    ok = true;
-    for (int r = 0; r < blocks; ++r) ok = ok && ld_dsmem_u32(map_to_cta(smem_u32(&verdict), r)) != 0;
-    cluster_sync_all();  // (a thread block that ends takes its shared memory with it)
-  }
+  bool ok = slots_distinct(slots, n, v.max_seqs, seen);
+  ok = __syncthreads_and(ok && rows_sound(v, slots, n, thread, threads));
+  if (threadIdx.x == 0) verdict = ok;
+  cluster_sync_all();
+  for (int r = 0; r < blocks; ++r) ok = ok && ld_dsmem_u32(map_to_cta(smem_u32(&verdict), r)) != 0;
+  cluster_sync_all();  // (every thread block comes here: one that ended before would take its shared memory with it)
   if (!ok) {
     if (thread == 0) cache_fault(status);
     return;
