@@ -464,6 +464,77 @@ int32_t essa_cache_read(essa_ctx* ctx, const essa_cache_desc* cache, int32_t lay
 int32_t essa_cache_attend(essa_ctx* ctx, const essa_cache_desc* cache, int32_t layer, const void* q, int64_t ld_q, int32_t q_heads, int32_t T,
                           const int32_t* slots, const int32_t* tok_offsets, int32_t n, int32_t max_new, float scale, void* out, int64_t ld_out,
                           void* workspace, int64_t workspace_bytes, void* stream);
+/* The same attention, rows seeing less of their sequence.  mask NULL: as essa_cache_attend.
+ *   window W >= 1: a row at position pos sees s <= pos with s > pos - W, its own token among them (0: no window);
+ *   sinks S >= 0: and the first S tokens of its sequence (up to pos), however far back they are;
+ *   drafts (dev, 4-byte aligned, or NULL): an entry's rows are drafted tokens that need not follow one another.  Row r sees all tokens before its
+ *     entry's rows, and of these draft j exactly if bit j % 32 of word drafts[r * draft_words + j / 32] is set (its own has to be set for it to see itself;
+ *     bits of drafts that the entry does not have are not looked at; drafts from 32 * draft_words on are seen by nobody).  essa_cache_tree makes the bits of
+ *     a tree; others (blocks of tokens that all see one another) serve as well.  1 <= draft_words <= ESSA_CACHE_MAX_DRAFTS / 32.
+ * With both, a row's position is the number of tokens before its entry's rows plus the drafts that it sees, less one, and W >= 32 * draft_words, so that
+ * no draft leaves the window.  Tokens on pages that no row can see (between the first ones and the window, whole pages) are not read and may be
+ * missing from the table.  A row that sees no token is 0.  Workspace: essa_cache_attend_workspace. */
+#define ESSA_CACHE_MAX_DRAFTS 256
+typedef struct essa_attend_mask {
+  int32_t window;
+  int32_t sinks;
+  const uint32_t* drafts;
+  int32_t draft_words;
+} essa_attend_mask;
+int32_t essa_cache_attend_masked(essa_ctx* ctx, const essa_cache_desc* cache, const essa_attend_mask* mask, int32_t layer, const void* q, int64_t ld_q,
+                                 int32_t q_heads, int32_t T, const int32_t* slots, const int32_t* tok_offsets, int32_t n, int32_t max_new, float scale, void* out,
+                                 int64_t ld_out, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Trees of drafted tokens, made once per step for all layers.  Entry i's rows (its sequence's last tokens) are drafts; parents[t] (dev, [T]) is the
+ * place of row t's parent among its entry's rows (-1: the token before them), and a parent comes before its children.
+ *   drafts (dev, [T][draft_words], 4-byte aligned): row t's bits for essa_attend_mask, itself and all that it descends from;
+ *   positions (dev, [T], may be NULL): the number of tokens before the entry's rows plus the row's depth (0 for a parent of -1), for a rotation.
+ * A row whose parent is not before it counts as a child of the token before the rows, one from 32 * draft_words on has no bits and counts likewise;
+ * a slot outside the cache leaves the rows' positions as they are (ESSA_ERR_CACHE for each of these).  Rows outside all entries are left as they are. */
+int32_t essa_cache_tree(essa_ctx* ctx, const essa_cache_desc* cache, const int32_t* parents, int32_t T, const int32_t* slots, const int32_t* tok_offsets, int32_t n,
+                        uint32_t* drafts, int32_t draft_words, int32_t* positions, void* stream);
+/* Of the last L = tok_offsets[i + 1] - tok_offsets[i] (NULL: 1) tokens of sequence slots[i] (NULL: i), counts[i] stay, i < n: those that
+ * picks[i * ld_picks + m], m < counts[i] (dev, ascending, each in 0 .. L - 1; picks NULL: the first counts[i]) name, moved together in all layers, as
+ * after a tree of drafts has been checked.  The sequence becomes L - counts[i] tokens shorter; its pages behind its new end are given back.
+ * Refused as a whole (ESSA_ERR_CACHE, nothing changes): a slot outside the cache or named twice; offsets that descend; L or counts[i] not in 0 .. length
+ * and 0 .. L; with picks, L > ESSA_CACHE_MAX_DRAFTS, counts[i] > ld_picks, or picks that are not ascending within 0 .. L - 1; a page from that of the first of the L tokens on
+ * that is not a page in use, or one that a token moves to and that another sequence shares. */
+int32_t essa_cache_keep_workspace(int32_t n, int64_t* bytes);
+int32_t essa_cache_keep(essa_ctx* ctx, const essa_cache_desc* cache, const int32_t* slots, const int32_t* tok_offsets, const int32_t* counts, const int32_t* picks,
+                        int64_t ld_picks, int32_t n, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* ---- Rotary positions with several axes -----------------------------------------------------------------------------
+ * A row of head_dim channels is turned pair by pair: with t = positions[axis[i]] * frequencies[i] (radians) pair i becomes
+ *   a' = magnitude (a cos t - b sin t),  b' = magnitude (b cos t + a sin t),
+ * where (a, b) are channels i and i + head_dim / 2, or, with adjacent != 0, 2 i and 2 i + 1.  Every pair has an axis (time, height and width of images and
+ * video; one axis for text) and a frequency of its own, so that any layout of sections and any scaling of frequencies can be given; a frequency of 0 leaves a pair as
+ * it is (times magnitude), and negated positions turn back.
+ * Angles are exact: a frequency is held as a 64-bit fraction of a turn, turns[i] = frac(frequency / 2 pi) 2^64, the product with a position
+ * is taken modulo a turn in integers, and sine and cosine see a fraction that is wrong by 2^-32 of a turn at most, however far the position. */
+#define ESSA_ROTARY_MAX_DIM 256
+#define ESSA_ROTARY_MAX_AXES 4
+typedef struct essa_rotary {
+  int32_t head_dim;   /* a multiple of 16 up to ESSA_ROTARY_MAX_DIM */
+  int32_t axes;       /* 1 .. ESSA_ROTARY_MAX_AXES                  */
+  int32_t adjacent;
+  float magnitude;
+  uint64_t turns[ESSA_ROTARY_MAX_DIM / 2];
+  uint8_t axis[ESSA_ROTARY_MAX_DIM / 2];
+} essa_rotary;
+/* Fill *out from frequencies [head_dim / 2] (radians per position, finite) and axis [head_dim / 2] (NULL: all 0), both on the host.  Needs no device. */
+int32_t essa_rotary_make(int32_t head_dim, int32_t axes, int32_t adjacent, float magnitude, const double* frequencies, const int32_t* axis, essa_rotary* out);
+/* out[t][h] = x[t][h] turned by positions[.][t], t < T, h < heads.  x, out [T] rows of heads * head_dim bf16 dev, ld_x / ld_out elements apart (multiples of 8;
+ * 16-byte aligned); out may be x (with the same pitch), and overlaps it in no other way.  positions [axes] rows of T int32 dev, ld_positions apart.  Sine, cosine and the
+ * products are fp32, rounded to bf16 once. */
+int32_t essa_rotary_apply(essa_ctx* ctx, const essa_rotary* rotary, const void* x, int64_t ld_x, int32_t heads, int32_t T, const int32_t* positions,
+                          int64_t ld_positions, void* out, int64_t ld_out, void* stream);
+/* essa_rotary_apply on q and k, and essa_cache_append of the turned k (rounded to bf16) and of v, in one launch: q_out [T] rows of q_heads * head_dim bf16
+ * (may be q).  positions NULL: every axis is the token's position in its sequence; such a row of q is left as it is if its slot is bad or the token would lie
+ * before the sequence's first.  k and v as in essa_cache_append, entries too; rows of q outside all entries are left as they are. */
+int32_t essa_cache_append_rotary(essa_ctx* ctx, const essa_cache_desc* cache, int32_t layer, const essa_rotary* rotary, const void* q, int64_t ld_q, int32_t q_heads,
+                                 const void* k, int64_t ld_k, const void* v, int64_t ld_v, int32_t T, const int32_t* positions, int64_t ld_positions,
+                                 const int32_t* slots, const int32_t* tok_offsets, int32_t n, void* q_out, int64_t ld_q_out, void* stream);
+
 /* Sequence dst[i] becomes a copy of the first lens[i] (dev; NULL: all) tokens of sequence src[i], i < n: it shares the full
  * pages and gets a copy, in all layers, of a partly filled last one (the free pages with the lowest numbers, in the order of
  * the entries).  What dst[i] held is freed first.  The dst are distinct and none of them is a src. */

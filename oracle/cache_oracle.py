@@ -204,3 +204,112 @@ def attend(q, k, v, length, scale):
             weights[j, h, :see] = p
             out[j, h] = p @ v[h // group, :see]
     return out, weights
+
+
+# -- masks, trees, rotation
+def attend_seen(q, k, v, seen, scale):
+    """q [rows, heads, d], k, v [kv_heads, length, d] fp64, seen [rows, length]: (out, p) as attend; a row that sees nothing is 0."""
+    rows, heads, d = q.shape
+    group = heads // k.shape[0]
+    out, weights = np.zeros((rows, heads, d)), np.zeros((rows, heads, k.shape[1]))
+    for j in range(rows):
+        at = np.flatnonzero(seen[j])
+        if not len(at):
+            continue
+        for h in range(heads):
+            s = k[h // group, at] @ q[j, h].astype(np.float64) * scale
+            p = np.exp(s - s.max())
+            p /= p.sum()
+            weights[j, h, at] = p
+            out[j, h] = p @ v[h // group, at]
+    return out, weights
+
+
+def seen_mask(length, rows, window=None, sinks=0, drafts=None):
+    """[rows, length]: what the last `rows` tokens of a sequence see.  window, sinks as in essa_attend_mask; drafts [rows, rows] bool: which draft sees which."""
+    past = length - rows
+    seen = np.zeros((rows, length), bool)
+    for j in range(rows):
+        pos = past + (j if drafts is None else int(drafts[j].sum()) - 1)
+        for s in range(length):
+            known = s <= pos if drafts is None else s < past
+            near = window is None or s > pos - window or s < sinks
+            seen[j, s] = known and near
+            if drafts is not None and s >= past:
+                seen[j, s] = drafts[j, s - past]
+    return seen
+
+
+def ancestors(parents):
+    """(bits [n, n] bool, depth [n]) of drafted tokens; a parent that is not before its child counts as -1."""
+    n = len(parents)
+    bits, depth = np.zeros((n, n), bool), np.zeros(n, np.int64)
+    for j in range(n):
+        at, depth[j] = j, -1
+        while at >= 0:
+            bits[j, at] = True
+            depth[j] += 1
+            at = parents[at] if -1 <= parents[at] < at else -1
+    return bits, depth
+
+
+def pack_bits(bits, words):
+    """[n, n] bool -> [n, words] uint32, bit j % 32 of word j / 32."""
+    out = np.zeros((len(bits), words), np.uint32)
+    for r, row in enumerate(bits):
+        for j in np.flatnonzero(row[:32 * words]):
+            out[r, j // 32] |= np.uint32(1 << (int(j) % 32))
+    return out
+
+
+def keep(cache, slots, rows, counts, picks=None):
+    """essa_cache_keep on a Cache: of the last rows[i] tokens of slots[i], picks[i][:counts[i]] (None: the first) stay."""
+    slots = cache._check_slots(slots)
+    for i, s in enumerate(slots):
+        length, L, c = int(cache.lengths[s]), int(rows[i]), int(counts[i])
+        if not (0 <= L <= length and 0 <= c <= L):
+            raise Refused("length")
+        mine = list(range(c)) if picks is None else [int(x) for x in picks[i][:c]]
+        if picks is not None and (L > 256 or c > len(picks[i]) or any(b <= a for a, b in zip(mine, mine[1:])) or any(p < 0 or p >= L for p in mine)):
+            raise Refused("picks")
+        base = length - L
+        for j in range(base // PAGE, pages_of(length)):
+            p = int(cache.table[s, j])
+            if not 0 <= p < cache.num_pages or cache.refs[p] <= 0:
+                raise Refused("page")
+        moved = [m for m, p in enumerate(mine) if p != m]
+        if moved:
+            for j in range((base + moved[0]) // PAGE, (base + c - 1) // PAGE + 1):
+                if cache.refs[cache.table[s, j]] != 1:
+                    raise Refused("shared")
+    for i, s in enumerate(slots):
+        length, L, c = int(cache.lengths[s]), int(rows[i]), int(counts[i])
+        base = length - L
+        at = lambda t: (int(cache.table[s, t // PAGE]), t % PAGE)
+        for m, p in enumerate([] if picks is None else picks[i][:c]):
+            (p0, o0), (p1, o1) = at(base + int(p)), at(base + m)
+            for a in (cache.codes, cache.scale, cache.low):
+                a[:, p1, :, :, o1] = a[:, p0, :, :, o0]
+        for j in range(pages_of(base + c), pages_of(length)):
+            cache.refs[cache.table[s, j]] -= 1
+            cache.table[s, j] = -1
+        cache.lengths[s] = base + c
+
+
+def rotate(x, positions, frequencies, axis, adjacent=False, magnitude=1.0):
+    """x [T, heads, d], positions [axes, T]: fp64, angles modulo a turn in exact rational arithmetic of the fp64 frequencies (2 pi to 50 digits)."""
+    from fractions import Fraction
+    two_pi = Fraction("6.28318530717958647692528676655900576839433879875021")
+    T, heads, d = x.shape
+    half = d // 2
+    y, out = x.astype(np.float64), np.zeros(x.shape)
+    for i in range(half):
+        turn = Fraction(float(frequencies[i])) / two_pi
+        a, b = (2 * i, 2 * i + 1) if adjacent else (i, i + half)
+        for t in range(T):
+            part = turn * int(positions[axis[i]][t])
+            angle = 2 * np.pi * float(part - (part.numerator // part.denominator))
+            c, s = magnitude * np.cos(angle), magnitude * np.sin(angle)
+            out[t, :, a] = y[t, :, a] * c - y[t, :, b] * s
+            out[t, :, b] = y[t, :, b] * c + y[t, :, a] * s
+    return out

@@ -51,7 +51,8 @@ EXPORTED_SYMBOLS = (
     "essa_apply_layers", "essa_cma_create", "essa_cma_destroy", "essa_cma_ask", "essa_tell", "essa_cma_set", "essa_cma_get", "essa_cma_params",
     "essa_cache_page_bytes", "essa_cache_validate", "essa_cache_pages_workspace", "essa_cache_attend_workspace",
     "essa_cache_reset", "essa_cache_grow", "essa_cache_append", "essa_cache_read", "essa_cache_attend", "essa_cache_fork",
-    "essa_cache_free", "essa_cache_compact",
+    "essa_cache_free", "essa_cache_compact", "essa_cache_attend_masked", "essa_cache_tree", "essa_cache_keep_workspace", "essa_cache_keep",
+    "essa_rotary_make", "essa_rotary_apply", "essa_cache_append_rotary",
 )
 
 
@@ -92,6 +93,19 @@ class CacheDesc(C.Structure):
     _fields_ = [("layers", C.c_int32), ("num_pages", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32),
                 ("max_seqs", C.c_int32), ("max_pages", C.c_int32), ("pages", C.c_void_p), ("table", C.c_void_p),
                 ("lengths", C.c_void_p), ("refs", C.c_void_p)]
+
+
+CACHE_MAX_DRAFTS = 256
+ROTARY_MAX_DIM = 256
+
+
+class AttendMask(C.Structure):
+    _fields_ = [("window", C.c_int32), ("sinks", C.c_int32), ("drafts", C.c_void_p), ("draft_words", C.c_int32)]
+
+
+class RotaryDesc(C.Structure):
+    _fields_ = [("head_dim", C.c_int32), ("axes", C.c_int32), ("adjacent", C.c_int32), ("magnitude", C.c_float),
+                ("turns", C.c_uint64 * (ROTARY_MAX_DIM // 2)), ("axis", C.c_uint8 * (ROTARY_MAX_DIM // 2))]
 
 
 class Plan(C.Structure):
@@ -173,6 +187,13 @@ def load_library() -> C.CDLL:
         "essa_cache_fork": (i32, [vp, C.POINTER(CacheDesc), vp, vp, vp, i32, vp, i64, vp]),
         "essa_cache_free": (i32, [vp, C.POINTER(CacheDesc), vp, i32, vp]),
         "essa_cache_compact": (i32, [vp, C.POINTER(CacheDesc), vp, vp, i64, vp]),
+        "essa_cache_attend_masked": (i32, [vp, C.POINTER(CacheDesc), C.POINTER(AttendMask), i32, vp, i64, i32, i32, vp, vp, i32, i32, f32, vp, i64, vp, i64, vp]),
+        "essa_cache_tree": (i32, [vp, C.POINTER(CacheDesc), vp, i32, vp, vp, i32, vp, i32, vp, vp]),
+        "essa_cache_keep_workspace": (i32, [i32, C.POINTER(i64)]),
+        "essa_cache_keep": (i32, [vp, C.POINTER(CacheDesc), vp, vp, vp, vp, i64, i32, vp, i64, vp]),
+        "essa_rotary_make": (i32, [i32, i32, i32, f32, vp, vp, C.POINTER(RotaryDesc)]),
+        "essa_rotary_apply": (i32, [vp, C.POINTER(RotaryDesc), vp, i64, i32, i32, vp, i64, vp, i64, vp]),
+        "essa_cache_append_rotary": (i32, [vp, C.POINTER(CacheDesc), i32, C.POINTER(RotaryDesc), vp, i64, i32, vp, i64, vp, i64, i32, vp, i64, vp, vp, i32, vp, i64, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -373,6 +394,59 @@ class CmaState:
         return dict(zip(names, (float(x) for x in v)))
 
 
+class Rotary:
+    """Which turn every pair of channels makes per position (essa_rotary), made on the host once per model.
+
+    head_dim: a multiple of 16 up to 256.  base: pair i turns by base ** (-2 i / head_dim) radians per position; or frequencies: head_dim / 2 of them.
+    sections: how many pairs each axis has (their sum is head_dim / 2; None: one axis), one axis after another or, interleaved, the axes in turns until
+    each has its share; or axis: the axis of every pair.  adjacent: pairs are channels 2 i and 2 i + 1 instead of i and i + head_dim / 2.
+    magnitude: what cosine and sine are multiplied with."""
+
+    def __init__(self, head_dim: int, base: float = 10000.0, sections=None, interleaved: bool = False, adjacent: bool = False, frequencies=None, axis=None,
+                 magnitude: float = 1.0):
+        half = head_dim // 2
+        if frequencies is None:
+            if not base > 0:
+                raise EssaError(ESSA_ERR_INVALID_ARG, "rotary: base must be positive")
+            frequencies = float(base) ** (-2.0 * np.arange(half) / max(head_dim, 1))
+        frequencies = np.ascontiguousarray(frequencies, dtype=np.float64)
+        if axis is None:
+            left = [half] if sections is None else [int(n) for n in sections]
+            if sum(left) != half or min(left, default=-1) < 0:
+                raise EssaError(ESSA_ERR_INVALID_ARG, "rotary: the sections must add up to head_dim / 2")
+            self.axes, axis = len(left), []
+            while len(axis) < half:
+                for a, n in enumerate(left):
+                    take = min(n, 1) if interleaved else n
+                    axis += [a] * take
+                    left[a] -= take
+        elif sections is not None:
+            raise EssaError(ESSA_ERR_INVALID_ARG, "rotary: pass sections or axis, not both")
+        else:
+            self.axes = int(max(axis, default=0)) + 1
+        axis = np.ascontiguousarray(axis, dtype=np.int32)
+        if frequencies.shape != (half,) or axis.shape != (half,):
+            raise EssaError(ESSA_ERR_INVALID_ARG, "rotary: frequencies and axis must have head_dim / 2 elements")
+        self.head_dim, self.desc = head_dim, RotaryDesc()
+        lib = load_library()
+        st = lib.essa_rotary_make(head_dim, self.axes, int(adjacent), magnitude, frequencies.ctypes.data_as(C.c_void_p), axis.ctypes.data_as(C.c_void_p),
+                                  C.byref(self.desc))
+        if st != ESSA_OK:
+            raise EssaError(st, "rotary: " + lib.essa_status_string(st).decode())
+        self._ref = C.byref(self.desc)
+
+    def _positions(self, torch, positions, T, index):
+        """Checks positions, [axes, T] (or [T] for one axis) int32 with contiguous rows; (pointer, elements between rows)."""
+        shape = positions.shape
+        if positions.dtype is not torch.int32 or positions.get_device() != index or tuple(shape) not in (((self.axes, T), (T,)) if self.axes == 1 else ((self.axes, T),)) \
+                or (T > 1 and positions.stride(-1) != 1):
+            raise EssaError(ESSA_ERR_INVALID_ARG, f"rotary: positions must be int32 [{self.axes}, {T}] with contiguous rows, on the data's device")
+        ld = positions.stride(0) if len(shape) == 2 and self.axes > 1 else T
+        if ld < T:
+            raise EssaError(ESSA_ERR_INVALID_ARG, "rotary: the rows of positions overlap")
+        return positions.data_ptr() or None, ld
+
+
 class KvCache:
     """A paged 4-bit key / value cache (essa_cache_*): four torch tensors and the calls on them, argument marshalling only.
 
@@ -412,6 +486,8 @@ class KvCache:
         self._pages_ws = need.value
         self._sms = torch.cuda.get_device_properties(self.device).multi_processor_count
         self._attend_ws = {}  # (q_heads, max_new) -> bytes
+        self._mask_desc = AttendMask()
+        self._mask_ref = C.byref(self._mask_desc)
         self._ws = {}         # cudaStream_t -> workspace
         self._lib, self._ref, self._index = ctx.lib, C.byref(self.desc), self.device.index
         self._int32, self._bf16, self._scale = torch.int32, torch.bfloat16, head_dim ** -0.5
@@ -516,7 +592,63 @@ class KvCache:
         ws = self._workspace(self._pages_ws, raw, stream)
         self._check(self._lib.essa_cache_compact(self.ctx.handle, self._ref, u, ws.data_ptr(), ws.shape[0], raw))
 
+    def keep(self, counts, tok_offsets=None, picks=None, slots=None, stream=None):
+        """essa_cache_keep: of the last tok_offsets[i + 1] - tok_offsets[i] (None: 1) tokens of the sequence slots[i] (None: i), the counts[i] that
+        picks[i, :counts[i]] names (ascending; None: the first) stay and move together; the sequence's end behind them is given back."""
+        n = counts.shape[0]
+        a, b, c, raw = self._ints("slots", slots, n), self._ints("tok_offsets", tok_offsets, n + 1), self._ints("counts", counts), self._raw(stream)
+        pp, ldp = None, 0
+        if picks is not None:
+            if picks.dtype is not self._int32 or picks.dim() != 2 or picks.shape[0] != n or picks.get_device() != self._index or not picks.is_contiguous():
+                self._fail("picks", f"a contiguous int32 tensor of {n} rows")
+            # (without a column nothing can be picked: counts other than 0 are refused as with any that are too large)
+            pp, ldp = picks.data_ptr() or self.refs.data_ptr(), picks.shape[1]
+        ws = self._workspace(256 + 32 * n, raw, stream)
+        self._check(self._lib.essa_cache_keep(self.ctx.handle, self._ref, a, b, c, pp, ldp, n, ws.data_ptr(), ws.shape[0], raw))
+
     # -- tokens
+    def append_rotary(self, layer: int, rotary, q, k, v, positions=None, tok_offsets=None, slots=None, q_out=None, stream=None):
+        """essa_cache_append_rotary: q [T, heads, head_dim] and k turned by positions [axes, T] int32 (None: every axis is the token's position in its
+        sequence); k and v become the last tokens of the entries' sequences, as append does it.  Returns the turned q (q_out may be q)."""
+        shape = q.shape
+        T = shape[0]
+        if v.shape[0] != T or k.shape[0] != T:
+            raise EssaError(ESSA_ERR_INVALID_ARG, "kv_cache: q, k and v must have the same number of rows")
+        heads = shape[1] if len(shape) == 3 else shape[-1] // self.head_dim
+        pq, ldq = self._rows("q", q, heads)
+        pk, ldk = self._rows("k", k, self.kv_heads)
+        pv, ldv = self._rows("v", v, self.kv_heads)
+        a, b, n = self._entries(T, slots, tok_offsets)
+        pp, ldp = (None, 0) if positions is None else rotary._positions(self.ctx.torch, positions, T, self._index)
+        if q_out is None:
+            q_out = self._empty_like(q) if stream is None and q.is_contiguous() else self._empty(shape, stream)
+            po, ldo = q_out.data_ptr() or None, heads * self.head_dim
+        else:
+            if q_out.shape != shape:
+                raise EssaError(ESSA_ERR_INVALID_ARG, "kv_cache: q_out must have q's shape")
+            po, ldo = self._rows("q_out", q_out, heads)
+        self._check(self._lib.essa_cache_append_rotary(self.ctx.handle, self._ref, layer, rotary._ref, pq, ldq, heads, pk, ldk, pv, ldv, T, pp, ldp, a, b, n,
+                                                       po, ldo, self._raw(stream)))
+        return q_out
+
+    def tree(self, parents, tok_offsets, max_new: int, slots=None, positions: bool = True, stream=None):
+        """essa_cache_tree: (drafts, positions) of the drafted tokens that are the entries' rows: parents [T] int32, the place of a row's parent among its entry's
+        rows (-1: the token before them).  drafts [T, words] int32 is attend's `tree`; positions [T] int32 (None unless asked for) is for append_rotary.
+        max_new: the most rows of an entry, up to CACHE_MAX_DRAFTS.  (Rows outside all entries are not written.)"""
+        if not 1 <= max_new <= CACHE_MAX_DRAFTS:
+            raise EssaError(ESSA_ERR_UNSUPPORTED_SHAPE, f"kv_cache: a tree has 1 .. {CACHE_MAX_DRAFTS} tokens")
+        T, words = parents.shape[0], (max_new + 31) // 32
+        p = self._ints("parents", parents)
+        a, b, n = self._entries(T, slots, tok_offsets)
+        if stream is None:
+            drafts, pos = parents.new_empty((T, words)), parents.new_empty((T,)) if positions else None
+        else:
+            with self.ctx.torch.cuda.stream(stream):
+                drafts, pos = parents.new_empty((T, words)), parents.new_empty((T,)) if positions else None
+        self._check(self._lib.essa_cache_tree(self.ctx.handle, self._ref, p, T, a, b, n, drafts.data_ptr() or None, words, pos.data_ptr() or None if positions else None,
+                                              self._raw(stream)))
+        return drafts, pos
+
     def append(self, layer: int, k, v, tok_offsets=None, slots=None, stream=None):
         """essa_cache_append: k, v [T, kv_heads, head_dim] bf16 become the last tokens of the entries' sequences."""
         T = k.shape[0]
@@ -543,9 +675,24 @@ class KvCache:
         self._check(self._lib.essa_cache_read(self.ctx.handle, self._ref, layer, pk, pv, T, a, b, n, self._raw(stream)))
         return k_out, v_out
 
-    def attend(self, layer: int, q, tok_offsets=None, slots=None, max_new: int = 1, scale=None, out=None, stream=None):
+    def _mask(self, window, sinks, tree, T):
+        """The mask of a call (None: rows see all up to themselves)."""
+        words, ptr = 0, None
+        if tree is not None:
+            if tree.dtype is not self._int32 or tree.dim() != 2 or tree.shape[0] != T or tree.get_device() != self._index or not tree.is_contiguous():
+                self._fail("tree", f"a contiguous int32 tensor [{T}, words]")
+            words, ptr = tree.shape[1], tree.data_ptr() or None
+        if window is not None and window < 1:
+            raise EssaError(ESSA_ERR_INVALID_ARG, "kv_cache: a window has at least one token")
+        m = self._mask_desc
+        m.window, m.sinks, m.drafts, m.draft_words = window or 0, sinks, ptr, words
+        return self._mask_ref
+
+    def attend(self, layer: int, q, tok_offsets=None, slots=None, max_new: int = 1, scale=None, out=None, stream=None, window=None, sinks: int = 0, tree=None):
         """essa_cache_attend: q [T, heads, head_dim] (or [T, heads * head_dim]) bf16 over the cached tokens; the result has q's
-        shape.  max_new: the most rows an entry is expected to have (chooses the schedule only); scale: None = head_dim ** -0.5."""
+        shape.  max_new: the most rows an entry is expected to have (chooses the schedule only); scale: None = head_dim ** -0.5.
+        essa_cache_attend_masked: window: a row sees the last `window` tokens up to itself (None: all), and the first `sinks` of its sequence; tree: an
+        entry's rows are drafted tokens that see what comes before the rows and the drafts whose bits [T, words] int32 (of tree()) are set."""
         shape = q.shape
         heads = shape[1] if len(shape) == 3 else shape[-1] // self.head_dim
         pq, ldq = self._rows("q", q, heads)
@@ -557,6 +704,7 @@ class KvCache:
             if st != ESSA_OK:
                 raise EssaError(st, "kv_cache: the number of query heads must be a multiple of kv_heads and max_new at least 1")
             need = self._attend_ws[(heads, max_new)] = got.value
+        mask = None if window is None and tree is None else self._mask(window, sinks, tree, shape[0])
         if out is None:
             out = self._empty_like(q) if stream is None and q.is_contiguous() else self._empty(shape, stream)
             po, ldo = out.data_ptr() or None, heads * self.head_dim
@@ -566,8 +714,13 @@ class KvCache:
             po, ldo = self._rows("out", out, heads)
         raw = self._raw(stream)
         ws = self._workspace(need, raw, stream)
-        self._check(self._lib.essa_cache_attend(self.ctx.handle, self._ref, layer, pq, ldq, heads, shape[0], a, b, n, max_new, self._scale if scale is None else scale,
-                                                po, ldo, ws.data_ptr(), ws.shape[0], raw))
+        scale = self._scale if scale is None else scale
+        if mask is None:
+            st = self._lib.essa_cache_attend(self.ctx.handle, self._ref, layer, pq, ldq, heads, shape[0], a, b, n, max_new, scale, po, ldo, ws.data_ptr(), ws.shape[0], raw)
+        else:
+            st = self._lib.essa_cache_attend_masked(self.ctx.handle, self._ref, mask, layer, pq, ldq, heads, shape[0], a, b, n, max_new, scale, po, ldo, ws.data_ptr(),
+                                                    ws.shape[0], raw)
+        self._check(st)
         return out
 
 
@@ -657,6 +810,28 @@ class Context:
     def kv_cache(self, layers: int, num_pages: int, kv_heads: int, head_dim: int, max_seqs: int, max_pages: int, **buffers) -> "KvCache":
         """A paged 4-bit key / value cache on this context's device; buffers: the four tensors of an existing one."""
         return KvCache(self, layers, num_pages, kv_heads, head_dim, max_seqs, max_pages, **buffers)
+
+    def rotary(self, rotary: "Rotary", x, positions, out=None, stream=None):
+        """essa_rotary_apply: x [T, heads, head_dim] bf16 (rows may be strided) turned by positions [axes, T] int32 (or [T] for one axis); out may be x."""
+        torch = self.torch
+        if x.dim() != 3 or x.shape[2] != rotary.head_dim or x.shape[1] < 1:
+            raise EssaError(ESSA_ERR_INVALID_ARG, f"rotary: x must be a tensor [T, heads, {rotary.head_dim}]")
+        T, heads, d = x.shape
+        if out is None:
+            if stream is None:
+                out = x.new_empty(x.shape)
+            else:
+                with torch.cuda.stream(stream):
+                    out = x.new_empty(x.shape)
+        for name, t in (("x", x), ("out", out)):
+            if t.dtype is not torch.bfloat16 or t.get_device() != self.device.index or t.shape != x.shape or \
+                    (T and not t.is_contiguous() and not (t.stride(2) == 1 and (heads == 1 or t.stride(1) == d))):
+                raise EssaError(ESSA_ERR_INVALID_ARG, f"rotary: {name} must be a bf16 tensor [T, heads, {d}] on {self.device} whose rows are contiguous")
+        pp, ldp = rotary._positions(torch, positions, T, self.device.index)
+        ld = [heads * d if T < 2 else t.stride(0) for t in (x, out)]
+        raw = (torch._C._cuda_getCurrentRawStream(self.device.index) if stream is None else stream.cuda_stream) or None
+        self._check(self.lib.essa_rotary_apply(self.handle, rotary._ref, x.data_ptr() or None, ld[0], heads, T, pp, ldp, out.data_ptr() or None, ld[1], raw))
+        return out
 
     # -- sampling
     def sample_population(self, mean, step: float, Bfactor, Dvec, seed: int, P: int, out=None, k_begin: int = 0,

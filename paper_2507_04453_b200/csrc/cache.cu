@@ -1,5 +1,7 @@
 // Paged 4-bit key / value cache: storing and reading tokens, page management, and the C entry points of include/essa.h.
+#include "cache_api.cuh"
 #include "cache_list.cuh"
+#include "cache_store.cuh"
 
 namespace essa {
 namespace {
@@ -7,127 +9,6 @@ namespace {
 constexpr int kPlanThreads = 1024;
 
 // ------------------------------------------------------------------------------------------------ tokens
-constexpr int kOffsetsMax = 2048;  // offsets that a thread block searches in shared memory
-
-// The offsets of a call in shared memory, if they fit (all threads of the block; a search of dependent loads from L2 would take
-// longer than the rest of a decode step's append).
-__device__ __forceinline__ void stage_offsets(const CacheEntries& e, int32_t* sm) {
-  if (!e.off || e.n >= kOffsetsMax) return;
-  for (int i = threadIdx.x; i <= e.n; i += blockDim.x) sm[i] = __ldg(e.off + i);
-  __syncthreads();
-}
-// The entry that row t belongs to (off[i] <= t < off[i + 1]); -1 if none.
-__device__ __forceinline__ int entry_of(const CacheEntries& e, const int32_t* sm, int t) {
-  if (!e.off) return t;
-  if (e.n == 0) return -1;
-  if (e.n >= kOffsetsMax) return t < __ldg(e.off) || t >= __ldg(e.off + e.n) ? -1 : find_candidate(e.off, e.n, t);
-  if (t < sm[0] || t >= sm[e.n]) return -1;
-  int lo = 0, hi = e.n;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (sm[mid] <= t) lo = mid; else hi = mid;
-  }
-  return lo;
-}
-
-// Where row t of the call is cached: page (>= 0) and offset in it; -1 if the row belongs to no entry, -2 if it should be in
-// the cache and is not.
-__device__ __forceinline__ int locate_token(const CacheView& v, const CacheEntries& e, const int32_t* sm, int t, int* offset, int* end) {
-  *end = t + 1;  // (rows up to here follow in the same entry and page)
-  const int i = entry_of(e, sm, t);
-  if (i < 0) return -1;
-  const EntryInfo info = load_entry(v, e, i);
-  const int pos = info.len - info.rows + (t - info.row0);
-  if (info.slot < 0 || t >= info.row0 + info.rows || pos < 0) return -2;
-  const int page = __ldg(v.table + (int64_t)info.slot * v.max_pages + pos / kPageTokens);
-  if (page < 0 || page >= v.num_pages) return -2;
-  *offset = pos % kPageTokens;
-  *end = min(t + kPageTokens - *offset, info.row0 + info.rows);
-  return page;
-}
-
-// Sixteen channels of a group of 64; the other three neighbours (lanes of an aligned group of four) hold the rest.  (With eight channels a
-// lane, what every lane does for a token made it 20 instructions a value instead of 16: 54 us for 32 thousand tokens of 8 heads of 128, now 51.)
-struct Piece {
-  uint4 raw[2];  // bf16
-  __device__ __forceinline__ float value(int i) const {
-    const uint4& r = raw[i >> 3];
-    const uint32_t w = (i & 7) < 2 ? r.x : (i & 7) < 4 ? r.y : (i & 7) < 6 ? r.z : r.w;
-    return __uint_as_float(i & 1 ? w & 0xffff0000u : w << 16);
-  }
-};
-struct Packed {
-  uint2 codes;
-  __half scale, low;
-  bool fits;
-};
-__device__ __forceinline__ __nv_bfloat162 as_bf162(uint32_t v) { return *reinterpret_cast<__nv_bfloat162*>(&v); }
-
-// 4-bit storage of the group.  The minimum and maximum are found on bf16 pairs (exact, NaN stays NaN); one shuffle a step carries
-// (max, -min).
-__device__ __forceinline__ Packed pack_group(const Piece& x) {
-  __nv_bfloat162 top = as_bf162(x.raw[0].x), low = top;
-#pragma unroll
-  for (int i = 1; i < 8; ++i) {
-    const uint4& r = x.raw[i >> 2];
-    const __nv_bfloat162 v = as_bf162((i & 3) == 0 ? r.x : (i & 3) == 1 ? r.y : (i & 3) == 2 ? r.z : r.w);
-    top = __hmax2_nan(top, v);
-    low = __hmin2_nan(low, v);
-  }
-  low = __hneg2(low);
-  __nv_bfloat162 both = __hmax2_nan(__lows2bfloat162(top, low), __highs2bfloat162(top, low));
-#pragma unroll
-  for (int step = 1; step < 4; step <<= 1) both = __hmax2_nan(both, __shfl_xor_sync(0xffffffffu, both, step));
-  const float high = __low2float(both);
-  Packed p;
-  p.low = __float2half_rn(-__high2float(both));
-  const float base = __half2float(p.low);
-  // (high - base) / 15, correctly rounded (Markstein: a quotient from the rounded reciprocal, corrected by its exact remainder)
-  const float range = high - base, q0 = range * (1.f / 15.f);
-  p.scale = __float2half_rn(fmaf(fmaf(-15.f, q0, range), 1.f / 15.f, q0));
-  const float s = __half2float(p.scale);
-  p.fits = s < INFINITY && fabsf(base) < INFINITY;  // (false for NaN)
-  p.codes = make_uint2(0, 0);
-  if (s > 0.f) {
-    // rint((x - base) / s), clipped to 0 .. 15, as x * k - base * k with k = 1 / (15 s): the saturating multiply-add clips it to 0 .. 1 and
-    // the next one takes it to 0 .. 15 and rounds.  With |base| <= 100 s the products are wrong by (115 + 100) 2^-22 < 10^-4 steps at most,
-    // which matters next to a half only; then, and with a larger base, the division is made.  (The division, the rounding and the conversion of
-    // every value kept the kernel at a quarter of the memory's rate: 128 us for 32 thousand tokens of 8 heads of 128, 209 MB; a subtraction, a
-    // multiplication and two comparisons to clip every value: 64 us, so 54.)
-    float inv;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));
-    const float magic = 12582912.f;  // 1.5 * 2^23: what is added to it is rounded to an integer, ties to even
-    const float k = inv * (1.f / 15.f), offset = -base * k;
-    const uint64_t magic2 = pack_f32x2(magic, magic), back2 = pack_f32x2(-magic, -magic), up2 = pack_f32x2(15.f, 15.f), down2 = pack_f32x2(-15.f, -15.f);
-    float far = fabsf(base) <= 100.f * s ? 0.f : 1.f;
-    uint32_t half[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      float n[4], first = 0.f;
-#pragma unroll
-      for (int i = 0; i < 4; i += 2) {
-        const uint64_t t = pack_f32x2(__saturatef(fmaf(x.value(4 * j + i), k, offset)), __saturatef(fmaf(x.value(4 * j + i + 1), k, offset)));
-        const uint64_t c = fma_f32x2(t, up2, magic2), r = add_f32x2(c, back2);
-        float c0, c1, d0, d1;
-        unpack_f32x2(c, c0, c1);
-        unpack_f32x2(r, n[i], n[i + 1]);
-        unpack_f32x2(fma_f32x2(t, down2, r), d0, d1);
-        far = fmaxf(far, fmaxf(fabsf(d0), fabsf(d1)));
-        if (i == 0) first = c0;
-      }
-      half[j] = __float_as_uint(fmaf(n[3], 4096.f, fmaf(n[2], 256.f, fmaf(n[1], 16.f, first))));  // (four codes in the lowest 16 bits)
-    }
-    p.codes = make_uint2(__byte_perm(half[0], half[1], 0x5410), __byte_perm(half[2], half[3], 0x5410));
-    if (far > 0.4999f) {
-      p.codes = make_uint2(0, 0);
-#pragma unroll
-      for (int i = 0; i < 16; ++i)
-        (i < 8 ? p.codes.x : p.codes.y) |= (__float_as_uint(fminf(fmaxf(__fdiv_rn(x.value(i) - base, s), 0.f), 15.f) + magic) & 15u) << (4 * (i & 7));
-    }
-  }
-  return p;
-}
-
 // D / 16 neighbouring lanes take a token of a kv head, sixteen channels of K and of V each, kTokens tokens in turn; a thread block has
 // consecutive tokens of a head, so that the pieces of neighbouring tokens (adjacent in a page) meet in one sector.  Bytes: 4 * D in
 // and 1.125 * D out per (token, kv head).  32 thousand tokens of 8 heads of 128: 51 us, 3.4 TB/s; two thirds of the issue slots are taken (16
@@ -166,24 +47,7 @@ __global__ void __launch_bounds__(256, 5) append_kernel(CacheView v, CacheEntrie
       if (page >= 0 && __ldg(v.refs + page) != 1) page = -2;  // shared (or free): not this sequence's to write
       if (page == -2) cache_fault(status);
     }
-    Packed pk = pack_group(xk), pv = pack_group(xv);
-    // one lane that does not fit makes the token (its L lanes) NaN
-    const uint32_t misfits = __ballot_sync(0xffffffffu, !(pk.fits && pv.fits)) >> ((threadIdx.x & 31) / L * L) & ((1u << L) - 1);
-    if (misfits) {
-      pk.codes = pv.codes = make_uint2(0, 0);
-      pk.scale = pv.scale = pv.low = __ushort_as_half(0);  // (V 0: it meets weights 0 in the rows that do not see the token)
-      pk.low = __ushort_as_half(0x7e00);
-    }
-    if (!in || page < 0) continue;
-    uint8_t* run = v.pages + page * v.page_bytes + (int64_t)h * 72 * D;
-    uint8_t* code = run + (lane >> 1) * 1024 + offset * 16 + (lane & 1) * 8;
-    *reinterpret_cast<uint2*>(code) = pk.codes;
-    *reinterpret_cast<uint2*>(code + 32 * D) = pv.codes;
-    if ((lane & 3) == 0) {
-      __half2* meta = reinterpret_cast<__half2*>(run + 64 * D + ((lane >> 2) * kPageTokens + offset) * 4);
-      meta[0] = __halves2half2(pk.scale, pk.low);
-      meta[D] = __halves2half2(pv.scale, pv.low);
-    }
+    store_token<D>(v, h, lane, in ? page : -1, offset, xk, xv);
   }
 }
 
@@ -266,25 +130,6 @@ PlanSpace plan_space(void* ws, const CacheView& v) {
   p.to = p.from + v.num_pages;
   p.extra = p.to + v.num_pages;
   return p;
-}
-
-__device__ __forceinline__ int pages_of(int tokens) { return tokens / kPageTokens + (tokens % kPageTokens != 0); }
-
-// How many sequences hold the page that a table entry names: 0 for one that is free, or not in the pool.
-__device__ __forceinline__ int holders(const CacheView& v, int page) { return page >= 0 && page < v.num_pages ? v.refs[page] : 0; }
-
-// Whether the n slots lie in [0, max_seqs) and are distinct.  `seen`: shared bitmap of max_seqs bits, left with the slots' bits
-// set.  Every thread of the block gets the answer.
-__device__ bool slots_distinct(const int32_t* slots, int n, int max_seqs, uint32_t* seen) {
-  for (int i = threadIdx.x; i < (max_seqs + 31) / 32; i += blockDim.x) seen[i] = 0;
-  __syncthreads();
-  bool ok = true;
-  for (int i = threadIdx.x; i < n; i += blockDim.x) {
-    const int s = slots ? slots[i] : i;
-    if (s < 0 || s >= max_seqs) { ok = false; continue; }
-    if (atomicOr(&seen[s >> 5], 1u << (s & 31)) >> (s & 31) & 1) ok = false;
-  }
-  return __syncthreads_and(ok);
 }
 
 // The numbers of the first `want` pages with refs 0 into list (in global memory, visible to the block afterwards); false if there are fewer.
@@ -627,82 +472,8 @@ __global__ void __launch_bounds__(256) compact_kernel(CacheView v, PlanSpace ws,
 }
 
 // ------------------------------------------------------------------------------------------------ host side
-// The context's device is made current for the length of a call (the caller's is put back).
-class DeviceGuard {
- public:
-  explicit DeviceGuard(int device) {
-    if (cudaGetDevice(&before_) != cudaSuccess) before_ = device;
-    if (before_ != device) cudaSetDevice(device);
-    device_ = device;
-  }
-  ~DeviceGuard() {
-    if (before_ != device_) cudaSetDevice(before_);
-  }
-  DeviceGuard(const DeviceGuard&) = delete;
-
- private:
-  int before_ = 0, device_ = 0;
-};
-
-const char* desc_problem(const essa_cache_desc* c, int32_t* code) {
-  *code = ESSA_ERR_INVALID_ARG;
-  if (!c) return "NULL descriptor";
-  if (c->layers < 1 || c->num_pages < 1 || c->kv_heads < 1 || c->max_seqs < 1 || c->max_pages < 1) return "sizes must be positive";
-  if (!c->pages || !c->table || !c->lengths || !c->refs) return "NULL buffer in the descriptor";
-  if (reinterpret_cast<uintptr_t>(c->pages) & 15) return "pages must be 16-byte aligned";
-  if ((reinterpret_cast<uintptr_t>(c->table) | reinterpret_cast<uintptr_t>(c->lengths) | reinterpret_cast<uintptr_t>(c->refs)) & 3) return "table, lengths and refs must be 4-byte aligned";
-  *code = ESSA_ERR_UNSUPPORTED_SHAPE;
-  if (c->head_dim != 64 && c->head_dim != 128) return "head_dim must be 64 or 128";
-  if (c->max_seqs > ESSA_CACHE_MAX_SEQS) return "max_seqs > ESSA_CACHE_MAX_SEQS";
-  if (c->max_pages > 0x7fffffff / ESSA_CACHE_PAGE_TOKENS) return "max_pages * 64 must be below 2^31";
-  if (c->kv_heads > 4096) return "kv_heads > 4096";
-  *code = ESSA_OK;
-  return nullptr;
-}
-
-int32_t view_of(essa_ctx* ctx, const char* what, const essa_cache_desc* c, int32_t layer, CacheView* v) {
-  if (!ctx) return ESSA_ERR_INVALID_ARG;
-  int32_t code;
-  if (const char* why = desc_problem(c, &code)) return fail(ctx, code, std::string(what) + ": " + why);
-  if (layer < 0 || layer >= c->layers) return fail(ctx, ESSA_ERR_INVALID_ARG, std::string(what) + ": layer outside the cache");
-  v->page_bytes = essa_cache_page_bytes(c->kv_heads, c->head_dim);
-  v->layer_bytes = v->page_bytes * c->num_pages;
-  v->pages = static_cast<uint8_t*>(c->pages) + layer * v->layer_bytes;
-  v->table = c->table;
-  v->lengths = c->lengths;
-  v->refs = c->refs;
-  v->num_pages = c->num_pages;
-  v->kv_heads = c->kv_heads;
-  v->head_dim = c->head_dim;
-  v->max_seqs = c->max_seqs;
-  v->max_pages = c->max_pages;
-  v->layers = c->layers;
-  return ESSA_OK;
-}
-
-int32_t check_entries(essa_ctx* ctx, const char* what, const CacheEntries& e) {
-  if (e.n < 0 || e.T < 0) return fail(ctx, ESSA_ERR_INVALID_ARG, std::string(what) + ": negative n or T");
-  if (!e.off && e.n != e.T) return fail(ctx, ESSA_ERR_INVALID_ARG, std::string(what) + ": without tok_offsets every entry has one row (n = T)");
-  return ESSA_OK;
-}
-// A token-major bf16 buffer of `width` elements per row.
-int32_t check_rows(essa_ctx* ctx, const char* what, const char* name, const void* p, int64_t ld, int64_t width) {
-  if (!p) return fail(ctx, ESSA_ERR_INVALID_ARG, std::string(what) + ": " + name + " is NULL");
-  if (reinterpret_cast<uintptr_t>(p) & 15) return fail(ctx, ESSA_ERR_INVALID_ARG, std::string(what) + ": " + name + " must be 16-byte aligned");
-  if (ld < width || ld % 8) return fail(ctx, ESSA_ERR_INVALID_ARG, std::string(what) + ": the row pitch of " + name + " must be a multiple of 8 elements and hold a row");
-  return ESSA_OK;
-}
 int64_t pages_workspace(const essa_cache_desc* c) {
   return 256 + 4 * (2 * (int64_t)c->num_pages + (c->num_pages > c->max_seqs ? c->num_pages : c->max_seqs));
-}
-int32_t check_workspace(essa_ctx* ctx, const char* what, const void* ws, int64_t bytes, int64_t need) {
-  if (!ws || (reinterpret_cast<uintptr_t>(ws) & 15)) return fail(ctx, ESSA_ERR_INVALID_ARG, std::string(what) + ": the workspace must be a 16-byte aligned device buffer");
-  if (bytes < need) return fail(ctx, ESSA_ERR_INVALID_ARG, std::string(what) + ": the workspace is too small");
-  return ESSA_OK;
-}
-int32_t launched(essa_ctx* ctx, const char* what, int kernels) {
-  ctx->launches += kernels;
-  return check_cuda(ctx, cudaGetLastError(), what);
 }
 // Which attention kernel: up to 16 query rows per (entry, kv head) take the one that widens codes straight into mma operands; with more the
 // 256-row tiles of tcgen05 re-use a widened page often enough.  Few rows / tiles, us, heads of 128 channels: 32 sequences of 4096 tokens, 8 kv
@@ -718,31 +489,10 @@ int64_t token_blocks(int32_t T, const CacheView& v, int channels, int per) {
 // back: 124 us, with one token per thread 159 (before other steps); 256 tokens (too few for the rule): 45 us with either.
 bool four_tokens(const essa_ctx* ctx, int32_t T, const CacheView& v, int channels) { return token_blocks(T, v, channels, 4) >= 4 * ctx->sm_count; }
 constexpr int kAppendChannels = 16, kReadChannels = 8;
-// The kernel behind a plan: its thread blocks are on their SMs when the plan is ready (they wait for the end of the plan's launch).
-template <class... Args>
-cudaError_t launch_behind_plan(const essa_ctx* ctx, cudaStream_t stream, void (*kernel)(Args...), Args... args) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(ctx->sm_count * 8);
-  cfg.blockDim = dim3(256);
-  cfg.stream = stream;
-  cudaLaunchAttribute attr;
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kernel, args...);
-}
-
 }  // namespace
 }  // namespace essa
 
 using namespace essa;
-
-#define ESSA_TRY(call)                     \
-  do {                                     \
-    const int32_t st_ = (call);            \
-    if (st_ != ESSA_OK) return st_;        \
-  } while (0)
 
 extern "C" {
 
@@ -840,6 +590,13 @@ int32_t essa_cache_read(essa_ctx* ctx, const essa_cache_desc* cache, int32_t lay
 int32_t essa_cache_attend(essa_ctx* ctx, const essa_cache_desc* cache, int32_t layer, const void* q, int64_t ld_q, int32_t q_heads, int32_t T,
                           const int32_t* slots, const int32_t* tok_offsets, int32_t n, int32_t max_new, float scale, void* out, int64_t ld_out,
                           void* workspace, int64_t workspace_bytes, void* stream) {
+  return essa_cache_attend_masked(ctx, cache, nullptr, layer, q, ld_q, q_heads, T, slots, tok_offsets, n, max_new, scale, out, ld_out, workspace, workspace_bytes,
+                                  stream);
+}
+
+int32_t essa_cache_attend_masked(essa_ctx* ctx, const essa_cache_desc* cache, const essa_attend_mask* mask, int32_t layer, const void* q, int64_t ld_q,
+                                 int32_t q_heads, int32_t T, const int32_t* slots, const int32_t* tok_offsets, int32_t n, int32_t max_new, float scale, void* out,
+                                 int64_t ld_out, void* workspace, int64_t workspace_bytes, void* stream) {
   CacheView v;
   ESSA_TRY(view_of(ctx, "cache_attend", cache, layer, &v));
   const CacheEntries e{slots, tok_offsets, n, T};
@@ -849,6 +606,21 @@ int32_t essa_cache_attend(essa_ctx* ctx, const essa_cache_desc* cache, int32_t l
   if (!(scale > 0.f && scale <= 0x1p127f)) return fail(ctx, ESSA_ERR_INVALID_ARG, "cache_attend: scale must be positive and at most 2^127");
   const int64_t group = q_heads / v.kv_heads;
   if (group * T > 0x7fffffff) return fail(ctx, ESSA_ERR_UNSUPPORTED_SHAPE, "cache_attend: T * (q_heads / kv_heads) must be below 2^31");
+  AttendMask m{0x7fffffff, 0, nullptr, 0};
+  if (mask) {
+    if (mask->window < 0 || mask->sinks < 0) return fail(ctx, ESSA_ERR_INVALID_ARG, "cache_attend: negative window or sinks");
+    if (mask->drafts) {
+      if (reinterpret_cast<uintptr_t>(mask->drafts) & 3) return fail(ctx, ESSA_ERR_INVALID_ARG, "cache_attend: drafts must be 4-byte aligned");
+      if (mask->draft_words < 1 || mask->draft_words > ESSA_CACHE_MAX_DRAFTS / 32) return fail(ctx, ESSA_ERR_UNSUPPORTED_SHAPE, "cache_attend: draft_words outside 1 .. ESSA_CACHE_MAX_DRAFTS / 32");
+      if (mask->window && mask->window < 32 * mask->draft_words) return fail(ctx, ESSA_ERR_UNSUPPORTED_SHAPE, "cache_attend: with drafts, the window must be at least 32 * draft_words");
+      m.drafts = mask->drafts;
+      m.words = mask->draft_words;
+    }
+    if (mask->window) {
+      m.window = mask->window;
+      m.sinks = mask->sinks < v.max_pages * kPageTokens ? mask->sinks : v.max_pages * kPageTokens;  // (first tokens are always seen without a window)
+    }
+  }
   if (T == 0 || n == 0) return ESSA_OK;
   ESSA_TRY(check_rows(ctx, "cache_attend", "q", q, ld_q, (int64_t)q_heads * v.head_dim));
   ESSA_TRY(check_rows(ctx, "cache_attend", "out", out, ld_out, (int64_t)q_heads * v.head_dim));
@@ -868,6 +640,8 @@ int32_t essa_cache_attend(essa_ctx* ctx, const essa_cache_desc* cache, int32_t l
   a.scale = scale * 1.4426950408889634f;
   a.ws = static_cast<float*>(workspace);
   a.status = ctx->d_status;
+  a.m = m;
+  a.masked = m.window != 0x7fffffff || m.drafts;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   return few_rows(max_new * group) ? launch_attend_decode(ctx, a, max_new * group, s) : launch_attend_tiles(ctx, a, s);
 }

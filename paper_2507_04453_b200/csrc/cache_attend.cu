@@ -32,11 +32,22 @@ constexpr int kThreads = kWarps * 32 + 32;    // + one copying warp
 
 // Row blocks of R rows; every row block of an entry walks all its pages (the few rows of an entry see nearly the same ones).
 // kSetup: 256 sequences of up to 1024 tokens take 43.3 us with 2, 40.2 with 3, 38.8 with 5, 38.6 with 7, 39.6 with 10 (cut anywhere).
-template <int ROWS>
+template <int ROWS, bool MASKED>
 struct DecodeList {
   static constexpr int R = ROWS, kMinRun = 2, kSetup = 5;
-  __device__ static int tiles(const EntryInfo& e, const AttendArgs&, int) { return max((e.len + kPageTokens - 1) / kPageTokens, 1); }
-  __device__ static long long per_head(const EntryInfo& e, const AttendArgs& a) { return (long long)row_blocks(e, a.group, R) * (tiles(e, a, 0) + kSetup); }
+  static int64_t most_tiles(const AttendArgs& a) { return MASKED ? most_masked_tiles(a, (R - 1) / a.group + 2) : a.v.max_pages; }
+  __device__ static Span span(const EntryInfo& e, const AttendArgs& a, int rb) {
+    if (!MASKED) return {0, 0, max((e.len + kPageTokens - 1) / kPageTokens, 1)};
+    return span_of(e, a.m, first_token(a, rb, R), last_token(e, a, rb, R));
+  }
+  __device__ static int tiles(const EntryInfo& e, const AttendArgs& a, int rb) { return span(e, a, rb).tiles; }
+  __device__ static long long per_head(const EntryInfo& e, const AttendArgs& a) {
+    const int blocks = row_blocks(e, a.group, R);
+    if (!MASKED) return (long long)blocks * (tiles(e, a, 0) + kSetup);
+    long long sum = 0;
+    for (int rb = 0; rb < blocks; ++rb) sum += tiles(e, a, rb) + kSetup;
+    return sum;
+  }
 };
 
 __device__ __forceinline__ void ldmatrix_x4(uint32_t addr, uint32_t (&r)[4]) {
@@ -92,11 +103,11 @@ struct Shape {
 // Thread blocks per SM: what shared memory and registers allow.
 constexpr int attend_blocks_per_sm(int head_dim, int nt) { return nt == 1 ? 3 : 2; }
 
-template <int D, int NT>
+template <int D, int NT, bool MASKED>
 __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_decode_kernel(AttendArgs a) {
   using S = Shape<D, NT>;
   constexpr int R = S::R, G = D / kCacheGroup, CH = D / 32;
-  using L = DecodeList<R>;
+  using L = DecodeList<R, MASKED>;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ RunShared run_sm;
   __shared__ volatile int abort_flag;
@@ -126,9 +137,10 @@ __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_
       take_block<L>(a, c, left, tile, stop);
       const int32_t* row = a.v.table + (int64_t)max(c.info.slot, 0) * a.v.max_pages;
       const bool none = c.info.len == 0;
+      const Span span = L::span(c.info, a, c.rb);
       for (; tile < stop; ++tile) {
         if (filled >= S::kStages && !wait_napping(empty + 8 * st, phase ^ 1, &abort_flag, a.status)) { ok = false; break; }
-        const int page = none ? -1 : __ldg(row + tile);
+        const int page = none ? -1 : __ldg(row + (MASKED ? span.page(tile) : tile));
         const bool there = page >= 0 && page < a.v.num_pages;
         if (!there && (!none || c.info.slot < 0)) cache_fault(a.status);
         bad_page[st] = !there;
@@ -168,7 +180,14 @@ __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_
     uint32_t qf[NT][CH][4];
     float qsum[NT][G][2], start[NT][G][4];  // per group: the sum of q; minus what the 1024 in the codes' numbers adds
     float sc[NT][2], back[NT][2];           // softmax scale in the units of the row; what the row was divided by
-    int limit[NT][2], lowest = 0x7fffffff;
+    int limit[NT][2], lowest = 0x7fffffff;  // (with a mask: the token of the entry that the column is, -1 for a column without a row)
+    Span span;
+    int reach = 0;
+    if (MASKED) {
+      span = L::span(c.info, a, c.rb);
+      lowest = seen_by_all(a.m, c.info, first_token(a, c.rb, R));
+      reach = hidden_to_some(a.m, c.info, last_token(c.info, a, c.rb, R));
+    }
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       const int r = r0 + nt * 8 + g;
@@ -222,12 +241,18 @@ __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_
         back[nt][x] = __shfl_sync(0xffffffffu, down, 8 * t + 4 * x);
         sc[nt][x] = softmax_scale(a.scale * back[nt][x]);
         const int rc = r0 + nt * 8 + 2 * t + x;  // tokens that column 2 t + x sees; a column without a row sees all and is not written
-        limit[nt][x] = rc < rows ? c.info.len - c.info.rows + a.by_group(rc) + 1 : 0x7fffffff;
-        lowest = min(lowest, limit[nt][x]);
+        if (MASKED) {
+          limit[nt][x] = rc < rows ? a.by_group(rc) : -1;
+        } else {
+          limit[nt][x] = rc < rows ? c.info.len - c.info.rows + a.by_group(rc) + 1 : 0x7fffffff;
+          lowest = min(lowest, limit[nt][x]);
+        }
       }
     }
-    lowest = min(lowest, __shfl_xor_sync(0xffffffffu, lowest, 1));
-    lowest = min(lowest, __shfl_xor_sync(0xffffffffu, lowest, 2));
+    if (!MASKED) {
+      lowest = min(lowest, __shfl_xor_sync(0xffffffffu, lowest, 1));
+      lowest = min(lowest, __shfl_xor_sync(0xffffffffu, lowest, 2));
+    }
     float o[NT][CH][2][4];
     // running maximum, the score that moves it, what weights are relative to (the maximum, or 0 before there is one); sum of weights; second
     // term of O
@@ -254,7 +279,7 @@ __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_
       if (dead) continue;
       const uint32_t blk = ring + st * S::kBytes;
       const __half2* meta = reinterpret_cast<const __half2*>(smem + st * S::kBytes + 64 * D) + key0 + g;  // (scale, minimum) of K, then of V
-      const int pos0 = tile * kPageTokens + key0, pos = pos0 + g;  // tokens of this lane's scores: pos + 8 n, n < 2 KS
+      const int pos0 = (MASKED ? span.page(tile) : tile) * kPageTokens + key0, pos = pos0 + g;  // tokens of this lane's scores: pos + 8 n, n < 2 KS
       if (!bad_page[st] && pos0 < c.info.len) {
         // --- scores; of slice k: token pos + 16 k in [0..1], + 8 in [2..3]
         float s[KS][NT][4];
@@ -307,7 +332,27 @@ __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_
           for (int y = 0; y < 2; ++y)
 #pragma unroll
             for (int i = 0; i < G; ++i) mv[k][y][i] = __half22float2(meta[(G + i) * kPageTokens + 16 * k + 8 * y]);
-        if (pos0 + 16 * KS > lowest || pos0 + 16 * KS > c.info.len) {
+        if (MASKED && (pos0 + 16 * KS > lowest || pos0 + 16 * KS > c.info.len || (pos0 < reach && pos0 + 16 * KS > a.m.sinks))) {
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+              const uint32_t see = (limit[nt][x] < 0 ? 0xffffffffu : visible(a.m, c.info, limit[nt][x], pos0)) & low_bits(c.info.len - pos0);
+#pragma unroll
+              for (int k = 0; k < KS; ++k)
+#pragma unroll
+                for (int y = 0; y < 2; ++y)
+                  if (!(see >> (g + 16 * k + 8 * y) & 1)) s[k][nt][2 * y + x] = -INFINITY;
+            }
+#pragma unroll
+          for (int k = 0; k < KS; ++k)
+#pragma unroll
+            for (int y = 0; y < 2; ++y)
+#pragma unroll
+              for (int i = 0; i < G; ++i)
+                if (pos + 16 * k + 8 * y >= c.info.len) mv[k][y][i] = make_float2(0.f, 0.f);
+        }
+        if (!MASKED && (pos0 + 16 * KS > lowest || pos0 + 16 * KS > c.info.len)) {
           // hidden tokens (whatever their scores are, NaN too); behind the sequence's end the page holds anything
 #pragma unroll
           for (int k = 0; k < KS; ++k)
@@ -505,19 +550,25 @@ __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_
   }
 }
 
-template <int D, int NT>
+template <int D, int NT, bool MASKED>
 int32_t launch(essa_ctx* ctx, AttendArgs& a, cudaStream_t stream) {
   using S = Shape<D, NT>;
+  using L = DecodeList<S::R, MASKED>;
   const int grid = ctx->sm_count * attend_blocks_per_sm(D, NT);
   a.partials_at = partials_at(grid);
-  a.whole = whole_blocks<DecodeList<S::R>>(a, grid);
-  cudaError_t e = allow_shared<attend_decode_kernel<D, NT>>(S::kSmem, ctx->device);
+  a.whole = whole_blocks<L>(a, grid);
+  cudaError_t e = allow_shared<attend_decode_kernel<D, NT, MASKED>>(S::kSmem, ctx->device);
   if (e != cudaSuccess) return check_cuda(ctx, e, "cudaFuncSetAttribute (attend)");
-  attend_decode_kernel<D, NT><<<grid, kThreads, S::kSmem, stream>>>(a);
+  attend_decode_kernel<D, NT, MASKED><<<grid, kThreads, S::kSmem, stream>>>(a);
   e = cudaGetLastError();
   if (e != cudaSuccess) return check_cuda(ctx, e, "attend launch");
   ++ctx->launches;
-  return launch_join<DecodeList<S::R>, D>(ctx, a, grid, S::R / 4, stream);
+  return launch_join<L, D>(ctx, a, grid, S::R / 4, stream);
+}
+template <bool MASKED>
+int32_t launch_shape(essa_ctx* ctx, AttendArgs& a, int nt, cudaStream_t stream) {
+  if (a.v.head_dim == 64) return nt == 1 ? launch<64, 1, MASKED>(ctx, a, stream) : launch<64, 2, MASKED>(ctx, a, stream);
+  return nt == 1 ? launch<128, 1, MASKED>(ctx, a, stream) : launch<128, 2, MASKED>(ctx, a, stream);
 }
 
 }  // namespace
@@ -532,8 +583,7 @@ int64_t attend_decode_workspace(int head_dim, int64_t rows_hint, int sm_count) {
 
 int32_t launch_attend_decode(essa_ctx* ctx, AttendArgs& a, int64_t rows_hint, cudaStream_t stream) {
   const int nt = attend_nt(rows_hint);
-  if (a.v.head_dim == 64) return nt == 1 ? launch<64, 1>(ctx, a, stream) : launch<64, 2>(ctx, a, stream);
-  return nt == 1 ? launch<128, 1>(ctx, a, stream) : launch<128, 2>(ctx, a, stream);
+  return a.masked ? launch_shape<true>(ctx, a, nt, stream) : launch_shape<false>(ctx, a, nt, stream);
 }
 
 }  // namespace essa

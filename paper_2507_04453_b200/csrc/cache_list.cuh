@@ -8,7 +8,9 @@
 // followed by its key tiles; a cut between those leaves it whole to the run behind the cut.
 //
 // A list policy L gives R (query rows of a row block), tiles(info, args, rb) >= 1 (key tiles of a row block, so that rows that
-// see nothing are still written), per_head(info, args) (the elements of all row blocks of an entry), kSetup and kMinRun.
+// see nothing are still written), per_head(info, args) (the elements of all row blocks of an entry), most_tiles(args) (an upper bound of
+// tiles that the host knows), kSetup and kMinRun.  With a mask (a window, drafted tokens) a row block's tiles are the pages that some row of it can
+// see: those of the first tokens, then, some pages on, those from its first row's window to its last row's end (struct Span).
 #pragma once
 
 #include <atomic>
@@ -33,6 +35,13 @@ struct Divisor {
 #endif
 };
 
+// What rows see besides the tokens up to their own (essa_attend_mask).
+struct AttendMask {
+  int32_t window, sinks;   // 0x7fffffff: no window
+  const uint32_t* drafts;  // NULL: no drafted tokens
+  int32_t words;
+};
+
 struct AttendArgs {
   CacheView v;
   CacheEntries e;
@@ -46,6 +55,8 @@ struct AttendArgs {
   int64_t partials_at;  // floats before the partial results
   int32_t whole;        // a run has the row blocks that begin in it, to their ends
   int32_t* status;
+  int32_t masked;
+  AttendMask m;
 };
 
 // Bytes of the workspace for `grid` thread blocks, two partial results of `floats` each; the partial results begin after the run places.
@@ -66,7 +77,14 @@ bool whole_blocks(const AttendArgs& a, int grid) {
   const int64_t by_rows = (int64_t)a.e.T * ((a.group + L::R - 1) / L::R), by_entries = (int64_t)a.e.T * a.group / L::R + a.e.n;
   const int64_t blocks = (by_rows < by_entries ? by_rows : by_entries) * a.v.kv_heads;  // at most
   const int64_t idle = blocks > 4 * (int64_t)grid ? grid / 2 : (blocks + grid - 1) / grid * grid - blocks;
-  return a.v.max_pages <= kWholePages && idle * (a.v.max_pages + L::kSetup) <= (int64_t)kJoin * grid;
+  const int64_t pages = L::most_tiles(a);
+  return pages <= kWholePages && idle * (pages + L::kSetup) <= (int64_t)kJoin * grid;
+}
+// Most pages that a row block of `tokens` tokens can see under a.m.
+inline int64_t most_masked_tiles(const AttendArgs& a, int64_t tokens) {
+  const int64_t reach = (int64_t)a.m.window + tokens + (a.m.drafts ? 32 * a.m.words : 0);
+  const int64_t pages = (reach + kPageTokens - 1) / kPageTokens + 1 + ((int64_t)a.m.sinks + kPageTokens - 1) / kPageTokens;
+  return pages < a.v.max_pages ? pages : a.v.max_pages;
 }
 
 #ifdef __CUDACC__
@@ -129,6 +147,50 @@ struct Cursor {  // a place in the list
   int entry, kvh, rb, at, blocks, tiles;  // at: element of the row block
   EntryInfo info;
 };
+
+// The key tiles that some row of a row block sees: list place j is page j of the first `head`, page j + skip of the rest.
+struct Span {
+  int head, skip, tiles;
+  __device__ __forceinline__ int page(int j) const { return j < head ? j : j + skip; }
+};
+// First token that a row at position pos sees through the window.
+__device__ __forceinline__ int window_start(const AttendMask& m, int pos) { return pos >= m.window ? pos - m.window + 1 : 0; }
+// Of the rows that are tokens t0 .. t1 of an entry.  A draft's position is the history's length plus the drafts it sees less one, and it may see any draft.
+__device__ __forceinline__ Span span_of(const EntryInfo& e, const AttendMask& m, int t0, int t1) {
+  const int past = e.len - e.rows, end = max(m.drafts ? e.len : past + t1 + 1, 0);
+  const int first = window_start(m, m.drafts ? past - 1 : past + t0) / kPageTokens, head = min((m.sinks + kPageTokens - 1) / kPageTokens, first);
+  return {head, first - head, max((end + kPageTokens - 1) / kPageTokens - (first - head), 1)};
+}
+// The lowest n bits (n is brought to 0 .. 32).
+__device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1; }
+// Which of the 32 tokens from key0 on a row sees that is a token of an entry.  (For tiles at the edges only.)
+__device__ __forceinline__ uint32_t visible(const AttendMask& m, const EntryInfo& e, int token, int key0) {
+  const int past = e.len - e.rows;
+  if (!m.drafts) {
+    const int limit = past + token + 1;
+    return low_bits(limit - key0) & (~low_bits(window_start(m, limit - 1) - key0) | low_bits(m.sinks - key0));
+  }
+  const uint32_t* mine = m.drafts + (int64_t)(e.row0 + token) * m.words;
+  uint32_t bits = low_bits(past - key0);
+  if (m.window != 0x7fffffff) {
+    int seen = 0;
+    for (int w = 0; w < m.words; ++w) seen += __popc(__ldg(mine + w));
+    bits &= ~low_bits(window_start(m, past + seen - 1) - key0) | low_bits(m.sinks - key0);
+  }
+  const int at = key0 - past;  // the draft that is the first of the 32 tokens
+  if (at > -32 && at < 32 * m.words) {
+    const int w = at >> 5;
+    const uint32_t lo = w >= 0 ? __ldg(mine + w) : 0u, hi = w + 1 < m.words ? __ldg(mine + w + 1) : 0u;
+    bits |= __funnelshift_r(lo, hi, at & 31) & low_bits(e.len - key0);
+  }
+  return bits;
+}
+// All rows from token t0 of an entry on see the tokens before this one that their windows leave; all up to token t1 have windows that reach back to
+// that one.
+__device__ __forceinline__ int seen_by_all(const AttendMask& m, const EntryInfo& e, int t0) { return m.drafts ? e.len - e.rows : e.len - e.rows + t0 + 1; }
+__device__ __forceinline__ int hidden_to_some(const AttendMask& m, const EntryInfo& e, int t1) {
+  return window_start(m, m.drafts ? e.len - e.rows + min(32 * m.words, e.rows) : e.len - e.rows + t1);
+}
 
 // (rows * group < 2^31 is checked on the host)
 __device__ __forceinline__ int row_blocks(const EntryInfo& e, int group, int R) { return (int)(((uint32_t)e.rows * (uint32_t)group + R - 1) / R); }
@@ -230,6 +292,12 @@ __device__ __forceinline__ void next_block(const AttendArgs& a, Cursor& c) {
     }
   }
   c.tiles = L::tiles(c.info, a, c.rb);
+}
+
+// First and last token of an entry's row block rb of R rows.
+__device__ __forceinline__ int first_token(const AttendArgs& a, int rb, int R) { return a.by_group(rb * R); }
+__device__ __forceinline__ int last_token(const EntryInfo& e, const AttendArgs& a, int rb, int R) {
+  return min(e.rows - 1, a.by_group(min(rb * R, 0x7fffffff - R) + R - 1));
 }
 
 template <class L, int D>

@@ -30,13 +30,17 @@ namespace essa {
 namespace {
 
 // kSetup: the ragged prompts take 483 us with 3, 479 with 4, 483 with 5, 493 with 6.
+template <bool MASKED>
 struct TileList {
   static constexpr int R = 256, kKeys = kPageTokens, kMinRun = 2, kSetup = 4;
+  static int64_t most_tiles(const AttendArgs& a) { return MASKED ? most_masked_tiles(a, (R - 1) / a.group + 2) : a.v.max_pages; }
   // keys that the last row of the row block sees, in tiles
-  __device__ static int tiles(const EntryInfo& e, const AttendArgs& a, int rb) {
-    const int last = min(e.rows - 1, a.by_group(min(rb * R, 0x7fffffff - R) + R - 1));
-    return max((e.len - e.rows + last + 1 + kKeys - 1) / kKeys, 1);
+  __device__ static Span span(const EntryInfo& e, const AttendArgs& a, int rb) {
+    const int last = last_token(e, a, rb, R);
+    if (MASKED) return span_of(e, a.m, first_token(a, rb, R), last);
+    return {0, 0, max((e.len - e.rows + last + 1 + kKeys - 1) / kKeys, 1)};
   }
+  __device__ static int tiles(const EntryInfo& e, const AttendArgs& a, int rb) { return span(e, a, rb).tiles; }
   __device__ static long long per_head(const EntryInfo& e, const AttendArgs& a) {
     long long sum = 0;
     const int blocks = row_blocks(e, a.group, R);
@@ -151,10 +155,10 @@ __device__ __forceinline__ uint4 widen_clipped(uint32_t w, float2 m) {
   }
   return make_uint4(r[0], r[1], r[2], r[3]);
 }
-template <int D>
+template <int D, bool MASKED>
 __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a) {
   using M = Mem<D>;
-  using L = TileList;
+  using L = TileList<MASKED>;
   extern __shared__ uint8_t smem_raw[];
   __shared__ RunShared run_sm;
   __shared__ volatile int abort_flag;
@@ -170,6 +174,13 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
   };
   __shared__ Place places[kSoftWarps + kWidenWarps];
   __shared__ int out_of[kSoftWarps][2][3];  // a softmax warp's present and next row block: first row of q, kv head, row of the group
+  // ... and, with a mask, its entry, its key tiles, and the tokens from which on (up to which) some row may not see all
+  struct Seen {
+    EntryInfo info;
+    Span span;
+    int lowest, reach;
+  };
+  __shared__ Seen seen_of[MASKED ? kSoftWarps : 1];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const uint32_t bars = base + M::kBars;
   const auto bar = [&](int i) { return bars + 8 * i; };
@@ -221,7 +232,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
     // What a thread needs of the row block that it is at.
     struct Block {
       int first, n;
-      int limit, lowest;  // keys that the row sees (0x7fffffff: no such row); the fewest of the warp's rows
+      int limit, lowest;  // keys that the row sees (0x7fffffff: no such row); the fewest of the warp's rows.  With a mask: the row's token of the entry, -1
       float back;         // what the row of Q was divided by
       bool whole;
     };
@@ -243,6 +254,16 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
           if (c.rb * L::R + h * 128 < c.info.rows * a.group) break;
           tile += b.n;
           if (left <= 0) return false;
+        }
+        if (MASKED) {
+          // (the present row block's have been used: all its tiles are done)
+          __syncwarp();
+          if (lane == 0) {
+            const int last = c.info.rows * a.group - 1, r = c.rb * L::R + h * 128 + quad * 32;
+            seen_of[warp] = Seen{c.info, L::span(c.info, a, c.rb), seen_by_all(a.m, c.info, a.by_group(min(r, last))),
+                                 hidden_to_some(a.m, c.info, a.by_group(min(r + 31, last)))};
+          }
+          __syncwarp();
         }
         rows = c.info.rows * a.group;
         r0 = c.rb * L::R + h * 128;
@@ -304,8 +325,12 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
       const int r = r0 + row;
       b.back = row_scale[h * 128 + row];
       // rows behind the last one have q = 0 and are not written, whatever they see
-      b.limit = r < rows ? past + a.by_group(r) + 1 : 0x7fffffff;
-      b.lowest = __shfl_sync(0xffffffffu, b.limit, 0);
+      if (MASKED) {
+        b.limit = r < rows ? a.by_group(r) : -1;
+      } else {
+        b.limit = r < rows ? past + a.by_group(r) + 1 : 0x7fffffff;
+        b.lowest = __shfl_sync(0xffffffffu, b.limit, 0);
+      }
       return true;
     };
     const bool wide_out = !(reinterpret_cast<uintptr_t>(a.out) & 31) && a.ld_out % 16 == 0;  // whole 32-byte sectors
@@ -334,7 +359,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
         const int* o = out_of[warp][parity ^ (more ? 1 : 0)];
         const int r = o[2] + row, tok = a.by_group(r);
         __nv_bfloat16* out = a.out + (int64_t)(o[0] + tok) * a.ld_out + (int64_t)(o[1] * a.group + r - tok * a.group) * D;
-        const bool there = b.limit != 0x7fffffff;
+        const bool there = MASKED ? b.limit >= 0 : b.limit != 0x7fffffff;
         float* partial = partial_of<L, D>(a, blockIdx.x, b.first == 0);
 #pragma unroll 1
         for (int d = 0; d < D / 2; d += 32) {
@@ -387,7 +412,23 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
       const auto arrived = [&](int j, int t) {
         await(kSFull + 2 * h + (t & 1), s_ph >> (t & 1) & 1);
         s_ph ^= 1u << (t & 1);
-        const int key0 = (b.first + j) * L::kKeys, bad = tile_bad[t & 7];
+        const int bad = tile_bad[t & 7];
+        if (MASKED) {
+          const Seen& at = seen_of[warp];
+          const int key0 = at.span.page(b.first + j) * L::kKeys;
+          if (key0 + L::kKeys > at.lowest || (key0 < at.reach && key0 + L::kKeys > a.m.sinks) || bad) {
+            const uint32_t see = bad ? 0u : b.limit < 0 ? 0xffffffffu : visible(a.m, at.info, b.limit, key0 + 32 * part);
+            uint32_t v[32];
+            tmem_ld32_issue(scores_at(t) + 32 * part, v);
+            tmem_ld_done(v);
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if (!(see >> i & 1)) v[i] = 0xff800000u;
+            tmem_st32(scores_at(t) + 32 * part, v);
+          }
+          return;
+        }
+        const int key0 = (b.first + j) * L::kKeys;
         if (key0 + L::kKeys > b.lowest || bad) {
           const int see = bad ? 0 : b.limit - key0 - 32 * part;  // this thread's keys before this one are seen
           uint32_t v[32];
@@ -407,7 +448,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
         // Whether to look for the maximum before the weights: in the first tile, and where the weights by the one so far turn out too large or
         // there is none yet though the row sees the tile (the pages before are not there): weights by 0 could then all vanish.  (A row's two
         // threads have the same m and limit, so the two warps decide alike.)
-        bool look = j == 0 || __any_sync(0xffffffffu, m == -INFINITY && b.limit > (b.first + j) * L::kKeys);
+        // (With a mask a row may have seen nothing yet wherever the tile lies.)
+        bool look = j == 0 || __any_sync(0xffffffffu, m == -INFINITY && (MASKED || b.limit > (b.first + j) * L::kKeys));
         for (;;) {
           uint32_t v[32];
           tmem_ld32_issue(s_at + 32 * part, v);
@@ -496,7 +538,9 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
             const int t0 = a.by_group(c.rb * L::R), t1 = min(c.info.rows, a.by_group(min(c.rb * L::R, 0x7fffffff - L::R) + L::R - 1) + 1);
             for (int t = t0; t < t1; ++t) prefetch_l2(a.q + (int64_t)(c.info.row0 + t) * a.ld_q + (int64_t)c.kvh * a.group * D, a.group * D * 2);
           }
-          for (int p = first; p < stop; ++p) {
+          const Span span = L::span(c.info, a, c.rb);
+          for (int j = first; j < stop; ++j) {
+            const int p = MASKED ? span.page(j) : j;
             if (filled >= kRaw && !wait(kRawEmpty + slot, phase ^ 1)) { ok = false; break; }
             const int page = p < pages ? __ldg(row + p) : -1;
             const bool there = page >= 0 && page < a.v.num_pages;
@@ -590,11 +634,13 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
       bool ok = true;
       for (;;) {
         int j, stop, len;
+        Span span;
         {
           Cursor c = places[warp].c;
           long long left = places[warp].left;
           if (left <= 0) break;
           take_block<L>(a, c, left, j, stop);
+          if (MASKED) span = L::span(c.info, a, c.rb);
           len = c.info.len;
           if (left > 0) next_block<L>(a, c);
           keep_place(c, left);
@@ -606,7 +652,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
           if (!(ok = wait_warp(kRawFull + slot, phase))) break;
           const uint32_t raw = base + M::kRawAt + slot * M::kRun;
           const bool bad = raw_bad[slot] != 0;
-          const bool in = !bad && j * kPageTokens + token < len;
+          const bool in = !bad && (MASKED ? span.page(j) : j) * kPageTokens + token < len;
           const uint32_t sw = (uint32_t)(token & 7);
           float2 mk = lds_half2(raw + 64 * D + (group * kPageTokens + token) * 4), mv = lds_half2(raw + 68 * D + (group * kPageTokens + token) * 4);
           uint4 ck[kWords / 4], cv[kWords / 4];
@@ -653,26 +699,27 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
   if (warp == kMmaWarp) tmem_dealloc(tmem, 512);
 }
 
-template <int D>
+template <int D, bool MASKED>
 int32_t launch(essa_ctx* ctx, AttendArgs& a, cudaStream_t stream) {
   constexpr int smem = Mem<D>::kBytes + 1024;
   a.partials_at = partials_at(ctx->sm_count);
-  a.whole = whole_blocks<TileList>(a, ctx->sm_count);
-  cudaError_t e = allow_shared<attend_tiles_kernel<D>>(smem, ctx->device);
+  a.whole = whole_blocks<TileList<MASKED>>(a, ctx->sm_count);
+  cudaError_t e = allow_shared<attend_tiles_kernel<D, MASKED>>(smem, ctx->device);
   if (e != cudaSuccess) return check_cuda(ctx, e, "cudaFuncSetAttribute (attend tiles)");
-  attend_tiles_kernel<D><<<ctx->sm_count, kThreads, smem, stream>>>(a);
+  attend_tiles_kernel<D, MASKED><<<ctx->sm_count, kThreads, smem, stream>>>(a);
   e = cudaGetLastError();
   if (e != cudaSuccess) return check_cuda(ctx, e, "attend tiles launch");
   ++ctx->launches;
-  return launch_join<TileList, D>(ctx, a, ctx->sm_count, 16, stream);
+  return launch_join<TileList<MASKED>, D>(ctx, a, ctx->sm_count, 16, stream);
 }
 
 }  // namespace
 
-int64_t attend_tiles_workspace(int head_dim, int sm_count) { return attend_workspace(sm_count, (int64_t)TileList::R * (head_dim + 2)); }
+int64_t attend_tiles_workspace(int head_dim, int sm_count) { return attend_workspace(sm_count, (int64_t)TileList<false>::R * (head_dim + 2)); }
 
 int32_t launch_attend_tiles(essa_ctx* ctx, AttendArgs& a, cudaStream_t stream) {
-  return a.v.head_dim == 64 ? launch<64>(ctx, a, stream) : launch<128>(ctx, a, stream);
+  if (a.masked) return a.v.head_dim == 64 ? launch<64, true>(ctx, a, stream) : launch<128, true>(ctx, a, stream);
+  return a.v.head_dim == 64 ? launch<64, false>(ctx, a, stream) : launch<128, false>(ctx, a, stream);
 }
 
 }  // namespace essa
