@@ -510,7 +510,7 @@ int32_t essa_cache_keep(essa_ctx* ctx, const essa_cache_desc* cache, const int32
  * video; one axis for text) and a frequency of its own, so that any layout of sections and any scaling of frequencies can be given; a frequency of 0 leaves a pair as
  * it is (times magnitude), and negated positions turn back.
  * Angles are exact: a frequency is held as a 64-bit fraction of a turn, turns[i] = frac(frequency / 2 pi) 2^64, the product with a position
- * is taken modulo a turn in integers, and sine and cosine see a fraction that is wrong by 2^-32 of a turn at most, however far the position. */
+ * is taken modulo a turn in integers: wrong by the position times 2^-64 of a turn, however far the position. */
 #define ESSA_ROTARY_MAX_DIM 256
 #define ESSA_ROTARY_MAX_AXES 4
 typedef struct essa_rotary {
@@ -524,8 +524,8 @@ typedef struct essa_rotary {
 /* Fill *out from frequencies [head_dim / 2] (radians per position, finite) and axis [head_dim / 2] (NULL: all 0), both on the host.  Needs no device. */
 int32_t essa_rotary_make(int32_t head_dim, int32_t axes, int32_t adjacent, float magnitude, const double* frequencies, const int32_t* axis, essa_rotary* out);
 /* out[t][h] = x[t][h] turned by positions[.][t], t < T, h < heads.  x, out [T] rows of heads * head_dim bf16 dev, ld_x / ld_out elements apart (multiples of 8;
- * 16-byte aligned); out may be x (with the same pitch), and overlaps it in no other way.  positions [axes] rows of T int32 dev, ld_positions apart.  Sine, cosine and the
- * products are fp32, rounded to bf16 once. */
+ * 16-byte aligned); out may be x (with the same pitch), and overlaps it in no other way.  positions [axes] rows of T int32 dev, ld_positions apart.  Sine and cosine are rounded
+ * to fp32, the products and their sum are fp32, the result is rounded to bf16 once. */
 int32_t essa_rotary_apply(essa_ctx* ctx, const essa_rotary* rotary, const void* x, int64_t ld_x, int32_t heads, int32_t T, const int32_t* positions,
                           int64_t ld_positions, void* out, int64_t ld_out, void* stream);
 /* essa_rotary_apply on q and k, and essa_cache_append of the turned k (rounded to bf16) and of v, in one launch: q_out [T] rows of q_heads * head_dim bf16

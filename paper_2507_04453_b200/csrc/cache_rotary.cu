@@ -3,10 +3,12 @@
 //
 // Pair (a, b) with t = position * frequency: (a cos t - b sin t, b cos t + a sin t).  In fp32 the angle of a far position loses its fraction (2^-24 of
 // 10^5 radians is a hundredth); here a frequency is a 64-bit fraction of a turn, and the product with a position modulo 2^64 is the angle's fraction, exact but for
-// the frequency's own 2^-64: one wide multiplication, then sincospif of its upper 32 bits.
+// the frequency's own 2^-64: one wide multiplication, then sincospi.
 //
 // What bounds it: bytes.  Sine and cosine depend on the token and the pair only, so a thread block computes them once for its tokens and
 // all their heads use them: a lane keeps those of its eight pairs in registers while its warp walks the heads.
+// 33 thousand tokens of 40 + 8 heads of 128, stored too (844 MB): 160 us, 5.3 TB/s.  217 us with one head's loads at a time, three thread blocks per SM and four
+// tokens per thread block; two heads at a time 199, eight tokens 175, four thread blocks per SM 160.  Four heads at a time, sixteen tokens: the same.
 #include <cmath>
 
 #include "cache_api.cuh"
@@ -16,6 +18,8 @@ namespace essa {
 namespace {
 
 constexpr int kRotaryWarps = 8;
+constexpr int kUnroll = 2;     // heads of a warp whose loads are on their way together
+constexpr int kMaxGroups = 2;  // see rotary_kernel
 
 struct RotaryArgs {
   essa_rotary r;
@@ -27,16 +31,18 @@ struct RotaryArgs {
   int32_t q_heads, T;
 };
 
+// Both products rounded, so that the pair's two members are treated alike (a multiply-add would round one product and not the other).
+__device__ __forceinline__ float turned(float x, float y, float c, float s) { return __fadd_rn(__fmul_rn(x, c), __fmul_rn(y, s)); }
 // Two channels times (cos, sin): the low halves of a and b, then the high ones.
 __device__ __forceinline__ void turn_pair(uint32_t& a, uint32_t& b, float2 c0, float2 c1) {
   const float a0 = __uint_as_float(a << 16), a1 = __uint_as_float(a & 0xffff0000u), b0 = __uint_as_float(b << 16), b1 = __uint_as_float(b & 0xffff0000u);
-  a = pack_bf16x2(fmaf(a0, c0.x, -b0 * c0.y), fmaf(a1, c1.x, -b1 * c1.y));
-  b = pack_bf16x2(fmaf(b0, c0.x, a0 * c0.y), fmaf(b1, c1.x, a1 * c1.y));
+  a = pack_bf16x2(turned(a0, b0, c0.x, -c0.y), turned(a1, b1, c1.x, -c1.y));
+  b = pack_bf16x2(turned(b0, a0, c0.x, c0.y), turned(b1, a1, c1.x, c1.y));
 }
 // Two neighbouring channels as one pair.
 __device__ __forceinline__ uint32_t turn_word(uint32_t w, float2 c) {
   const float a = __uint_as_float(w << 16), b = __uint_as_float(w & 0xffff0000u);
-  return pack_bf16x2(fmaf(a, c.x, -b * c.y), fmaf(b, c.x, a * c.y));
+  return pack_bf16x2(turned(a, b, c.x, -c.y), turned(b, a, c.x, c.y));
 }
 // A lane's sixteen channels of a row: eight pairs.
 struct Chunk {
@@ -63,21 +69,41 @@ struct TokenPlace {
   int pos;           // -1: unknown
 };
 
-// A warp has 32 / (D / 16) tokens, D / 16 lanes each (D = 0: of a.r.head_dim channels, some lanes may have none); the thread block's warps take the
-// heads in turn, those of blockIdx.y too.  STORE: K and V are stored (D = 64 or 128).
+// A warp has 32 / (D / 16) tokens, D / 16 lanes each (D = 0: of a.r.head_dim channels, some lanes may have none).  A thread block has `groups` times as many
+// (1 or 2): that many sets of warps, each of which deals the heads to its warps and to blockIdx.y in turn.  STORE: K and V are stored (D = 64 or 128).
 template <int D, bool STORE>
-__global__ void __launch_bounds__(kRotaryWarps * 32) rotary_kernel(const __grid_constant__ RotaryArgs a, CacheView v, CacheEntries e, const __nv_bfloat16* k, int64_t ld_k,
-                                                                   const __nv_bfloat16* val, int64_t ld_v, int32_t* status) {
+__global__ void __launch_bounds__(kRotaryWarps * 32, 4)
+    rotary_kernel(const __grid_constant__ RotaryArgs a, CacheView v, CacheEntries e, const __nv_bfloat16* k, int64_t ld_k, const __nv_bfloat16* val, int64_t ld_v,
+                  int groups, int32_t* status) {
   const int dim = D ? D : a.r.head_dim, lanes = dim / 16, tokens = 32 / lanes, half = dim / 2;
-  __shared__ float2 cs_of[256];  // [token][pair]
-  __shared__ TokenPlace place[16];
+  __shared__ float2 cs_of[256 * kMaxGroups];  // [token][pair]
+  __shared__ TokenPlace place[8 * kMaxGroups];
   __shared__ int32_t offsets[STORE ? kOffsetsMax : 1];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int64_t t0 = (int64_t)blockIdx.x * tokens;
+  const int64_t t0 = (int64_t)blockIdx.x * tokens * groups;
   const bool adjacent = a.r.adjacent != 0;
+  const int set = kRotaryWarps / groups;  // warps that share tokens
+  const int token = lane / lanes + warp / set * tokens, l = lane % lanes;
+  const int64_t t = t0 + token;
+  const bool in = lane / lanes < tokens && t < a.T;
+  // which eight pairs: with halves of a row apart, lanes l and l + lanes / 2 have neighbouring ones (see below)
+  const int chunk = adjacent || !STORE ? l : 2 * (l % (lanes / 2)) + l / (lanes / 2);
+  const int lo_at = adjacent ? 16 * chunk : 8 * chunk, hi_at = adjacent ? lo_at + 8 : half + lo_at;
+  const int first = blockIdx.y * set + warp % set, step = gridDim.y * set;
+  const __nv_bfloat16* from = a.q + t * a.ld_q;
+  Chunk x[kUnroll];
+  const auto load = [&](int h) {
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      if (h + u * step >= a.q_heads) break;
+      x[u].lo = *reinterpret_cast<const uint4*>(from + (int64_t)(h + u * step) * dim + lo_at);
+      x[u].hi = *reinterpret_cast<const uint4*>(from + (int64_t)(h + u * step) * dim + hi_at);
+    }
+  };
+  if (in) load(first);  // (on its way while the tokens are looked up)
   if (STORE) {
     stage_offsets(e, offsets);
-    if (tid < tokens) {
+    if (tid < tokens * groups) {
       TokenPlace p{-1, 0, -1};
       const int64_t t = t0 + tid;
       const int i = t < a.T ? entry_of(e, offsets, (int)t) : -1;
@@ -97,7 +123,7 @@ __global__ void __launch_bounds__(kRotaryWarps * 32) rotary_kernel(const __grid_
     }
     __syncthreads();
   }
-  for (int i = tid; i < tokens * half; i += kRotaryWarps * 32) {
+  for (int i = tid; i < groups * tokens * half; i += kRotaryWarps * 32) {
     const int j = i / half, pair = i - j * half;
     const int64_t t = t0 + j;
     int pos = 0;
@@ -106,41 +132,36 @@ __global__ void __launch_bounds__(kRotaryWarps * 32) rotary_kernel(const __grid_
     } else if (STORE) {
       pos = place[j].pos;
     }
-    const uint64_t turns = (uint64_t)(int64_t)pos * a.r.turns[pair] + (1ull << 31);
-    float s, c;
-    sincospif((float)(int32_t)(turns >> 32) * 0x1p-31f, &s, &c);
-    cs_of[i] = make_float2(c * a.r.magnitude, s * a.r.magnitude);
+    const uint64_t turns = (uint64_t)(int64_t)pos * a.r.turns[pair];
+    // (in fp64: no slower here, and sine and cosine are the nearest fp32 numbers)
+    double s, c;
+    sincospi((double)(int64_t)turns * 0x1p-63, &s, &c);
+    cs_of[i] = make_float2((float)c * a.r.magnitude, (float)s * a.r.magnitude);
   }
   __syncthreads();
-  const int token = lane / lanes, l = lane % lanes;
-  const int64_t t = t0 + token;
-  // which eight pairs: with halves of a row apart, lanes l and l + lanes / 2 have neighbouring ones (see below)
-  const int chunk = adjacent || !STORE ? l : 2 * (l % (lanes / 2)) + l / (lanes / 2);
-  const int lo_at = adjacent ? 16 * chunk : 8 * chunk, hi_at = adjacent ? lo_at + 8 : half + lo_at;
   float2 cs[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) cs[i] = token < tokens ? cs_of[token * half + 8 * chunk + i] : make_float2(0.f, 0.f);
-  const bool in = token < tokens && t < a.T;
+  for (int i = 0; i < 8; ++i) cs[i] = in ? cs_of[token * half + 8 * chunk + i] : make_float2(0.f, 0.f);
   TokenPlace p{-1, 0, -1};
   if (STORE && in) p = place[token];
   const bool writes_q = in && (!STORE || (p.page != -1 && (a.positions || p.pos >= 0)));
-  const int first = blockIdx.y * kRotaryWarps + warp, step = gridDim.y * kRotaryWarps;
-  int h = first;
   if (writes_q) {
-    const __nv_bfloat16* from = a.q + t * a.ld_q;
     __nv_bfloat16* to = a.q_out + t * a.ld_q_out;
-    for (; h < a.q_heads; h += step) {
-      Chunk x;
-      x.lo = *reinterpret_cast<const uint4*>(from + (int64_t)h * dim + lo_at);
-      x.hi = *reinterpret_cast<const uint4*>(from + (int64_t)h * dim + hi_at);
-      turn(x, cs, adjacent);
-      *reinterpret_cast<uint4*>(to + (int64_t)h * dim + lo_at) = x.lo;
-      *reinterpret_cast<uint4*>(to + (int64_t)h * dim + hi_at) = x.hi;
+    for (int h = first; h < a.q_heads;) {
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) {
+        if (h + u * step >= a.q_heads) break;
+        turn(x[u], cs, adjacent);
+        *reinterpret_cast<uint4*>(to + (int64_t)(h + u * step) * dim + lo_at) = x[u].lo;
+        *reinterpret_cast<uint4*>(to + (int64_t)(h + u * step) * dim + hi_at) = x[u].hi;
+      }
+      h += kUnroll * step;
+      load(h);
     }
   }
   if constexpr (STORE) {
     constexpr int L = D / 16;
-    h = first - a.q_heads % step;  // (the warps go on in turn)
+    int h = first - a.q_heads % step;  // (the warps go on in turn)
     if (h < 0) h += step;
     for (; h < v.kv_heads; h += step) {
       Chunk xk;
@@ -191,11 +212,21 @@ int32_t check_positions(essa_ctx* ctx, const char* what, const int32_t* position
   if (ld < T) return fail(ctx, ESSA_ERR_INVALID_ARG, std::string(what) + ": the rows of positions must hold T of them");
   return ESSA_OK;
 }
-// Heads are dealt to blockIdx.y until there are two thread blocks for every SM (a decode step's few tokens), a head or more for each warp.
-int head_splits(const essa_ctx* ctx, int64_t blocks, int heads) {
+// How a call of T tokens is divided: token groups of a thread block, and what share of the heads.
+struct RotaryGrid {
+  dim3 grid;
+  int groups;
+};
+// Two groups share a thread block's look-ups where that leaves every SM two thread blocks (9 thousand tokens of 14 heads of 64: 10 us, with one group 11.5); a
+// decode step's few tokens have their heads dealt to several thread blocks, until there are two for every SM or a head for each warp.
+RotaryGrid rotary_grid(const essa_ctx* ctx, int64_t T, int head_dim, int heads) {
+  const int64_t tokens = 32 / (head_dim / 16);
+  int groups = kMaxGroups;
+  while (groups > 1 && (T + tokens * groups - 1) / (tokens * groups) < 2 * ctx->sm_count) groups /= 2;
+  const int64_t blocks = (T + tokens * groups - 1) / (tokens * groups);
   int splits = 1;
-  while (blocks * splits < 2 * ctx->sm_count && splits * kRotaryWarps < heads) splits *= 2;
-  return splits;
+  while (blocks * splits < 2 * ctx->sm_count && splits * (kRotaryWarps / groups) < heads) splits *= 2;
+  return {dim3((unsigned)blocks, splits), groups};
 }
 
 }  // namespace
@@ -240,10 +271,9 @@ int32_t essa_rotary_apply(essa_ctx* ctx, const essa_rotary* rotary, const void* 
   ESSA_TRY(check_positions(ctx, "rotary_apply", positions, ld_positions, T));
   DeviceGuard guard(ctx->device);
   const RotaryArgs a{*rotary, positions, ld_positions, static_cast<const __nv_bfloat16*>(x), static_cast<__nv_bfloat16*>(out), ld_x, ld_out, heads, T};
-  const int64_t tokens = 32 / (rotary->head_dim / 16), blocks = (T + tokens - 1) / tokens;
-  const dim3 grid((unsigned)blocks, head_splits(ctx, blocks, heads));
+  const RotaryGrid g = rotary_grid(ctx, T, rotary->head_dim, heads);
   const auto run = [&](auto kernel) {
-    kernel<<<grid, kRotaryWarps * 32, 0, static_cast<cudaStream_t>(stream_v)>>>(a, CacheView{}, CacheEntries{}, nullptr, 0, nullptr, 0, ctx->d_status);
+    kernel<<<g.grid, kRotaryWarps * 32, 0, static_cast<cudaStream_t>(stream_v)>>>(a, CacheView{}, CacheEntries{}, nullptr, 0, nullptr, 0, g.groups, ctx->d_status);
   };
   if (rotary->head_dim == 64) run(rotary_kernel<64, false>);
   else if (rotary->head_dim == 128) run(rotary_kernel<128, false>);
@@ -272,11 +302,10 @@ int32_t essa_cache_append_rotary(essa_ctx* ctx, const essa_cache_desc* cache, in
   if (positions) ESSA_TRY(check_positions(ctx, "cache_append_rotary", positions, ld_positions, T));
   DeviceGuard guard(ctx->device);
   const RotaryArgs a{*rotary, positions, ld_positions, static_cast<const __nv_bfloat16*>(q), static_cast<__nv_bfloat16*>(q_out), ld_q, ld_q_out, q_heads, T};
-  const int64_t tokens = 32 / (v.head_dim / 16), blocks = (T + tokens - 1) / tokens;
-  const dim3 grid((unsigned)blocks, head_splits(ctx, blocks, q_heads + v.kv_heads));
+  const RotaryGrid g = rotary_grid(ctx, T, v.head_dim, q_heads + v.kv_heads);
   const auto run = [&](auto kernel) {
-    kernel<<<grid, kRotaryWarps * 32, 0, static_cast<cudaStream_t>(stream_v)>>>(a, v, e, static_cast<const __nv_bfloat16*>(k), ld_k, static_cast<const __nv_bfloat16*>(val),
-                                                                               ld_v, ctx->d_status);
+    kernel<<<g.grid, kRotaryWarps * 32, 0, static_cast<cudaStream_t>(stream_v)>>>(a, v, e, static_cast<const __nv_bfloat16*>(k), ld_k,
+                                                                                 static_cast<const __nv_bfloat16*>(val), ld_v, g.groups, ctx->d_status);
   };
   v.head_dim == 64 ? run(rotary_kernel<64, true>) : run(rotary_kernel<128, true>);
   return launched(ctx, "cache_append_rotary", 1);
