@@ -437,13 +437,15 @@ class Rotary:
 
     def _positions(self, torch, positions, T, index):
         """Checks positions, [axes, T] (or [T] for one axis) int32 with contiguous rows; (pointer, elements between rows)."""
-        shape = positions.shape
-        if positions.dtype is not torch.int32 or positions.get_device() != index or tuple(shape) not in (((self.axes, T), (T,)) if self.axes == 1 else ((self.axes, T),)) \
-                or (T > 1 and positions.stride(-1) != 1):
-            raise EssaError(ESSA_ERR_INVALID_ARG, f"rotary: positions must be int32 [{self.axes}, {T}] with contiguous rows, on the data's device")
-        ld = positions.stride(0) if len(shape) == 2 and self.axes > 1 else T
-        if ld < T:
-            raise EssaError(ESSA_ERR_INVALID_ARG, "rotary: the rows of positions overlap")
+        shape, axes, ld = positions.shape, self.axes, T
+        ok = positions.dtype is torch.int32 and positions.get_device() == index and shape[-1:] == (T,) and shape[:-1] in ((axes,), () if axes == 1 else (axes,))
+        if ok and not positions.is_contiguous():
+            ok = T < 2 or positions.stride(-1) == 1
+            if ok and axes > 1:
+                ld = positions.stride(0)
+                ok = ld >= T  # (rows that do not overlap)
+        if not ok:
+            raise EssaError(ESSA_ERR_INVALID_ARG, f"rotary: positions must be int32 [{axes}, {T}] with contiguous rows, on the data's device")
         return positions.data_ptr() or None, ld
 
 
@@ -641,10 +643,10 @@ class KvCache:
         p = self._ints("parents", parents)
         a, b, n = self._entries(T, slots, tok_offsets)
         if stream is None:
-            drafts, pos = parents.new_empty((T, words)), parents.new_empty((T,)) if positions else None
+            drafts, pos = parents.new_empty((T, words)), self._empty_like(parents) if positions else None
         else:
             with self.ctx.torch.cuda.stream(stream):
-                drafts, pos = parents.new_empty((T, words)), parents.new_empty((T,)) if positions else None
+                drafts, pos = parents.new_empty((T, words)), self._empty_like(parents) if positions else None
         self._check(self._lib.essa_cache_tree(self.ctx.handle, self._ref, p, T, a, b, n, drafts.data_ptr() or None, words, pos.data_ptr() or None if positions else None,
                                               self._raw(stream)))
         return drafts, pos
@@ -813,24 +815,33 @@ class Context:
 
     def rotary(self, rotary: "Rotary", x, positions, out=None, stream=None):
         """essa_rotary_apply: x [T, heads, head_dim] bf16 (rows may be strided) turned by positions [axes, T] int32 (or [T] for one axis); out may be x."""
-        torch = self.torch
-        if x.dim() != 3 or x.shape[2] != rotary.head_dim or x.shape[1] < 1:
+        torch, index, shape = self.torch, self.device.index, x.shape
+        if len(shape) != 3 or shape[2] != rotary.head_dim or shape[1] < 1:
             raise EssaError(ESSA_ERR_INVALID_ARG, f"rotary: x must be a tensor [T, heads, {rotary.head_dim}]")
-        T, heads, d = x.shape
-        if out is None:
+        T, heads, d = shape
+
+        def pitch(name, t):  # elements between rows
+            ok = t.dtype is torch.bfloat16 and t.get_device() == index and t.shape == shape
+            if ok and t.is_contiguous():
+                return heads * d
+            if ok and T:
+                stride = t.stride()
+                if stride[2] == 1 and (heads == 1 or stride[1] == d):
+                    return stride[0] if T > 1 else heads * d
+            raise EssaError(ESSA_ERR_INVALID_ARG, f"rotary: {name} must be a bf16 tensor [T, heads, {d}] on {self.device} whose rows are contiguous")
+        ldx = pitch("x", x)
+        pp, ldp = rotary._positions(torch, positions, T, index)
+        if out is not None:
+            ldo = pitch("out", out)
+        else:
+            ldo = heads * d
             if stream is None:
-                out = x.new_empty(x.shape)
+                out = torch.empty_like(x) if x.is_contiguous() else x.new_empty(shape)
             else:
                 with torch.cuda.stream(stream):
-                    out = x.new_empty(x.shape)
-        for name, t in (("x", x), ("out", out)):
-            if t.dtype is not torch.bfloat16 or t.get_device() != self.device.index or t.shape != x.shape or \
-                    (T and not t.is_contiguous() and not (t.stride(2) == 1 and (heads == 1 or t.stride(1) == d))):
-                raise EssaError(ESSA_ERR_INVALID_ARG, f"rotary: {name} must be a bf16 tensor [T, heads, {d}] on {self.device} whose rows are contiguous")
-        pp, ldp = rotary._positions(torch, positions, T, self.device.index)
-        ld = [heads * d if T < 2 else t.stride(0) for t in (x, out)]
-        raw = (torch._C._cuda_getCurrentRawStream(self.device.index) if stream is None else stream.cuda_stream) or None
-        self._check(self.lib.essa_rotary_apply(self.handle, rotary._ref, x.data_ptr() or None, ld[0], heads, T, pp, ldp, out.data_ptr() or None, ld[1], raw))
+                    out = x.new_empty(shape)
+        raw = (torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream) or None
+        self._check(self.lib.essa_rotary_apply(self.handle, rotary._ref, x.data_ptr() or None, ldx, heads, T, pp, ldp, out.data_ptr() or None, ldo, raw))
         return out
 
     # -- sampling

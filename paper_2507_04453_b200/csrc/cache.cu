@@ -660,7 +660,7 @@ int32_t essa_cache_fork(essa_ctx* ctx, const essa_cache_desc* cache, const int32
   fork_plan_kernel<<<1, kPlanThreads, seen_bytes(v), stream>>>(v, src, dst, lens, n, ws, ctx->d_status);
   ESSA_TRY(launched(ctx, "cache_fork", 1));
   ++ctx->launches;
-  return check_cuda(ctx, launch_behind_plan(ctx, stream, fork_kernel, v, src, dst, lens, (int)n, ws), "cache_fork");
+  return check_cuda(ctx, launch_behind_plan(stream, dim3(ctx->sm_count * 8), fork_kernel, v, src, dst, lens, (int)n, ws), "cache_fork");
 }
 
 int32_t essa_cache_free(essa_ctx* ctx, const essa_cache_desc* cache, const int32_t* slots, int32_t n, void* stream) {
@@ -700,7 +700,7 @@ int32_t essa_cache_compact(essa_ctx* ctx, const essa_cache_desc* cache, int32_t*
   compact_plan_kernel<<<1 + checks, kPlanThreads, 0, stream>>>(v, ws);
   ESSA_TRY(launched(ctx, "cache_compact", 1));
   ++ctx->launches;
-  return check_cuda(ctx, launch_behind_plan(ctx, stream, compact_kernel, v, ws, checks, used, ctx->d_status), "cache_compact");
+  return check_cuda(ctx, launch_behind_plan(stream, dim3(ctx->sm_count * 8), compact_kernel, v, ws, checks, used, ctx->d_status), "cache_compact");
 }
 
 }  // extern "C"

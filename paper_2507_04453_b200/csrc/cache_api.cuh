@@ -82,9 +82,9 @@ inline int32_t launched(essa_ctx* ctx, const char* what, int kernels) {
 
 // The kernel behind a plan: its thread blocks are on their SMs when the plan is ready (they wait for the end of the plan's launch).
 template <class... Args>
-cudaError_t launch_behind_plan(const essa_ctx* ctx, cudaStream_t stream, void (*kernel)(Args...), Args... args) {
+cudaError_t launch_behind_plan(cudaStream_t stream, dim3 grid, void (*kernel)(Args...), Args... args) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(ctx->sm_count * 8);
+  cfg.gridDim = grid;
   cfg.blockDim = dim3(256);
   cfg.stream = stream;
   cudaLaunchAttribute attr;

@@ -115,29 +115,31 @@ __global__ void __launch_bounds__(kKeepThreads) keep_plan_kernel(CacheView v, co
   }
 }
 
-// A thread takes one piece (sixteen bytes of codes, or a scale and a minimum) of an entry's tokens in one layer and kv head and walks the tokens that
-// stay.  A token moves forward or not at all, and ascending: eight are read before they are written, and what is read later lies behind all that has been
-// written.  Bytes: the tokens that move, in and out; pieces of 16 bytes take half of a sector each.
+// A thread block has an entry and a share of the layers (blockIdx.y of gridDim.y); a thread takes one piece (sixteen bytes of codes, or a scale and a minimum) of the
+// tokens in one layer and kv head after the other, and walks the tokens that stay.  A token moves forward or not at all, and ascending: eight are read before they are
+// written, and what is read later lies behind all that has been written.  Bytes: the tokens that move, in and out; pieces of 16 bytes take half of a sector each.
 template <int D>
-__global__ void __launch_bounds__(256) keep_move_kernel(CacheView v, const int32_t* picks, int64_t ld_picks, int n, const KeepHead* head, const KeepEntry* entries) {
+__global__ void __launch_bounds__(256) keep_move_kernel(CacheView v, const int32_t* picks, int64_t ld_picks, const KeepHead* head, const KeepEntry* entries) {
   constexpr int kCodes = 2 * (D / 32), kPieces = kCodes + 2 * (D / 64);
+  __shared__ KeepEntry k;
+  __shared__ int32_t mine[kMaxDrafts];
   grid_dep_wait();
   if (!head->ok) return;
-  const int64_t units = (int64_t)n * v.layers * v.kv_heads * kPieces;
-  for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < units; u += (int64_t)gridDim.x * 256) {
-    const int piece = (int)(u % kPieces);
-    int64_t rest = u / kPieces;
-    const int h = (int)(rest % v.kv_heads);
-    rest /= v.kv_heads;
-    const int layer = (int)(rest % v.layers), i = (int)(rest / v.layers);
-    const KeepEntry* k = entries + i;
-    if (!k->moves) continue;
-    const int offset = k->offset, count = k->count;
-    const int32_t* mine = picks + i * ld_picks;
-    uint8_t* base = v.pages + layer * v.layer_bytes + (int64_t)h * 72 * D + (piece < kCodes ? piece * 1024 : 64 * D + (piece - kCodes) * 256);
+  const int i = blockIdx.x, tid = threadIdx.x;
+  if (tid < (int)(sizeof(KeepEntry) / 4)) reinterpret_cast<int32_t*>(&k)[tid] = reinterpret_cast<const int32_t*>(entries + i)[tid];
+  __syncthreads();
+  if (!k.moves) return;
+  const int offset = k.offset, count = k.count;
+  if (tid < count) mine[tid] = picks[i * ld_picks + tid];
+  __syncthreads();
+  const int per_layer = v.kv_heads * kPieces, first = (int)((int64_t)v.layers * blockIdx.y / gridDim.y), layers = (int)((int64_t)v.layers * (blockIdx.y + 1) / gridDim.y) - first;
+  for (int64_t u = tid; u < (int64_t)layers * per_layer; u += 256) {
+    const int layer = first + (int)(u / per_layer), rest = (int)(u % per_layer), h = rest / kPieces, piece = rest % kPieces;
+    const bool wide = piece < kCodes;
+    uint8_t* base = v.pages + layer * v.layer_bytes + (int64_t)h * 72 * D + (wide ? piece * 1024 : 64 * D + (piece - kCodes) * 256);
     const auto at = [&](int token) {
       const int place = offset + token;
-      return base + k->pages[place / kPageTokens] * v.page_bytes + place % kPageTokens * (piece < kCodes ? 16 : 4);
+      return base + k.pages[place / kPageTokens] * v.page_bytes + place % kPageTokens * (wide ? 16 : 4);
     };
     for (int m0 = 0; m0 < count; m0 += 8) {
       uint4 x[8];
@@ -148,14 +150,14 @@ __global__ void __launch_bounds__(256) keep_move_kernel(CacheView v, const int32
       for (int j = 0; j < 8; ++j) {
         if (from[j] == m0 + j) continue;
         const uint8_t* p = at(from[j]);
-        if (piece < kCodes) x[j] = *reinterpret_cast<const uint4*>(p);
+        if (wide) x[j] = *reinterpret_cast<const uint4*>(p);
         else x[j].x = *reinterpret_cast<const uint32_t*>(p);
       }
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         if (from[j] == m0 + j) continue;
         uint8_t* p = at(m0 + j);
-        if (piece < kCodes) *reinterpret_cast<uint4*>(p) = x[j];
+        if (wide) *reinterpret_cast<uint4*>(p) = x[j];
         else *reinterpret_cast<uint32_t*>(p) = x[j].x;
       }
     }
@@ -210,8 +212,11 @@ int32_t essa_cache_keep(essa_ctx* ctx, const essa_cache_desc* cache, const int32
   ESSA_TRY(launched(ctx, "cache_keep", 1));
   if (!picks) return ESSA_OK;  // (nothing moves)
   ++ctx->launches;
+  // eight thread blocks per SM, or one for every layer of every entry
+  const int64_t want = (8 * (int64_t)ctx->sm_count + n - 1) / n;
+  const dim3 grid(n, (unsigned)(want < v.layers ? want : v.layers));
   const auto move = v.head_dim == 64 ? keep_move_kernel<64> : keep_move_kernel<128>;
-  return check_cuda(ctx, launch_behind_plan(ctx, stream, move, v, picks, ld_picks, n, (const KeepHead*)head, (const KeepEntry*)entries), "cache_keep");
+  return check_cuda(ctx, launch_behind_plan(stream, grid, move, v, picks, ld_picks, (const KeepHead*)head, (const KeepEntry*)entries), "cache_keep");
 }
 
 }  // extern "C"
