@@ -706,7 +706,7 @@ class KvCache:
             if st != ESSA_OK:
                 raise EssaError(st, "kv_cache: the number of query heads must be a multiple of kv_heads and max_new at least 1")
             need = self._attend_ws[(heads, max_new)] = got.value
-        mask = None if window is None and tree is None else self._mask(window, sinks, tree, shape[0])
+        mask = None if window is None and tree is None and sinks == 0 else self._mask(window, sinks, tree, shape[0])
         if out is None:
             out = self._empty_like(q) if stream is None and q.is_contiguous() else self._empty(shape, stream)
             po, ldo = out.data_ptr() or None, heads * self.head_dim

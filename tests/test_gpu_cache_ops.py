@@ -344,6 +344,21 @@ def test_long_window_is_split_and_joined(torch, ctx, rows, hint, window, sinks):
 
 
 @pytest.mark.parametrize("hint", [1, 100])
+@pytest.mark.parametrize("window,sinks", [(1, 0), (40, 3), (300, 0)])
+def test_rows_that_see_nothing_through_a_window_are_zero(torch, ctx, hint, window, sinks):
+    """Empty sequences, and entries with more rows than their sequence has tokens."""
+    rng = np.random.default_rng(6)
+    p = Pair(torch, ctx, 1, 8, 2, 64, 3, 2)
+    p.place([0, 3, 70], rng)
+    rows = [2, 40, 100]
+    seen = [np.zeros((r, max(n, 0)), bool) for n, r in zip([0, 3, 70], rows)]
+    for n, r, s in zip([0, 3, 70], rows, seen):
+        s[max(0, r - n):] = co.seen_mask(n, min(n, r), window, sinks)
+    got = check_attend(torch, ctx, p, rows, range(3), 8, rng, hint, seen, window=window, sinks=sinks)
+    assert (got[:2] == 0).all() and (got[2:39] == 0).all() and (got[39:42] != 0).any()
+
+
+@pytest.mark.parametrize("hint", [1, 100])
 def test_pages_out_of_every_window_may_be_missing(torch, ctx, hint):
     """... and hold anything: their tokens are not read.  A page that a row can see and that is missing is reported."""
     rng = np.random.default_rng(5)
@@ -527,7 +542,7 @@ def test_masked_attention_refuses(torch, ctx):
     p.place([5], np.random.default_rng(0))
     q, tree = torch.zeros((3, 2, 64), dtype=torch.bfloat16, device="cuda"), torch.zeros((3, 1), dtype=torch.int32, device="cuda")
     off = p.ints([0, 3])
-    for kw in (dict(window=0), dict(window=-1), dict(window=4, sinks=-1), dict(tree=tree[:2]), dict(tree=tree.long()), dict(tree=tree.cpu()), dict(tree=tree[:, 0]),
+    for kw in (dict(window=0), dict(window=-1), dict(window=4, sinks=-1), dict(sinks=-1), dict(tree=tree[:2]), dict(tree=tree.long()), dict(tree=tree.cpu()), dict(tree=tree[:, 0]),
                dict(tree=torch.zeros((3, 9), dtype=torch.int32, device="cuda")), dict(tree=torch.zeros((3, 2), dtype=torch.int32, device="cuda")[:, :1]),
                dict(tree=tree, window=31)):
         with pytest.raises(binding.EssaError):
@@ -787,6 +802,38 @@ def test_a_run_between_the_projections_is_captured_and_replayed(torch, ctx):
         assert all(torch.equal(x, y) for x, y in zip(outs, want))
         for name in ("pages", "table", "lengths", "refs"):
             assert torch.equal(getattr(a.gpu, name), getattr(b.gpu, name)), name
+    assert ctx.get_status() == 0
+
+
+def test_two_graphs_at_once(torch, ctx):
+    """Two masked calls captured on one stream, replayed side by side on two: each has a workspace of its own (both are joined from parts)."""
+    rng = np.random.default_rng(23)
+    p = Pair(torch, ctx, 1, 700, 2, 128, 2, 340)
+    p.place([20001, 19000], rng)
+    tree = p.gpu.tree(p.ints([-1, 0, 0, 2, 1, 3, 3, -1]), p.ints([0, 8]), 8, slots=p.ints([0]))[0]
+    q, off, a, b = p.bf(bf16(rng, (8, 14, 128))), p.ints([0, 8]), p.ints([0]), p.ints([1])
+    calls = [lambda: p.gpu.attend(0, q, off, slots=a, max_new=8, tree=tree), lambda: p.gpu.attend(0, q[:1], off[:2] // 8, slots=b, window=15000, sinks=70),
+             lambda: p.gpu.attend(0, q, off, slots=b, max_new=8, window=18000, sinks=1)]
+    want = [f() for f in calls]
+    side, streams, graphs, outs = torch.cuda.Stream(), [torch.cuda.Stream() for _ in calls], [], []
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        [f() for f in calls]
+    torch.cuda.synchronize()
+    for f in calls:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=side):
+            outs.append(f())
+    for _ in range(20):
+        for x in outs:
+            x.zero_()
+        torch.cuda.synchronize()
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                g.replay()
+                g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(outs, want))
     assert ctx.get_status() == 0
 
 
