@@ -356,7 +356,8 @@ __global__ void __launch_bounds__(128) attend_join_kernel(AttendArgs a) {
         float x[8][V];
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
-          const int at = k0 + min(k + u, n - 1);
+          if (k + u >= n) break;  // (most row blocks have two parts)
+          const int at = k0 + k + u;
           const float* q = partial_of<L, D>(a, at, at == run) + row * D + lane * V;
 #pragma unroll
           for (int i = 0; i < V; i += 2) {
@@ -367,9 +368,10 @@ __global__ void __launch_bounds__(128) attend_join_kernel(AttendArgs a) {
         }
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
-          const float w = __shfl_sync(0xffffffffu, f, min(k + u, n - 1));
+          if (k + u >= n) break;
+          const float w = __shfl_sync(0xffffffffu, f, k + u);
 #pragma unroll
-          for (int i = 0; i < V; ++i) v[i] = fmaf(k + u < n ? w : 0.f, x[u][i], v[i]);
+          for (int i = 0; i < V; ++i) v[i] = fmaf(w, x[u][i], v[i]);
         }
       }
     }
