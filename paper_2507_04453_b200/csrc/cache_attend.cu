@@ -21,6 +21,9 @@
 // group of up to eight heads fills the tensor core's tile, where q as the M operand would leave half of it empty.
 //
 // Work split: cache_list.cuh, with row blocks of 8 or 16 query rows and key tiles of one page.
+// With a mask the list has the pages that a row block can see, and a page at an edge (of a window, of the first tokens, among drafts) is masked by 32 bits per row.
+// A window of 1024 and 4 first tokens of those long sequences (156 MB): 59 us, 2.6 TB/s: seventeen pages of a row block beside five pages' worth of fixed cost, and
+// a join of 5 us.  Queries and row blocks found ahead by the copying warp: 58 (and 36 -> 34 for 256 short ones), left out for its second path of synchronisation.
 #include "cache_list.cuh"
 
 namespace essa {

@@ -17,6 +17,11 @@
 // an eighth, a quarter or a half of the exponentials by a polynomial on the FMA pipe: 486, 498 and 535 (issue slots are as short as the
 // special function units); O through shared memory, so that stores are whole rows: 502 and 481 (an SM stores 32 bytes a cycle either way).
 //
+// With a mask (template) the list has the pages that a row block can see; scores at its edges are masked in tensor memory by 32 bits per thread.  Two chunks of 450 tokens
+// after 16 thousand through a window of 4096 (122 GFLOP): 174 us.  Shared memory is what the products wait for: a tile's operands are 128 KB read by the MMAs and
+// 50 KB of widening, 1390 cycles at 128 bytes a cycle; the MMAs alone, back to back, take 1250.  Eight widening warps: 187 us; row blocks of 128 rows in two
+// streams per thread block, which widen a page twice as often: 238.
+//
 // Roundings: K and V become fp16 as their scale and minimum are applied, (code - 8) * scale + (minimum + 8 scale), with the offset and the
 // result rounded (2^-11 each).  Q is bf16; a row times a power of two, its largest element at 2^13 .. 2^14, is fp16 without loss (elements
 // 2^-27 below the largest lose bits).  P is fp16 (2^-11; weights below 6e-8 of the largest lose bits).  With bf16 operands instead, K's

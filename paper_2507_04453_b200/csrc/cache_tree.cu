@@ -8,7 +8,7 @@ namespace {
 
 // ------------------------------------------------------------------------------------------------ ancestors
 // A thread block per entry, a thread per draft, which climbs from parent to parent in shared memory: as many steps as it is deep (a dozen in the
-// trees that are drafted, 255 at most).  Floor: latency.
+// trees that are drafted, 255 at most).  Bound by latency: 3 us for 64 trees of up to 26 drafts.
 constexpr int kMaxDrafts = ESSA_CACHE_MAX_DRAFTS;
 __global__ void __launch_bounds__(kMaxDrafts) tree_kernel(CacheView v, CacheEntries e, const int32_t* parents, uint32_t* drafts, int words, int32_t* positions, int32_t* status) {
   __shared__ int16_t parent[kMaxDrafts];
@@ -117,7 +117,8 @@ __global__ void __launch_bounds__(kKeepThreads) keep_plan_kernel(CacheView v, co
 
 // A thread block has an entry and a share of the layers (blockIdx.y of gridDim.y); a thread takes one piece (sixteen bytes of codes, or a scale and a minimum) of the
 // tokens in one layer and kv head after the other, and walks the tokens that stay.  A token moves forward or not at all, and ascending: eight are read before they are
-// written, and what is read later lies behind all that has been written.  Bytes: the tokens that move, in and out; pieces of 16 bytes take half of a sector each.
+// written, and what is read later lies behind all that has been written.  Bytes: the tokens that move, in and out; pieces of 16 bytes take half of a sector each.  128 entries of 28 layers and 4 kv heads, three of some 40
+// tokens each: 12 us under ncu (28 MB read for 7), 17 with the plan before it.
 template <int D>
 __global__ void __launch_bounds__(256) keep_move_kernel(CacheView v, const int32_t* picks, int64_t ld_picks, const KeepHead* head, const KeepEntry* entries) {
   constexpr int kCodes = 2 * (D / 32), kPieces = kCodes + 2 * (D / 64);
