@@ -892,3 +892,30 @@ def test_pages_beyond_32_bits(torch, ctx):
     k3, v3 = g.read(0, ints([0, 3]), 3, slots=ints([0]))
     assert torch.equal(k3, rk[[95, 130, 149]]) and torch.equal(v3, rv[[95, 130, 149]]) and g.lengths.tolist() == [93, 0]
     assert g.table[0].tolist() == [pages - 6, pages - 5, -1, -1] and ctx.get_status() == 0
+
+
+def test_more_elements_than_32_bits(torch, ctx):
+    """q of more than 2^31 elements: the last rows are turned, attended to and written at their own addresses."""
+    heads, kv_heads, d, T = 64, 1, 128, (1 << 18) + 300
+    rng = np.random.default_rng(31)
+    g = ctx.kv_cache(1, T // 64 + 1, kv_heads, d, 1, T // 64 + 1)
+    ints = lambda a: torch.tensor(a, dtype=torch.int32, device="cuda")
+    q = torch.empty((T, heads, d), dtype=torch.bfloat16, device="cuda")
+    assert q.numel() > 1 << 31
+    some = to_dev(torch, bf16(rng, (300, heads, d)), torch.bfloat16)
+    q.copy_(some[:1].expand_as(q))
+    q[-300:] = some
+    rot, pos = binding.Rotary(d, base=1e4), torch.arange(T, dtype=torch.int32, device="cuda")
+    k, v = (torch.randn((T, kv_heads, d), device="cuda").bfloat16() for _ in range(2))
+    g.grow(None, ints([T]))
+    out = g.append_rotary(0, rot, q, k, v, None, ints([0, T]), q_out=q)
+    assert torch.equal(q[-300:], ctx.rotary(rot, some, pos[-300:])) and torch.equal(ctx.rotary(rot, out, -pos)[-300:], ctx.rotary(rot, out[-300:], -pos[-300:]))
+    want = g.attend(0, q[-300:], ints([0, 300]), max_new=300, window=90, sinks=5)
+    got = g.attend(0, out, ints([0, T]), max_new=T, window=90, sinks=5)
+    assert ctx.get_status() == 0
+    # (row blocks begin at other rows: other tiles, the same numbers but for their roundings)
+    assert norm_error(f32(got[-300:]), f32(want).astype(np.float64)).max() <= 2 * NORM_LIMIT
+    kk, vv = g.read(0, ints([0, T]), T)
+    vals = [np.moveaxis(f32(torch.cat([x[:5], x[-90:]])).astype(np.float64), 0, 1) for x in (kk, vv)]
+    ref, _ = co.attend_seen(f32(q[-1:]), *vals, np.ones((1, 95), bool), d ** -0.5)
+    assert norm_error(f32(got[-1:]), ref).max() <= 2 * NORM_LIMIT  # (the values that were read back are rounded to bf16 too)
