@@ -179,11 +179,10 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
   };
   __shared__ Place places[kSoftWarps + kWidenWarps];
   __shared__ int out_of[kSoftWarps][2][3];  // a softmax warp's present and next row block: first row of q, kv head, row of the group
-  // ... and, with a mask, its entry, its key tiles, and the tokens from which on (up to which) some row may not see all
+  // ... and, with a mask, its entry and key tiles
   struct Seen {
     EntryInfo info;
     Span span;
-    int lowest, reach;
   };
   __shared__ Seen seen_of[MASKED ? kSoftWarps : 1];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -240,6 +239,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
       int limit, lowest;  // keys that the row sees (0x7fffffff: no such row); the fewest of the warp's rows.  With a mask: the row's token of the entry, -1
       float back;         // what the row of Q was divided by
       bool whole;
+      int clear, cleared;  // with a mask: of the block's tiles, from which to before which the warp's rows see all
     };
     // Moves on to the next row block in which this half has rows (false: none left) and puts its rows of Q into shared memory: D / 8
     // lanes per row, channels in the order of the widened codes.
@@ -263,12 +263,13 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
         if (MASKED) {
           // (the present row block's have been used: all its tiles are done)
           __syncwarp();
-          if (lane == 0) {
-            const int last = c.info.rows * a.group - 1, r = c.rb * L::R + h * 128 + quad * 32;
-            seen_of[warp] = Seen{c.info, L::span(c.info, a, c.rb), seen_by_all(a.m, c.info, a.by_group(min(r, last))),
-                                 hidden_to_some(a.m, c.info, a.by_group(min(r + 31, last)))};
-          }
+          const Span span = L::span(c.info, a, c.rb);
+          if (lane == 0) seen_of[warp] = Seen{c.info, span};
           __syncwarp();
+          const int last = c.info.rows * a.group - 1, r = c.rb * L::R + h * 128 + quad * 32;
+          b.clear = (hidden_to_some(a.m, c.info, a.by_group(min(r + 31, last))) + L::kKeys - 1) / L::kKeys - span.skip - b.first;
+          b.clear = max(b.clear, span.head - b.first);  // (first tokens' pages are looked at)
+          b.cleared = max(seen_by_all(a.m, c.info, a.by_group(min(r, last))), 0) / L::kKeys - span.skip - b.first;
         }
         rows = c.info.rows * a.group;
         r0 = c.rb * L::R + h * 128;
@@ -419,9 +420,9 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
         s_ph ^= 1u << (t & 1);
         const int bad = tile_bad[t & 7];
         if (MASKED) {
-          const Seen& at = seen_of[warp];
-          const int key0 = at.span.page(b.first + j) * L::kKeys;
-          if (key0 + L::kKeys > at.lowest || (key0 < at.reach && key0 + L::kKeys > a.m.sinks) || bad) {
+          if (j < b.clear || j >= b.cleared || bad) {
+            const Seen& at = seen_of[warp];
+            const int key0 = at.span.page(b.first + j) * L::kKeys;
             const uint32_t see = bad ? 0u : b.limit < 0 ? 0xffffffffu : visible(a.m, at.info, b.limit, key0 + 32 * part);
             uint32_t v[32];
             tmem_ld32_issue(scores_at(t) + 32 * part, v);
