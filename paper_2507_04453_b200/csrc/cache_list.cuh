@@ -161,8 +161,12 @@ __device__ __forceinline__ Span span_of(const EntryInfo& e, const AttendMask& m,
   const int first = window_start(m, m.drafts ? past - 1 : past + t0) / kPageTokens, head = min((m.sinks + kPageTokens - 1) / kPageTokens, first);
   return {head, first - head, max((end + kPageTokens - 1) / kPageTokens - (first - head), 1)};
 }
-// The lowest n bits (n is brought to 0 .. 32).
-__device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1; }
+// The lowest n bits (n is brought to 0 .. 32: the instruction's shift by 32 or more leaves nothing).
+__device__ __forceinline__ uint32_t low_bits(int n) {
+  uint32_t r;
+  asm("shl.b32 %0, 1, %1;" : "=r"(r) : "r"(max(n, 0)));
+  return r - 1;
+}
 // Which of the 32 tokens from key0 on a row sees that is a token of an entry.  (For tiles at the edges only.)
 __device__ __forceinline__ uint32_t visible(const AttendMask& m, const EntryInfo& e, int token, int key0) {
   const int past = e.len - e.rows;

@@ -18,8 +18,10 @@
 // special function units); O through shared memory, so that stores are whole rows: 502 and 481 (an SM stores 32 bytes a cycle either way).
 //
 // With a mask (template) the list has the pages that a row block can see; scores at its edges are masked in tensor memory by 32 bits per thread.  Two chunks of 450 tokens
-// after 16 thousand through a window of 4096 (122 GFLOP): 174 us.  Shared memory is what the products wait for: a tile's operands are 128 KB read by the MMAs and
-// 50 KB of widening, 1390 cycles at 128 bytes a cycle; the MMAs alone, back to back, take 1250.  Eight widening warps: 187 us; row blocks of 128 rows in two
+// after 16 thousand through a window of 4096 (122 GFLOP): 168 us.  No unit is full: with the exponentials left out it would be 156, without the stores of the widened pages
+// 171 of 174 then, with half of Q K^T 169.  A tile is a chain of waits for each softmax warp (scores' barrier 300 cycles, loading 250, exponentials 700 to 1000,
+// agreeing 100 to 300, storing and signalling 300), and the slowest of a half's eight warps sets the pace.  To ask at every tile whether it has an edge took 400 cycles
+// of that (174 us); now each warp knows from which tile to which it has none.  Eight widening warps: 187 us; row blocks of 128 rows in two
 // streams per thread block, which widen a page twice as often: 238.
 //
 // Roundings: K and V become fp16 as their scale and minimum are applied, (code - 8) * scale + (minimum + 8 scale), with the offset and the
