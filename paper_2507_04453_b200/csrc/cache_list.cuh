@@ -178,7 +178,7 @@ __device__ __forceinline__ uint32_t visible(const AttendMask& m, const EntryInfo
   uint32_t bits = low_bits(past - key0);
   if (m.window != 0x7fffffff) {
     int seen = 0;
-    for (int w = 0; w < m.words; ++w) seen += __popc(__ldg(mine + w));
+    for (int w = 0; w < m.words; ++w) seen += __popc(__ldg(mine + w) & low_bits(e.rows - 32 * w));
     bits &= ~low_bits(window_start(m, past + seen - 1) - key0) | low_bits(m.sinks - key0);
   }
   const int at = key0 - past;  // the draft that is the first of the 32 tokens

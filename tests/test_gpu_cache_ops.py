@@ -526,6 +526,24 @@ def test_trees_through_a_window(torch, ctx, heads, kv_heads, d, hint, window, si
     check_attend(torch, ctx, p, sizes, range(len(sizes)), heads, rng, hint, seen, tree=drafts, window=window, sinks=sinks)
 
 
+@pytest.mark.parametrize("hint", [1, 100])
+def test_bits_of_drafts_that_do_not_exist_do_not_move_a_window(torch, ctx, hint):
+    """A row's position counts the drafts that it sees; set bits behind its entry's rows are not among them."""
+    rng = np.random.default_rng(40)
+    sizes, lengths, words = [5, 40], [300, 500], 2
+    p = Pair(torch, ctx, 1, 20, 2, 64, 2, 9)
+    p.place(lengths, rng)
+    trees = [random_tree(rng, n) for n in sizes]
+    bits = [co.ancestors(t)[0] for t in trees]
+    packed = np.concatenate([co.pack_bits(b, words) for b in bits])
+    packed[:5, 0] |= np.uint32(0xffffffe0)
+    packed[:5, 1] = 0xffffffff
+    packed[5:, 1] |= np.uint32(0xffffff00)
+    for window, sinks in ((64, 0), (100, 70)):
+        seen = [co.seen_mask(n, r, window, sinks, b) for n, r, b in zip(lengths, sizes, bits)]
+        check_attend(torch, ctx, p, sizes, range(2), 6, rng, hint, seen, tree=torch.from_numpy(packed.view(np.int32)).cuda(), window=window, sinks=sinks)
+
+
 def test_long_history_of_a_tree_is_split_and_joined(torch, ctx):
     rng = np.random.default_rng(11)
     p = Pair(torch, ctx, 1, 400, 1, 128, 1, 390)
