@@ -513,6 +513,7 @@ int32_t essa_cache_keep(essa_ctx* ctx, const essa_cache_desc* cache, const int32
  * is taken modulo a turn in integers: wrong by the position times 2^-64 of a turn, however far the position. */
 #define ESSA_ROTARY_MAX_DIM 256
 #define ESSA_ROTARY_MAX_AXES 4
+#define ESSA_ROTARY_MAX_HEADS (1 << 20) /* heads of a row that the calls below accept */
 typedef struct essa_rotary {
   int32_t head_dim;   /* a multiple of 16 up to ESSA_ROTARY_MAX_DIM */
   int32_t axes;       /* 1 .. ESSA_ROTARY_MAX_AXES                  */

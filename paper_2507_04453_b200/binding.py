@@ -687,7 +687,8 @@ class KvCache:
         if window is not None and window < 1:
             raise EssaError(ESSA_ERR_INVALID_ARG, "kv_cache: a window has at least one token")
         m = self._mask_desc
-        m.window, m.sinks, m.drafts, m.draft_words = window or 0, sinks, ptr, words
+        # (beyond 32 bits: all tokens; the structure would take the low bits)
+        m.window, m.sinks, m.drafts, m.draft_words = min(window or 0, 0x7fffffff), max(min(sinks, 0x7fffffff), -1), ptr, words
         return self._mask_ref
 
     def attend(self, layer: int, q, tok_offsets=None, slots=None, max_new: int = 1, scale=None, out=None, stream=None, window=None, sinks: int = 0, tree=None):

@@ -20,6 +20,7 @@ namespace {
 constexpr int kRotaryWarps = 8;
 constexpr int kUnroll = 2;     // heads of a warp whose loads are on their way together
 constexpr int kMaxGroups = 2;  // see rotary_kernel
+static_assert(ESSA_ROTARY_MAX_HEADS <= 1 << 30, "");  // (a warp's walk passes the last head by a step or two, in 32 bits)
 
 struct RotaryArgs {
   essa_rotary r;
@@ -262,6 +263,7 @@ int32_t essa_rotary_apply(essa_ctx* ctx, const essa_rotary* rotary, const void* 
   int32_t code;
   if (const char* why = rotary_problem(rotary, &code)) return fail(ctx, code, std::string("rotary_apply: ") + why);
   if (heads < 1 || T < 0) return fail(ctx, ESSA_ERR_INVALID_ARG, "rotary_apply: heads must be positive, T not negative");
+  if (heads > ESSA_ROTARY_MAX_HEADS) return fail(ctx, ESSA_ERR_UNSUPPORTED_SHAPE, "rotary_apply: heads > ESSA_ROTARY_MAX_HEADS");
   if (T == 0) return ESSA_OK;
   const int64_t width = (int64_t)heads * rotary->head_dim;
   ESSA_TRY(check_rows(ctx, "rotary_apply", "x", x, ld_x, width));
@@ -292,6 +294,7 @@ int32_t essa_cache_append_rotary(essa_ctx* ctx, const essa_cache_desc* cache, in
   const CacheEntries e{slots, tok_offsets, n, T};
   ESSA_TRY(check_entries(ctx, "cache_append_rotary", e));
   if (q_heads < 1) return fail(ctx, ESSA_ERR_INVALID_ARG, "cache_append_rotary: q_heads must be positive");
+  if (q_heads > ESSA_ROTARY_MAX_HEADS) return fail(ctx, ESSA_ERR_UNSUPPORTED_SHAPE, "cache_append_rotary: q_heads > ESSA_ROTARY_MAX_HEADS");
   if (T == 0 || n == 0) return ESSA_OK;
   const int64_t width = (int64_t)v.kv_heads * v.head_dim, q_width = (int64_t)q_heads * v.head_dim;
   ESSA_TRY(check_rows(ctx, "cache_append_rotary", "q", q, ld_q, q_width));

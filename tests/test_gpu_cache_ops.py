@@ -330,6 +330,34 @@ def test_a_window_that_reaches_everything_gives_the_same_bits(torch, ctx, hint):
     assert norm_error(f32(a), f32(b).astype(np.float64)).max() <= NORM_LIMIT
 
 
+@pytest.mark.parametrize("window,sinks,like", [(2 ** 32 + 5, 0, None), (2 ** 63, 3, None), (5, 2 ** 32 + 1, None), (5, 2 ** 40, None), (5, 0, 5)])
+def test_windows_and_first_tokens_beyond_32_bits_are_all_of_them(torch, ctx, window, sinks, like):
+    rng = np.random.default_rng(41)
+    p = Pair(torch, ctx, 1, 9, 2, 64, 2, 9)
+    p.place([70, 200], rng)
+    q = p.bf(bf16(rng, (2, 6, 64)))
+    a, b = p.gpu.attend(0, q, window=like), p.gpu.attend(0, q, window=window, sinks=sinks)
+    assert norm_error(f32(a), f32(b).astype(np.float64)).max() <= NORM_LIMIT
+    with pytest.raises(binding.EssaError):
+        p.gpu.attend(0, q, window=5, sinks=-2 ** 32)
+
+
+def test_rotary_refuses_more_heads_than_a_row_has(torch, ctx):
+    """Refused on the host: nothing of this size is read."""
+    rot, x, pos = binding.Rotary(16), torch.zeros((1, 1, 16), dtype=torch.bfloat16, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    for heads in (2 ** 20 + 1, 2 ** 31 - 1):
+        assert ctx.lib.essa_rotary_apply(ctx.handle, rot._ref, x.data_ptr(), 16 * heads, heads, 1, pos.data_ptr(), 1, x.data_ptr(), 16 * heads,
+                                         None) == binding.ESSA_ERR_UNSUPPORTED_SHAPE
+    p = Pair(torch, ctx, 1, 2, 1, 64, 1, 1)
+    p.place([3], np.random.default_rng(0))
+    rot, x = binding.Rotary(64), torch.zeros((1, 1, 64), dtype=torch.bfloat16, device="cuda")
+    for heads in (2 ** 20 + 1, 2 ** 31 - 1):
+        assert ctx.lib.essa_cache_append_rotary(ctx.handle, p.gpu._ref, 0, rot._ref, x.data_ptr(), 64 * heads, heads, x.data_ptr(), 64, x.data_ptr(), 64, 1, None, 0, None, None, 1,
+                                                x.data_ptr(), 64 * heads, None) == binding.ESSA_ERR_UNSUPPORTED_SHAPE
+    p.assert_same()
+    assert ctx.get_status() == 0
+
+
 @pytest.mark.parametrize("rows,hint", [(1, 1), (37, 64)])
 @pytest.mark.parametrize("window,sinks", [(20000, 0), (5000, 1000)])
 def test_long_window_is_split_and_joined(torch, ctx, rows, hint, window, sinks):
