@@ -386,14 +386,14 @@ int32_t essa_apply_projection_simt(essa_ctx* ctx, const essa_adapter* adapter, c
  *   (scale, minimum) of K, then of V: [head_dim / 64][64 tokens][2] fp16.
  *
  * Sequences.  Sequence s holds lengths[s] tokens; token i lives in page table[s][i / 64] of every layer.  refs[p] is the
- * number of table entries that name page p; a page with refs 0 is free.  Only full pages are ever shared: the page a
- * sequence is still filling is its own.  The caller owns the four buffers (essa_cache_reset makes them an empty cache) and
+ * number of table entries that name page p; a page with refs 0 is free.  Only full pages are ever shared, and the page that a
+ * sequence is filling is its own: one that essa_cache_keep has shortened into a shared page gets a copy of it when it grows.  The caller owns the four buffers (essa_cache_reset makes them an empty cache) and
  * may read them at any time; they are device-resident, so that a whole decode step (grow, append, attend) can be captured
  * into a CUDA graph and replayed while the sequences grow.
  *
  * Errors that only the device can see are recorded as ESSA_ERR_CACHE in the status word that essa_get_status reads.  The calls on pages look at
  * all that they use first, and then change nothing at all if a slot lies outside the cache or is named twice (a fork's sources may be), and
- *   essa_cache_grow     if a count is negative, a length is negative or becomes longer than the table, or there are too few free pages;
+ *   essa_cache_grow     if a count is negative, a length is negative or becomes longer than the table, or there are too few free pages (copies included);
  *   essa_cache_fork     if a dst is a src, lens[i] is negative or more than the source holds, there are too few free pages, a page that a source
  *                       shares or that is copied is not a page in use (one of the pool, with refs > 0), or a destination's table row holds
  *                       anything but pages in use and -1;
@@ -437,7 +437,8 @@ int32_t essa_cache_attend_workspace(const essa_cache_desc* cache, int32_t q_head
 /* All sequences empty, all pages free. */
 int32_t essa_cache_reset(essa_ctx* ctx, const essa_cache_desc* cache, void* stream);
 /* Make room: sequence slots[i] (dev; NULL: i) becomes counts[i] (dev, >= 0) tokens longer, i < n, and gets the pages for
- * them: the free pages with the lowest numbers, in the order of the entries. */
+ * them: the free pages with the lowest numbers, in the order of the entries.  One that ends in the middle of a page that another
+ * sequence shares (counts[i] > 0, refs > 1 before the call) first gets a copy of that page, in all layers, and gives up its share. */
 int32_t essa_cache_grow(essa_ctx* ctx, const essa_cache_desc* cache, const int32_t* slots, const int32_t* counts, int32_t n, void* workspace,
                         int64_t workspace_bytes, void* stream);
 /* Store k and v ([T] rows of kv_heads * head_dim bf16, ld_k / ld_v elements apart: multiples of 8; 16-byte aligned) of the
@@ -495,7 +496,8 @@ int32_t essa_cache_tree(essa_ctx* ctx, const essa_cache_desc* cache, const int32
                         uint32_t* drafts, int32_t draft_words, int32_t* positions, void* stream);
 /* Of the last L = tok_offsets[i + 1] - tok_offsets[i] (NULL: 1) tokens of sequence slots[i] (NULL: i), counts[i] stay, i < n: those that
  * picks[i * ld_picks + m], m < counts[i] (dev, ascending, each in 0 .. L - 1; picks NULL: the first counts[i]) name, moved together in all layers, as
- * after a tree of drafts has been checked.  The sequence becomes L - counts[i] tokens shorter; its pages behind its new end are given back.
+ * after a tree of drafts has been checked.  The sequence becomes L - counts[i] tokens shorter; its pages behind its new end are given back.  Its end may
+ * then lie in the middle of a page that another sequence shares: essa_cache_grow has to come before new tokens, as ever, and copies it.
  * Refused as a whole (ESSA_ERR_CACHE, nothing changes): a slot outside the cache or named twice; offsets that descend; L or counts[i] not in 0 .. length
  * and 0 .. L; with picks, L > ESSA_CACHE_MAX_DRAFTS, counts[i] > ld_picks, or picks that are not ascending within 0 .. L - 1; a page from that of the first of the L tokens on
  * that is not a page in use, or one that a token moves to and that another sequence shares. */

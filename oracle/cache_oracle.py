@@ -105,15 +105,29 @@ class Cache:
         self.table[s] = -1
         self.lengths[s] = 0
 
+    def _shared_end(self, s):
+        """The page that sequence s ends in the middle of and that another one shares; None: it does not."""
+        n = int(self.lengths[s])
+        p = int(self.table[s, n // PAGE]) if n % PAGE else -1
+        return p if 0 <= p < self.num_pages and self.refs[p] > 1 else None
+
     def grow(self, slots, counts):
         slots = self._check_slots(slots)
-        need = []
+        need, ends = [], []
         for s, c in zip(slots, counts):
             if c < 0 or self.lengths[s] + int(c) > self.max_pages * PAGE:
                 raise Refused("length")
             need.append(pages_of(self.lengths[s] + c) - pages_of(self.lengths[s]))
-        new = list(self._take(sum(need)))
-        for s, c, k in zip(slots, counts, need):
+            ends.append(self._shared_end(s) if c > 0 else None)
+        new = list(self._take(sum(need) + sum(e is not None for e in ends)))
+        for s, c, k, old in zip(slots, counts, need, ends):
+            if old is not None:
+                p = new.pop(0)
+                for a in (self.codes, self.scale, self.low):
+                    a[:, p] = a[:, old]
+                self.table[s, self.lengths[s] // PAGE] = p
+                self.refs[p] = 1
+                self.refs[old] -= 1
             at = pages_of(self.lengths[s])
             for j in range(k):
                 p = new.pop(0)

@@ -156,43 +156,113 @@ __device__ bool first_free(const CacheView& v, int want, int32_t* list, long lon
   return have >= want;
 }
 
+// Page copies from[i] -> to[i], i < copies, in every layer: units of THREADS (a thread block's) x 4 x 16 bytes over the whole grid.  Bound by HBM: 900
+// pages of 288 KB (2 x 265 MB) take 80 us, 6.6 TB/s.
+template <int THREADS>
+__device__ __forceinline__ void copy_pages(const CacheView& v, const int32_t* from, const int32_t* to, int copies) {
+  constexpr int kPer = 4;
+  const int per_page = (int)(v.page_bytes / 16);  // 16-byte words (a multiple of 288)
+  const int pieces = (per_page + THREADS * kPer - 1) / (THREADS * kPer);
+  const int64_t units = (int64_t)copies * v.layers * pieces;
+  for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
+    const int piece = (int)(u % pieces);
+    const int64_t rest = u / pieces;
+    const int i = (int)(rest % copies), layer = (int)(rest / copies);
+    uint8_t* base = v.pages + layer * v.layer_bytes;
+    const uint4* src = reinterpret_cast<const uint4*>(base + from[i] * v.page_bytes);
+    uint4* dst = reinterpret_cast<uint4*>(base + to[i] * v.page_bytes);
+    uint4 x[kPer];
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      const int at = (piece * kPer + j) * THREADS + threadIdx.x;
+      if (at < per_page) x[j] = __ldcs(src + at);
+    }
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      const int at = (piece * kPer + j) * THREADS + threadIdx.x;
+      if (at < per_page) __stcs(dst + at, x[j]);
+    }
+  }
+}
+
+// A thread per entry.  Tokens may only be written to a page of the sequence's own, so that one that ends in a shared page (it has been shortened)
+// gets a copy of it.  This thread block makes the copies too: a kernel behind it would cost every decode step a launch, and copies are rare.  256
+// entries by a token: 5.1 us (4.7 without a look at the pages that they end on); one that is copied in 28 layers of 4 heads of 128 (1 MB): 29, sixteen 327.
 __global__ void __launch_bounds__(kPlanThreads) grow_kernel(CacheView v, const int32_t* slots, const int32_t* counts, int n, PlanSpace ws, int32_t* status) {
   extern __shared__ uint32_t seen[];
   __shared__ long long scan_sm[33];
-  bool ok = slots_distinct(slots, n, v.max_seqs, seen);
-  long long want = 0;
+  bool ok = slots_distinct(slots, n, v.max_seqs, seen), copies = false;
+  long long want = 0, total;
+  int page0 = -1, held0 = 0;  // the page that the thread's first entry ends in the middle of, and its holders
   if (ok) {
     bool fine = true;
     for (int base = 0; base < n; base += blockDim.x) {
       const int i = base + threadIdx.x;
-      long long need = 0, total;
+      long long need = 0;
+      int page = -1;
       if (i < n) {
-        const int len = v.lengths[slots ? slots[i] : i], add = counts[i];
-        if (len < 0 || add < 0 || (long long)len + add > (long long)v.max_pages * kPageTokens) fine = false;
-        else need = pages_of(len + add) - pages_of(len);
+        const int slot = slots ? slots[i] : i, len = v.lengths[slot], add = counts[i];
+        if (len < 0 || add < 0 || (long long)len + add > (long long)v.max_pages * kPageTokens) {
+          fine = false;
+        } else {
+          need = pages_of(len + add) - pages_of(len);
+          if (add > 0 && len % kPageTokens) page = v.table[(int64_t)slot * v.max_pages + len / kPageTokens];
+        }
       }
       block_scan(need, &total, scan_sm);
       want += total;
+      const int held = holders(v, page);
+      if (base == 0) {  // (on its way while free pages are looked for)
+        page0 = page;
+        held0 = held;
+      } else if (i < n) {
+        ws.extra[i] = held > 1 ? page : -1;
+        copies |= held > 1;
+      }
     }
     ok = __syncthreads_and(fine) && want <= v.num_pages && first_free(v, (int)want, ws.from, scan_sm);
+  }
+  copies = __syncthreads_or(ok && (copies || held0 > 1));
+  if (copies) {  // pages for them, too
+    long long mine = 0;
+    if (threadIdx.x < n) ws.extra[threadIdx.x] = held0 > 1 ? page0 : -1;
+    for (int i = threadIdx.x; i < n; i += blockDim.x) mine += ws.extra[i] >= 0;
+    block_scan(mine, &total, scan_sm);
+    want += total;
+    ok = want <= v.num_pages && first_free(v, (int)want, ws.from, scan_sm);
   }
   if (!ok) {
     if (threadIdx.x == 0) cache_fault(status);
     return;
   }
-  long long before = 0;
+  long long before = 0, copied = 0;
   for (int base = 0; base < n; base += blockDim.x) {
     const int i = base + threadIdx.x;
-    long long need = 0, total;
-    int slot = 0, len = 0, add = 0;
+    long long need = 0;
+    int slot = 0, len = 0, add = 0, old = -1;  // old: the shared page
     if (i < n) {
       slot = slots ? slots[i] : i;
       len = v.lengths[slot];
       add = counts[i];
-      need = pages_of(len + add) - pages_of(len);
+      if (copies) old = ws.extra[i];
+      need = pages_of(len + add) - pages_of(len) + (old >= 0);
     }
-    const long long at = before + block_scan(need, &total, scan_sm);
+    long long at = before + block_scan(need, &total, scan_sm);
     before += total;
+    if (copies) {
+      const long long copy = copied + block_scan(old >= 0, &total, scan_sm);
+      copied += total;
+      if (old >= 0) {  // the first of the entry's pages
+        const int page = ws.from[at];
+        v.table[(int64_t)slot * v.max_pages + len / kPageTokens] = page;
+        v.refs[page] = 1;
+        atomicSub(v.refs + old, 1);  // (the page is free when its last holder leaves it)
+        ws.extra[copy] = old;        // (copy <= i, and these threads' have been read)
+        ws.to[copy] = page;
+        ++at;
+        --need;
+      }
+    }
     // A few pages each (decode steps): every thread writes its entry's.  Many (long prompts): the warp writes them, an entry after the
     // other, 32 pages at a time; a thread alone would wait for memory once a page (one sequence of 100 thousand tokens: 64 us, so 14).
     const auto give = [&](int to, int first, int64_t from, int j) {
@@ -211,6 +281,9 @@ __global__ void __launch_bounds__(kPlanThreads) grow_kernel(CacheView v, const i
     }
     if (i < n) v.lengths[slot] = len + add;
   }
+  if (!copies) return;
+  __syncthreads();
+  copy_pages<kPlanThreads>(v, ws.extra, ws.to, (int)copied);
 }
 
 // The entries of n table rows that are one thread's, of `threads` threads: first, and from each to the next.
@@ -363,34 +436,6 @@ __global__ void __launch_bounds__(kPlanThreads) fork_plan_kernel(CacheView v, co
   }
 }
 
-// Page copies from[i] -> to[i], i < copies, in every layer: units of 256 threads x 4 x 16 bytes over the whole grid.  Bound by HBM: 900
-// pages of 288 KB (2 x 265 MB) take 80 us, 6.6 TB/s.
-__device__ __forceinline__ void copy_pages(const CacheView& v, const PlanSpace& ws, int copies) {
-  constexpr int kPer = 4;
-  const int per_page = (int)(v.page_bytes / 16);  // 16-byte words (a multiple of 288)
-  const int pieces = (per_page + 256 * kPer - 1) / (256 * kPer);
-  const int64_t units = (int64_t)copies * v.layers * pieces;
-  for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
-    const int piece = (int)(u % pieces);
-    const int64_t rest = u / pieces;
-    const int i = (int)(rest % copies), layer = (int)(rest / copies);
-    uint8_t* base = v.pages + layer * v.layer_bytes;
-    const uint4* src = reinterpret_cast<const uint4*>(base + ws.from[i] * v.page_bytes);
-    uint4* dst = reinterpret_cast<uint4*>(base + ws.to[i] * v.page_bytes);
-    uint4 x[kPer];
-#pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-      const int at = (piece * kPer + j) * 256 + threadIdx.x;
-      if (at < per_page) x[j] = __ldcs(src + at);
-    }
-#pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-      const int at = (piece * kPer + j) * 256 + threadIdx.x;
-      if (at < per_page) __stcs(dst + at, x[j]);
-    }
-  }
-}
-
 __global__ void __launch_bounds__(256) fork_kernel(CacheView v, const int32_t* src, const int32_t* dst, const int32_t* lens, int n, PlanSpace ws) {
   grid_dep_wait();
   if (!ws.head->ok) return;
@@ -405,7 +450,7 @@ __global__ void __launch_bounds__(256) fork_kernel(CacheView v, const int32_t* s
     }
     if (threadIdx.x == 0) v.lengths[d] = len;
   }
-  copy_pages(v, ws, ws.head->copies);
+  copy_pages<256>(v, ws.from, ws.to, ws.head->copies);
 }
 
 // Thread block 0 plans, from the counts of the pages; the others look at the table, so that the kernel behind this one can tell before it
@@ -468,7 +513,7 @@ __global__ void __launch_bounds__(256) compact_kernel(CacheView v, PlanSpace ws,
       if (to != page) v.table[i] = to;
     }
   }
-  copy_pages(v, ws, copies);
+  copy_pages<256>(v, ws.from, ws.to, copies);
 }
 
 // ------------------------------------------------------------------------------------------------ host side

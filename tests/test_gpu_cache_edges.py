@@ -1,0 +1,158 @@
+"""GPU tests of calls around the key / value cache that meet one another: sequences shortened into pages that others share and grown again."""
+import numpy as np
+import pytest
+
+from oracle import cache_oracle as co
+from paper_2507_04453_b200 import binding
+from tests.cache_utils import Pair, attend_bound, bf16
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def torch():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.fail("CUDA device required for -m gpu tests")
+    return torch
+
+
+@pytest.fixture(scope="module")
+def ctx(torch):
+    c = binding.Context(0)
+    yield c
+    assert c.get_status() == 0
+    c.close()
+
+
+def f32(t):
+    return t.float().cpu().numpy()
+
+
+# ------------------------------------------------------------------------------------------------ shortened into a shared page
+def fork(p, src, dst, lens=None):
+    p.gpu.fork(p.ints(src), p.ints(dst), p.ints(lens))
+    p.cpu.fork(src, dst, lens)
+
+
+def shorten(p, slots, lengths):
+    """The sequences slots[i] to lengths[i] tokens."""
+    rows = [int(p.cpu.lengths[s]) for s in slots]
+    p.gpu.keep(p.ints(lengths), p.ints(np.concatenate([[0], np.cumsum(rows)])), slots=p.ints(slots))
+    co.keep(p.cpu, slots, rows, lengths)
+
+
+def grow_and_append(p, rng, slots, counts):
+    p.gpu.grow(p.ints(slots), p.ints(counts))
+    p.cpu.grow(slots, counts)
+    off = np.concatenate([[0], np.cumsum(counts)])
+    layers, _, kv_heads, d = p.cpu.shape
+    for layer in range(layers):
+        k, v = bf16(rng, (off[-1], kv_heads, d)), bf16(rng, (off[-1], kv_heads, d))
+        p.gpu.append(layer, p.bf(k), p.bf(v), p.ints(off), slots=p.ints(slots))
+        p.cpu.append(layer, k, v, off, slots)
+
+
+@pytest.mark.parametrize("kv_heads,d", [(1, 64), (3, 128)])
+@pytest.mark.parametrize("end,add", [(12, 1), (63, 1), (63, 2), (65, 5), (100, 130), (64, 3), (128, 1), (0, 7), (190, 10)])
+def test_a_sequence_shortened_into_a_shared_page_grows_on_a_copy_of_it(torch, ctx, kv_heads, d, end, add):
+    """What both sequences hold and what is attended to afterwards is the model's; tokens go to the page of the one that grows."""
+    rng = np.random.default_rng(end + d)
+    p = Pair(torch, ctx, 2, 14, kv_heads, d, 3, 6)
+    p.place([200, 0, 10], rng)
+    fork(p, [0], [1])
+    shorten(p, [1], [end])
+    p.assert_same()
+    grow_and_append(p, rng, [1, 2], [add, 3])
+    p.assert_same()
+    assert ctx.get_status() == 0
+    q = bf16(rng, (2, 2 * kv_heads, d))
+    for layer in range(2):
+        out = f32(p.gpu.attend(layer, p.bf(q), slots=p.ints([1, 0])))
+        for i, s in enumerate((1, 0)):
+            k, v, codes, sc = p.cpu.sequence(layer, s)
+            want, w = co.attend(q[i:i + 1], k, v, int(p.cpu.lengths[s]), d ** -0.5)
+            assert (np.abs(out[i:i + 1] - want) <= attend_bound(q[i:i + 1], v, codes, sc, want, w, d ** -0.5, k)).all()
+    assert ctx.get_status() == 0
+
+
+def test_sequences_that_end_in_the_same_page_grow_together(torch, ctx):
+    """Three of four sequences shortened into one page and grown by one call each get a copy; one that does not grow keeps its share; the last
+    holder of a page needs none; a page that nobody holds any more is free."""
+    rng = np.random.default_rng(1)
+    p = Pair(torch, ctx, 2, 20, 2, 64, 5, 4)
+    p.place([130, 0, 0, 0, 64], rng)
+    fork(p, [0, 0, 0], [1, 2, 3])
+    shorten(p, [0, 1, 2, 3], [70, 90, 127, 100])
+    p.assert_same()
+    grow_and_append(p, rng, [2, 4, 0, 1, 3], [1, 70, 60, 0, 2])  # (sequence 1 stays as it is)
+    p.assert_same()
+    assert p.cpu.refs[p.cpu.table[1, 1]] == 1
+    before = int(p.cpu.table[1, 1])
+    grow_and_append(p, rng, [1], [3])
+    p.assert_same()
+    assert int(p.cpu.table[1, 1]) == before
+    shorten(p, [0, 3], [10, 20])  # page 0 of all four
+    grow_and_append(p, rng, [3, 0], [1, 1])
+    p.assert_same()
+    shorten(p, [1, 2], [33, 34])
+    grow_and_append(p, rng, [1, 2], [1, 1])  # both, though the second could have had the page itself
+    p.assert_same()
+    assert ctx.get_status() == 0
+
+
+def test_growing_on_a_copy_needs_a_page_for_it(torch, ctx):
+    """Too few pages with the copy among them: refused, nothing changes; enough for the rest after another sequence has gone."""
+    rng = np.random.default_rng(2)
+    p = Pair(torch, ctx, 1, 4, 1, 64, 3, 4)
+    p.place([130, 0, 0], rng)
+    fork(p, [0], [1])  # pages: two shared, two of their own
+    shorten(p, [1], [100])
+    fork(p, [0], [2], [64])
+    grow_and_append(p, rng, [2], [1])  # the page that the shortened one gave back
+    p.gpu.grow(p.ints([1]), p.ints([1]))
+    assert ctx.get_status() == binding.ESSA_ERR_CACHE
+    with pytest.raises(co.Refused):
+        p.cpu.grow([1], [1])
+    p.assert_same()
+    p.gpu.free(p.ints([0]))
+    p.cpu.free([0])
+    grow_and_append(p, rng, [1], [1])
+    p.assert_same()
+    assert ctx.get_status() == 0
+
+
+def test_more_sequences_than_threads_grow_on_copies(torch, ctx):
+    rng = np.random.default_rng(3)
+    n = 1500
+    p = Pair(torch, ctx, 1, 2 * n + 10, 1, 64, n + 1, 3)
+    p.place([64] + [0] * n, rng)
+    others = list(range(1, n + 1))
+    fork(p, [0] * n, others)
+    shorten(p, others, [int(x) for x in rng.integers(1, 65, n)])
+    counts = [int(x) for x in rng.integers(0, 90, n)]
+    order = [int(s) for s in 1 + rng.permutation(n)]
+    grow_and_append(p, rng, order, counts)
+    p.assert_same()
+    assert ctx.get_status() == 0
+
+
+def test_a_captured_growth_copies_when_it_is_replayed(torch, ctx):
+    """The graph is captured while no end is shared, and replayed when one is."""
+    rng = np.random.default_rng(4)
+    p = Pair(torch, ctx, 2, 14, 2, 64, 2, 4)
+    p.place([150, 0], rng)
+    slots, counts = p.ints([1]), p.ints([1])
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        p.gpu.grow(slots, counts)
+    torch.cuda.current_stream().wait_stream(stream)
+    fork(p, [0], [1])
+    shorten(p, [1], [70])
+    for _ in range(3):
+        graph.replay()
+        p.cpu.grow([1], [1])
+        p.assert_same()
+    assert ctx.get_status() == 0
