@@ -144,9 +144,9 @@ __global__ void __launch_bounds__(kThreads, attend_blocks_per_sm(D, NT)) attend_
       const Span span = L::span(c.info, a, c.rb);
       for (; tile < stop; ++tile) {
         if (filled >= S::kStages && !wait_napping(empty + 8 * st, phase ^ 1, &abort_flag, a.status)) { ok = false; break; }
-        const int page = none ? -1 : __ldg(row + (MASKED ? span.page(tile) : tile));
+        const int at = MASKED ? span.page(tile) : tile, page = none ? -1 : __ldg(row + at);
         const bool there = page >= 0 && page < a.v.num_pages;
-        if (!there && (!none || c.info.slot < 0)) cache_fault(a.status);
+        if (!there && (!none || c.info.slot < 0) && (!MASKED || page_seen(a.m, c.info, first_token(a, c.rb, R), last_token(c.info, a, c.rb, R), at))) cache_fault(a.status);
         bad_page[st] = !there;
         if (there) {
           mbar_expect_tx(full + 8 * st, S::kBytes);

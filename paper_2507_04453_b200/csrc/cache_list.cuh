@@ -167,6 +167,21 @@ __device__ __forceinline__ uint32_t low_bits(int n) {
   asm("shl.b32 %0, 1, %1;" : "=r"(r) : "r"(max(n, 0)));
   return r - 1;
 }
+// The position of a row that is a token of an entry, with drafts.
+__device__ __forceinline__ int draft_position(const AttendMask& m, const EntryInfo& e, int token) {
+  const uint32_t* mine = m.drafts + (int64_t)(e.row0 + token) * m.words;
+  int seen = 0;
+  for (int w = 0; w < m.words; ++w) seen += __popc(__ldg(mine + w) & low_bits(e.rows - 32 * w));
+  return e.len - e.rows + seen - 1;
+}
+// Whether one of the tokens t0 .. t1 of an entry sees a token of a page of their span.  (Without drafts a span has no other pages; with them it begins
+// where the window of a row that sees no draft does, and the others' begin later.  For pages that are not there only.)
+__device__ inline bool page_seen(const AttendMask& m, const EntryInfo& e, int t0, int t1, int page) {
+  if (!m.drafts || m.window == 0x7fffffff || (int64_t)page * kPageTokens < m.sinks) return true;
+  for (int t = t0; t <= t1; ++t)
+    if (window_start(m, draft_position(m, e, t)) < (page + 1) * kPageTokens) return true;
+  return false;
+}
 // Which of the 32 tokens from key0 on a row sees that is a token of an entry.  (For tiles at the edges only.)
 __device__ __forceinline__ uint32_t visible(const AttendMask& m, const EntryInfo& e, int token, int key0) {
   const int past = e.len - e.rows;
@@ -177,9 +192,7 @@ __device__ __forceinline__ uint32_t visible(const AttendMask& m, const EntryInfo
   const uint32_t* mine = m.drafts + (int64_t)(e.row0 + token) * m.words;
   uint32_t bits = low_bits(past - key0);
   if (m.window != 0x7fffffff) {
-    int seen = 0;
-    for (int w = 0; w < m.words; ++w) seen += __popc(__ldg(mine + w) & low_bits(e.rows - 32 * w));
-    bits &= ~low_bits(window_start(m, past + seen - 1) - key0) | low_bits(m.sinks - key0);
+    bits &= ~low_bits(window_start(m, draft_position(m, e, token)) - key0) | low_bits(m.sinks - key0);
   }
   const int at = key0 - past;  // the draft that is the first of the 32 tokens
   if (at > -32 && at < 32 * m.words) {

@@ -552,7 +552,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs a)
             if (filled >= kRaw && !wait(kRawEmpty + slot, phase ^ 1)) { ok = false; break; }
             const int page = p < pages ? __ldg(row + p) : -1;
             const bool there = page >= 0 && page < a.v.num_pages;
-            if (!there && p < pages) cache_fault(a.status);
+            if (!there && p < pages && (!MASKED || page_seen(a.m, c.info, first_token(a, c.rb, L::R), last_token(c.info, a, c.rb, L::R), p))) cache_fault(a.status);
             raw_bad[slot] = !there;
             if (there) {
               mbar_expect_tx(bar(kRawFull + slot), M::kRun);

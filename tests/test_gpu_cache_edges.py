@@ -1,4 +1,5 @@
-"""GPU tests of calls around the key / value cache that meet one another: sequences shortened into pages that others share and grown again."""
+"""GPU tests of calls around the key / value cache that meet one another: sequences shortened into pages that others share and grown again, pages that
+have left every window, padded batches."""
 import numpy as np
 import pytest
 
@@ -156,3 +157,38 @@ def test_a_captured_growth_copies_when_it_is_replayed(torch, ctx):
         p.cpu.grow([1], [1])
         p.assert_same()
     assert ctx.get_status() == 0
+
+
+# ------------------------------------------------------------------------------------------------ pages that no draft sees
+@pytest.mark.parametrize("hint", [1, 100])
+@pytest.mark.parametrize("past,window,sinks,gone", [(127, 64, 0, [0]), (127, 64, 1, []), (319, 128, 70, [2]), (255, 64, 0, [0, 1, 2]), (256, 64, 0, [0, 1, 2])])
+def test_pages_that_no_draft_sees_may_be_missing(torch, ctx, hint, past, window, sinks, gone):
+    """A tree's first draft sees the tokens from past - window + 1 on: a page that ends right before that one may be missing, and no other."""
+    rng = np.random.default_rng(past)
+    sizes = [5, 20]
+    p = Pair(torch, ctx, 1, 24, 2, 64, 2, 7)
+    p.place([past + 5, past + 20], rng)
+    trees = [[-1, 0, 0, 1, -1], [-1] + list(range(19))]
+    off = p.ints([0, 5, 25])
+    q = p.bf(bf16(rng, (25, 6, 64)))
+    drafts, _ = p.gpu.tree(p.ints(sum(trees, [])), off, 20)
+    want = p.gpu.attend(0, q, off, max_new=hint, window=window, sinks=sinks, tree=drafts)
+    assert ctx.get_status() == 0
+    for s in range(2):
+        for j in gone:
+            p.gpu.table[s, j] = -1
+    assert torch.equal(p.gpu.attend(0, q, off, max_new=hint, window=window, sinks=sinks, tree=drafts), want)
+    assert ctx.get_status() == 0
+    for s in range(2):
+        keep, first = p.gpu.table[s].clone(), (past - window + 1) // 64
+        for j in [first] + ([0] if sinks else []):  # (seen by the first draft)
+            p.gpu.table[s, j] = 99
+            p.gpu.attend(0, q, off, max_new=hint, window=window, sinks=sinks, tree=drafts)
+            assert ctx.get_status() == binding.ESSA_ERR_CACHE
+            p.gpu.table[s] = keep
+    none = drafts.clone()
+    none[3] = 0  # a row that sees no draft is at past - 1, and sees a token more
+    p.gpu.attend(0, q, off, max_new=hint, window=window, sinks=sinks, tree=none)
+    assert ctx.get_status() == (binding.ESSA_ERR_CACHE if (past - window) // 64 in gone else 0)
+
+
