@@ -491,7 +491,8 @@ int32_t essa_cache_attend_masked(essa_ctx* ctx, const essa_cache_desc* cache, co
  *   drafts (dev, [T][draft_words], 4-byte aligned): row t's bits for essa_attend_mask, itself and all that it descends from;
  *   positions (dev, [T], may be NULL): the number of tokens before the entry's rows plus the row's depth (0 for a parent of -1), for a rotation.
  * A row whose parent is not before it counts as a child of the token before the rows, one from 32 * draft_words on has no bits and counts likewise;
- * a slot outside the cache leaves the rows' positions as they are (ESSA_ERR_CACHE for each of these).  Rows outside all entries are left as they are. */
+ * a slot outside the cache leaves the rows' positions as they are (ESSA_ERR_CACHE for each of these, if the entry has a row).  Rows outside all
+ * entries are left as they are. */
 int32_t essa_cache_tree(essa_ctx* ctx, const essa_cache_desc* cache, const int32_t* parents, int32_t T, const int32_t* slots, const int32_t* tok_offsets, int32_t n,
                         uint32_t* drafts, int32_t draft_words, int32_t* positions, void* stream);
 /* Of the last L = tok_offsets[i + 1] - tok_offsets[i] (NULL: 1) tokens of sequence slots[i] (NULL: i), counts[i] stay, i < n: those that

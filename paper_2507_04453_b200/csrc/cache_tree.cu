@@ -15,7 +15,7 @@ __global__ void __launch_bounds__(kMaxDrafts) tree_kernel(CacheView v, CacheEntr
   __shared__ uint32_t bits[kMaxDrafts * (kMaxDrafts / 32 + 1)];  // (a word more per row: the rows' words in different banks)
   const EntryInfo info = load_entry(v, e, blockIdx.x);
   const int rows = min(info.rows, 32 * words), j = threadIdx.x, past = info.len - info.rows;
-  bool fault = info.slot < 0 || info.rows > rows;
+  bool fault = (info.slot < 0 && info.rows > 0) || info.rows > rows;  // (an entry without rows stands for nothing)
   if (j < rows) {
     const int up = __ldg(parents + info.row0 + j);
     const bool fine = up >= -1 && up < j;

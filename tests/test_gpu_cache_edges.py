@@ -192,3 +192,19 @@ def test_pages_that_no_draft_sees_may_be_missing(torch, ctx, hint, past, window,
     assert ctx.get_status() == (binding.ESSA_ERR_CACHE if (past - window) // 64 in gone else 0)
 
 
+
+
+# ------------------------------------------------------------------------------------------------ padded batches
+def test_empty_entries_of_a_tree_need_no_sequence(torch, ctx):
+    """A batch padded with entries without rows and slots of -1, as append, attend and read take them."""
+    p = Pair(torch, ctx, 1, 4, 1, 64, 2, 2)
+    p.place([10, 40], np.random.default_rng(0))
+    slots, off, parents = p.ints([1, -1, 0, -1]), p.ints([0, 3, 3, 5, 5]), p.ints([-1, 0, 0, -1, 0])
+    drafts, pos = p.gpu.tree(parents, off, 3, slots=slots)
+    assert ctx.get_status() == 0
+    assert pos.tolist() == [37, 38, 38, 8, 9] and drafts[:, 0].tolist() == [1, 3, 5, 1, 3]
+    x = torch.zeros((5, 1, 64), dtype=torch.bfloat16, device="cuda")
+    p.gpu.append_rotary(0, binding.Rotary(64), x, x, x, pos, off, slots=slots)
+    p.gpu.attend(0, x, off, slots=slots, max_new=3, tree=drafts)
+    p.gpu.read(0, off, 5, slots=slots)
+    assert ctx.get_status() == 0
