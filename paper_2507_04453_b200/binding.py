@@ -684,6 +684,8 @@ class KvCache:
             if tree.dtype is not self._int32 or tree.dim() != 2 or tree.shape[0] != T or tree.get_device() != self._index or not tree.is_contiguous():
                 self._fail("tree", f"a contiguous int32 tensor [{T}, words]")
             words, ptr = tree.shape[1], tree.data_ptr() or None
+            if words < 1:  # (its pointer is NULL, which would stand for no tree)
+                raise EssaError(ESSA_ERR_UNSUPPORTED_SHAPE, "kv_cache: a tree has at least one word of bits per row")
         if window is not None and window < 1:
             raise EssaError(ESSA_ERR_INVALID_ARG, "kv_cache: a window has at least one token")
         m = self._mask_desc

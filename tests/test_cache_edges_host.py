@@ -1,7 +1,11 @@
 """Host side of calls around the key / value cache that meet one another (no GPU)."""
+import ctypes
+
 import numpy as np
+import pytest
 
 from oracle import cache_oracle as co
+from paper_2507_04453_b200 import binding
 
 
 def test_the_model_grows_on_a_copy_of_a_shared_page():
@@ -25,3 +29,47 @@ def test_the_model_grows_on_a_copy_of_a_shared_page():
             np.testing.assert_array_equal(a[:, :70], b[:, :70])
     c.grow([1], [1])
     assert c.refs.sum() == (c.table >= 0).sum()
+
+
+@pytest.fixture
+def cache():
+    """A KvCache on CPU tensors whose library only notes the masks that it is called with."""
+    import torch
+
+    class Library:
+        masks = []
+
+        def essa_cache_attend_workspace(self, cache, heads, max_new, sms, out):
+            out._obj.value = 16
+            return binding.ESSA_OK
+
+        def essa_cache_attend(self, *args):
+            self.masks.append(None)
+            return binding.ESSA_OK
+
+        def essa_cache_attend_masked(self, handle, cache, mask, *args):
+            self.masks.append(mask._obj)
+            return binding.ESSA_OK
+
+    class Ctx:
+        handle = None
+
+    kv, Ctx.torch = binding.KvCache.__new__(binding.KvCache), torch
+    kv.ctx, kv._lib, kv._ref, kv.device, kv._index = Ctx, Library(), None, torch.device("cpu"), -1
+    kv.head_dim, kv.kv_heads, kv._sms, kv._scale, kv._attend_ws = 64, 1, 148, 0.125, {}
+    kv._int32, kv._bf16, kv._empty_like = torch.int32, torch.bfloat16, torch.empty_like
+    kv._mask_desc = binding.AttendMask()
+    kv._mask_ref = ctypes.byref(kv._mask_desc)
+    kv._raw, kv._workspace = lambda stream: None, lambda n, raw, stream: torch.empty(n, dtype=torch.uint8)
+    return kv
+
+
+def test_a_tree_without_words_is_refused(cache):
+    """(Not taken for a call without a tree, in which the drafts see one another.)"""
+    torch = cache.ctx.torch
+    q, off = torch.zeros((3, 2, 64), dtype=torch.bfloat16), torch.tensor([0, 3], dtype=torch.int32)
+    for T in (3, 0):
+        with pytest.raises(binding.EssaError):
+            cache.attend(0, q[:T], off, max_new=3, tree=torch.zeros((T, 0), dtype=torch.int32))
+        cache.attend(0, q[:T], off, max_new=3, tree=torch.zeros((T, 1), dtype=torch.int32))
+    assert len(cache._lib.masks) == 2 and cache._lib.masks[0].draft_words == 1
