@@ -488,8 +488,6 @@ class KvCache:
         self._pages_ws = need.value
         self._sms = torch.cuda.get_device_properties(self.device).multi_processor_count
         self._attend_ws = {}  # (q_heads, max_new) -> bytes
-        self._mask_desc = AttendMask()
-        self._mask_ref = C.byref(self._mask_desc)
         self._ws = {}         # cudaStream_t -> workspace
         self._lib, self._ref, self._index = ctx.lib, C.byref(self.desc), self.device.index
         self._int32, self._bf16, self._scale = torch.int32, torch.bfloat16, head_dim ** -0.5
@@ -688,10 +686,8 @@ class KvCache:
                 raise EssaError(ESSA_ERR_UNSUPPORTED_SHAPE, "kv_cache: a tree has at least one word of bits per row")
         if window is not None and window < 1:
             raise EssaError(ESSA_ERR_INVALID_ARG, "kv_cache: a window has at least one token")
-        m = self._mask_desc
         # (beyond 32 bits: all tokens; the structure would take the low bits)
-        m.window, m.sinks, m.drafts, m.draft_words = min(window or 0, 0x7fffffff), max(min(sinks, 0x7fffffff), -1), ptr, words
-        return self._mask_ref
+        return C.byref(AttendMask(min(window or 0, 0x7fffffff), max(min(sinks, 0x7fffffff), -1), ptr, words))
 
     def attend(self, layer: int, q, tok_offsets=None, slots=None, max_new: int = 1, scale=None, out=None, stream=None, window=None, sinks: int = 0, tree=None):
         """essa_cache_attend: q [T, heads, head_dim] (or [T, heads * head_dim]) bf16 over the cached tokens; the result has q's

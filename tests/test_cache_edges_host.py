@@ -1,6 +1,4 @@
 """Host side of calls around the key / value cache that meet one another (no GPU)."""
-import ctypes
-
 import numpy as np
 import pytest
 
@@ -58,8 +56,6 @@ def cache():
     kv.ctx, kv._lib, kv._ref, kv.device, kv._index = Ctx, Library(), None, torch.device("cpu"), -1
     kv.head_dim, kv.kv_heads, kv._sms, kv._scale, kv._attend_ws = 64, 1, 148, 0.125, {}
     kv._int32, kv._bf16, kv._empty_like = torch.int32, torch.bfloat16, torch.empty_like
-    kv._mask_desc = binding.AttendMask()
-    kv._mask_ref = ctypes.byref(kv._mask_desc)
     kv._raw, kv._workspace = lambda stream: None, lambda n, raw, stream: torch.empty(n, dtype=torch.uint8)
     return kv
 
@@ -73,3 +69,15 @@ def test_a_tree_without_words_is_refused(cache):
             cache.attend(0, q[:T], off, max_new=3, tree=torch.zeros((T, 0), dtype=torch.int32))
         cache.attend(0, q[:T], off, max_new=3, tree=torch.zeros((T, 1), dtype=torch.int32))
     assert len(cache._lib.masks) == 2 and cache._lib.masks[0].draft_words == 1
+
+
+def test_a_call_has_a_mask_of_its_own(cache):
+    """What one call hands over is not what another makes of it (ctypes lets other threads run before the library reads it)."""
+    torch = cache.ctx.torch
+    q, off = torch.zeros((3, 2, 64), dtype=torch.bfloat16), torch.tensor([0, 3], dtype=torch.int32)
+    tree = torch.zeros((3, 2), dtype=torch.int32)
+    cache.attend(0, q, off, max_new=3, window=100, sinks=7, tree=tree)
+    cache.attend(0, q, off, max_new=3, window=5, sinks=1)
+    first, second = cache._lib.masks
+    assert (first.window, first.sinks, first.draft_words, first.drafts) == (100, 7, 2, tree.data_ptr())
+    assert (second.window, second.sinks, second.draft_words, second.drafts) == (5, 1, 0, None)
