@@ -510,10 +510,10 @@ int32_t essa_cache_keep(essa_ctx* ctx, const essa_cache_desc* cache, const int32
  * A row of head_dim channels is turned pair by pair: with t = positions[axis[i]] * frequencies[i] (radians) pair i becomes
  *   a' = magnitude (a cos t - b sin t),  b' = magnitude (b cos t + a sin t),
  * where (a, b) are channels i and i + head_dim / 2, or, with adjacent != 0, 2 i and 2 i + 1.  Every pair has an axis (time, height and width of images and
- * video; one axis for text) and a frequency of its own, so that any layout of sections and any scaling of frequencies can be given; a frequency of 0 leaves a pair as
- * it is (times magnitude), and negated positions turn back.
- * Angles are exact: a frequency is held as a 64-bit fraction of a turn, turns[i] = frac(frequency / 2 pi) 2^64, the product with a position
- * is taken modulo a turn in integers: wrong by the position times 2^-64 of a turn, however far the position. */
+ * video; one axis for text) and a frequency of its own, so that any layout of sections and any scaling of frequencies can be given; a frequency of 0 leaves a pair of
+ * finite members as it is (times magnitude), and negated positions turn back.
+ * Angles: a frequency is held as the 64-bit fraction of a turn that is nearest to it, turns[i] = frac(frequency / 2 pi) 2^64, and the product with a position
+ * is taken modulo a turn in integers: wrong by the position times 2^-65 of a turn (2^-34 for the farthest), whatever the frequency. */
 #define ESSA_ROTARY_MAX_DIM 256
 #define ESSA_ROTARY_MAX_AXES 4
 #define ESSA_ROTARY_MAX_HEADS (1 << 20) /* heads of a row that the calls below accept */
@@ -525,7 +525,7 @@ typedef struct essa_rotary {
   uint64_t turns[ESSA_ROTARY_MAX_DIM / 2];
   uint8_t axis[ESSA_ROTARY_MAX_DIM / 2];
 } essa_rotary;
-/* Fill *out from frequencies [head_dim / 2] (radians per position, finite) and axis [head_dim / 2] (NULL: all 0), both on the host.  Needs no device. */
+/* Fill *out from frequencies [head_dim / 2] (radians per position, up to 2^32 in magnitude) and axis [head_dim / 2] (NULL: all 0), both on the host.  Needs no device. */
 int32_t essa_rotary_make(int32_t head_dim, int32_t axes, int32_t adjacent, float magnitude, const double* frequencies, const int32_t* axis, essa_rotary* out);
 /* out[t][h] = x[t][h] turned by positions[.][t], t < T, h < heads.  x, out [T] rows of heads * head_dim bf16 dev, ld_x / ld_out elements apart (multiples of 8;
  * 16-byte aligned); out may be x (with the same pitch), and overlaps it in no other way.  positions [axes] rows of T int32 dev, ld_positions apart.  Sine and cosine are rounded

@@ -397,7 +397,8 @@ class CmaState:
 class Rotary:
     """Which turn every pair of channels makes per position (essa_rotary), made on the host once per model.
 
-    head_dim: a multiple of 16 up to 256.  base: pair i turns by base ** (-2 i / head_dim) radians per position; or frequencies: head_dim / 2 of them.
+    head_dim: a multiple of 16 up to 256.  base: pair i turns by base ** (-2 i / head_dim) radians per position; or frequencies: head_dim / 2 of them,
+    up to 2 ** 32 in magnitude.
     sections: how many pairs each axis has (their sum is head_dim / 2; None: one axis), one axis after another or, interleaved, the axes in turns until
     each has its share; or axis: the axis of every pair.  adjacent: pairs are channels 2 i and 2 i + 1 instead of i and i + head_dim / 2.
     magnitude: what cosine and sine are multiplied with."""

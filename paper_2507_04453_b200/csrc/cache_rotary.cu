@@ -3,7 +3,7 @@
 //
 // Pair (a, b) with t = position * frequency: (a cos t - b sin t, b cos t + a sin t).  In fp32 the angle of a far position loses its fraction (2^-24 of
 // 10^5 radians is a hundredth); here a frequency is a 64-bit fraction of a turn, and the product with a position modulo 2^64 is the angle's fraction, exact but for
-// the frequency's own 2^-64: one wide multiplication, then sincospi.
+// the frequency's own 2^-65: one wide multiplication, then sincospi.
 //
 // What bounds it: bytes.  Sine and cosine depend on the token and the pair only, so a thread block computes them once for its tokens and
 // all their heads use them: a lane keeps those of its eight pairs in registers while its warp walks the heads.
@@ -213,6 +213,20 @@ int32_t check_positions(essa_ctx* ctx, const char* what, const int32_t* position
   if (ld < T) return fail(ctx, ESSA_ERR_INVALID_ARG, std::string(what) + ": the rows of positions must hold T of them");
   return ESSA_OK;
 }
+// frac(f / 2 pi) in units of 2^-64, to the nearest, for |f| <= kMaxFrequency: |f| is an integer m below 2^53 times 2^e, e <= -20, and 2^128 / 2 pi (the
+// constant, in two halves) times m has to be shifted by 64 - e.  The constant's missing end is m 2^(e - 64) < 2^-31 units, what
+// the product leaves out 2^-20.
+constexpr double kMaxFrequency = 4294967296.0;
+uint64_t turns_of(double f) {
+  constexpr uint64_t kHigh = 0x28be60db9391054aull, kLow = 0x7f09d5f47d4d3770ull;
+  int e;
+  const uint64_t m = (uint64_t)std::ldexp(std::frexp(std::fabs(f), &e), 53);
+  const int shift = 53 - e;  // (by 64 already)
+  if (shift > 120) return 0;  // (less than half a unit)
+  const unsigned __int128 product = (unsigned __int128)m * kHigh + (uint64_t)((unsigned __int128)m * kLow >> 64);  // < 2^115
+  const uint64_t turns = (uint64_t)((product + ((unsigned __int128)1 << (shift - 1))) >> shift);
+  return f < 0 ? 0 - turns : turns;
+}
 // How a call of T tokens is divided: token groups of a thread block, and what share of the heads.
 struct RotaryGrid {
   dim3 grid;
@@ -247,10 +261,9 @@ int32_t essa_rotary_make(int32_t head_dim, int32_t axes, int32_t adjacent, float
   int32_t code;
   if (rotary_problem(&r, &code)) return code;
   for (int i = 0; i < head_dim / 2; ++i) {
-    if (!(std::fabs(frequencies[i]) <= 1e300)) return ESSA_ERR_INVALID_ARG;
+    if (!(std::fabs(frequencies[i]) <= kMaxFrequency)) return ESSA_ERR_INVALID_ARG;
     if (axis && (axis[i] < 0 || axis[i] >= axes)) return ESSA_ERR_INVALID_ARG;
-    const long double turn = (long double)frequencies[i] / 6.283185307179586476925286766559005768L, part = turn - std::floor(turn);
-    r.turns[i] = part >= 1.0L ? 0 : (uint64_t)(part * 18446744073709551616.0L);
+    r.turns[i] = turns_of(frequencies[i]);
     r.axis[i] = (uint8_t)(axis ? axis[i] : 0);
   }
   *out = r;

@@ -1,9 +1,14 @@
 """Host side of calls around the key / value cache that meet one another (no GPU)."""
+from fractions import Fraction
+
 import numpy as np
 import pytest
 
 from oracle import cache_oracle as co
 from paper_2507_04453_b200 import binding
+
+# pi in 60 digits: the angle of 2^32 radians is some 2^96 units of 2^-64 turns, of which it leaves 2^-100
+TWO_PI = 2 * Fraction("3.14159265358979323846264338327950288419716939937510582097494")
 
 
 def test_the_model_grows_on_a_copy_of_a_shared_page():
@@ -81,3 +86,22 @@ def test_a_call_has_a_mask_of_its_own(cache):
     first, second = cache._lib.masks
     assert (first.window, first.sinks, first.draft_words, first.drafts) == (100, 7, 2, tree.data_ptr())
     assert (second.window, second.sinks, second.draft_words, second.drafts) == (5, 1, 0, None)
+
+
+@pytest.mark.parametrize("scale", [0, 10, 20, 31])
+def test_turns_are_exact_however_high_the_frequency(scale):
+    """The nearest 64-bit fraction of a turn (half a unit, and the hundredth of one that the constant's end may cost)."""
+    rng = np.random.default_rng(scale)
+    freq = np.ldexp(rng.uniform(1, 2, 128), scale) * rng.choice([-1, 1], 128)
+    freq[:5] = 2.0 ** 32, -2.0 ** 32, 2.0 ** 32 - 2.0 ** -20, 5e-324, np.pi * 2.0 ** (scale - 1)
+    r = binding.Rotary(256, frequencies=freq)
+    for t, f in zip(r.desc.turns, freq):
+        want = Fraction(float(f)) / TWO_PI * 2 ** 64
+        off = abs(int(t) - want) % 2 ** 64
+        assert min(off, 2 ** 64 - off) <= Fraction(51, 100), f
+
+
+@pytest.mark.parametrize("f", [np.nextafter(2.0 ** 32, np.inf), -1e10, 1e19, 1e300])
+def test_frequencies_that_no_position_needs_are_refused(f):
+    with pytest.raises(binding.EssaError):
+        binding.Rotary(16, frequencies=[0.5] * 7 + [f])

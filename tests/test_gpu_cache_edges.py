@@ -1,11 +1,12 @@
 """GPU tests of calls around the key / value cache that meet one another: sequences shortened into pages that others share and grown again, pages that
-have left every window, padded batches."""
+have left every window, padded batches, far positions."""
 import numpy as np
 import pytest
 
 from oracle import cache_oracle as co
 from paper_2507_04453_b200 import binding
 from tests.cache_utils import Pair, attend_bound, bf16
+from tests.parity_utils import to_dev
 
 pytestmark = pytest.mark.gpu
 
@@ -208,3 +209,27 @@ def test_empty_entries_of_a_tree_need_no_sequence(torch, ctx):
     p.gpu.attend(0, x, off, slots=slots, max_new=3, tree=drafts)
     p.gpu.read(0, off, 5, slots=slots)
     assert ctx.get_status() == 0
+
+
+# ------------------------------------------------------------------------------------------------ rotation
+# Of a pair (a, b): the angle is wrong by the position times 0.51 2^-64 of a turn (2^-30 radians for 2^31); cosine and sine, nearest fp32 numbers of at most 1, by
+# 2^-25, and by as much again when they are multiplied with the magnitude; the products and their sum are rounded to fp32 (2^-24 each, of no more than
+# magnitude (|a| + |b|)), the result to bf16 (2^-8 of it, or 2^-134 absolutely).  So before bf16 (2^-24 + 2^-30 + 2 2^-24) magnitude (|a| + |b|).
+def rotate_bound(x, want, adjacent, magnitude):
+    y = np.abs(x.astype(np.float64))
+    d = x.shape[-1]
+    both = (y[..., 0::2] + y[..., 1::2]) if adjacent else (y[..., :d // 2] + y[..., d // 2:])
+    both = np.repeat(both, 2, -1) if adjacent else np.concatenate([both, both], -1)
+    return 2.0 ** -8 * np.abs(want) + 3.03 * 2.0 ** -24 * (1 + 2.0 ** -8) * abs(magnitude) * both + 2.0 ** -133
+
+
+@pytest.mark.parametrize("d,adjacent", [(64, False), (128, True), (48, False)])
+@pytest.mark.parametrize("top", [1.0, 1e5, 4e9])
+def test_far_positions_of_any_frequency(torch, ctx, d, adjacent, top):
+    rng = np.random.default_rng(int(top) + d)
+    freq = top * rng.uniform(-1, 1, d // 2)
+    pos = np.concatenate([2 ** 31 - 1 - np.arange(20), -2 ** 31 + np.arange(20), rng.integers(-2 ** 31, 2 ** 31, 60)]).astype(np.int32)
+    x = bf16(rng, (100, 3, d))
+    want = co.rotate(x, pos[None], freq, [0] * (d // 2), adjacent, 0.75)
+    got = f32(ctx.rotary(binding.Rotary(d, frequencies=freq, adjacent=adjacent, magnitude=0.75), to_dev(torch, x, torch.bfloat16), torch.from_numpy(pos).cuda()))
+    assert (np.abs(got - want) <= rotate_bound(x, want, adjacent, 0.75)).all()
