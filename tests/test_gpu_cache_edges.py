@@ -1,5 +1,5 @@
 """GPU tests of calls around the key / value cache that meet one another: sequences shortened into pages that others share and grown again, pages that
-have left every window, padded batches, far positions."""
+have left every window, padded batches, far positions, masks that hide nothing."""
 import numpy as np
 import pytest
 
@@ -233,3 +233,30 @@ def test_far_positions_of_any_frequency(torch, ctx, d, adjacent, top):
     want = co.rotate(x, pos[None], freq, [0] * (d // 2), adjacent, 0.75)
     got = f32(ctx.rotary(binding.Rotary(d, frequencies=freq, adjacent=adjacent, magnitude=0.75), to_dev(torch, x, torch.bfloat16), torch.from_numpy(pos).cuda()))
     assert (np.abs(got - want) <= rotate_bound(x, want, adjacent, 0.75)).all()
+
+
+# ------------------------------------------------------------------------------------------------ masks that hide nothing
+@pytest.mark.parametrize("heads,kv_heads,d", [(1, 1, 64), (14, 2, 128), (8, 8, 64)])
+@pytest.mark.parametrize("hint", [1, 100])
+@pytest.mark.parametrize("window,sinks", [(10 ** 6, 7), (513, 0), (1, 10 ** 6), (200, 400)])
+def test_a_mask_that_hides_nothing_gives_what_no_mask_gives(torch, ctx, heads, kv_heads, d, hint, window, sinks):
+    """The kernels with a mask (a window of 2^31 - 1 would choose those without): the model's values; and the bits of no mask where the work is divided alike,
+    which it is but for several row blocks of few rows (without a mask each walks all of the entry's pages)."""
+    rng = np.random.default_rng(heads + hint)
+    lengths, rows = [1, 5, 64, 130, 200, 257, 300, 90, 513], [1, 5, 64, 3, 77, 257, 0, 90, 2]
+    p = Pair(torch, ctx, 1, 45, kv_heads, d, len(lengths), 9)
+    p.place(lengths, rng)
+    ends = np.concatenate([[0], np.cumsum(rows)])
+    q, off = bf16(rng, (sum(rows), heads, d)), p.ints(ends)
+    got, want = p.gpu.attend(0, p.bf(q), off, max_new=hint, window=window, sinks=sinks), p.gpu.attend(0, p.bf(q), off, max_new=hint)
+    assert hint == 1 or torch.equal(got, want)
+    for i, n in enumerate(lengths):
+        if rows[i] == 0:
+            continue
+        k, v, codes, sc = p.cpu.sequence(0, i)
+        mine, here = q[ends[i]:ends[i + 1]], f32(got)[ends[i]:ends[i + 1]]
+        model, w = co.attend(mine, k, v, n, d ** -0.5)
+        assert (np.abs(here - model) <= attend_bound(mine, v, codes, sc, model, w, d ** -0.5, k)).all()
+    one = p.bf(bf16(rng, (len(lengths), heads, d)))
+    assert torch.equal(p.gpu.attend(0, one, max_new=hint, window=window, sinks=sinks), p.gpu.attend(0, one, max_new=hint))
+    assert ctx.get_status() == 0
