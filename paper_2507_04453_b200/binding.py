@@ -570,7 +570,7 @@ class KvCache:
         self._check(self._lib.essa_cache_reset(self.ctx.handle, self._ref, self._raw(stream)))
 
     def grow(self, slots, counts, stream=None):
-        """essa_cache_grow: sequence slots[i] (None: i) becomes counts[i] tokens longer."""
+        """essa_cache_grow: sequence slots[i] (None: i) becomes counts[i] tokens longer (on a copy of its last page, if another shares that)."""
         n = counts.shape[0]
         a, b, raw = self._ints("slots", slots, n), self._ints("counts", counts), self._raw(stream)
         ws = self._workspace(self._pages_ws, raw, stream)

@@ -24,7 +24,8 @@
 // With a mask the list has the pages that a row block can see, and a page at an edge (of a window, of the first tokens, among drafts) is masked by 32 bits per row.
 // A window of 1024 and 4 first tokens of those long sequences (156 MB): 59 us, 2.6 TB/s: seventeen pages of a row block beside five pages' worth of fixed cost, and
 // a join of 5 us.  Queries and row blocks found ahead by the copying warp: 58 (and 36 -> 34 for 256 short ones), left out for its second path of synchronisation.
-// Tokens per column instead of limits, and a mask per different token: 35.9 -> 35.3 for the short ones.
+// Tokens per column instead of limits, and a mask per different token: 35.9 -> 35.3 for the short ones.  The masked instance spills 208 bytes a thread (64 without a
+// mask; heads of 64 with two column tiles 192, and none).
 #include "cache_list.cuh"
 
 namespace essa {

@@ -52,7 +52,8 @@ struct KeepHead {
 };
 constexpr int kKeepThreads = 1024;
 
-// Checks everything, then writes down where the tokens are that move, and takes the sequences' ends away.
+// Checks everything, then writes down where the tokens are that move, and takes the sequences' ends away.  A thread per entry: a few pages each after trees;
+// an end of 100 thousand tokens, a load, a check and an atomic per page in turn, takes it 260 us.
 __global__ void __launch_bounds__(kKeepThreads) keep_plan_kernel(CacheView v, const int32_t* slots, const int32_t* off, const int32_t* counts, const int32_t* picks,
                                                                  int64_t ld_picks, int n, KeepHead* head, KeepEntry* entries, int32_t* status) {
   grid_dep_launch();
